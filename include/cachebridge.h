@@ -39,6 +39,11 @@
  *
  *   cb_plan_create_multi, cb_plan_feature_width, cb_ridge_solve_ws
  *
+ * and what a receiver does next with its decode-ready cache (Sec. 1: it decodes
+ * from the handed-off rows), serving it from the pages of a pool:
+ *
+ *   cb_page_tables, cb_rope_axes, cb_page_write, cb_attn_paged
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Row vectors: a map is W~ = [W ; b^T], a P x d_t fp32 matrix with
@@ -608,6 +613,166 @@ int64_t cb_ridge_solve_noalloc_max_bytes(void);
 
 /* Feature width P of a plan's maps (d_s + 1, or k d_s + 1) and its k. */
 cb_status cb_plan_feature_width(const cb_plan *plan, int32_t *P, int32_t *k);
+
+/*
+ * ---------------------------------------------------------------- serving from pages
+ *
+ * A receiver that decodes from a handed-off cache holds its K and V rows in
+ * pages of a pool: page_size consecutive tokens of one request share a page,
+ * and row r of the block table lists request r's pages in order.  A step gives
+ * every request some new tokens (one when it decodes, more when it reads a
+ * chunk of its prompt, none when it waits); token rows of all requests are
+ * packed, request r's at q_starts[r] .. q_starts[r + 1] - 1.  The lengths live
+ * on the device: no call below reads them on the host, so a step can be
+ * captured into a graph and replayed with other lengths.  Lengths, slots, page
+ * numbers and positions are checked by the kernels: a value outside its range
+ * takes its row or request out as described, and nothing is read or written
+ * outside the buffers.
+ */
+
+/* Element types of a pool. */
+#define CB_PAGES_BF16 0   /* bfloat16 */
+#define CB_PAGES_E4M3 1   /* 8-bit floats (4 exponent, 3 mantissa bits, largest 448, no infinities), with scales */
+
+/*
+ * A pool of pages, [layer][kv][page][head][tok][ch]: a cb_cache whose n_seqs
+ * is the number of pages and whose seq_len is the page size (any size from 1),
+ * with any strides.  A contiguous cache, such as cb_apply writes, is a pool
+ * whose pages are its sequences.  E4M3: data holds bytes, strides count
+ * elements, every row 16-byte aligned (multiples of 16 elements), and a stored
+ * element e stands for e * scales[(layer * 2 + kv) * n_heads + head]
+ * (fp32, device, positive and finite; NULL for CB_PAGES_BF16).  pages *
+ * page_size < 2^31, and the pages of one (layer, kv) span less than 64 GiB.
+ */
+typedef struct {
+    cb_cache cache;
+    int32_t dtype;              /* CB_PAGES_BF16 or CB_PAGES_E4M3 */
+    const float *scales;
+} cb_pages;
+
+/*
+ * Packed token rows (queries, attention outputs): element (token, head, ch) at
+ *   data[token * s_tok + head * s_head + ch]   (bfloat16, ch stride 1),
+ * every row 16-byte aligned.
+ */
+typedef struct {
+    void *data;
+    int32_t n_tokens;
+    int32_t n_heads;
+    int32_t head_dim;
+    int64_t s_tok, s_head;
+} cb_rows;
+
+/*
+ * Rotary positions with several axes: text has one, images and video three
+ * (time, height, width).  Channel pair i of token t is turned by the angle of
+ * position positions[axis[i] * axis_stride + t] in a cb_rope_table of head_dim
+ * and n_pos.  Tokens of a cache are numbered seq * seq_len + tok.  A position
+ * outside 0 .. n_pos - 1 turns its pairs into NaN.
+ */
+typedef struct {
+    const float *table;         /* cb_rope_table(theta, head_dim, n_pos) output: device, 16-byte aligned */
+    int32_t head_dim;
+    int32_t n_pos;
+    int32_t style;              /* CB_ROPE_HALF_SPLIT or CB_ROPE_INTERLEAVED */
+    int32_t n_axes;             /* 1 .. 4 */
+    const int32_t *positions;   /* device, [n_axes][axis_stride] */
+    int64_t axis_stride;        /* >= tokens of the call */
+    uint8_t axis[128];          /* axis of pair i, i < head_dim / 2 */
+} cb_rope_axes_spec;
+
+/*
+ * Block tables and slot maps of a step, from the requests' lengths.  Request r
+ * holds ctx_lens[r] tokens in the first have_r = ceil(ctx_lens[r] / page_size)
+ * entries of its block table row and gets q_lens[r] new ones, so it needs
+ * need_r = ceil((ctx_lens[r] + q_lens[r]) / page_size) - have_r new pages,
+ * taken from free_pages in order, request 0 first.  Written:
+ *   block_table[r * table_stride + have_r + j] = the j-th of them (j < need_r),
+ *   q_starts [n_reqs + 1] = the sums of q_lens before r (at most max_tokens),
+ *   kv_lens [n_reqs] = ctx_lens[r] + q_lens[r],
+ *   slots [max_tokens], positions [max_tokens]: for new token i of request r, at
+ *     q_starts[r] + i, its position pos = ctx_lens[r] + i and its slot
+ *     page * page_size + pos % page_size; -1 and -1 behind the last request,
+ *   n_used [1] = free pages taken: the next step's list starts there,
+ *   info [n_reqs] = 0, or why the request takes no part in the step (no page
+ *     taken, its row left as it was, kv_lens 0, slots and positions -1):
+ *     1 the free list is used up (so is it for every later request that needs
+ *     a page), 2 its pages exceed table_width, 3 a length is negative,
+ *     4 its tokens exceed max_tokens.
+ * Device pointers; block_table is read and written, the rest of the outputs
+ * only written; no two of the arrays may overlap.  page_size >= 1, table_width
+ * * page_size < 2^31, n_reqs <= 4096.
+ */
+cb_status cb_page_tables(int32_t n_reqs, const int32_t *ctx_lens, const int32_t *q_lens, const int32_t *free_pages,
+                         int32_t n_free, int32_t page_size, int32_t *block_table, int64_t table_stride,
+                         int32_t table_width, int32_t max_tokens, int32_t *q_starts, int32_t *kv_lens, int32_t *slots,
+                         int32_t *positions, int32_t *info, int32_t *n_used, void *stream);
+
+/*
+ * cb_rope with explicit positions of several axes: every K row of `in` turned
+ * by its token's positions (turned back when `inverse` is non-zero) into
+ * `out`, in fp32 from the exact bf16 values with one rounding.  V rows, in
+ * place use, geometry, widths and overlaps as in cb_rope.
+ */
+cb_status cb_rope_axes(const cb_cache *in, const cb_cache *out, const cb_rope_axes_spec *rope, int32_t inverse,
+                       void *stream);
+
+/*
+ * Write rows into pages: the K and V rows of token t of `rows` (all its
+ * layers, into the pool's layers layer0, layer0 + 1, ...) go to slot slots[t]
+ * (int32, device, one per token): page slots[t] / page_size, token
+ * slots[t] % page_size.  rows: any cb_cache view -- a whole mapped cache, or
+ * the new tokens of one layer (n_layers = n_seqs = 1).  rope, if not NULL,
+ * turns the K rows by their positions in fp32 before their only rounding.
+ * E4M3 pages hold x * (1 / scale) rounded to nearest even, clamped to +-448 (NaN
+ * stays NaN).  q, q_out (both or neither, only with rope): query rows
+ * turned in the same launch, token t of q into token t of q_out (q_out may be
+ * q; q->n_tokens = the tokens of rows).  A token whose slot is outside the pool
+ * (-1: padding) is skipped, its query too.  Two tokens must not name one slot;
+ * rows, q and the pool must not overlap.  head_dim a multiple of 16 up to 256.
+ */
+cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t layer0, const int32_t *slots,
+                        const cb_rope_axes_spec *rope, const cb_rows *q, const cb_rows *q_out, void *stream);
+
+/*
+ * Attention of every request's new tokens over its pages in one layer.  Row
+ * (new token i of request r, query head u) stands at position p =
+ * kv_lens[r] - q_len_r + i, q_len_r = q_starts[r + 1] - q_starts[r], and sees
+ * the keys j of KV head u / (n_qheads / n_heads) with
+ *   j <= p   and   (window = 0, or j > p - window, or j < n_sinks)
+ * whose page, block_table[r * table_stride + j / page_size], is inside the pool
+ * (an entry such as -1 hides its keys: a page given back behind the window).
+ *   s_j = scale q . k_j,   out = sum_j exp(s_j) v_j / sum_j exp(s_j),   lse = log(sum_j exp(s_j))
+ * over the visible keys; out = 0 and lse = -infinity for a row whose visible
+ * keys have no weight or that sees none (a request with kv_lens 0).  What
+ * masked or unwritten places hold, NaN and infinities among it, does not reach
+ * a row that does not see them.  Rows of no request, such as those behind
+ * q_starts[n_reqs], are left as they were.
+ *   q, out: n_tokens rows of n_qheads = G * n_heads heads; they must not overlap.
+ *   q_starts must not decrease; kv_lens beyond table_width * page_size count as that.
+ *   max_q_len: the largest number of new tokens of any request, a hint that
+ *     picks the kernels; results do not depend on its being right.
+ *   scale: finite.  window, n_sinks >= 0.
+ *   lse: fp32 [n_tokens][n_qheads], or NULL.
+ *   workspace: device memory, 16-byte aligned, for the partial results of long
+ *     rows that several workgroups share; cb_attn_paged_workspace_bytes gives
+ *     what the call can use.  With less (or NULL) rows are split less.  The call
+ *     leaves nothing in it that another reads; calls that overlap in time need
+ *     one each.
+ * Scores and sums are fp32 from exact products; the weights exp(s_j - m) are
+ * rounded to bf16 for their product with V (m the running maximum) and summed
+ * unrounded.  Results do not depend on the other requests but for the order of
+ * fp32 sums (where a row is split), and are bitwise reproducible.  head_dim in
+ * {64, 96, 128}.
+ */
+cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,
+                        const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                        const cb_rows *out, int32_t max_q_len, float scale, int32_t window, int32_t n_sinks, float *lse,
+                        void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Workspace bytes with which cb_attn_paged splits rows as far as it wants to (on any device). */
+int64_t cb_attn_paged_workspace_bytes(int32_t n_tokens, int32_t n_reqs, int32_t n_qheads, int32_t n_heads,
+                                      int32_t head_dim, int32_t max_q_len);
 
 /* Static name of a status code. */
 const char *cb_status_string(cb_status status);

@@ -654,3 +654,200 @@ def cb_stats_accumulate_rope(plan: Plan, src: torch.Tensor, tgt: torch.Tensor, w
                                          int(w_row_stride), _ptr(G), _ptr(C),
                                          None if sr is None else ctypes.byref(sr),
                                          None if tr is None else ctypes.byref(tr), _stream(stream)))
+
+
+# ------------------------------------------------------------------ serving from pages
+
+CB_PAGES_BF16 = 0
+CB_PAGES_E4M3 = 1
+
+
+class CbPages(ctypes.Structure):
+    _fields_ = [("cache", CbCache), ("dtype", ctypes.c_int32), ("scales", _vp)]
+
+
+class CbRows(ctypes.Structure):
+    _fields_ = [("data", _vp), ("n_tokens", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("s_tok", ctypes.c_int64), ("s_head", ctypes.c_int64)]
+
+
+class CbRopeAxesSpec(ctypes.Structure):
+    _fields_ = [("table", _vp), ("head_dim", ctypes.c_int32), ("n_pos", ctypes.c_int32), ("style", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("positions", _vp), ("axis_stride", ctypes.c_int64),
+                ("axis", ctypes.c_uint8 * 128)]
+
+
+_i32, _i64 = ctypes.c_int32, ctypes.c_int64
+_lib.cb_page_tables.restype = ctypes.c_int
+_lib.cb_page_tables.argtypes = [_i32, _vp, _vp, _vp, _i32, _i32, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.cb_rope_axes.restype = ctypes.c_int
+_lib.cb_rope_axes.argtypes = [ctypes.POINTER(CbCache), ctypes.POINTER(CbCache), ctypes.POINTER(CbRopeAxesSpec), _i32, _vp]
+_lib.cb_page_write.restype = ctypes.c_int
+_lib.cb_page_write.argtypes = [ctypes.POINTER(CbCache), ctypes.POINTER(CbPages), _i32, _vp, ctypes.POINTER(CbRopeAxesSpec),
+                               ctypes.POINTER(CbRows), ctypes.POINTER(CbRows), _vp]
+_lib.cb_attn_paged.restype = ctypes.c_int
+_lib.cb_attn_paged.argtypes = [ctypes.POINTER(CbRows), ctypes.POINTER(CbPages), _i32, _i32, _vp, _vp, _vp, _i64, _i32,
+                               ctypes.POINTER(CbRows), _i32, ctypes.c_float, _i32, _i32, _vp, _vp, _i64, _vp]
+_lib.cb_attn_paged_workspace_bytes.restype = _i64
+_lib.cb_attn_paged_workspace_bytes.argtypes = [_i32] * 6
+
+
+def _ints(t: torch.Tensor, n: int, name: str):
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements, got {t.dtype} {tuple(t.shape)}")
+
+
+def _on_current_device(**tensors):
+    """The library works on the current device: tensors of another (or of the host) are refused here."""
+    for name, t in tensors.items():
+        if t is not None and (t.device.type != "cuda" or t.device.index != torch.cuda.current_device()):
+            raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+
+
+def page_pool(t: torch.Tensor, scales: Optional[torch.Tensor] = None) -> CbPages:
+    """Describe a pool of pages: a [layer][2][page][head][token][dim] tensor (any strides, unit dim stride) of
+    bfloat16, or of float8_e4m3fn with its float32 ``scales`` [layer][2][head].  A contiguous cache is a pool whose
+    pages are its sequences."""
+    p = CbPages()
+    if t.dtype == torch.bfloat16:
+        if scales is not None:
+            raise ValueError("bfloat16 pages have no scales")
+        p.cache, p.dtype = cache_view(t), CB_PAGES_BF16
+    elif t.dtype == torch.float8_e4m3fn:
+        if t.dim() != 6 or t.shape[1] != 2 or (t.shape[5] > 1 and t.stride(5) != 1):
+            raise ValueError("8-bit pages are float8_e4m3fn [layer][2][page][head][token][dim] with unit dim stride")
+        _need(scales, (t.shape[0], 2, t.shape[3]), torch.float32, "scales")
+        c = p.cache
+        c.data = t.data_ptr()
+        c.n_layers, _, c.n_seqs, c.n_heads, c.seq_len, c.head_dim = t.shape
+        c.s_layer, c.s_kv, c.s_seq, c.s_head, c.s_tok = (t.stride(i) for i in range(5))
+        p.dtype, p.scales = CB_PAGES_E4M3, scales.data_ptr()
+    else:
+        raise ValueError("pages are bfloat16 or float8_e4m3fn")
+    p._keep = (t, scales)
+    return p
+
+
+def _rows_view(t: torch.Tensor, name: str) -> CbRows:
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} is bfloat16 [token][head][dim] with unit dim stride")
+    r = CbRows()
+    r.data = t.data_ptr()
+    r.n_tokens, r.n_heads, r.head_dim = t.shape
+    r.s_tok, r.s_head = t.stride(0), t.stride(1)
+    return r
+
+
+def rope_axes_spec(table: torch.Tensor, positions: torch.Tensor, axis=None,
+                   style: int = CB_ROPE_HALF_SPLIT) -> CbRopeAxesSpec:
+    """Rotary positions with several axes: ``table`` a :func:`cb_rope_table` output [n_pos][head_dim/2][2],
+    ``positions`` int32 [axis][token] (or [token] for one axis), ``axis`` the axis of each of the head_dim/2 channel
+    pairs (None: axis 0 for all)."""
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise ValueError("a rope table is a contiguous float32 [n_pos][head_dim/2][2] tensor")
+    if positions.dtype != torch.int32 or positions.dim() not in (1, 2) or (positions.shape[-1] > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions are int32 [axis][token] with unit token stride")
+    pairs = table.shape[1]
+    which = [0] * pairs if axis is None else [int(a) for a in axis]
+    if len(which) != pairs or pairs > 128 or any(a < 0 or a > 255 for a in which):
+        raise ValueError(f"axis must name the axis of each of the {pairs} channel pairs")
+    sp = CbRopeAxesSpec()
+    sp.table, sp.head_dim, sp.n_pos, sp.style = table.data_ptr(), 2 * pairs, table.shape[0], int(style)
+    sp.positions = positions.data_ptr()
+    sp.n_axes = 1 if positions.dim() == 1 else positions.shape[0]
+    sp.axis_stride = positions.shape[-1] if positions.dim() == 1 else positions.stride(0)
+    for i, a in enumerate(which):
+        sp.axis[i] = a
+    sp._keep = (table, positions)
+    return sp
+
+
+def _check_axes_tokens(rope: Optional[CbRopeAxesSpec], n_tokens: int):
+    if rope is not None and rope._keep[1].shape[-1] < n_tokens:
+        raise ValueError(f"positions hold {rope._keep[1].shape[-1]} tokens, the call has {n_tokens}")
+
+
+def cb_page_tables(ctx_lens: torch.Tensor, q_lens: torch.Tensor, free_pages: torch.Tensor, page_size: int,
+                   block_table: torch.Tensor, q_starts: torch.Tensor, kv_lens: torch.Tensor, slots: torch.Tensor,
+                   positions: torch.Tensor, info: torch.Tensor, n_used: torch.Tensor, stream=None):
+    """Block tables, slot map and positions of a step from the requests' cached (``ctx_lens``) and new (``q_lens``)
+    tokens, new pages from ``free_pages`` in order.  All int32 on the device; block_table [request][entry] is extended
+    in place, q_starts [n + 1], kv_lens [n], info [n], n_used [1], slots and positions [tokens] are written."""
+    n = ctx_lens.numel()
+    for t, m, name in ((ctx_lens, n, "ctx_lens"), (q_lens, n, "q_lens"), (free_pages, free_pages.numel(), "free_pages"),
+                       (q_starts, n + 1, "q_starts"), (kv_lens, n, "kv_lens"), (slots, slots.numel(), "slots"),
+                       (positions, slots.numel(), "positions"), (info, n, "info"), (n_used, 1, "n_used")):
+        _ints(t, m, name)
+    _check_table(block_table, n)
+    _on_current_device(ctx_lens=ctx_lens, q_lens=q_lens, free_pages=free_pages, block_table=block_table, q_starts=q_starts,
+                       kv_lens=kv_lens, slots=slots, positions=positions, info=info, n_used=n_used)
+    _check(_lib.cb_page_tables(n, _ptr(ctx_lens), _ptr(q_lens), _ptr(free_pages), free_pages.numel(), int(page_size),
+                               _ptr(block_table), block_table.stride(0), block_table.shape[1], slots.numel(),
+                               _ptr(q_starts), _ptr(kv_lens), _ptr(slots), _ptr(positions), _ptr(info), _ptr(n_used),
+                               _stream(stream)))
+
+
+def _check_table(block_table: torch.Tensor, n: int):
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != n \
+            or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise ValueError(f"block_table must be int32 [{n}][entries] with unit entry stride")
+
+
+def cb_rope_axes(cache_in: torch.Tensor, cache_out: torch.Tensor, rope: CbRopeAxesSpec, inverse: bool = False, stream=None):
+    """Turn (inverse: turn back) the K rows of a cache by explicit positions of several axes
+    (:func:`rope_axes_spec`) into cache_out (may be cache_in); V rows copied."""
+    iv, ov = cache_view(cache_in), cache_view(cache_out)
+    _check_axes_tokens(rope, cache_in.shape[2] * cache_in.shape[4])
+    _on_current_device(cache_in=cache_in, cache_out=cache_out, table=rope._keep[0], positions=rope._keep[1])
+    _check(_lib.cb_rope_axes(ctypes.byref(iv), ctypes.byref(ov), ctypes.byref(rope), int(bool(inverse)), _stream(stream)))
+
+
+def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer: int = 0,
+                  rope: Optional[CbRopeAxesSpec] = None, q: Optional[torch.Tensor] = None,
+                  q_out: Optional[torch.Tensor] = None, stream=None):
+    """Write the K and V rows of a cache tensor into the pool's layers ``layer`` ... at ``slots`` (int32, one per
+    token, -1 skips it); ``rope`` turns the keys before their rounding, and the queries q [token][head][dim] into
+    q_out."""
+    n = rows.shape[2] * rows.shape[4] if rows.dim() == 6 else 0
+    rv = cache_view(rows)
+    _ints(slots, n, "slots")
+    _check_axes_tokens(rope, n)
+    qv = None if q is None else _rows_view(q, "q")
+    ov = None if q_out is None else _rows_view(q_out, "q_out")
+    _on_current_device(rows=rows, pages=pages._keep[0], scales=pages._keep[1], slots=slots, q=q, q_out=q_out,
+                       table=None if rope is None else rope._keep[0], positions=None if rope is None else rope._keep[1])
+    _check(_lib.cb_page_write(ctypes.byref(rv), ctypes.byref(pages), int(layer), _ptr(slots),
+                              None if rope is None else ctypes.byref(rope), None if qv is None else ctypes.byref(qv),
+                              None if ov is None else ctypes.byref(ov), _stream(stream)))
+
+
+def cb_attn_paged_workspace_bytes(n_tokens: int, n_reqs: int, n_qheads: int, n_heads: int, head_dim: int,
+                                  max_q_len: int) -> int:
+    """Workspace bytes with which :func:`cb_attn_paged` splits long rows as far as it wants to."""
+    return int(_lib.cb_attn_paged_workspace_bytes(int(n_tokens), int(n_reqs), int(n_qheads), int(n_heads), int(head_dim),
+                                                  int(max_q_len)))
+
+
+def cb_attn_paged(q: torch.Tensor, pages: CbPages, layer: int, q_starts: torch.Tensor, kv_lens: torch.Tensor,
+                  block_table: torch.Tensor, out: torch.Tensor, max_q_len: int, scale: Optional[float] = None,
+                  window: int = 0, sinks: int = 0, lse: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None):
+    """out[t, u] = attention of query q[t, u] over its request's visible keys in the pool's ``layer`` (the new tokens
+    are the last of kv_lens; causal, optionally the last ``window`` keys and the first ``sinks`` only).  ``scale``
+    defaults to head_dim ** -0.5; ``lse`` float32 [token][head] gets the log of each row's sum of weights."""
+    n = kv_lens.numel()
+    qv, ov = _rows_view(q, "q"), _rows_view(out, "out")
+    _ints(q_starts, n + 1, "q_starts")
+    _ints(kv_lens, n, "kv_lens")
+    _check_table(block_table, n)
+    if lse is not None:
+        _need(lse, (q.shape[0], q.shape[1]), torch.float32, "lse")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _on_current_device(q=q, pages=pages._keep[0], scales=pages._keep[1], q_starts=q_starts, kv_lens=kv_lens,
+                       block_table=block_table, out=out, lse=lse, workspace=workspace)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.cb_attn_paged(ctypes.byref(qv), ctypes.byref(pages), int(layer), n, _ptr(q_starts), _ptr(kv_lens),
+                              _ptr(block_table), block_table.stride(0), block_table.shape[1], ctypes.byref(ov),
+                              int(max_q_len), float(q.shape[2] ** -0.5 if scale is None else scale), int(window), int(sinks),
+                              _ptr(lse), _ptr(workspace), int(ws_bytes), _stream(stream)))

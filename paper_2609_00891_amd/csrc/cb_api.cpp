@@ -310,6 +310,12 @@ cb::ReduceArgs reduce_args(const cb_plan *p, const cb::StatsArgs &a) {
 
 }  // namespace
 
+namespace cb {
+cb_status api_error(cb_status s, const char *message) { return fail(s, "%s", message); }
+cb_status api_ok() { return ok(); }
+cb_status api_check_cache(const char *name, const cb_cache *c, int L, int H, int d) { return check_cache(name, c, L, H, d); }
+}  // namespace cb
+
 extern "C" {
 
 const char *cb_status_string(cb_status s) {

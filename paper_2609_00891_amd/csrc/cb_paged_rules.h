@@ -1,0 +1,93 @@
+// cb_paged_rules.h -- how attention over pages is cut into workgroups: rules on
+// lengths that every workgroup evaluates for itself from the requests' lengths
+// on the device (so no plan has to be built or kept), shared with the host that
+// sizes grids and workspaces, and free of the HIP runtime so that they can be
+// checked on the CPU.
+#pragma once
+#include <cstdint>
+
+#ifdef __HIPCC__
+#define CB_HD __host__ __device__ __forceinline__
+#else
+#define CB_HD inline
+#endif
+
+namespace cb {
+
+// Rows of a request (new token i, query head of one KV head) are numbered
+// i * G + head; a row tile holds M of them.  Keys are visited in tiles of KT.
+// The keys that some row of a row tile sees: tiles 0 .. sink - 1 (the first
+// tokens that stay visible) and first .. first + n - sink - 1, as one list v =
+// 0 .. n - 1.
+struct KeyTiles {
+    int32_t n, sink, first;
+    CB_HD int32_t tile(int32_t v) const { return v < sink ? v : v - sink + first; }
+};
+
+// p_lo, p_hi: positions of the first and last row of the tile (p_hi may be
+// negative: nothing to see).
+CB_HD KeyTiles key_tiles(int32_t p_lo, int32_t p_hi, int32_t window, int32_t n_sinks, int32_t KT) {
+    KeyTiles k = {0, 0, 0};
+    if (p_hi < 0) return k;
+    const int32_t end = p_hi / KT + 1;
+    if (window > 0 && p_lo - window + 1 > 0) {
+        const int32_t lo = p_lo - window + 1;
+        k.first = lo / KT;
+        const int32_t s = n_sinks < lo ? n_sinks : lo;
+        k.sink = s > 0 ? (s - 1) / KT + 1 : 0;
+        if (k.sink >= k.first) k.sink = k.first = 0;
+    }
+    k.n = k.sink + end - k.first;
+    return k;
+}
+
+// Bound on the key tiles of any of a request's row tiles: the work that one of
+// them stands for where work is divided (tokens: most tokens in a row tile).
+CB_HD int64_t key_tiles_bound(int32_t kv_len, int32_t tokens, int32_t window, int32_t n_sinks, int32_t KT) {
+    const int64_t all = ((int64_t)kv_len + KT - 1) / KT;
+    if (window <= 0) return all;
+    const int64_t w = ((int64_t)window + tokens + KT - 2) / KT + 1 + ((int64_t)n_sinks + KT - 1) / KT;
+    return w < all ? w : all;
+}
+
+// Key tiles of one part when W = sum of (row tiles x bound) over the requests is
+// to make about `target` workgroups with H heads, at least c_min.
+CB_HD int64_t part_tiles(int64_t W, int32_t H, int32_t target, int32_t c_min) {
+    if (target <= 0) return INT64_MAX;
+    const int64_t c = (W * H + target - 1) / target;
+    return c > c_min ? c : c_min;
+}
+
+// Parts of a row tile with `bound` key tiles.  A tile in two parts or more has
+// bound > c, so parts < 2 bound / c: over all requests the parts of divided
+// tiles are fewer than 2 target / H, and the parts beyond the first fewer than
+// target / H.  (Workspace and grid are sized by these.)
+CB_HD int32_t parts_of(int64_t bound, int64_t c) { return bound <= c ? 1 : (int32_t)((bound + c - 1) / c); }
+
+// Part s of `parts` of a list of n key tiles: v in [begin, end).
+CB_HD int32_t part_begin(int32_t n, int32_t s, int32_t parts) { return (int32_t)((int64_t)n * s / parts); }
+
+// What a request is to one of the two kernels: those with row_min < rows <= row_max.
+struct RequestWork {
+    int32_t tiles;   // row tiles, 0: not this kernel's
+    int32_t tokens;  // most tokens in a row tile
+    int64_t bound;   // key tiles of a row tile
+};
+CB_HD RequestWork request_work(int32_t q_len, int32_t kv_len, int32_t G, int32_t M, int32_t KT, int64_t row_min,
+                               int64_t row_max, int32_t window, int32_t n_sinks) {
+    RequestWork w = {0, 0, 0};
+    const int64_t rows = (int64_t)q_len * G;
+    if (rows <= row_min || rows > row_max) return w;
+    w.tiles = (int32_t)((rows + M - 1) / M);
+    const int32_t t = (M - 1) / G + 2;
+    w.tokens = t < q_len ? t : q_len;
+    w.bound = key_tiles_bound(kv_len, w.tokens, window, n_sinks, KT);
+    return w;
+}
+
+// Host side: row tiles that requests of n_tokens tokens can have together.
+inline int64_t row_tiles_bound(int64_t n_tokens, int64_t n_reqs, int64_t G, int64_t M) {
+    return n_tokens * G / M + n_reqs;
+}
+
+}  // namespace cb
