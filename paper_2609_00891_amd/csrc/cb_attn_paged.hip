@@ -35,6 +35,9 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 
+#ifndef CB_SCHED
+#define CB_SCHED 0
+#endif
 constexpr int kKT = 32;                 // keys of a tile
 constexpr int kPartMin = 8;             // least key tiles of a part: two for each of the four waves
 constexpr int kTarget = 2048;           // workgroups that long rows are divided into
@@ -52,6 +55,16 @@ __device__ __forceinline__ bf16x8_t frag(uint32_t a, uint32_t b, uint32_t c, uin
 // Whether one of the two bf16 values is an infinity or a NaN.
 __device__ __forceinline__ bool not_finite(uint32_t u) {
     return (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
+}
+// The bits of the bf16 values, and of the e4m3 ones, that are infinities or NaNs.
+__device__ __forceinline__ uint32_t not_finite_halves(uint32_t u) {
+    return ((u & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((u & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t u) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int b = 0; b < 32; b += 8) r |= ((u >> b) & 0x7fu) == 0x7fu ? 0xffu << b : 0u;
+    return r;
 }
 // Two e4m3 values (exact in bf16).
 template <bool HI> __device__ __forceinline__ uint32_t e4m3_pair(uint32_t u) {
@@ -78,14 +91,14 @@ struct SchedLds { int64_t wsum[4]; Item item; int32_t found; };
 
 // The row tile and part of index `idx` (JOIN: of the idx-th row tile in more
 // than one part), or false behind the last.
-template <int M, bool JOIN>
+template <int M, int KT, bool JOIN>
 __device__ __forceinline__ bool find_item(const PagedArgs &a, int64_t idx, SchedLds &sh, Item &out) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     auto work_of = [&](int r) __attribute__((always_inline)) {
         RequestWork w = {0, 0, 0};
         if (r < a.n_reqs) {
             const Request q = request(a, r);
-            w = request_work(q.q_len, q.kv_len, (int32_t)a.G.d, M, kKT, a.c.row_min, a.c.row_max, a.window, a.n_sinks);
+            w = request_work(q.q_len, q.kv_len, (int32_t)a.G.d, M, KT, a.c.row_min, a.c.row_max, a.window, a.n_sinks);
         }
         return w;
     };
@@ -169,7 +182,7 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
     __shared__ float ml[4][16][2];
     const int head = (int)(blockIdx.x % (uint32_t)a.n_heads);
     Item it;
-    if (!find_item<M, false>(a, blockIdx.x / (uint32_t)a.n_heads, sched, it)) return;
+    if (!find_item<M, kKT, false>(a, blockIdx.x / (uint32_t)a.n_heads, sched, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -462,17 +475,359 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
     }
 }
 
+// ------------------------------------------------------------------ tile kernel
+
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+// Key of accumulator register v in lane half h of S^T's 32-key subtile.
+__device__ __forceinline__ int acc_key(int v, int h) { return 8 * (v >> 2) + 4 * h + (v & 3); }
+
+// A NaN among the three is the maximum (v_maximum3_f32: no extra instruction quiets its operands).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
+template <int D, int RT, bool F8>
+__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedArgs a) {
+    constexpr int M = 128 * RT, KT = 64, NS = D / 16, ND = D / 32;
+    constexpr int KS = 2 * D + 16, VS = 2 * D + 32;            // bytes between rows of K and V in LDS
+    constexpr int CPR = F8 ? D / 16 : D / 8;                   // 16-byte pieces of a row in memory
+    constexpr int NP = (KT * CPR + 255) / 256;                 // pieces of a thread, for each of K and V
+    constexpr bool RAGGED = KT * CPR % 256 != 0;
+    constexpr int STAGE = KT * (KS + VS);
+    constexpr float kLag = 8.f;
+    __shared__ SchedLds sched;
+    __shared__ int32_t odd;
+    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
+    const int head = (int)(blockIdx.x % (uint32_t)a.n_heads);
+    Item it;
+    if (!find_item<M, KT, false>(a, blockIdx.x / (uint32_t)a.n_heads, sched, it)) return;
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, h = lane >> 5;
+    const Request rq = request(a, it.req);
+    const int32_t G = (int32_t)a.G.d;
+    const int32_t row0 = it.tile * M;
+    const int32_t n_rows = (int32_t)min((int64_t)rq.q_len * G - row0, (int64_t)M);
+    const int32_t base = rq.kv_len - rq.q_len;                 // position of new token 0
+    const int32_t p_lo = base + (int32_t)fast_div((uint32_t)row0, a.G);
+    const int32_t p_hi = base + (int32_t)fast_div((uint32_t)(row0 + n_rows - 1), a.G);
+    const KeyTiles kt = key_tiles(p_lo, p_hi, a.window, a.n_sinks, KT);
+    const int32_t v0 = part_begin(kt.n, it.part, it.parts), v1 = part_begin(kt.n, it.part + 1, it.parts);
+    const int32_t *table = a.table + it.req * a.table_stride;
+    const char *kp = a.k + head * a.s_head, *vp = a.v + head * a.s_head;
+    // weights are exp2(c2 s - m) with c2 > 0: a negative scale turns the queries' signs, and a zero
+    // one becomes the least number (a masked score, -infinity, stays what it is)
+    float c2 = F8 ? a.scale_log2 * a.kscale[head] : a.scale_log2;
+    const uint32_t flip = c2 < 0.f ? 0x80008000u : 0u;
+    c2 = fmaxf(fabsf(c2), 1.17549435e-38f);
+    if (tid == 0) odd = 0;
+
+    // queries of this wave's RT subtiles of 32 rows (rows behind the last repeat it)
+    bf16x8_t qf[RT][NS];
+    int32_t pos[RT];                                           // of the lane's rows
+    const int w0 = 32 * RT * wave;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int32_t row = row0 + min(w0 + 32 * rt + n, n_rows - 1);
+        const int32_t tok = (int32_t)fast_div((uint32_t)row, a.G), u = row - tok * G;
+        pos[rt] = base + tok;
+        const uint16_t *q = a.q + (int64_t)(rq.row0 + tok) * a.q_tok + (int64_t)(head * G + u) * a.q_head;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const uint4 x = *(const uint4 *)(q + 16 * s + 8 * h);
+            qf[rt][s] = frag(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+        }
+    }
+    const int32_t s_lo = __builtin_amdgcn_readfirstlane(pos[0]);
+    const int32_t s_hi = __builtin_amdgcn_readlane(pos[RT - 1], 31);
+
+    // the places of a tile's 64 rows: lane l looks up key l
+    auto locate = [&](int32_t tile, uint64_t &there) __attribute__((always_inline)) {
+        const int32_t key = tile * KT + lane;
+        bool ok = key < rq.kv_len;
+        uint32_t off = 0;
+        if (ok) {
+            const uint32_t idx = fast_div((uint32_t)key, a.page_size);
+            const int32_t page = table[idx];
+            ok = page >= 0 && page < a.n_pages;
+            if (ok) off = (uint32_t)page * a.s_page + ((uint32_t)key - idx * a.page_size.d) * a.s_tok;
+        }
+        there = __ballot(ok);
+        return off;
+    };
+    uint4 kr[NP], vr[NP];
+    auto load = [&](uint32_t off) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int id = tid + 256 * i;
+            const int row = id / CPR, c = id - row * CPR;
+            const uint64_t at = (uint64_t)(uint32_t)__shfl((int)off, row & 63) * 16 + 16 * c;
+            if (RAGGED && id >= KT * CPR) continue;
+            kr[i] = *(const uint4 *)(kp + at);
+            vr[i] = *(const uint4 *)(vp + at);
+        }
+    };
+    // In a tile with a key that some row does not see (edge) a NaN or infinity of V would meet zero
+    // weights: it becomes a zero here and reaches the rows that see it after the last tile.  V's rows
+    // that are not there become zeros as well.
+    auto store = [&](int st, uint64_t there, bool edge) __attribute__((always_inline)) {
+        char *ks = lds + st * STAGE, *vs = ks + KT * KS;
+        if (edge) {
+            asm volatile("");
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int id = tid + 256 * i, row = id / CPR;
+                const bool is = (there >> (row & 63)) & 1;
+                uint32_t v4[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t bad;                              // the bits of the values that are no number
+                    if constexpr (F8) bad = nan_bytes(v4[w]);
+                    else bad = not_finite_halves(v4[w]);
+                    if (is && bad) odd = 1;
+                    v4[w] = is ? v4[w] & ~bad : 0u;
+                }
+                vr[i] = make_uint4(v4[0], v4[1], v4[2], v4[3]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int id = tid + 256 * i;
+            if (RAGGED && id >= KT * CPR) continue;
+            const int row = id / CPR, c = id - row * CPR;
+            if constexpr (F8) {
+                const uint32_t k4[4] = {kr[i].x, kr[i].y, kr[i].z, kr[i].w}, v4[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const uint32_t k0 = k4[2 * w], k1 = k4[2 * w + 1], x0 = v4[2 * w], x1 = v4[2 * w + 1];
+                    *(uint4 *)(ks + row * KS + 32 * c + 16 * w) =
+                        make_uint4(e4m3_pair<false>(k0), e4m3_pair<true>(k0), e4m3_pair<false>(k1), e4m3_pair<true>(k1));
+                    *(uint4 *)(vs + row * VS + 32 * c + 16 * w) =
+                        make_uint4(e4m3_pair<false>(x0), e4m3_pair<true>(x0), e4m3_pair<false>(x1), e4m3_pair<true>(x1));
+                }
+            } else {
+                *(uint4 *)(ks + row * KS + 16 * c) = kr[i];
+                *(uint4 *)(vs + row * VS + 16 * c) = vr[i];
+            }
+        }
+    };
+    // every key of the tile is there and seen by every row from position lo to hi
+    auto seen = [&](int32_t k0, uint64_t there, int32_t lo, int32_t hi) __attribute__((always_inline)) {
+        return there == ~0ull && k0 + KT - 1 <= lo && (a.window == 0 || k0 > hi - a.window || k0 + KT <= a.n_sinks);
+    };
+
+    f32x16_t o[RT][ND];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = -HUGE_VALF;
+        l[rt] = 0.f;
+#pragma unroll
+        for (int q = 0; q < ND; ++q) o[rt][q] = f32x16_t{};
+    }
+    // V^T operand: keys 16 kk + 4 h + {0 .. 3} and + 8, channel 32 q + (lane & 31)
+    const int vt = (4 * h + ((lane >> 2) & 3)) * VS + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+
+    uint64_t there = 0, there_n = 0;
+    if (v0 < v1) {
+        load(locate(kt.tile(v0), there));
+        __syncthreads();                                       // odd is set
+        store(0, there, !seen(kt.tile(v0) * KT, there, p_lo, p_hi));
+    }
+    __syncthreads();
+    for (int32_t v = v0; v < v1; ++v) {
+        const int st = (v - v0) & 1;
+        const int32_t k0 = kt.tile(v) * KT;
+        if (v + 1 < v1) load(locate(kt.tile(v + 1), there_n));
+        const char *ks = lds + st * STAGE, *vs = ks + KT * KS;
+        f32x16_t s[RT][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][t] = f32x16_t{};
+#pragma unroll
+            for (int q = 0; q < NS; ++q) {
+                const bf16x8_t kf = *(const bf16x8_t *)(ks + (32 * t + n) * KS + 32 * q + 16 * h);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    s[rt][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[rt][q], s[rt][t], 0, 0, 0);
+            }
+        }
+#if CB_SCHED & 1
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * NS - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, RT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4 * RT, 0);
+#endif
+        if (!seen(k0, there, s_lo, s_hi)) {
+            asm volatile("");                                  // a branch, not selects on every tile
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                // key k0 + 4 h + c is register e's, c = 32 (e >> 4) + acc_key(e & 15, 0)
+                const int hi = pos[rt] - k0 - 4 * h, lo = a.window == 0 ? INT32_MIN : hi - a.window;
+                const int sink = a.n_sinks - k0 - 4 * h;
+                const uint64_t bits = there >> (4 * h);
+                const uint32_t bit2[2] = {(uint32_t)bits, (uint32_t)(bits >> 32)};
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const int c = 32 * (e >> 4) + acc_key(e & 15, 0);
+                    const bool see = (bit2[e >> 4] & (1u << (c & 31))) && c <= hi && (c > lo || c < sink);
+                    s[rt][e >> 4][e & 15] = see ? s[rt][e >> 4][e & 15] : -HUGE_VALF;
+                }
+            }
+        }
+        uint32_t pk[RT][16];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float mx = max3(s[rt][0][0], s[rt][0][1], s[rt][0][2]);
+#pragma unroll
+            for (int e = 3; e < 31; e += 2) mx = max3(mx, s[rt][e >> 4][e & 15], s[rt][(e + 1) >> 4][(e + 1) & 15]);
+            mx = max3(mx, s[rt][1][15], s[rt][1][15]);
+            mx = max3(mx, __shfl_xor(mx, 32), mx) * c2;
+            // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
+            if (__any(mx > m[rt] + kLag)) {
+                const float mn = fmaxf(m[rt], mx);
+                const float al = __builtin_amdgcn_exp2f(m[rt] - (mn == -HUGE_VALF ? 0.f : mn));
+                m[rt] = mn;
+                l[rt] *= al;
+#pragma unroll
+                for (int q = 0; q < ND; ++q) o[rt][q] *= al;
+            }
+            const float ref = m[rt] == -HUGE_VALF ? 0.f : m[rt];
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e >> 3][2 * e & 15], c2, -ref));
+                const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e >> 3][(2 * e & 15) + 1], c2, -ref));
+                sum += x0;
+                sum += x1;
+                pk[rt][e] = pack_bf16(x0, x1);
+            }
+            l[rt] += sum;
+        }
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+            for (int q = 0; q < ND; ++q) {
+                const char *pp = vs + vt + 16 * kk * VS + 64 * q;
+                const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)pp);
+                const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(pp + 8 * VS));
+                typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+                const s16x8_t v8 = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    o[rt][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(bf16x8_t, v8),
+                        frag(pk[rt][4 * kk], pk[rt][4 * kk + 1], pk[rt][4 * kk + 2], pk[rt][4 * kk + 3]), o[rt][q], 0, 0, 0);
+            }
+        }
+#if CB_SCHED & 2
+        // a quarter of the weights, then its products beside the next quarter
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+        __builtin_amdgcn_sched_group_barrier(0x402, 28, 1);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+#pragma unroll
+            for (int q = 0; q < ND; ++q) {
+                __builtin_amdgcn_sched_group_barrier(0x008, RT, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+                __builtin_amdgcn_sched_group_barrier(0x402, 28 / ND, 1);
+            }
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * RT, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * RT, 1);
+#endif
+        if (v + 1 < v1) store(st ^ 1, there_n, !seen(kt.tile(v + 1) * KT, there_n, p_lo, p_hi));
+        there = there_n;
+        __syncthreads();
+    }
+    if (odd) {
+        // NaNs and infinities of V that were left out of tiles which some row does not see whole: they
+        // come to the rows that see their keys (whatever finite weight they have)
+#pragma unroll 1
+        for (int32_t v = v0; v < v1; ++v) {
+            const int32_t k0 = kt.tile(v) * KT;
+            const uint32_t off = locate(kt.tile(v), there);
+            if (seen(k0, there, p_lo, p_hi)) continue;
+#pragma unroll 1
+            for (int kk = 0; kk < KT; ++kk) {
+                if (!((there >> kk) & 1)) continue;
+                const char *vrow = vp + (uint64_t)(uint32_t)__shfl((int)off, kk) * 16;
+                const int32_t key = k0 + kk;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const bool see = key <= pos[rt] && (a.window == 0 || key > pos[rt] - a.window || key < a.n_sinks);
+#pragma unroll
+                    for (int q = 0; q < ND; ++q)
+#pragma unroll
+                        for (int r = 0; r < 16; r += 2) {
+                            const int c = 32 * q + acc_key(r, h);
+                            const uint32_t u = F8 ? e4m3_pair<false>(*(const uint16_t *)(vrow + c)) : *(const uint32_t *)(vrow + 2 * c);
+                            if (see && not_finite(u & 0xffffu)) o[rt][q][r] += bf_lo(u);
+                            if (see && not_finite(u & 0xffff0000u)) o[rt][q][r + 1] += bf_hi(u);
+                        }
+                }
+            }
+        }
+    }
+
+    const float vsc = F8 ? a.vscale[head] : 1.f;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int rr = w0 + 32 * rt + n;
+        const float lr = l[rt] + __shfl_xor(l[rt], 32);
+        if (rr >= n_rows) continue;
+        if (it.parts > 1) {
+            float *w = a.c.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
+#pragma unroll
+            for (int q = 0; q < ND; ++q)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *(float4 *)(w + rr * D + 32 * q + acc_key(r, h)) =
+                        make_float4(o[rt][q][r], o[rt][q][r + 1], o[rt][q][r + 2], o[rt][q][r + 3]);
+            if (h == 0) {
+                w[M * D + rr] = m[rt];
+                w[M * D + M + rr] = lr;
+            }
+        } else {
+            const int32_t tok = (int32_t)fast_div((uint32_t)(row0 + rr), a.G), u = row0 + rr - tok * G;
+            uint16_t *out = a.out + (int64_t)(rq.row0 + tok) * a.o_tok + (int64_t)(head * G + u) * a.o_head;
+            const float inv = vsc / lr;
+#pragma unroll
+            for (int q = 0; q < ND; ++q)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    uint2 y = make_uint2(pack_bf16(o[rt][q][r] * inv, o[rt][q][r + 1] * inv),
+                                         pack_bf16(o[rt][q][r + 2] * inv, o[rt][q][r + 3] * inv));
+                    if (lr == 0.f) y = make_uint2(0u, 0u);
+                    *(uint2 *)(out + 32 * q + acc_key(r, h)) = y;
+                }
+            if (a.lse && h == 0)
+                a.lse[(int64_t)(rq.row0 + tok) * (a.n_heads * G) + head * G + u] =
+                    lr == 0.f ? -HUGE_VALF : 0.6931471805599453f * (m[rt] + __log2f(lr));
+        }
+    }
+}
+
 // ------------------------------------------------------------------ joining parts
 
 // One workgroup per 16 rows of a row tile that went in parts: their partial
 // sums, brought to the common maximum and added in the order of the parts.
-template <int D, int M, bool F8>
+template <int D, int M, int KT, bool F8>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
     __shared__ SchedLds sched;
     const int head = (int)(blockIdx.x % (uint32_t)a.n_heads);
     Item it;
     const int64_t idx = blockIdx.x / (uint32_t)a.n_heads;
-    if (!find_item<M, true>(a, idx / (M / 16), sched, it)) return;
+    if (!find_item<M, KT, true>(a, idx / (M / 16), sched, it)) return;
     const int tid = threadIdx.x;
     const Request rq = request(a, it.req);
     const int32_t G = (int32_t)a.G.d;
@@ -508,42 +863,67 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
             lr == 0.f ? -HUGE_VALF : 0.6931471805599453f * (mx + __log2f(lr));
 }
 
-template <int D, bool F8>
-hipError_t launch(PagedArgs a, void *ws, int64_t ws_bytes, hipStream_t s) {
-    constexpr int M = 16;
-    const int64_t G = a.G.d;
+constexpr int kSmallRows = 16;          // rows of a request up to which attn_rows_kernel takes it beside the tile kernel
+constexpr int kTileTarget = 512;        // workgroups of the tile kernel that long rows are divided into
+#ifndef CB_RT
+#define CB_RT 1
+#endif
+constexpr int kRT = CB_RT, kTileM = 128 * kRT;
+
+// One kernel over its requests, and the joining of their parts.
+template <int D, int M, int KT, bool F8, typename K>
+hipError_t launch_class(PagedArgs a, K kernel, int target, int64_t row_min, int64_t row_max, char *&ws, int64_t &ws_bytes,
+                        hipStream_t s) {
     const int64_t slot = (int64_t)M * (D + 2) * 4;
-    a.c.row_min = 0;
-    a.c.row_max = INT64_MAX;
-    a.c.target = (int32_t)(ws ? std::min<int64_t>(kTarget, ws_bytes / (2 * slot)) : 0);
-    a.c.ws = (float *)ws;
+    a.c.row_min = row_min;
+    a.c.row_max = row_max;
+    a.c.target = (int32_t)std::min<int64_t>(target, ws_bytes / (2 * slot));
     // no row is long enough to be divided
-    if ((int64_t)a.table_width * a.page_size.d <= (int64_t)kPartMin * kKT) a.c.target = 0;
-    const int64_t tiles = row_tiles_bound(a.n_tokens, a.n_reqs, G, M);
+    if ((int64_t)a.table_width * a.page_size.d <= (int64_t)kPartMin * KT) a.c.target = 0;
+    a.c.ws = (float *)ws;
+    ws += 2 * slot * a.c.target;
+    ws_bytes -= 2 * slot * a.c.target;
+    const int64_t tiles = row_tiles_bound(a.n_tokens, a.n_reqs, a.G.d, M);
     const int64_t items = (tiles + a.c.target / a.n_heads) * a.n_heads;
     const int64_t join = std::min<int64_t>(tiles, a.c.target / a.n_heads) * (M / 16) * a.n_heads;
     if (items > INT32_MAX || join > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((attn_rows_kernel<D, 1, F8>), dim3((unsigned)items), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
-    if (join > 0) hipLaunchKernelGGL((attn_join_kernel<D, M, F8>), dim3((unsigned)join), dim3(256), 0, s, a);
+    if (join > 0) hipLaunchKernelGGL((attn_join_kernel<D, M, KT, F8>), dim3((unsigned)join), dim3(256), 0, s, a);
     return hipGetLastError();
+}
+
+template <int D, bool F8>
+hipError_t launch(PagedArgs a, int32_t max_q_len, void *ws, int64_t ws_bytes, hipStream_t s) {
+    const int64_t G = a.G.d;
+    char *w = (char *)ws;
+    // few rows everywhere: the rows kernel alone, whatever the lengths turn out to be
+    if ((int64_t)max_q_len * G <= 32)
+        return launch_class<D, 16, kKT, F8>(a, attn_rows_kernel<D, 1, F8>, kTarget, 0, INT64_MAX, w, ws_bytes, s);
+    int64_t least = 0;
+    if (G <= kSmallRows && a.n_reqs > 1) {
+        least = kSmallRows;
+        if (hipError_t e = launch_class<D, 16, kKT, F8>(a, attn_rows_kernel<D, 1, F8>, kTarget, 0, least, w, ws_bytes, s)) return e;
+    }
+    return launch_class<D, kTileM, 64, F8>(a, attn_tile_kernel<D, kRT, F8>, kTileTarget, least, INT64_MAX, w, ws_bytes, s);
 }
 
 }  // namespace
 
 int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_tokens, int32_t n_reqs, int32_t max_q_len) {
-    return (int64_t)2 * kTarget * 16 * (d + 2) * 4;
+    const int64_t rows = (int64_t)2 * kTarget * 16 * (d + 2) * 4, tile = (int64_t)2 * kTileTarget * kTileM * (d + 2) * 4;
+    return (int64_t)max_q_len * G <= 32 ? rows : rows + tile;
 }
 
 hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, bool f8, int32_t max_q_len, void *ws, int64_t ws_bytes,
                              hipStream_t s) {
     switch (d * 2 + f8) {
-        case 128: return launch<64, false>(a, ws, ws_bytes, s);
-        case 129: return launch<64, true>(a, ws, ws_bytes, s);
-        case 192: return launch<96, false>(a, ws, ws_bytes, s);
-        case 193: return launch<96, true>(a, ws, ws_bytes, s);
-        case 256: return launch<128, false>(a, ws, ws_bytes, s);
-        case 257: return launch<128, true>(a, ws, ws_bytes, s);
+        case 128: return launch<64, false>(a, max_q_len, ws, ws_bytes, s);
+        case 129: return launch<64, true>(a, max_q_len, ws, ws_bytes, s);
+        case 192: return launch<96, false>(a, max_q_len, ws, ws_bytes, s);
+        case 193: return launch<96, true>(a, max_q_len, ws, ws_bytes, s);
+        case 256: return launch<128, false>(a, max_q_len, ws, ws_bytes, s);
+        case 257: return launch<128, true>(a, max_q_len, ws, ws_bytes, s);
     }
     return hipErrorInvalidValue;
 }
