@@ -31,16 +31,24 @@ namespace cb {
 namespace {
 
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 
+#define CB_IL 1
+#define CB_PRIO 1
 #ifndef CB_SCHED
-#define CB_SCHED 0
+#define CB_SCHED 1
 #endif
 constexpr int kKT = 32;                 // keys of a tile
 constexpr int kPartMin = 8;             // least key tiles of a part: two for each of the four waves
-constexpr int kTarget = 2048;           // workgroups that long rows are divided into
+constexpr float kLag = 8.f;              // log2 by which the maximum in use may lag the true one
+#ifndef CB_T
+#define CB_T 2048
+#endif
+constexpr int kTarget = CB_T;           // workgroups that long rows are divided into
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     f32x2_t v = {lo, hi};
@@ -56,15 +64,15 @@ __device__ __forceinline__ bf16x8_t frag(uint32_t a, uint32_t b, uint32_t c, uin
 __device__ __forceinline__ bool not_finite(uint32_t u) {
     return (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
 }
-// The bits of the bf16 values, and of the e4m3 ones, that are infinities or NaNs.
+// The bits of the bf16 values, and of the e4m3 ones, that are infinities or NaNs: an exponent (e4m3:
+// a magnitude) of all ones carries into the sign's place when one is added to it.
 __device__ __forceinline__ uint32_t not_finite_halves(uint32_t u) {
-    return ((u & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((u & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+    const uint32_t t = ((u & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    return t | (t - (t >> 15));
 }
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t u) {
-    uint32_t r = 0;
-#pragma unroll
-    for (int b = 0; b < 32; b += 8) r |= ((u >> b) & 0x7fu) == 0x7fu ? 0xffu << b : 0u;
-    return r;
+    const uint32_t t = ((u & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    return t | (t - (t >> 7));
 }
 // Two e4m3 values (exact in bf16).
 template <bool HI> __device__ __forceinline__ uint32_t e4m3_pair(uint32_t u) {
@@ -213,56 +221,74 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
     }
     const float c2 = F8 ? a.scale_log2 * a.kscale[head] : a.scale_log2;
 
-    // where the rows of a tile's keys are: lane's key 32 tile + (lane & 31), its place in 16-byte units
-    uint32_t off = 0, there = 0;                               // there: bit per key, its page is in the pool
-    auto locate = [&](int32_t tile) __attribute__((always_inline)) {
+    // where the rows of a tile's keys are: lane's key 32 tile + (lane & 31), a tile ahead of the loads
+    int32_t page = 0;
+    uint32_t in_page = 0, off = 0;
+    bool in_kv = false;
+    auto look_up = [&](int32_t tile) __attribute__((always_inline)) {
         const int32_t key = tile * kKT + (lane & 31);
-        bool ok = key < rq.kv_len;
-        off = 0;
-        if (ok) {
-            const uint32_t idx = fast_div((uint32_t)key, a.page_size);
-            const int32_t page = table[idx];
-            ok = page >= 0 && page < a.n_pages;
-            if (ok) off = (uint32_t)page * a.s_page + ((uint32_t)key - idx * a.page_size.d) * a.s_tok;
-        }
-        there = (uint32_t)__ballot(ok);
+        in_kv = key < rq.kv_len;
+        const uint32_t k = (uint32_t)min(key, rq.kv_len - 1);
+        const uint32_t idx = fast_div(k, a.page_size);
+        in_page = k - idx * a.page_size.d;
+        page = table[idx];
+    };
+    // off: the row's place in 16-byte units (of a row that is not there: the pool's first); returns a
+    // bit per key whose row is there
+    uint32_t ko[2], vo[8];                                     // places of the rows that this lane loads from
+    auto place = [&]() __attribute__((always_inline)) {
+        const bool ok = in_kv && (uint32_t)page < (uint32_t)a.n_pages;
+        off = (ok ? (uint32_t)page : 0u) * a.s_page + (ok ? in_page : 0u) * a.s_tok;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) ko[t] = (uint32_t)__shfl((int)off, 16 * t + n);
+        // V rows in the order of S^T's registers: place j of lane group g is key 4 g + j, 16 + 4 g + j - 4
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vo[j] = (uint32_t)__shfl((int)off, (j >> 2) * 16 + 4 * g + (j & 3));
+        return (uint32_t)__ballot(ok);
     };
     uint32_t kr[2][Ge::KW], vr[8][Ge::VW];
     auto load_k = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const char *p = kp + (uint64_t)(uint32_t)__shfl((int)off, 16 * t + n) * 16;
+            const char *p = kp + (uint64_t)ko[t] * 16;
             if constexpr (!F8 || Ge::PAIR) {
 #pragma unroll
                 for (int s = 0; s < Ge::KW / 4; ++s) {
-                    const uint4 x = *(const uint4 *)(p + 64 * s + 16 * g);
-                    kr[t][4 * s] = x.x; kr[t][4 * s + 1] = x.y; kr[t][4 * s + 2] = x.z; kr[t][4 * s + 3] = x.w;
+                    const u32x4_t x = *(const u32x4_t *)(p + 64 * s + 16 * g);
+                    kr[t][4 * s] = x[0]; kr[t][4 * s + 1] = x[1]; kr[t][4 * s + 2] = x[2]; kr[t][4 * s + 3] = x[3];
                 }
             } else {
 #pragma unroll
                 for (int s = 0; s < Ge::NS; ++s) {
-                    const uint2 x = *(const uint2 *)(p + 32 * s + 8 * g);
-                    kr[t][2 * s] = x.x; kr[t][2 * s + 1] = x.y;
+                    const u32x2_t x = *(const u32x2_t *)(p + 32 * s + 8 * g);
+                    kr[t][2 * s] = x[0]; kr[t][2 * s + 1] = x[1];
                 }
             }
         }
     };
-    // V rows in the order of S^T's registers: place j of lane group g is key 4 g + j, 16 + 4 g + j - 4
     auto load_v = [&]() __attribute__((always_inline)) {
         const int c = min(n, Ge::NC - 1);                      // 96: lanes 12 .. 15 repeat lane 11, unused
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const char *p = vp + (uint64_t)(uint32_t)__shfl((int)off, (j >> 2) * 16 + 4 * g + (j & 3)) * 16 + c * (F8 ? E : 2 * E);
+            const char *p = vp + (uint64_t)vo[j] * 16 + c * (F8 ? E : 2 * E);
             if constexpr (Ge::VW == 4) {
-                const uint4 x = *(const uint4 *)p;
-                vr[j][0] = x.x; vr[j][1] = x.y; vr[j][2] = x.z; vr[j][3] = x.w;
+                const u32x4_t x = *(const u32x4_t *)p;
+                vr[j][0] = x[0]; vr[j][1] = x[1]; vr[j][2] = x[2]; vr[j][3] = x[3];
             } else if constexpr (Ge::VW == 2) {
-                const uint2 x = *(const uint2 *)p;
-                vr[j][0] = x.x; vr[j][1] = x.y;
+                const u32x2_t x = *(const u32x2_t *)p;
+                vr[j][0] = x[0]; vr[j][1] = x[1];
             } else {
                 vr[j][0] = *(const uint32_t *)p;
             }
         }
+    };
+    auto sees = [&](int32_t key, int32_t p) __attribute__((always_inline)) {
+        return key <= p && (a.window == 0 || key > p - a.window || key < a.n_sinks);
+    };
+    // every key of the tile is there and seen by every row
+    auto whole_tile = [&](int32_t k0, uint32_t there) __attribute__((always_inline)) {
+        return there == 0xffffffffu && k0 + kKT - 1 <= p_lo &&
+               (a.window == 0 || k0 > p_hi - a.window || k0 + kKT <= a.n_sinks);
     };
 
     f32x4_t o[MT][E];
@@ -275,64 +301,98 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
         for (int i = 0; i < E; ++i) o[mt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
 
-    for (int32_t v = part_begin(kt.n, it.part, it.parts) + wave; v < v1; v += 4) {
-        const int32_t k0 = kt.tile(v) * kKT;
-        locate(kt.tile(v));
+    // A tile's K and V are requested while the tile before it is worked on: K as soon as its registers
+    // have met the queries, V as soon as its own have become operands.
+    const int32_t v0 = part_begin(kt.n, it.part, it.parts) + wave;
+    uint32_t there = 0, there_n = 0;
+    uint32_t odd = 0;
+    if (v0 < v1) {
+        look_up(kt.tile(v0));
+        there = place();
         load_k();
         load_v();
-        // every key of the tile is seen by every row
-        const bool whole = there == 0xffffffffu && k0 + kKT - 1 <= p_lo &&
-                           (a.window == 0 || k0 > p_hi - a.window || k0 + kKT <= a.n_sinks);
+        if (v0 + 4 < v1) look_up(kt.tile(v0 + 4));
+    }
+    for (int32_t v = v0; v < v1; v += 4) {
+        const int32_t k0 = kt.tile(v) * kKT;
+        const bool whole = whole_tile(k0, there);
+        f32x4_t s[MT][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) s[mt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < Ge::NS; ++st) {
+                bf16x8_t kf;
+                if constexpr (F8) {
+                    const uint32_t x = kr[t][2 * st], y = kr[t][2 * st + 1];
+                    kf = frag(e4m3_pair<false>(x), e4m3_pair<true>(x), e4m3_pair<false>(y), e4m3_pair<true>(y));
+                } else {
+                    kf = frag(kr[t][4 * st], kr[t][4 * st + 1], kr[t][4 * st + 2], kr[t][4 * st + 3]);
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) s[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][st], s[mt][t], 0, 0, 0);
+            }
+        }
+        if (v + 4 < v1) {
+            there_n = place();
+            if (v + 8 < v1) look_up(kt.tile(v + 8));
+            load_k();
+        }
         uint32_t p2[MT][4];                                    // exp2(s - m) as the operand of P V
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            f32x4_t s[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int st = 0; st < Ge::NS; ++st) {
-                    bf16x8_t kf;
-                    if constexpr (F8) {
-                        const uint32_t x = kr[t][2 * st], y = kr[t][2 * st + 1];
-                        kf = frag(e4m3_pair<false>(x), e4m3_pair<true>(x), e4m3_pair<false>(y), e4m3_pair<true>(y));
-                    } else {
-                        kf = frag(kr[t][4 * st], kr[t][4 * st + 1], kr[t][4 * st + 2], kr[t][4 * st + 3]);
-                    }
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][st], s[t], 0, 0, 0);
-                }
-            }
             float x[8];
-            float mx = m[mt];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * c2;
+            for (int e = 0; e < 8; ++e) x[e] = s[mt][e >> 2][e & 3] * c2;
             if (!whole) {
+                asm volatile("");                              // a branch, not selects on every tile
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int kk = (e >> 2) * 16 + 4 * g + (e & 3), key = k0 + kk;
-                    const bool see = ((there >> kk) & 1) && key <= pos[mt] &&
-                                     (a.window == 0 || key > pos[mt] - a.window || key < a.n_sinks);
-                    x[e] = see ? x[e] : -HUGE_VALF;
+                    const int kk = (e >> 2) * 16 + 4 * g + (e & 3);
+                    x[e] = ((there >> kk) & 1) && sees(k0 + kk, pos[mt]) ? x[e] : -HUGE_VALF;
                 }
             }
+            float mx = x[0];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[e]);
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float ref = mx == -HUGE_VALF ? 0.f : mx;     // nothing seen so far: every weight is zero
-            const float al = __builtin_amdgcn_exp2f(m[mt] - ref);
-            m[mt] = mx;
+            for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+            // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
+            if (__any(mx > m[mt] + kLag)) {
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                mx = fmaxf(mx, m[mt]);
+                const float al = __builtin_amdgcn_exp2f(m[mt] - (mx == -HUGE_VALF ? 0.f : mx));
+                m[mt] = mx;
+                l[mt] *= al;
+#pragma unroll
+                for (int i = 0; i < E; ++i) o[mt][i] *= al;
+            }
+            const float ref = m[mt] == -HUGE_VALF ? 0.f : m[mt];   // nothing seen so far: every weight is zero
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
                 sum += x[e];
             }
-            l[mt] = l[mt] * al + sum;
+            l[mt] += sum;
 #pragma unroll
             for (int q = 0; q < 4; ++q) p2[mt][q] = pack_bf16(x[2 * q], x[2 * q + 1]);
+        }
+        if (!whole) {
+            // In a tile with a key that some row does not see a NaN or infinity of V would meet zero
+            // weights: it becomes a zero here and reaches the rows that see it after the last tile.
+            // Rows that are not there become zeros as well.
+            asm volatile("");
 #pragma unroll
-            for (int i = 0; i < E; ++i) o[mt][i] *= al;
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t is = 0u - ((there >> ((j >> 2) * 16 + 4 * g + (j & 3))) & 1u);
+#pragma unroll
+                for (int w = 0; w < Ge::VW; ++w) {
+                    const uint32_t bad = F8 ? nan_bytes(vr[j][w]) : not_finite_halves(vr[j][w]);
+                    odd |= bad & is;
+                    vr[j][w] &= ~bad & is;
+                }
+            }
         }
         // V as bf16 pairs of channels
         uint32_t vb[8][E / 2];
@@ -345,67 +405,46 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
                 else
                     vb[j][w] = vr[j][w];
             }
-        bool odd = false;
-        if (!whole) {
-            // rows that are not there are zeros; and a NaN or infinity of V must not meet the zero
-            // weight of a row that does not see its key
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool is = (there >> ((j >> 2) * 16 + 4 * g + (j & 3))) & 1;
+        for (int i = 0; i < E; ++i) {
+            uint32_t f[4];
 #pragma unroll
-                for (int w = 0; w < E / 2; ++w) {
-                    vb[j][w] = is ? vb[j][w] : 0u;
-                    odd |= not_finite(vb[j][w]);
-                }
-            }
-            odd = __ballot(odd) != 0;
+            for (int q = 0; q < 4; ++q)
+                f[q] = __builtin_amdgcn_perm(vb[2 * q + 1][i >> 1], vb[2 * q][i >> 1], (i & 1) ? 0x07060302u : 0x05040100u);
+            const bf16x8_t vf = frag(f[0], f[1], f[2], f[3]);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                o[mt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(p2[mt][0], p2[mt][1], p2[mt][2], p2[mt][3]),
+                                                                  o[mt][i], 0, 0, 0);
         }
-        if (!odd) {
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                uint32_t f[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    f[q] = __builtin_amdgcn_perm(vb[2 * q + 1][i >> 1], vb[2 * q][i >> 1], (i & 1) ? 0x07060302u : 0x05040100u);
-                const bf16x8_t vf = frag(f[0], f[1], f[2], f[3]);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-                    o[mt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(p2[mt][0], p2[mt][1], p2[mt][2], p2[mt][3]),
-                                                                      o[mt][i], 0, 0, 0);
-            }
-        } else {
-            // one key after the other, for the rows that see it only
+        if (v + 4 < v1) load_v();
+        there = there_n;
+    }
+    if (__any(odd != 0)) {
+        // NaNs and infinities of V that were left out of tiles which some row does not see whole: they
+        // come to the rows that see their keys (whatever finite weight they have)
+#pragma unroll 1
+        for (int32_t v = v0; v < v1; v += 4) {
+            const int32_t k0 = kt.tile(v) * kKT;
+            look_up(kt.tile(v));
+            there = place();
+            if (whole_tile(k0, there)) continue;
+#pragma unroll 1
             for (int kk = 0; kk < kKT; ++kk) {
                 if (!((there >> kk) & 1)) continue;
-                const int src = 16 * ((kk & 15) >> 2) + n, key = k0 + kk, e = (kk >> 4) * 4 + (kk & 3);
-                const uint32_t at = (uint32_t)__shfl((int)off, kk);
-                float pk[MT];
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const uint32_t w = e < 2 ? p2[mt][0] : e < 4 ? p2[mt][1] : e < 6 ? p2[mt][2] : p2[mt][3];
-                    const float pw = (e & 1) ? bf_hi(w) : bf_lo(w);
-                    pk[mt] = __shfl(pw, src);
-                }
+                const char *vrow = vp + (uint64_t)(uint32_t)__shfl((int)off, kk) * 16;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int c = 4 * g + r;
-                    if (c >= Ge::NC) continue;
-                    float vv[E];
-                    const char *p = vp + (uint64_t)at * 16 + c * (F8 ? E : 2 * E);
+                    const int c = min(4 * g + r, Ge::NC - 1) * E;
 #pragma unroll
-                    for (int w = 0; w < E / 2; ++w) {
-                        uint32_t u;
-                        if constexpr (F8) u = e4m3_pair<false>(*(const uint16_t *)(p + 2 * w));
-                        else u = *(const uint32_t *)(p + 4 * w);
-                        vv[2 * w] = bf_lo(u);
-                        vv[2 * w + 1] = bf_hi(u);
-                    }
+                    for (int i = 0; i < E; i += 2) {
+                        const uint32_t u = F8 ? e4m3_pair<false>(*(const uint16_t *)(vrow + c + i)) : *(const uint32_t *)(vrow + 2 * (c + i));
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        const bool see = key <= pos[mt] && (a.window == 0 || key > pos[mt] - a.window || key < a.n_sinks);
-#pragma unroll
-                        for (int i = 0; i < E; ++i)
-                            if (see) o[mt][i][r] = __builtin_fmaf(pk[mt], vv[i], o[mt][i][r]);
+                        for (int mt = 0; mt < MT; ++mt) {
+                            const bool see = sees(k0 + kk, pos[mt]);
+                            if (see && not_finite(u & 0xffffu)) o[mt][i][r] += bf_lo(u);
+                            if (see && not_finite(u & 0xffff0000u)) o[mt][i + 1][r] += bf_hi(u);
+                        }
                     }
                 }
             }
@@ -489,6 +528,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
+// The maximum over lanes l and l ^ 32.
+__device__ __forceinline__ float both_halves_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 template <int D, int RT, bool F8>
 __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedArgs a) {
     constexpr int M = 128 * RT, KT = 64, NS = D / 16, ND = D / 32;
@@ -497,7 +542,6 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
     constexpr int NP = (KT * CPR + 255) / 256;                 // pieces of a thread, for each of K and V
     constexpr bool RAGGED = KT * CPR % 256 != 0;
     constexpr int STAGE = KT * (KS + VS);
-    constexpr float kLag = 8.f;
     __shared__ SchedLds sched;
     __shared__ int32_t odd;
     __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
@@ -545,30 +589,37 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
     const int32_t s_lo = __builtin_amdgcn_readfirstlane(pos[0]);
     const int32_t s_hi = __builtin_amdgcn_readlane(pos[RT - 1], 31);
 
-    // the places of a tile's 64 rows: lane l looks up key l
-    auto locate = [&](int32_t tile, uint64_t &there) __attribute__((always_inline)) {
+    // the places of a tile's 64 rows: lane l looks up key l, a tile ahead of the loads that use it
+    int32_t page = 0;
+    uint32_t in_page = 0;
+    bool in_kv = false;
+    auto look_up = [&](int32_t tile) __attribute__((always_inline)) {
         const int32_t key = tile * KT + lane;
-        bool ok = key < rq.kv_len;
-        uint32_t off = 0;
-        if (ok) {
-            const uint32_t idx = fast_div((uint32_t)key, a.page_size);
-            const int32_t page = table[idx];
-            ok = page >= 0 && page < a.n_pages;
-            if (ok) off = (uint32_t)page * a.s_page + ((uint32_t)key - idx * a.page_size.d) * a.s_tok;
-        }
-        there = __ballot(ok);
-        return off;
+        in_kv = key < rq.kv_len;
+        const uint32_t k = (uint32_t)min(key, rq.kv_len - 1);
+        const uint32_t idx = fast_div(k, a.page_size);
+        in_page = k - idx * a.page_size.d;
+        page = table[idx];
     };
-    uint4 kr[NP], vr[NP];
+    auto place = [&](uint64_t &there) __attribute__((always_inline)) {
+        const bool ok = in_kv && (uint32_t)page < (uint32_t)a.n_pages;
+        there = __ballot(ok);
+        return (ok ? (uint32_t)page : 0u) * a.s_page + (ok ? in_page : 0u) * a.s_tok;
+    };
+    u32x4_t kr[NP], vr[NP];
     auto load = [&](uint32_t off) __attribute__((always_inline)) {
+        uint32_t ro[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) ro[i] = (uint32_t)__shfl((int)off, (tid + 256 * i) / CPR & 63);
+        __builtin_amdgcn_sched_barrier(0);                     // one trip to the other lanes for all of them
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int id = tid + 256 * i;
             const int row = id / CPR, c = id - row * CPR;
-            const uint64_t at = (uint64_t)(uint32_t)__shfl((int)off, row & 63) * 16 + 16 * c;
+            const uint64_t at = (uint64_t)ro[i] * 16 + 16 * c;
             if (RAGGED && id >= KT * CPR) continue;
-            kr[i] = *(const uint4 *)(kp + at);
-            vr[i] = *(const uint4 *)(vp + at);
+            kr[i] = *(const u32x4_t *)(kp + at);
+            vr[i] = *(const u32x4_t *)(vp + at);
         }
     };
     // In a tile with a key that some row does not see (edge) a NaN or infinity of V would meet zero
@@ -577,22 +628,20 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
     auto store = [&](int st, uint64_t there, bool edge) __attribute__((always_inline)) {
         char *ks = lds + st * STAGE, *vs = ks + KT * KS;
         if (edge) {
+            uint32_t found = 0;
             asm volatile("");
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int id = tid + 256 * i, row = id / CPR;
-                const bool is = (there >> (row & 63)) & 1;
-                uint32_t v4[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
+                const uint32_t is = 0u - (uint32_t)((there >> (row & 63)) & 1);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    uint32_t bad;                              // the bits of the values that are no number
-                    if constexpr (F8) bad = nan_bytes(v4[w]);
-                    else bad = not_finite_halves(v4[w]);
-                    if (is && bad) odd = 1;
-                    v4[w] = is ? v4[w] & ~bad : 0u;
+                    const uint32_t bad = F8 ? nan_bytes(vr[i][w]) : not_finite_halves(vr[i][w]);
+                    found |= bad & is;
+                    vr[i][w] &= ~bad & is;
                 }
-                vr[i] = make_uint4(v4[0], v4[1], v4[2], v4[3]);
             }
+            if (found) odd = 1;
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -600,25 +649,25 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
             if (RAGGED && id >= KT * CPR) continue;
             const int row = id / CPR, c = id - row * CPR;
             if constexpr (F8) {
-                const uint32_t k4[4] = {kr[i].x, kr[i].y, kr[i].z, kr[i].w}, v4[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    const uint32_t k0 = k4[2 * w], k1 = k4[2 * w + 1], x0 = v4[2 * w], x1 = v4[2 * w + 1];
+                    const uint32_t k0 = kr[i][2 * w], k1 = kr[i][2 * w + 1], x0 = vr[i][2 * w], x1 = vr[i][2 * w + 1];
                     *(uint4 *)(ks + row * KS + 32 * c + 16 * w) =
                         make_uint4(e4m3_pair<false>(k0), e4m3_pair<true>(k0), e4m3_pair<false>(k1), e4m3_pair<true>(k1));
                     *(uint4 *)(vs + row * VS + 32 * c + 16 * w) =
                         make_uint4(e4m3_pair<false>(x0), e4m3_pair<true>(x0), e4m3_pair<false>(x1), e4m3_pair<true>(x1));
                 }
             } else {
-                *(uint4 *)(ks + row * KS + 16 * c) = kr[i];
-                *(uint4 *)(vs + row * VS + 16 * c) = vr[i];
+                *(u32x4_t *)(ks + row * KS + 16 * c) = kr[i];
+                *(u32x4_t *)(vs + row * VS + 16 * c) = vr[i];
             }
         }
     };
-    // every key of the tile is there and seen by every row from position lo to hi
+    // every key of the tile is there and seen by every row, of the wave and of the workgroup
     auto seen = [&](int32_t k0, uint64_t there, int32_t lo, int32_t hi) __attribute__((always_inline)) {
-        return there == ~0ull && k0 + KT - 1 <= lo && (a.window == 0 || k0 > hi - a.window || k0 + KT <= a.n_sinks);
+        return there == ~0ull && k0 <= lo - (KT - 1) && (k0 > (a.window == 0 ? INT32_MIN : hi - a.window) || k0 <= a.n_sinks - KT);
     };
+    auto next_tile = [&](int32_t t) __attribute__((always_inline)) { return t + 1 == kt.sink ? kt.first : t + 1; };
 
     f32x16_t o[RT][ND];
     float m[RT], l[RT];
@@ -632,25 +681,44 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
     // V^T operand: keys 16 kk + 4 h + {0 .. 3} and + 8, channel 32 q + (lane & 31)
     const int vt = (4 * h + ((lane >> 2) & 3)) * VS + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
 
+    auto read_v = [&](const char *vs, int kk, bf16x8_t *f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < ND; ++q) {
+            const char *pp = vs + vt + 16 * kk * VS + 64 * q;
+            const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)pp);
+            const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(pp + 8 * VS));
+            typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+            const s16x8_t v8 = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            f[q] = __builtin_bit_cast(bf16x8_t, v8);
+        }
+    };
+
     uint64_t there = 0, there_n = 0;
+    int32_t t0 = kt.tile(v0), t1 = next_tile(t0), t2 = next_tile(t1);   // this tile and the two behind it
     if (v0 < v1) {
-        load(locate(kt.tile(v0), there));
+        look_up(t0);
+        load(place(there));
+        if (v0 + 1 < v1) look_up(t1);
         __syncthreads();                                       // odd is set
-        store(0, there, !seen(kt.tile(v0) * KT, there, p_lo, p_hi));
+        store(0, there, !seen(t0 * KT, there, p_lo, p_hi));
     }
     __syncthreads();
     for (int32_t v = v0; v < v1; ++v) {
         const int st = (v - v0) & 1;
-        const int32_t k0 = kt.tile(v) * KT;
-        if (v + 1 < v1) load(locate(kt.tile(v + 1), there_n));
+        const int32_t k0 = t0 * KT;
+        if (v + 1 < v1) load(place(there_n));
+        if (v + 2 < v1) look_up(t2);
         const char *ks = lds + st * STAGE, *vs = ks + KT * KS;
         f32x16_t s[RT][2];
+#if CB_PRIO
+        __builtin_amdgcn_s_setprio(1);
+#endif
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x16_t{};
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) s[rt][t] = f32x16_t{};
+        for (int q = 0; q < NS; ++q) {
 #pragma unroll
-            for (int q = 0; q < NS; ++q) {
+            for (int t = 0; t < 2; ++t) {
                 const bf16x8_t kf = *(const bf16x8_t *)(ks + (32 * t + n) * KS + 32 * q + 16 * h);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
@@ -665,6 +733,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4 * RT, 0);
+#endif
+#if CB_PRIO
+        __builtin_amdgcn_s_setprio(0);
 #endif
         if (!seen(k0, there, s_lo, s_hi)) {
             asm volatile("");                                  // a branch, not selects on every tile
@@ -683,6 +754,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
                 }
             }
         }
+        bf16x8_t vf[2][ND];
+        read_v(vs, 0, vf[0]);
+        __builtin_amdgcn_sched_barrier(0);
         uint32_t pk[RT][16];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -690,7 +764,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
 #pragma unroll
             for (int e = 3; e < 31; e += 2) mx = max3(mx, s[rt][e >> 4][e & 15], s[rt][(e + 1) >> 4][(e + 1) & 15]);
             mx = max3(mx, s[rt][1][15], s[rt][1][15]);
-            mx = max3(mx, __shfl_xor(mx, 32), mx) * c2;
+            mx = both_halves_max(mx) * c2;
             // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
             if (__any(mx > m[rt] + kLag)) {
                 const float mn = fmaxf(m[rt], mx);
@@ -712,41 +786,57 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
             }
             l[rt] += sum;
         }
+#if CB_IL
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
+            if (kk < 3) read_v(vs, kk + 1, vf[(kk + 1) & 1]);
 #pragma unroll
-            for (int q = 0; q < ND; ++q) {
-                const char *pp = vs + vt + 16 * kk * VS + 64 * q;
-                const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)pp);
-                const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(pp + 8 * VS));
-                typedef __attribute__((ext_vector_type(8))) short s16x8_t;
-                const s16x8_t v8 = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            for (int q = 0; q < ND; ++q)
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
                     o[rt][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        __builtin_bit_cast(bf16x8_t, v8),
-                        frag(pk[rt][4 * kk], pk[rt][4 * kk + 1], pk[rt][4 * kk + 2], pk[rt][4 * kk + 3]), o[rt][q], 0, 0, 0);
-            }
+                        vf[kk & 1][q], frag(pk[rt][4 * kk], pk[rt][4 * kk + 1], pk[rt][4 * kk + 2], pk[rt][4 * kk + 3]),
+                        o[rt][q], 0, 0, 0);
         }
-#if CB_SCHED & 2
-        // a quarter of the weights, then its products beside the next quarter
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
-        __builtin_amdgcn_sched_group_barrier(0x402, 28, 1);
+        // a quarter of the weights, then its products beside the next quarter's
+        __builtin_amdgcn_sched_group_barrier(0x406, 28, 1);
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
+        for (int kk = 0; kk < 4; ++kk) {
+            if (kk < 3) __builtin_amdgcn_sched_group_barrier(0x100, 2 * ND, 1);
 #pragma unroll
             for (int q = 0; q < ND; ++q) {
                 __builtin_amdgcn_sched_group_barrier(0x008, RT, 1);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-                __builtin_amdgcn_sched_group_barrier(0x402, 28 / ND, 1);
+                if (kk < 3) __builtin_amdgcn_sched_group_barrier(0x406, (28 + ND - 1) / ND, 1);
             }
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, 2 * RT, 1);
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
-        __builtin_amdgcn_sched_group_barrier(0x008, 2 * RT, 1);
+        __builtin_amdgcn_sched_barrier(0);
+#else
+#if CB_PRIO
+        __builtin_amdgcn_s_setprio(1);
 #endif
-        if (v + 1 < v1) store(st ^ 1, there_n, !seen(kt.tile(v + 1) * KT, there_n, p_lo, p_hi));
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            // the next step's operands are requested before this step's products
+            if (kk < 3) read_v(vs, kk + 1, vf[(kk + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < ND; ++q)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    o[rt][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        vf[kk & 1][q], frag(pk[rt][4 * kk], pk[rt][4 * kk + 1], pk[rt][4 * kk + 2], pk[rt][4 * kk + 3]),
+                        o[rt][q], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#endif
+#if CB_PRIO
+        __builtin_amdgcn_s_setprio(0);
+#endif
+        if (v + 1 < v1) store(st ^ 1, there_n, !seen(t1 * KT, there_n, p_lo, p_hi));
         there = there_n;
+        t0 = t1;
+        t1 = t2;
+        t2 = next_tile(t2);
         __syncthreads();
     }
     if (odd) {
@@ -755,7 +845,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
 #pragma unroll 1
         for (int32_t v = v0; v < v1; ++v) {
             const int32_t k0 = kt.tile(v) * KT;
-            const uint32_t off = locate(kt.tile(v), there);
+            look_up(kt.tile(v));
+            const uint32_t off = place(there);
             if (seen(k0, there, p_lo, p_hi)) continue;
 #pragma unroll 1
             for (int kk = 0; kk < KT; ++kk) {
@@ -819,48 +910,60 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
 
 // ------------------------------------------------------------------ joining parts
 
-// One workgroup per 16 rows of a row tile that went in parts: their partial
-// sums, brought to the common maximum and added in the order of the parts.
+// One wave per row of a row tile that went in parts: its partial sums, brought to the common maximum.
+// 4 D bytes a part; the wave's lanes take several parts at once (slot p0 parts p0, p0 + NP, ...) and
+// add the slots at the end, always in the same order.
 template <int D, int M, int KT, bool F8>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
+    constexpr int LP = D / 4, NP = 64 / LP;                    // lanes of a part, parts at once
     __shared__ SchedLds sched;
     const int head = (int)(blockIdx.x % (uint32_t)a.n_heads);
     Item it;
     const int64_t idx = blockIdx.x / (uint32_t)a.n_heads;
-    if (!find_item<M, KT, true>(a, idx / (M / 16), sched, it)) return;
-    const int tid = threadIdx.x;
+    if (!find_item<M, KT, true>(a, idx / (M / 4), sched, it)) return;
+    const int lane = threadIdx.x & 63;
     const Request rq = request(a, it.req);
     const int32_t G = (int32_t)a.G.d;
     const int32_t row0 = it.tile * M;
     const int32_t n_rows = (int32_t)min((int64_t)rq.q_len * G - row0, (int64_t)M);
-    const int rr = (int)(idx % (M / 16)) * 16 + tid / (D / 8), ch = tid % (D / 8) * 8;
-    if (tid >= 2 * D || rr >= n_rows) return;
+    const int rr = (int)(idx % (M / 4)) * 4 + (threadIdx.x >> 6);
+    if (rr >= n_rows) return;
+    const int ch = lane % LP * 4, p0 = lane / LP;
     const float *w0 = a.c.ws + ((int64_t)it.slot * a.n_heads + head) * (M * (D + 2));
     const int64_t step = (int64_t)a.n_heads * (M * (D + 2));
     float mx = -HUGE_VALF;
-    for (int p = 0; p < it.parts; ++p) mx = fmaxf(mx, w0[p * step + M * D + rr]);
-    const float ref = mx == -HUGE_VALF ? 0.f : mx;
-    float lr = 0.f, y[8] = {};
-    for (int p = 0; p < it.parts; ++p) {
-        const float *w = w0 + p * step;
-        const float f = __builtin_amdgcn_exp2f(w[M * D + rr] - ref);
-        const float4 x0 = *(const float4 *)(w + rr * D + ch), x1 = *(const float4 *)(w + rr * D + ch + 4);
-        lr += w[M * D + M + rr] * f;
-        y[0] += x0.x * f; y[1] += x0.y * f; y[2] += x0.z * f; y[3] += x0.w * f;
-        y[4] += x1.x * f; y[5] += x1.y * f; y[6] += x1.z * f; y[7] += x1.w * f;
-    }
-    const float inv = lr == 0.f ? 0.f : (F8 ? a.vscale[head] : 1.f) / lr;
-    if (lr == 0.f) {
+    for (int p = lane; p < it.parts; p += 64) mx = fmaxf(mx, w0[p * step + M * D + rr]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = 0.f;
+    for (int s = 1; s < 64; s <<= 1) mx = fmaxf(mx, __shfl_xor(mx, s));
+    const float ref = mx == -HUGE_VALF ? 0.f : mx;
+    float lr = 0.f;
+    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+    if (p0 < NP) {
+#pragma unroll 4
+        for (int p = p0; p < it.parts; p += NP) {
+            const float *w = w0 + p * step;
+            const float f = __builtin_amdgcn_exp2f(w[M * D + rr] - ref);
+            const f32x4_t x = *(const f32x4_t *)(w + rr * D + ch);
+            lr += w[M * D + M + rr] * f;
+            y += x * f;
+        }
     }
+    f32x4_t t = {0.f, 0.f, 0.f, 0.f};
+    float lt = 0.f;
+#pragma unroll
+    for (int s = 0; s < NP; ++s) {
+        lt += __shfl(lr, s * LP);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] += __shfl(y[e], s * LP + lane % LP);
+    }
+    if (lane >= LP) return;
+    const float inv = (F8 ? a.vscale[head] : 1.f) / lt;
     const int32_t tok = (int32_t)fast_div((uint32_t)(row0 + rr), a.G), u = row0 + rr - tok * G;
     uint16_t *out = a.out + (int64_t)(rq.row0 + tok) * a.o_tok + (int64_t)(head * G + u) * a.o_head + ch;
-    *(uint4 *)out = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
-                               pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
+    *(u32x2_t *)out = lt == 0.f ? u32x2_t{0u, 0u} : u32x2_t{pack_bf16(t[0] * inv, t[1] * inv), pack_bf16(t[2] * inv, t[3] * inv)};
     if (a.lse && ch == 0)
         a.lse[(int64_t)(rq.row0 + tok) * (a.n_heads * G) + head * G + u] =
-            lr == 0.f ? -HUGE_VALF : 0.6931471805599453f * (mx + __log2f(lr));
+            lt == 0.f ? -HUGE_VALF : 0.6931471805599453f * (mx + __log2f(lt));
 }
 
 constexpr int kSmallRows = 16;          // rows of a request up to which attn_rows_kernel takes it beside the tile kernel
@@ -883,9 +986,9 @@ hipError_t launch_class(PagedArgs a, K kernel, int target, int64_t row_min, int6
     a.c.ws = (float *)ws;
     ws += 2 * slot * a.c.target;
     ws_bytes -= 2 * slot * a.c.target;
-    const int64_t tiles = row_tiles_bound(a.n_tokens, a.n_reqs, a.G.d, M);
+    const int64_t tiles = row_tiles_bound(a.n_tokens, a.n_reqs, a.G.d, M, row_max);
     const int64_t items = (tiles + a.c.target / a.n_heads) * a.n_heads;
-    const int64_t join = std::min<int64_t>(tiles, a.c.target / a.n_heads) * (M / 16) * a.n_heads;
+    const int64_t join = std::min<int64_t>(tiles, a.c.target / a.n_heads) * (M / 4) * a.n_heads;
     if (items > INT32_MAX || join > INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;

@@ -58,11 +58,15 @@ CB_HD int64_t part_tiles(int64_t W, int32_t H, int32_t target, int32_t c_min) {
     return c > c_min ? c : c_min;
 }
 
-// Parts of a row tile with `bound` key tiles.  A tile in two parts or more has
-// bound > c, so parts < 2 bound / c: over all requests the parts of divided
-// tiles are fewer than 2 target / H, and the parts beyond the first fewer than
-// target / H.  (Workspace and grid are sized by these.)
-CB_HD int32_t parts_of(int64_t bound, int64_t c) { return bound <= c ? 1 : (int32_t)((bound + c - 1) / c); }
+// Parts of a row tile with `bound` key tiles: the nearest number to bound / c (a
+// tile a little longer than c is not worth the joining).  A tile in two parts or
+// more has bound >= 1.5 c, so parts <= 4/3 bound / c: over all requests the parts
+// of divided tiles are no more than 4/3 target / H, the divided tiles no more
+// than 2/3 target / H, and the parts beyond the first no more than target / H.
+// (Workspace and grid are sized by these.)
+CB_HD int32_t parts_of(int64_t bound, int64_t c) {
+    return bound <= c ? 1 : (int32_t)(bound / c + (bound % c >= c - c / 2 ? 1 : 0));
+}
 
 // Part s of `parts` of a list of n key tiles: v in [begin, end).
 CB_HD int32_t part_begin(int32_t n, int32_t s, int32_t parts) { return (int32_t)((int64_t)n * s / parts); }
@@ -85,9 +89,12 @@ CB_HD RequestWork request_work(int32_t q_len, int32_t kv_len, int32_t G, int32_t
     return w;
 }
 
-// Host side: row tiles that requests of n_tokens tokens can have together.
-inline int64_t row_tiles_bound(int64_t n_tokens, int64_t n_reqs, int64_t G, int64_t M) {
-    return n_tokens * G / M + n_reqs;
+// Host side: row tiles that requests of n_tokens tokens can have together, if
+// none counts that has more than row_max rows.
+inline int64_t row_tiles_bound(int64_t n_tokens, int64_t n_reqs, int64_t G, int64_t M, int64_t row_max) {
+    const int64_t all = n_tokens * G / M + n_reqs;
+    const int64_t each = row_max / M + (row_max % M != 0);
+    return each <= all / n_reqs ? n_reqs * each : all;
 }
 
 }  // namespace cb

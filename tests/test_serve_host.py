@@ -24,7 +24,7 @@ void work(int q, int kv, int G, int M, int KT, int64_t lo, int64_t hi, int windo
     cb::RequestWork w = cb::request_work(q, kv, G, M, KT, lo, hi, window, sinks);
     out[0] = w.tiles; out[1] = w.tokens; out[2] = w.bound;
 }
-int64_t row_tiles_bound(int64_t t, int64_t n, int64_t G, int64_t M) { return cb::row_tiles_bound(t, n, G, M); }
+int64_t row_tiles_bound(int64_t t, int64_t n, int64_t G, int64_t M, int64_t hi) { return cb::row_tiles_bound(t, n, G, M, hi); }
 }
 """
 
@@ -41,7 +41,7 @@ def rules(tmp_path_factory):
                             ("bound", i64, [i32] * 5), ("part_tiles", i64, [i64, i32, i32, i32]),
                             ("parts_of", i32, [i64, i64]), ("part_begin", i32, [i32] * 3),
                             ("work", None, [i32] * 5 + [i64, i64, i32, i32, ctypes.c_void_p]),
-                            ("row_tiles_bound", i64, [i64] * 4)):
+                            ("row_tiles_bound", i64, [i64] * 5)):
         f = getattr(lib, name)
         f.restype, f.argtypes = res, args
     return lib
@@ -106,9 +106,9 @@ def test_every_key_tile_of_every_row_tile_has_one_part(rules):
                 assert n_keys <= max(bound, 0)
                 cuts = [rules.part_begin(n_keys, s, parts) for s in range(parts + 1)]
                 assert cuts[0] == 0 and cuts[-1] == n_keys and cuts == sorted(cuts)
-        tiles_bound = rules.row_tiles_bound(int(q.sum()), n, G, M)
+        tiles_bound = rules.row_tiles_bound(int(q.sum()), n, G, M, hi)
         assert items <= tiles_bound + target // H
-        assert slots * H <= 2 * target or slots == 0
+        assert 3 * slots * H <= 4 * target
         assert joined <= min(tiles_bound, target // H)
         assert slots < 1 << 24
 
