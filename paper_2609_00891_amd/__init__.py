@@ -697,11 +697,18 @@ def _ints(t: torch.Tensor, n: int, name: str):
         raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements, got {t.dtype} {tuple(t.shape)}")
 
 
-def _on_current_device(**tensors):
-    """The library works on the current device: tensors of another (or of the host) are refused here."""
-    for name, t in tensors.items():
-        if t is not None and (t.device.type != "cuda" or t.device.index != torch.cuda.current_device()):
-            raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+def _on_current_device(names: str, *tensors) -> int:
+    """The library works on the current device: tensors of another (or of the host) are refused here.  Returns the
+    device's index."""
+    device = tensors[0].get_device()
+    if device < 0 or device != torch.cuda.current_device() or any(t is not None and t.get_device() != device for t in tensors):
+        where = ", ".join(f"{n} on {t.device}" for n, t in zip(names.split(), tensors) if t is not None)
+        raise ValueError(f"every tensor must be on the current CUDA device: {where}")
+    return device
+
+
+def _stream_on(device: int, stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
 
 
 def page_pool(t: torch.Tensor, scales: Optional[torch.Tensor] = None) -> CbPages:
@@ -731,11 +738,9 @@ def page_pool(t: torch.Tensor, scales: Optional[torch.Tensor] = None) -> CbPages
 def _rows_view(t: torch.Tensor, name: str) -> CbRows:
     if t.dtype != torch.bfloat16 or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
         raise ValueError(f"{name} is bfloat16 [token][head][dim] with unit dim stride")
-    r = CbRows()
-    r.data = t.data_ptr()
-    r.n_tokens, r.n_heads, r.head_dim = t.shape
-    r.s_tok, r.s_head = t.stride(0), t.stride(1)
-    return r
+    n, h, d = t.shape
+    s = t.stride()
+    return CbRows(t.data_ptr(), n, h, d, s[0], s[1])
 
 
 def rope_axes_spec(table: torch.Tensor, positions: torch.Tensor, axis=None,
@@ -779,12 +784,12 @@ def cb_page_tables(ctx_lens: torch.Tensor, q_lens: torch.Tensor, free_pages: tor
                        (positions, slots.numel(), "positions"), (info, n, "info"), (n_used, 1, "n_used")):
         _ints(t, m, name)
     _check_table(block_table, n)
-    _on_current_device(ctx_lens=ctx_lens, q_lens=q_lens, free_pages=free_pages, block_table=block_table, q_starts=q_starts,
-                       kv_lens=kv_lens, slots=slots, positions=positions, info=info, n_used=n_used)
+    dev = _on_current_device("ctx_lens q_lens free_pages block_table q_starts kv_lens slots positions info n_used", ctx_lens,
+                             q_lens, free_pages, block_table, q_starts, kv_lens, slots, positions, info, n_used)
     _check(_lib.cb_page_tables(n, _ptr(ctx_lens), _ptr(q_lens), _ptr(free_pages), free_pages.numel(), int(page_size),
                                _ptr(block_table), block_table.stride(0), block_table.shape[1], slots.numel(),
                                _ptr(q_starts), _ptr(kv_lens), _ptr(slots), _ptr(positions), _ptr(info), _ptr(n_used),
-                               _stream(stream)))
+                               _stream_on(dev, stream)))
 
 
 def _check_table(block_table: torch.Tensor, n: int):
@@ -798,8 +803,9 @@ def cb_rope_axes(cache_in: torch.Tensor, cache_out: torch.Tensor, rope: CbRopeAx
     (:func:`rope_axes_spec`) into cache_out (may be cache_in); V rows copied."""
     iv, ov = cache_view(cache_in), cache_view(cache_out)
     _check_axes_tokens(rope, cache_in.shape[2] * cache_in.shape[4])
-    _on_current_device(cache_in=cache_in, cache_out=cache_out, table=rope._keep[0], positions=rope._keep[1])
-    _check(_lib.cb_rope_axes(ctypes.byref(iv), ctypes.byref(ov), ctypes.byref(rope), int(bool(inverse)), _stream(stream)))
+    dev = _on_current_device("cache_in cache_out table positions", cache_in, cache_out, *rope._keep)
+    _check(_lib.cb_rope_axes(ctypes.byref(iv), ctypes.byref(ov), ctypes.byref(rope), int(bool(inverse)),
+                             _stream_on(dev, stream)))
 
 
 def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer: int = 0,
@@ -814,11 +820,11 @@ def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer
     _check_axes_tokens(rope, n)
     qv = None if q is None else _rows_view(q, "q")
     ov = None if q_out is None else _rows_view(q_out, "q_out")
-    _on_current_device(rows=rows, pages=pages._keep[0], scales=pages._keep[1], slots=slots, q=q, q_out=q_out,
-                       table=None if rope is None else rope._keep[0], positions=None if rope is None else rope._keep[1])
+    dev = _on_current_device("rows slots q q_out pages scales table positions", rows, slots, q, q_out, *pages._keep,
+                             *(() if rope is None else rope._keep))
     _check(_lib.cb_page_write(ctypes.byref(rv), ctypes.byref(pages), int(layer), _ptr(slots),
                               None if rope is None else ctypes.byref(rope), None if qv is None else ctypes.byref(qv),
-                              None if ov is None else ctypes.byref(ov), _stream(stream)))
+                              None if ov is None else ctypes.byref(ov), _stream_on(dev, stream)))
 
 
 def cb_attn_paged_workspace_bytes(n_tokens: int, n_reqs: int, n_qheads: int, n_heads: int, head_dim: int,
@@ -844,10 +850,10 @@ def cb_attn_paged(q: torch.Tensor, pages: CbPages, layer: int, q_starts: torch.T
         _need(lse, (q.shape[0], q.shape[1]), torch.float32, "lse")
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    _on_current_device(q=q, pages=pages._keep[0], scales=pages._keep[1], q_starts=q_starts, kv_lens=kv_lens,
-                       block_table=block_table, out=out, lse=lse, workspace=workspace)
+    dev = _on_current_device("q q_starts kv_lens block_table out lse workspace pages scales", q, q_starts, kv_lens,
+                             block_table, out, lse, workspace, *pages._keep)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_lib.cb_attn_paged(ctypes.byref(qv), ctypes.byref(pages), int(layer), n, _ptr(q_starts), _ptr(kv_lens),
                               _ptr(block_table), block_table.stride(0), block_table.shape[1], ctypes.byref(ov),
                               int(max_q_len), float(q.shape[2] ** -0.5 if scale is None else scale), int(window), int(sinks),
-                              _ptr(lse), _ptr(workspace), int(ws_bytes), _stream(stream)))
+                              _ptr(lse), _ptr(workspace), int(ws_bytes), _stream_on(dev, stream)))

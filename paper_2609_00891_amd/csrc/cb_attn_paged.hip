@@ -43,6 +43,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 #define CB_SCHED 1
 #endif
 constexpr int kKT = 32;                 // keys of a tile
+constexpr int kTileKT = 64;             // keys of a tile of the tile kernel
 constexpr int kPartMin = 8;             // least key tiles of a part: two for each of the four waves
 constexpr float kLag = 8.f;              // log2 by which the maximum in use may lag the true one
 #ifndef CB_T
@@ -95,65 +96,78 @@ __device__ __forceinline__ Request request(const PagedArgs &a, int r) {
 }
 
 struct Item { int32_t req, tile, part, parts, slot; };   // slot: of the first part's partial result
-struct SchedLds { int64_t wsum[4]; Item item; int32_t found; };
+struct SchedLds { double work[4]; uint32_t items[4], slots[4]; Item item; int32_t found; };
 
-// The row tile and part of index `idx` (JOIN: of the idx-th row tile in more
-// than one part), or false behind the last.
+// Inclusive sums over a wave by data-parallel moves: within rows of 16 lanes, then across them.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint64_t r = (uint64_t)moved<CTRL, ROWS>((uint32_t)(u >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)u);
+    return __builtin_bit_cast(double, r);
+}
+template <typename T> __device__ __forceinline__ T wave_sums(T x) {
+    x += moved<0x111, 0xf>(x);   // row_shr:1, 2, 4, 8
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);   // row_bcast:15, 31
+    x += moved<0x143, 0xc>(x);
+    return x;
+}
+
+// The row tile and part of index `idx` (JOIN: of the idx-th row tile in more than one part), or false
+// behind the last.  The work of all requests is summed in fp64: whole numbers, exact below 2^53, and
+// the same in every workgroup.
 template <int M, int KT, bool JOIN>
-__device__ __forceinline__ bool find_item(const PagedArgs &a, int64_t idx, SchedLds &sh, Item &out) {
+__device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &cl, uint32_t idx, SchedLds &sh, Item &out) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     auto work_of = [&](int r) __attribute__((always_inline)) {
         RequestWork w = {0, 0, 0};
         if (r < a.n_reqs) {
             const Request q = request(a, r);
-            w = request_work(q.q_len, q.kv_len, (int32_t)a.G.d, M, KT, a.c.row_min, a.c.row_max, a.window, a.n_sinks);
+            w = request_work(q.q_len, q.kv_len, (int32_t)a.G.d, M, KT, cl.row_min, cl.row_max, a.window, a.n_sinks);
         }
         return w;
     };
     if (tid == 0) sh.found = 0;
-    int64_t W = 0;
-    for (int r = tid; r < a.n_reqs; r += 256) {
+    const RequestWork w0 = work_of(tid);
+    double W = (double)w0.tiles * (double)w0.bound;
+    for (int r = tid + 256; r < a.n_reqs; r += 256) {
         const RequestWork w = work_of(r);
-        W += w.tiles * w.bound;
+        W += (double)w.tiles * (double)w.bound;
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) W += __shfl_xor(W, o);
-    if (lane == 0) sh.wsum[wave] = W;
+    W = wave_sums(W);
+    if (lane == 63) sh.work[wave] = W;
     __syncthreads();
-    W = sh.wsum[0] + sh.wsum[1] + sh.wsum[2] + sh.wsum[3];
-    const int64_t c = part_tiles(W, a.n_heads, a.c.target, kPartMin);
-    int64_t n_before = 0;
-    int32_t s_before = 0;
+    W = sh.work[0] + sh.work[1] + sh.work[2] + sh.work[3];
+    const int64_t c = part_tiles((int64_t)W, a.n_heads, cl.target, kPartMin);
+    uint32_t n_before = 0, s_before = 0;
     for (int r0 = 0; r0 < a.n_reqs; r0 += 256) {
-        const RequestWork w = work_of(r0 + tid);
+        const RequestWork w = r0 == 0 ? w0 : work_of(r0 + tid);
         const int32_t parts = parts_of(w.bound, c);
-        const int64_t n = JOIN ? (parts > 1 ? w.tiles : 0) : (int64_t)w.tiles * parts;
-        const int32_t s = parts > 1 ? w.tiles * parts : 0;
-        int64_t ni = n;
-        int32_t si = s;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t u = __shfl_up(ni, o);
-            const int32_t t = __shfl_up(si, o);
-            if (lane >= o) { ni += u; si += t; }
+        const uint32_t n = JOIN ? (parts > 1 ? w.tiles : 0) : (uint32_t)w.tiles * parts;
+        const uint32_t s = parts > 1 ? (uint32_t)w.tiles * parts : 0;
+        uint32_t ni = wave_sums(n), si = wave_sums(s);
+        if (r0 > 0) __syncthreads();                          // the last round's sums have been read
+        if (lane == 63) {
+            sh.items[wave] = ni;
+            sh.slots[wave] = si;
         }
-        __syncthreads();                                      // the last round's sums have been read
-        if (lane == 63) sh.wsum[wave] = ni << 24 | si;        // slots are fewer than 2^24 (see parts_of)
         __syncthreads();
-        int64_t total = 0;
-        int32_t s_total = 0;
+        uint32_t total = 0, s_total = 0;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int64_t x = sh.wsum[v];
-            if (v < wave) { ni += x >> 24; si += (int32_t)(x & 0xffffff); }
-            total += x >> 24;
-            s_total += (int32_t)(x & 0xffffff);
+            if (v < wave) { ni += sh.items[v]; si += sh.slots[v]; }
+            total += sh.items[v];
+            s_total += sh.slots[v];
         }
-        const int64_t first = n_before + ni - n;
-        if (idx >= first && idx < first + n) {
-            const int32_t k = (int32_t)(idx - first);
-            const int32_t tile = JOIN ? k : k / parts;
-            sh.item = {r0 + tid, tile, JOIN ? 0 : k - tile * parts, parts, s_before + si - s + tile * parts};
+        const uint32_t first = n_before + ni - n;
+        if (idx - first < n) {
+            const uint32_t k = idx - first, tile = JOIN ? k : k / (uint32_t)parts;
+            sh.item = {r0 + tid, (int32_t)tile, JOIN ? 0 : (int32_t)(k - tile * parts), parts,
+                       (int32_t)(s_before + si - s + tile * parts)};
             sh.found = 1;
         }
         n_before += total;
@@ -180,17 +194,21 @@ template <int D, bool F8> struct Geo {
     }
 };
 
+template <int D> struct RowsLds {
+    float o[4][16][D + 4];                                     // each wave's results
+    float ml[4][16][2];
+};
+
 template <int D, int MT, bool F8>
-__global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
+__device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds &sched,
+                                          RowsLds<D> &lds) {
     using Ge = Geo<D, F8>;
     constexpr int M = 16 * MT, E = Ge::E;
-    constexpr int OS = D + 4;                                  // floats between rows of the joined results
-    __shared__ SchedLds sched;
-    __shared__ __attribute__((aligned(16))) float ol[4][16][OS];
-    __shared__ float ml[4][16][2];
-    const int head = (int)(blockIdx.x % (uint32_t)a.n_heads);
+    auto &ol = lds.o;
+    auto &ml = lds.ml;
+    const int head = (int)(block % (uint32_t)a.n_heads);
     Item it;
-    if (!find_item<M, kKT, false>(a, blockIdx.x / (uint32_t)a.n_heads, sched, it)) return;
+    if (!find_item<M, kKT, false>(a, cl, block / (uint32_t)a.n_heads, sched, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -489,7 +507,7 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
                 for (int e = 0; e < 8; ++e) y[e] += ol[w][row][ch + e];
             }
             if (it.parts > 1) {
-                float *w = a.c.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
+                float *w = cl.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
                 *(float4 *)(w + rr * D + ch) = make_float4(y[0], y[1], y[2], y[3]);
                 *(float4 *)(w + rr * D + ch + 4) = make_float4(y[4], y[5], y[6], y[7]);
                 if (ch == 0) {
@@ -534,20 +552,26 @@ __device__ __forceinline__ float both_halves_max(float x) {
     return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+template <int D> struct TileLds {
+    static constexpr int KS = 2 * D + 16, VS = 2 * D + 32;     // bytes between rows of K and V
+    char kv[2][kTileKT * (KS + VS)];
+    int32_t odd;
+};
+
 template <int D, int RT, bool F8>
-__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedArgs a) {
-    constexpr int M = 128 * RT, KT = 64, NS = D / 16, ND = D / 32;
-    constexpr int KS = 2 * D + 16, VS = 2 * D + 32;            // bytes between rows of K and V in LDS
+__device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds &sched,
+                                          TileLds<D> &tl) {
+    constexpr int M = 128 * RT, KT = kTileKT, NS = D / 16, ND = D / 32;
+    constexpr int KS = TileLds<D>::KS, VS = TileLds<D>::VS;
     constexpr int CPR = F8 ? D / 16 : D / 8;                   // 16-byte pieces of a row in memory
     constexpr int NP = (KT * CPR + 255) / 256;                 // pieces of a thread, for each of K and V
     constexpr bool RAGGED = KT * CPR % 256 != 0;
     constexpr int STAGE = KT * (KS + VS);
-    __shared__ SchedLds sched;
-    __shared__ int32_t odd;
-    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
-    const int head = (int)(blockIdx.x % (uint32_t)a.n_heads);
+    char *lds = tl.kv[0];
+    int32_t &odd = tl.odd;
+    const int head = (int)(block % (uint32_t)a.n_heads);
     Item it;
-    if (!find_item<M, KT, false>(a, blockIdx.x / (uint32_t)a.n_heads, sched, it)) return;
+    if (!find_item<M, KT, false>(a, cl, block / (uint32_t)a.n_heads, sched, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -877,7 +901,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
         const float lr = l[rt] + __shfl_xor(l[rt], 32);
         if (rr >= n_rows) continue;
         if (it.parts > 1) {
-            float *w = a.c.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
+            float *w = cl.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
 #pragma unroll
             for (int q = 0; q < ND; ++q)
 #pragma unroll
@@ -914,22 +938,16 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void attn_tile_kernel(PagedAr
 // 4 D bytes a part; the wave's lanes take several parts at once (slot p0 parts p0, p0 + NP, ...) and
 // add the slots at the end, always in the same order.
 template <int D, int M, int KT, bool F8>
-__global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
+__device__ __forceinline__ void join_row(const PagedArgs &a, const PagedClass &cl, const Item &it, int head, int rr) {
     constexpr int LP = D / 4, NP = 64 / LP;                    // lanes of a part, parts at once
-    __shared__ SchedLds sched;
-    const int head = (int)(blockIdx.x % (uint32_t)a.n_heads);
-    Item it;
-    const int64_t idx = blockIdx.x / (uint32_t)a.n_heads;
-    if (!find_item<M, KT, true>(a, idx / (M / 4), sched, it)) return;
     const int lane = threadIdx.x & 63;
     const Request rq = request(a, it.req);
     const int32_t G = (int32_t)a.G.d;
     const int32_t row0 = it.tile * M;
     const int32_t n_rows = (int32_t)min((int64_t)rq.q_len * G - row0, (int64_t)M);
-    const int rr = (int)(idx % (M / 4)) * 4 + (threadIdx.x >> 6);
     if (rr >= n_rows) return;
     const int ch = lane % LP * 4, p0 = lane / LP;
-    const float *w0 = a.c.ws + ((int64_t)it.slot * a.n_heads + head) * (M * (D + 2));
+    const float *w0 = cl.ws + ((int64_t)it.slot * a.n_heads + head) * (M * (D + 2));
     const int64_t step = (int64_t)a.n_heads * (M * (D + 2));
     float mx = -HUGE_VALF;
     for (int p = lane; p < it.parts; p += 64) mx = fmaxf(mx, w0[p * step + M * D + rr]);
@@ -966,56 +984,98 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
             lt == 0.f ? -HUGE_VALF : 0.6931471805599453f * (mx + __log2f(lt));
 }
 
-constexpr int kSmallRows = 16;          // rows of a request up to which attn_rows_kernel takes it beside the tile kernel
-constexpr int kTileTarget = 512;        // workgroups of the tile kernel that long rows are divided into
-#ifndef CB_RT
-#define CB_RT 1
-#endif
-constexpr int kRT = CB_RT, kTileM = 128 * kRT;
+// Row tiles that went in parts, 16 rows a time; blocks go round while there are more of them.
+template <int D, int M, int KT, bool F8>
+__device__ __forceinline__ void join_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, uint32_t blocks,
+                                          SchedLds &sched) {
+    for (uint32_t b = block;; b += blocks) {
+        const uint32_t idx = b / (uint32_t)a.n_heads;
+        Item it;
+        if (!find_item<M, KT, true>(a, cl, idx / (M / 16), sched, it)) return;
+        for (int r = threadIdx.x >> 6; r < 16; r += 4)
+            join_row<D, M, KT, F8>(a, cl, it, (int)(b - idx * a.n_heads), (int)(idx % (M / 16)) * 16 + r);
+        __syncthreads();                                       // the item has been read
+    }
+}
 
-// One kernel over its requests, and the joining of their parts.
-template <int D, int M, int KT, bool F8, typename K>
-hipError_t launch_class(PagedArgs a, K kernel, int target, int64_t row_min, int64_t row_max, char *&ws, int64_t &ws_bytes,
-                        hipStream_t s) {
+// ------------------------------------------------------------------ kernels
+
+constexpr int kTileM = 128;
+
+template <int D, bool F8>
+__global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
+    __shared__ SchedLds sched;
+    __shared__ __attribute__((aligned(16))) RowsLds<D> lds;
+    rows_body<D, 1, F8>(a, a.rows, blockIdx.x, sched, lds);
+}
+
+// The requests with few rows and the others in one launch: the tiles, which take longer, first.
+template <int D, bool F8>
+__global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedArgs a) {
+    __shared__ SchedLds sched;
+    __shared__ __attribute__((aligned(16))) union { RowsLds<D> rows; TileLds<D> tile; } lds;
+    if (blockIdx.x < a.tile.blocks) tile_body<D, 1, F8>(a, a.tile, blockIdx.x, sched, lds.tile);
+    else rows_body<D, 1, F8>(a, a.rows, blockIdx.x - a.tile.blocks, sched, lds.rows);
+}
+
+template <int D, bool F8>
+__global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
+    __shared__ SchedLds sched;
+    if (blockIdx.x < a.tile.join_blocks) join_body<D, kTileM, kTileKT, F8>(a, a.tile, blockIdx.x, a.tile.join_blocks, sched);
+    else join_body<D, 16, kKT, F8>(a, a.rows, blockIdx.x - a.tile.join_blocks, a.rows.join_blocks, sched);
+}
+
+constexpr int kSmallRows = 16;          // rows of a request up to which rows_body takes it beside tile_body
+constexpr int kFewRows = 32;            // and alone, when no request is said to have more
+constexpr int kTileTarget = 512;        // workgroups of tile_body that long rows are divided into
+constexpr int kJoinBlocks = 1024;
+
+// The blocks of a class of requests and its part of the workspace.
+template <int D, int M, int KT>
+bool prepare_class(const PagedArgs &a, PagedClass &c, int target, int64_t row_min, int64_t row_max, char *&ws, int64_t &ws_bytes) {
     const int64_t slot = (int64_t)M * (D + 2) * 4;
-    a.c.row_min = row_min;
-    a.c.row_max = row_max;
-    a.c.target = (int32_t)std::min<int64_t>(target, ws_bytes / (2 * slot));
+    c.row_min = row_min;
+    c.row_max = row_max;
+    c.target = (int32_t)std::min<int64_t>(target, ws_bytes / (2 * slot));
     // no row is long enough to be divided
-    if ((int64_t)a.table_width * a.page_size.d <= (int64_t)kPartMin * KT) a.c.target = 0;
-    a.c.ws = (float *)ws;
-    ws += 2 * slot * a.c.target;
-    ws_bytes -= 2 * slot * a.c.target;
+    const int32_t most = (int32_t)std::min<int64_t>((int64_t)a.table_width * a.page_size.d, INT32_MAX);
+    if (parts_of(key_tiles_bound(most, M, a.window, a.n_sinks, KT), kPartMin) == 1) c.target = 0;
+    c.ws = (float *)ws;
+    ws += 2 * slot * c.target;
+    ws_bytes -= 2 * slot * c.target;
     const int64_t tiles = row_tiles_bound(a.n_tokens, a.n_reqs, a.G.d, M, row_max);
-    const int64_t items = (tiles + a.c.target / a.n_heads) * a.n_heads;
-    const int64_t join = std::min<int64_t>(tiles, a.c.target / a.n_heads) * (M / 4) * a.n_heads;
-    if (items > INT32_MAX || join > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(256), 0, s, a);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (join > 0) hipLaunchKernelGGL((attn_join_kernel<D, M, KT, F8>), dim3((unsigned)join), dim3(256), 0, s, a);
-    return hipGetLastError();
+    const int64_t blocks = (tiles + c.target / a.n_heads) * a.n_heads;
+    const int64_t join = std::min<int64_t>(tiles, c.target / a.n_heads) * (M / 16) * a.n_heads;
+    if (blocks > INT32_MAX / 2 || join > INT32_MAX / 2) return false;
+    c.blocks = (uint32_t)blocks;
+    c.join_blocks = (uint32_t)std::min<int64_t>(join, kJoinBlocks);
+    return true;
 }
 
 template <int D, bool F8>
 hipError_t launch(PagedArgs a, int32_t max_q_len, void *ws, int64_t ws_bytes, hipStream_t s) {
-    const int64_t G = a.G.d;
     char *w = (char *)ws;
-    // few rows everywhere: the rows kernel alone, whatever the lengths turn out to be
-    if ((int64_t)max_q_len * G <= 32)
-        return launch_class<D, 16, kKT, F8>(a, attn_rows_kernel<D, 1, F8>, kTarget, 0, INT64_MAX, w, ws_bytes, s);
-    int64_t least = 0;
-    if (G <= kSmallRows && a.n_reqs > 1) {
-        least = kSmallRows;
-        if (hipError_t e = launch_class<D, 16, kKT, F8>(a, attn_rows_kernel<D, 1, F8>, kTarget, 0, least, w, ws_bytes, s)) return e;
+    if ((int64_t)max_q_len * a.G.d <= kFewRows) {
+        // few rows everywhere: rows_body alone, whatever the lengths turn out to be
+        if (!prepare_class<D, 16, kKT>(a, a.rows, kTarget, 0, INT64_MAX, w, ws_bytes)) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((attn_rows_kernel<D, F8>), dim3(a.rows.blocks), dim3(256), 0, s, a);
+    } else {
+        const int64_t least = a.G.d <= kSmallRows && a.n_reqs > 1 ? kSmallRows : 0;
+        if (least > 0 && !prepare_class<D, 16, kKT>(a, a.rows, kTarget, 0, least, w, ws_bytes)) return hipErrorInvalidValue;
+        if (!prepare_class<D, kTileM, kTileKT>(a, a.tile, kTileTarget, least, INT64_MAX, w, ws_bytes)) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((attn_tile_kernel<D, F8>), dim3(a.tile.blocks + a.rows.blocks), dim3(256), 0, s, a);
     }
-    return launch_class<D, kTileM, 64, F8>(a, attn_tile_kernel<D, kRT, F8>, kTileTarget, least, INT64_MAX, w, ws_bytes, s);
+    if (hipError_t e = hipGetLastError()) return e;
+    const uint32_t join = a.tile.join_blocks + a.rows.join_blocks;
+    if (join > 0) hipLaunchKernelGGL((attn_join_kernel<D, F8>), dim3(join), dim3(256), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_tokens, int32_t n_reqs, int32_t max_q_len) {
     const int64_t rows = (int64_t)2 * kTarget * 16 * (d + 2) * 4, tile = (int64_t)2 * kTileTarget * kTileM * (d + 2) * 4;
-    return (int64_t)max_q_len * G <= 32 ? rows : rows + tile;
+    return (int64_t)max_q_len * G <= kFewRows ? rows : rows + tile;
 }
 
 hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, bool f8, int32_t max_q_len, void *ws, int64_t ws_bytes,

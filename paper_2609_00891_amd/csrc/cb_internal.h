@@ -283,10 +283,12 @@ struct RowsArgs {
 
 // Attention over pages (cb_attn_paged).  Strides of the pool in units of 16
 // bytes, so that a row's place is a 32-bit number.
-struct PagedClass {           // one of the two kernels' requests, and how their keys are divided
+struct PagedClass {           // requests that are worked on in one way, and how their keys are divided
     int64_t row_min, row_max; // requests with row_min < rows <= row_max
     int32_t target;           // workgroups to divide long rows into, 0: never divide
     float *ws;                // [2 target][M (d + 2)] partial results
+    uint32_t blocks;          // workgroups of the attention and of the joining, 0: no such requests
+    uint32_t join_blocks;
 };
 struct PagedArgs {
     const uint16_t *q;
@@ -307,7 +309,7 @@ struct PagedArgs {
     const float *kscale, *vscale;   // e4m3: [n_heads]
     int32_t window, n_sinks;
     float *lse;               // NULL or [n_tokens][n_heads * G]
-    PagedClass c;
+    PagedClass rows, tile;
 };
 
 // Launchers (return hipError_t of the launch).
