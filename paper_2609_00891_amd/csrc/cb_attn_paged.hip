@@ -44,7 +44,11 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 #endif
 constexpr int kKT = 32;                 // keys of a tile
 constexpr int kTileKT = 64;             // keys of a tile of the tile kernel
-constexpr int kPartMin = 8;             // least key tiles of a part: two for each of the four waves
+#ifndef CB_PM
+#define CB_PM 24
+#endif
+constexpr int kPartMin = CB_PM;            // least key tiles of a part of rows_body: six for each of the four waves
+constexpr int kTilePartMin = 16;        // and of tile_body
 constexpr float kLag = 8.f;              // log2 by which the maximum in use may lag the true one
 #ifndef CB_T
 #define CB_T 2048
@@ -79,6 +83,20 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t u) {
 template <bool HI> __device__ __forceinline__ uint32_t e4m3_pair(uint32_t u) {
     const bf16x2_t v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HI);
     return __builtin_bit_cast(uint32_t, v);
+}
+// Bits 0 .. k.
+__device__ __forceinline__ uint32_t bits_to(int32_t k) { return k < 0 ? 0u : 0xffffffffu >> (31 - min(k, 31)); }
+// Bit c: the key c places from the first is there and seen from the place p (c <= p, and c > p - window
+// or c < sink).
+__device__ __forceinline__ uint32_t visible(int32_t p, uint32_t there, int32_t window, int32_t sink) {
+    uint32_t v = bits_to(p);
+    if (window > 0 && p >= window) v &= ~bits_to(p - window) | bits_to(sink - 1);
+    return v & there;
+}
+// x if bit c is set, else -infinity; no condition register.
+__device__ __forceinline__ float keep_if(uint32_t bits, int c, float x) {
+    const uint32_t k = (uint32_t)((int32_t)(bits << (31 - c)) >> 31);
+    return __uint_as_float((__float_as_uint(x) & k) | (~k & 0xff800000u));
 }
 __device__ __forceinline__ uint32_t fast_div(uint32_t n, const FastDiv &f) {
     const uint32_t t = __umulhi(f.m, n);
@@ -117,14 +135,14 @@ template <typename T> __device__ __forceinline__ T wave_sums(T x) {
     return x;
 }
 
-// The row tile and part of index `idx` (JOIN: of the idx-th row tile in more than one part), or false
-// behind the last.  The work of all requests is summed in fp64: whole numbers, exact below 2^53, and
+// The row tile and part of index `idx`, or false behind the last.  JOIN: of the rows of all tiles in
+// more than one part, four at a time, the idx-th four (it.part: which four of the tile).  The work of all requests is summed in fp64: whole numbers, exact below 2^53, and
 // the same in every workgroup.
 template <int M, int KT, bool JOIN>
 __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &cl, uint32_t idx, SchedLds &sh, Item &out) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     auto work_of = [&](int r) __attribute__((always_inline)) {
-        RequestWork w = {0, 0, 0};
+        RequestWork w = {0, 0, 0, 0};
         if (r < a.n_reqs) {
             const Request q = request(a, r);
             w = request_work(q.q_len, q.kv_len, (int32_t)a.G.d, M, KT, cl.row_min, cl.row_max, a.window, a.n_sinks);
@@ -142,12 +160,12 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &
     if (lane == 63) sh.work[wave] = W;
     __syncthreads();
     W = sh.work[0] + sh.work[1] + sh.work[2] + sh.work[3];
-    const int64_t c = part_tiles((int64_t)W, a.n_heads, cl.target, kPartMin);
+    const int64_t c = part_tiles((int64_t)W, a.n_heads, cl.target, KT == kKT ? kPartMin : kTilePartMin);
     uint32_t n_before = 0, s_before = 0;
     for (int r0 = 0; r0 < a.n_reqs; r0 += 256) {
         const RequestWork w = r0 == 0 ? w0 : work_of(r0 + tid);
         const int32_t parts = parts_of(w.bound, c);
-        const uint32_t n = JOIN ? (parts > 1 ? w.tiles : 0) : (uint32_t)w.tiles * parts;
+        const uint32_t n = JOIN ? (parts > 1 ? (w.rows + 3) / 4 : 0) : (uint32_t)w.tiles * parts;
         const uint32_t s = parts > 1 ? (uint32_t)w.tiles * parts : 0;
         uint32_t ni = wave_sums(n), si = wave_sums(s);
         if (r0 > 0) __syncthreads();                          // the last round's sums have been read
@@ -165,9 +183,8 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &
         }
         const uint32_t first = n_before + ni - n;
         if (idx - first < n) {
-            const uint32_t k = idx - first, tile = JOIN ? k : k / (uint32_t)parts;
-            sh.item = {r0 + tid, (int32_t)tile, JOIN ? 0 : (int32_t)(k - tile * parts), parts,
-                       (int32_t)(s_before + si - s + tile * parts)};
+            const uint32_t k = idx - first, per = JOIN ? M / 4 : (uint32_t)parts, tile = k / per;
+            sh.item = {r0 + tid, (int32_t)tile, (int32_t)(k - tile * per), parts, (int32_t)(s_before + si - s + tile * parts)};
             sh.found = 1;
         }
         n_before += total;
@@ -365,11 +382,10 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
             for (int e = 0; e < 8; ++e) x[e] = s[mt][e >> 2][e & 3] * c2;
             if (!whole) {
                 asm volatile("");                              // a branch, not selects on every tile
+                // key k0 + 4 g + c is register e's, c = 16 (e >> 2) + (e & 3)
+                const uint32_t vis = visible(pos[mt] - k0 - 4 * g, there >> (4 * g), a.window, a.n_sinks - k0 - 4 * g);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int kk = (e >> 2) * 16 + 4 * g + (e & 3);
-                    x[e] = ((there >> kk) & 1) && sees(k0 + kk, pos[mt]) ? x[e] : -HUGE_VALF;
-                }
+                for (int e = 0; e < 8; ++e) x[e] = keep_if(vis, 16 * (e >> 2) + (e & 3), x[e]);
             }
             float mx = x[0];
 #pragma unroll
@@ -766,16 +782,13 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 // key k0 + 4 h + c is register e's, c = 32 (e >> 4) + acc_key(e & 15, 0)
-                const int hi = pos[rt] - k0 - 4 * h, lo = a.window == 0 ? INT32_MIN : hi - a.window;
-                const int sink = a.n_sinks - k0 - 4 * h;
+                const int32_t p = pos[rt] - k0 - 4 * h;
                 const uint64_t bits = there >> (4 * h);
-                const uint32_t bit2[2] = {(uint32_t)bits, (uint32_t)(bits >> 32)};
+                const uint32_t vis[2] = {visible(p, (uint32_t)bits, a.window, a.n_sinks - k0 - 4 * h),
+                                         visible(p - 32, (uint32_t)(bits >> 32), a.window, a.n_sinks - k0 - 4 * h - 32)};
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int c = 32 * (e >> 4) + acc_key(e & 15, 0);
-                    const bool see = (bit2[e >> 4] & (1u << (c & 31))) && c <= hi && (c > lo || c < sink);
-                    s[rt][e >> 4][e & 15] = see ? s[rt][e >> 4][e & 15] : -HUGE_VALF;
-                }
+                for (int e = 0; e < 32; ++e)
+                    s[rt][e >> 4][e & 15] = keep_if(vis[e >> 4], acc_key(e & 15, 0), s[rt][e >> 4][e & 15]);
             }
         }
         bf16x8_t vf[2][ND];
@@ -934,12 +947,13 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
 
 // ------------------------------------------------------------------ joining parts
 
-// One wave per row of a row tile that went in parts: its partial sums, brought to the common maximum.
-// 4 D bytes a part; the wave's lanes take several parts at once (slot p0 parts p0, p0 + NP, ...) and
-// add the slots at the end, always in the same order.
+// A row of a row tile that went in parts, by one wave: the partial sums, brought to the common maximum.
+// Lane p holds the weight of part p (64 parts at a time); 4 D bytes of a part are D / 4 lanes' loads,
+// so NP parts are added at once, slot p0 takes parts p0, p0 + NP, ..., and the slots are added at the
+// end: always the same order.
 template <int D, int M, int KT, bool F8>
 __device__ __forceinline__ void join_row(const PagedArgs &a, const PagedClass &cl, const Item &it, int head, int rr) {
-    constexpr int LP = D / 4, NP = 64 / LP;                    // lanes of a part, parts at once
+    constexpr int LP = D / 4, NP = 64 / LP;
     const int lane = threadIdx.x & 63;
     const Request rq = request(a, it.req);
     const int32_t G = (int32_t)a.G.d;
@@ -954,26 +968,30 @@ __device__ __forceinline__ void join_row(const PagedArgs &a, const PagedClass &c
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) mx = fmaxf(mx, __shfl_xor(mx, s));
     const float ref = mx == -HUGE_VALF ? 0.f : mx;
-    float lr = 0.f;
+    float lt = 0.f;
     f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-    if (p0 < NP) {
-#pragma unroll 4
-        for (int p = p0; p < it.parts; p += NP) {
-            const float *w = w0 + p * step;
-            const float f = __builtin_amdgcn_exp2f(w[M * D + rr] - ref);
-            const f32x4_t x = *(const f32x4_t *)(w + rr * D + ch);
-            lr += w[M * D + M + rr] * f;
-            y += x * f;
+    for (int pb = 0; pb < it.parts; pb += 64) {
+        const int np = min(64, it.parts - pb);
+        float f = 0.f;
+        if (lane < np) {
+            const float *w = w0 + (pb + lane) * step + M * D + rr;
+            f = __builtin_amdgcn_exp2f(w[0] - ref);
+            lt += w[M] * f;
+        }
+        const float *x0 = w0 + pb * step + rr * D + ch;
+#pragma unroll 8
+        for (int q = 0; q < np; q += NP) {
+            const float fq = __shfl(f, min(q + p0, 63));
+            if (p0 < NP && q + p0 < np) y += *(const f32x4_t *)(x0 + (q + p0) * step) * fq;
         }
     }
-    f32x4_t t = {0.f, 0.f, 0.f, 0.f};
-    float lt = 0.f;
 #pragma unroll
-    for (int s = 0; s < NP; ++s) {
-        lt += __shfl(lr, s * LP);
+    for (int s = 1; s < 64; s <<= 1) lt += __shfl_xor(lt, s);
+    f32x4_t t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < NP; ++s)
 #pragma unroll
         for (int e = 0; e < 4; ++e) t[e] += __shfl(y[e], s * LP + lane % LP);
-    }
     if (lane >= LP) return;
     const float inv = (F8 ? a.vscale[head] : 1.f) / lt;
     const int32_t tok = (int32_t)fast_div((uint32_t)(row0 + rr), a.G), u = row0 + rr - tok * G;
@@ -984,16 +1002,15 @@ __device__ __forceinline__ void join_row(const PagedArgs &a, const PagedClass &c
             lt == 0.f ? -HUGE_VALF : 0.6931471805599453f * (mx + __log2f(lt));
 }
 
-// Row tiles that went in parts, 16 rows a time; blocks go round while there are more of them.
+// Four rows a time; blocks go round while there are more of them.
 template <int D, int M, int KT, bool F8>
 __device__ __forceinline__ void join_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, uint32_t blocks,
                                           SchedLds &sched) {
     for (uint32_t b = block;; b += blocks) {
         const uint32_t idx = b / (uint32_t)a.n_heads;
         Item it;
-        if (!find_item<M, KT, true>(a, cl, idx / (M / 16), sched, it)) return;
-        for (int r = threadIdx.x >> 6; r < 16; r += 4)
-            join_row<D, M, KT, F8>(a, cl, it, (int)(b - idx * a.n_heads), (int)(idx % (M / 16)) * 16 + r);
+        if (!find_item<M, KT, true>(a, cl, idx, sched, it)) return;
+        join_row<D, M, KT, F8>(a, cl, it, (int)(b - idx * a.n_heads), 4 * it.part + (threadIdx.x >> 6));
         __syncthreads();                                       // the item has been read
     }
 }
@@ -1028,7 +1045,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
 constexpr int kSmallRows = 16;          // rows of a request up to which rows_body takes it beside tile_body
 constexpr int kFewRows = 32;            // and alone, when no request is said to have more
 constexpr int kTileTarget = 512;        // workgroups of tile_body that long rows are divided into
-constexpr int kJoinBlocks = 1024;
+constexpr int kJoinBlocks = 2048;
 
 // The blocks of a class of requests and its part of the workspace.
 template <int D, int M, int KT>
@@ -1039,13 +1056,13 @@ bool prepare_class(const PagedArgs &a, PagedClass &c, int target, int64_t row_mi
     c.target = (int32_t)std::min<int64_t>(target, ws_bytes / (2 * slot));
     // no row is long enough to be divided
     const int32_t most = (int32_t)std::min<int64_t>((int64_t)a.table_width * a.page_size.d, INT32_MAX);
-    if (parts_of(key_tiles_bound(most, M, a.window, a.n_sinks, KT), kPartMin) == 1) c.target = 0;
+    if (parts_of(key_tiles_bound(most, M, a.window, a.n_sinks, KT), KT == kKT ? kPartMin : kTilePartMin) == 1) c.target = 0;
     c.ws = (float *)ws;
     ws += 2 * slot * c.target;
     ws_bytes -= 2 * slot * c.target;
     const int64_t tiles = row_tiles_bound(a.n_tokens, a.n_reqs, a.G.d, M, row_max);
     const int64_t blocks = (tiles + c.target / a.n_heads) * a.n_heads;
-    const int64_t join = std::min<int64_t>(tiles, c.target / a.n_heads) * (M / 16) * a.n_heads;
+    const int64_t join = std::min<int64_t>(tiles, c.target / a.n_heads) * (M / 4) * a.n_heads;
     if (blocks > INT32_MAX / 2 || join > INT32_MAX / 2) return false;
     c.blocks = (uint32_t)blocks;
     c.join_blocks = (uint32_t)std::min<int64_t>(join, kJoinBlocks);

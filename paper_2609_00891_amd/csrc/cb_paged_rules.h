@@ -76,12 +76,14 @@ struct RequestWork {
     int32_t tiles;   // row tiles, 0: not this kernel's
     int32_t tokens;  // most tokens in a row tile
     int64_t bound;   // key tiles of a row tile
+    uint32_t rows;
 };
 CB_HD RequestWork request_work(int32_t q_len, int32_t kv_len, int32_t G, int32_t M, int32_t KT, int64_t row_min,
                                int64_t row_max, int32_t window, int32_t n_sinks) {
-    RequestWork w = {0, 0, 0};
+    RequestWork w = {0, 0, 0, 0};
     const int64_t rows = (int64_t)q_len * G;
     if (rows <= row_min || rows > row_max) return w;
+    w.rows = (uint32_t)rows;
     w.tiles = (int32_t)((rows + M - 1) / M);
     const int32_t t = (M - 1) / G + 2;
     w.tokens = t < q_len ? t : q_len;
