@@ -6,7 +6,7 @@
 // exp(m - m').  In log2 units throughout (scale carries log2 e).
 //
 // Rows of one request and KV head are (token, head of its group) pairs, so the
-// group's query heads share every K and V row read.  Row tiles of 16 MT rows.
+// group's query heads share every K and V row read.  Row tiles of 16 rows.
 //
 // attn_rows_kernel: four waves, each with its own key tiles of 32 keys, from
 //   memory straight into matrix-core operands:
@@ -37,23 +37,12 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 
-#define CB_IL 1
-#define CB_PRIO 1
-#ifndef CB_SCHED
-#define CB_SCHED 1
-#endif
 constexpr int kKT = 32;                 // keys of a tile
 constexpr int kTileKT = 64;             // keys of a tile of the tile kernel
-#ifndef CB_PM
-#define CB_PM 24
-#endif
-constexpr int kPartMin = CB_PM;            // least key tiles of a part of rows_body: six for each of the four waves
+constexpr int kPartMin = 24;            // least key tiles of a part of rows_body: six for each of the four waves
 constexpr int kTilePartMin = 16;        // and of tile_body
 constexpr float kLag = 8.f;              // log2 by which the maximum in use may lag the true one
-#ifndef CB_T
-#define CB_T 2048
-#endif
-constexpr int kTarget = CB_T;           // workgroups that long rows are divided into
+constexpr int kTarget = 2048;           // workgroups that long rows are divided into
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     f32x2_t v = {lo, hi};
@@ -114,7 +103,7 @@ __device__ __forceinline__ Request request(const PagedArgs &a, int r) {
 }
 
 struct Item { int32_t req, tile, part, parts, slot; };   // slot: of the first part's partial result
-struct SchedLds { double work[4]; uint32_t items[4], slots[4]; Item item; int32_t found; };
+template <int NW> struct SchedLds { double work[NW]; uint32_t items[NW], slots[NW]; Item item; int32_t found; };
 
 // Inclusive sums over a wave by data-parallel moves: within rows of 16 lanes, then across them.
 template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t x) {
@@ -138,8 +127,9 @@ template <typename T> __device__ __forceinline__ T wave_sums(T x) {
 // The row tile and part of index `idx`, or false behind the last.  JOIN: of the rows of all tiles in
 // more than one part, four at a time, the idx-th four (it.part: which four of the tile).  The work of all requests is summed in fp64: whole numbers, exact below 2^53, and
 // the same in every workgroup.
-template <int M, int KT, bool JOIN>
-__device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &cl, uint32_t idx, SchedLds &sh, Item &out) {
+template <int M, int KT, bool JOIN, int NW>
+__device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &cl, uint32_t idx, SchedLds<NW> &sh, Item &out) {
+    constexpr int NT = 64 * NW;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     auto work_of = [&](int r) __attribute__((always_inline)) {
         RequestWork w = {0, 0, 0, 0};
@@ -152,17 +142,19 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &
     if (tid == 0) sh.found = 0;
     const RequestWork w0 = work_of(tid);
     double W = (double)w0.tiles * (double)w0.bound;
-    for (int r = tid + 256; r < a.n_reqs; r += 256) {
+    for (int r = tid + NT; r < a.n_reqs; r += NT) {
         const RequestWork w = work_of(r);
         W += (double)w.tiles * (double)w.bound;
     }
     W = wave_sums(W);
     if (lane == 63) sh.work[wave] = W;
     __syncthreads();
-    W = sh.work[0] + sh.work[1] + sh.work[2] + sh.work[3];
+    W = 0.0;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) W += sh.work[v];
     const int64_t c = part_tiles((int64_t)W, a.n_heads, cl.target, KT == kKT ? kPartMin : kTilePartMin);
     uint32_t n_before = 0, s_before = 0;
-    for (int r0 = 0; r0 < a.n_reqs; r0 += 256) {
+    for (int r0 = 0; r0 < a.n_reqs; r0 += NT) {
         const RequestWork w = r0 == 0 ? w0 : work_of(r0 + tid);
         const int32_t parts = parts_of(w.bound, c);
         const uint32_t n = JOIN ? (parts > 1 ? (w.rows + 3) / 4 : 0) : (uint32_t)w.tiles * parts;
@@ -176,7 +168,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &
         __syncthreads();
         uint32_t total = 0, s_total = 0;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
+        for (int v = 0; v < NW; ++v) {
             if (v < wave) { ni += sh.items[v]; si += sh.slots[v]; }
             total += sh.items[v];
             s_total += sh.slots[v];
@@ -211,21 +203,21 @@ template <int D, bool F8> struct Geo {
     }
 };
 
-template <int D> struct RowsLds {
-    float o[4][16][D + 4];                                     // each wave's results
-    float ml[4][16][2];
+template <int D, int NW> struct RowsLds {
+    float o[NW][16][D + 4];                                    // each wave's results
+    float ml[NW][16][2];
 };
 
-template <int D, int MT, bool F8>
-__device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds &sched,
-                                          RowsLds<D> &lds) {
+template <int D, bool F8, int NW>
+__device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds<NW> &sched,
+                                          RowsLds<D, NW> &lds) {
     using Ge = Geo<D, F8>;
-    constexpr int M = 16 * MT, E = Ge::E;
+    constexpr int M = 16, E = Ge::E;
     auto &ol = lds.o;
     auto &ml = lds.ml;
     const int head = (int)(block % (uint32_t)a.n_heads);
     Item it;
-    if (!find_item<M, kKT, false>(a, cl, block / (uint32_t)a.n_heads, sched, it)) return;
+    if (!find_item<M, kKT, false, NW>(a, cl, block / (uint32_t)a.n_heads, sched, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -242,17 +234,16 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
     const int32_t *table = a.table + it.req * a.table_stride;
     const char *kp = a.k + head * a.s_head, *vp = a.v + head * a.s_head;
 
-    // queries: row n of subtile mt (rows behind the last repeat it)
-    bf16x8_t qf[MT][Ge::NS];
-    int32_t pos[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int32_t row = row0 + min(16 * mt + n, n_rows - 1);
+    // queries: row n (rows behind the last repeat it)
+    bf16x8_t qf[Ge::NS];
+    int32_t pos;
+    {
+        const int32_t row = row0 + min(n, n_rows - 1);
         const int32_t tok = (int32_t)fast_div((uint32_t)row, a.G), u = row - tok * G;
-        pos[mt] = rq.kv_len - rq.q_len + tok;
+        pos = rq.kv_len - rq.q_len + tok;
         const uint16_t *q = a.q + (int64_t)(rq.row0 + tok) * a.q_tok + (int64_t)(head * G + u) * a.q_head;
 #pragma unroll
-        for (int s = 0; s < Ge::NS; ++s) qf[mt][s] = *(const bf16x8_t *)(q + Ge::chan(s, g));
+        for (int s = 0; s < Ge::NS; ++s) qf[s] = *(const bf16x8_t *)(q + Ge::chan(s, g));
     }
     const float c2 = F8 ? a.scale_log2 * a.kscale[head] : a.scale_log2;
 
@@ -326,15 +317,12 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
                (a.window == 0 || k0 > p_hi - a.window || k0 + kKT <= a.n_sinks);
     };
 
-    f32x4_t o[MT][E];
-    float m[MT], l[MT];
+    f32x4_t o[E];
+    float m, l;
+    m = -HUGE_VALF;
+    l = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        m[mt] = -HUGE_VALF;
-        l[mt] = 0.f;
-#pragma unroll
-        for (int i = 0; i < E; ++i) o[mt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int i = 0; i < E; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
     // A tile's K and V are requested while the tile before it is worked on: K as soon as its registers
     // have met the queries, V as soon as its own have become operands.
@@ -346,16 +334,15 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
         there = place();
         load_k();
         load_v();
-        if (v0 + 4 < v1) look_up(kt.tile(v0 + 4));
+        if (v0 + NW < v1) look_up(kt.tile(v0 + NW));
     }
-    for (int32_t v = v0; v < v1; v += 4) {
+    for (int32_t v = v0; v < v1; v += NW) {
         const int32_t k0 = kt.tile(v) * kKT;
         const bool whole = whole_tile(k0, there);
-        f32x4_t s[MT][2];
+        f32x4_t s[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) s[mt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int st = 0; st < Ge::NS; ++st) {
                 bf16x8_t kf;
@@ -365,53 +352,49 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
                 } else {
                     kf = frag(kr[t][4 * st], kr[t][4 * st + 1], kr[t][4 * st + 2], kr[t][4 * st + 3]);
                 }
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) s[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][st], s[mt][t], 0, 0, 0);
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[st], s[t], 0, 0, 0);
             }
         }
-        if (v + 4 < v1) {
+        if (v + NW < v1) {
             there_n = place();
-            if (v + 8 < v1) look_up(kt.tile(v + 8));
+            if (v + 2 * NW < v1) look_up(kt.tile(v + 2 * NW));
             load_k();
         }
-        uint32_t p2[MT][4];                                    // exp2(s - m) as the operand of P V
+        uint32_t p2[4];                                    // exp2(s - m) as the operand of P V
+        float x[8];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            float x[8];
+        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * c2;
+        if (!whole) {
+            asm volatile("");                              // a branch, not selects on every tile
+            // key k0 + 4 g + c is register e's, c = 16 (e >> 2) + (e & 3)
+            const uint32_t vis = visible(pos - k0 - 4 * g, there >> (4 * g), a.window, a.n_sinks - k0 - 4 * g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = s[mt][e >> 2][e & 3] * c2;
-            if (!whole) {
-                asm volatile("");                              // a branch, not selects on every tile
-                // key k0 + 4 g + c is register e's, c = 16 (e >> 2) + (e & 3)
-                const uint32_t vis = visible(pos[mt] - k0 - 4 * g, there >> (4 * g), a.window, a.n_sinks - k0 - 4 * g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = keep_if(vis, 16 * (e >> 2) + (e & 3), x[e]);
-            }
-            float mx = x[0];
-#pragma unroll
-            for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
-            // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
-            if (__any(mx > m[mt] + kLag)) {
-                mx = fmaxf(mx, __shfl_xor(mx, 16));
-                mx = fmaxf(mx, __shfl_xor(mx, 32));
-                mx = fmaxf(mx, m[mt]);
-                const float al = __builtin_amdgcn_exp2f(m[mt] - (mx == -HUGE_VALF ? 0.f : mx));
-                m[mt] = mx;
-                l[mt] *= al;
-#pragma unroll
-                for (int i = 0; i < E; ++i) o[mt][i] *= al;
-            }
-            const float ref = m[mt] == -HUGE_VALF ? 0.f : m[mt];   // nothing seen so far: every weight is zero
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
-                sum += x[e];
-            }
-            l[mt] += sum;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) p2[mt][q] = pack_bf16(x[2 * q], x[2 * q + 1]);
+            for (int e = 0; e < 8; ++e) x[e] = keep_if(vis, 16 * (e >> 2) + (e & 3), x[e]);
         }
+        float mx = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+        // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
+        if (__any(mx > m + kLag)) {
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            mx = fmaxf(mx, m);
+            const float al = __builtin_amdgcn_exp2f(m - (mx == -HUGE_VALF ? 0.f : mx));
+            m = mx;
+            l *= al;
+#pragma unroll
+            for (int i = 0; i < E; ++i) o[i] *= al;
+        }
+        const float ref = m == -HUGE_VALF ? 0.f : m;   // nothing seen so far: every weight is zero
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
+            sum += x[e];
+        }
+        l += sum;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) p2[q] = pack_bf16(x[2 * q], x[2 * q + 1]);
         if (!whole) {
             // In a tile with a key that some row does not see a NaN or infinity of V would meet zero
             // weights: it becomes a zero here and reaches the rows that see it after the last tile.
@@ -446,19 +429,17 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
             for (int q = 0; q < 4; ++q)
                 f[q] = __builtin_amdgcn_perm(vb[2 * q + 1][i >> 1], vb[2 * q][i >> 1], (i & 1) ? 0x07060302u : 0x05040100u);
             const bf16x8_t vf = frag(f[0], f[1], f[2], f[3]);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-                o[mt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(p2[mt][0], p2[mt][1], p2[mt][2], p2[mt][3]),
-                                                                  o[mt][i], 0, 0, 0);
+            o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(p2[0], p2[1], p2[2], p2[3]),
+                                                              o[i], 0, 0, 0);
         }
-        if (v + 4 < v1) load_v();
+        if (v + NW < v1) load_v();
         there = there_n;
     }
     if (__any(odd != 0)) {
         // NaNs and infinities of V that were left out of tiles which some row does not see whole: they
         // come to the rows that see their keys (whatever finite weight they have)
 #pragma unroll 1
-        for (int32_t v = v0; v < v1; v += 4) {
+        for (int32_t v = v0; v < v1; v += NW) {
             const int32_t k0 = kt.tile(v) * kKT;
             look_up(kt.tile(v));
             there = place();
@@ -473,77 +454,74 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
 #pragma unroll
                     for (int i = 0; i < E; i += 2) {
                         const uint32_t u = F8 ? e4m3_pair<false>(*(const uint16_t *)(vrow + c + i)) : *(const uint32_t *)(vrow + 2 * (c + i));
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            const bool see = sees(k0 + kk, pos[mt]);
-                            if (see && not_finite(u & 0xffffu)) o[mt][i][r] += bf_lo(u);
-                            if (see && not_finite(u & 0xffff0000u)) o[mt][i + 1][r] += bf_hi(u);
-                        }
+                        const bool see = sees(k0 + kk, pos);
+                        if (see && not_finite(u & 0xffffu)) o[i][r] += bf_lo(u);
+                        if (see && not_finite(u & 0xffff0000u)) o[i + 1][r] += bf_hi(u);
                     }
                 }
             }
         }
     }
 
-    // ---- the four waves' results, joined in their order
+    // ---- the waves' results, joined in their order
     const float vs = F8 ? a.vscale[head] : 1.f;
+    float lt = l;
+    lt += __shfl_xor(lt, 16);
+    lt += __shfl_xor(lt, 32);
+    if (g == 0) {
+        ml[wave][n][0] = m;
+        ml[wave][n][1] = lt;
+    }
+    __syncthreads();
+    float mx = ml[0][n][0];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        float lt = l[mt];
-        lt += __shfl_xor(lt, 16);
-        lt += __shfl_xor(lt, 32);
-        if (mt > 0) __syncthreads();                           // the last subtile's results have been read
-        if (g == 0) {
-            ml[wave][n][0] = m[mt];
-            ml[wave][n][1] = lt;
+    for (int w = 1; w < NW; ++w) mx = fmaxf(mx, ml[w][n][0]);
+    const float f = __builtin_amdgcn_exp2f(m - (mx == -HUGE_VALF ? 0.f : mx));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int c = 4 * g + r;
+        if (c < Ge::NC) {
+#pragma unroll
+            for (int i = 0; i < E; i += 4)
+                *(float4 *)&ol[wave][n][E * c + i] = make_float4(o[i][r] * f, o[i + 1][r] * f,
+                                                                o[i + 2][r] * f, o[i + 3][r] * f);
         }
-        __syncthreads();
-        const float mx = fmaxf(fmaxf(ml[0][n][0], ml[1][n][0]), fmaxf(ml[2][n][0], ml[3][n][0]));
-        const float f = __builtin_amdgcn_exp2f(m[mt] - (mx == -HUGE_VALF ? 0.f : mx));
+    }
+    __syncthreads();
+    const int row = tid / (D / 8), ch = tid % (D / 8) * 8;
+    if (row < 16 && row < n_rows) {
+        float mr = ml[0][row][0];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int c = 4 * g + r;
-            if (c < Ge::NC) {
+        for (int w = 1; w < NW; ++w) mr = fmaxf(mr, ml[w][row][0]);
+        const float ref = mr == -HUGE_VALF ? 0.f : mr;
+        float lr = 0.f, y[8] = {};
 #pragma unroll
-                for (int i = 0; i < E; i += 4)
-                    *(float4 *)&ol[wave][n][E * c + i] = make_float4(o[mt][i][r] * f, o[mt][i + 1][r] * f,
-                                                                    o[mt][i + 2][r] * f, o[mt][i + 3][r] * f);
-            }
+        for (int w = 0; w < NW; ++w) {
+            lr += ml[w][row][1] * __builtin_amdgcn_exp2f(ml[w][row][0] - ref);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] += ol[w][row][ch + e];
         }
-        __syncthreads();
-        const int row = tid / (D / 8), ch = tid % (D / 8) * 8, rr = 16 * mt + row;
-        if (row < 16 && rr < n_rows) {
-            const float mr = fmaxf(fmaxf(ml[0][row][0], ml[1][row][0]), fmaxf(ml[2][row][0], ml[3][row][0]));
-            const float ref = mr == -HUGE_VALF ? 0.f : mr;
-            float lr = 0.f, y[8] = {};
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                lr += ml[w][row][1] * __builtin_amdgcn_exp2f(ml[w][row][0] - ref);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] += ol[w][row][ch + e];
+        if (it.parts > 1) {
+            float *w = cl.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
+            *(float4 *)(w + row * D + ch) = make_float4(y[0], y[1], y[2], y[3]);
+            *(float4 *)(w + row * D + ch + 4) = make_float4(y[4], y[5], y[6], y[7]);
+            if (ch == 0) {
+                w[M * D + row] = mr;
+                w[M * D + M + row] = lr;
             }
-            if (it.parts > 1) {
-                float *w = cl.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
-                *(float4 *)(w + rr * D + ch) = make_float4(y[0], y[1], y[2], y[3]);
-                *(float4 *)(w + rr * D + ch + 4) = make_float4(y[4], y[5], y[6], y[7]);
-                if (ch == 0) {
-                    w[M * D + rr] = mr;
-                    w[M * D + M + rr] = lr;
-                }
-            } else {
-                const float inv = lr == 0.f ? 0.f : vs / lr;
-                const int32_t tok = (int32_t)fast_div((uint32_t)(row0 + rr), a.G), u = row0 + rr - tok * G;
-                uint16_t *out = a.out + (int64_t)(rq.row0 + tok) * a.o_tok + (int64_t)(head * G + u) * a.o_head + ch;
-                if (lr == 0.f) {
+        } else {
+            const float inv = lr == 0.f ? 0.f : vs / lr;
+            const int32_t tok = (int32_t)fast_div((uint32_t)(row0 + row), a.G), u = row0 + row - tok * G;
+            uint16_t *out = a.out + (int64_t)(rq.row0 + tok) * a.o_tok + (int64_t)(head * G + u) * a.o_head + ch;
+            if (lr == 0.f) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = 0.f;
-                }
-                *(uint4 *)out = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
-                                           pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
-                if (a.lse && ch == 0)
-                    a.lse[(int64_t)(rq.row0 + tok) * (a.n_heads * G) + head * G + u] =
-                        lr == 0.f ? -HUGE_VALF : 0.6931471805599453f * (mr + __log2f(lr));
+                for (int e = 0; e < 8; ++e) y[e] = 0.f;
             }
+            *(uint4 *)out = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
+                                       pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
+            if (a.lse && ch == 0)
+                a.lse[(int64_t)(rq.row0 + tok) * (a.n_heads * G) + head * G + u] =
+                    lr == 0.f ? -HUGE_VALF : 0.6931471805599453f * (mr + __log2f(lr));
         }
     }
 }
@@ -569,25 +547,26 @@ __device__ __forceinline__ float both_halves_max(float x) {
 }
 
 template <int D> struct TileLds {
-    static constexpr int KS = 2 * D + 16, VS = 2 * D + 32;     // bytes between rows of K and V
+    // bytes between rows of K and V: 16 rows' 16-byte pieces, and 4 rows' 64 bytes, in 64 banks each
+    static constexpr int KS = 2 * D + 16, VS = D == 96 ? 192 : 2 * D + 64;
     char kv[2][kTileKT * (KS + VS)];
     int32_t odd;
 };
 
-template <int D, int RT, bool F8>
-__device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds &sched,
+template <int D, bool F8, int NW>
+__device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds<NW> &sched,
                                           TileLds<D> &tl) {
-    constexpr int M = 128 * RT, KT = kTileKT, NS = D / 16, ND = D / 32;
+    constexpr int M = 32 * NW, NT = 64 * NW, KT = kTileKT, NS = D / 16, ND = D / 32;
     constexpr int KS = TileLds<D>::KS, VS = TileLds<D>::VS;
     constexpr int CPR = F8 ? D / 16 : D / 8;                   // 16-byte pieces of a row in memory
-    constexpr int NP = (KT * CPR + 255) / 256;                 // pieces of a thread, for each of K and V
-    constexpr bool RAGGED = KT * CPR % 256 != 0;
+    constexpr int NP = (KT * CPR + NT - 1) / NT;                 // pieces of a thread, for each of K and V
+    constexpr bool RAGGED = KT * CPR % NT != 0;
     constexpr int STAGE = KT * (KS + VS);
     char *lds = tl.kv[0];
     int32_t &odd = tl.odd;
     const int head = (int)(block % (uint32_t)a.n_heads);
     Item it;
-    if (!find_item<M, KT, false>(a, cl, block / (uint32_t)a.n_heads, sched, it)) return;
+    if (!find_item<M, KT, false, NW>(a, cl, block / (uint32_t)a.n_heads, sched, it)) return;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -610,24 +589,23 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     c2 = fmaxf(fabsf(c2), 1.17549435e-38f);
     if (tid == 0) odd = 0;
 
-    // queries of this wave's RT subtiles of 32 rows (rows behind the last repeat it)
-    bf16x8_t qf[RT][NS];
-    int32_t pos[RT];                                           // of the lane's rows
-    const int w0 = 32 * RT * wave;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int32_t row = row0 + min(w0 + 32 * rt + n, n_rows - 1);
+    // queries of this wave's 32 rows (rows behind the last repeat it)
+    bf16x8_t qf[NS];
+    int32_t pos;                                           // of the lane's rows
+    const int w0 = 32 * wave;
+    {
+        const int32_t row = row0 + min(w0 + n, n_rows - 1);
         const int32_t tok = (int32_t)fast_div((uint32_t)row, a.G), u = row - tok * G;
-        pos[rt] = base + tok;
+        pos = base + tok;
         const uint16_t *q = a.q + (int64_t)(rq.row0 + tok) * a.q_tok + (int64_t)(head * G + u) * a.q_head;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const uint4 x = *(const uint4 *)(q + 16 * s + 8 * h);
-            qf[rt][s] = frag(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+            qf[s] = frag(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
         }
     }
-    const int32_t s_lo = __builtin_amdgcn_readfirstlane(pos[0]);
-    const int32_t s_hi = __builtin_amdgcn_readlane(pos[RT - 1], 31);
+    const int32_t s_lo = __builtin_amdgcn_readfirstlane(pos);
+    const int32_t s_hi = __builtin_amdgcn_readlane(pos, 31);
 
     // the places of a tile's 64 rows: lane l looks up key l, a tile ahead of the loads that use it
     int32_t page = 0;
@@ -650,11 +628,11 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     auto load = [&](uint32_t off) __attribute__((always_inline)) {
         uint32_t ro[NP];
 #pragma unroll
-        for (int i = 0; i < NP; ++i) ro[i] = (uint32_t)__shfl((int)off, (tid + 256 * i) / CPR & 63);
+        for (int i = 0; i < NP; ++i) ro[i] = (uint32_t)__shfl((int)off, (tid + NT * i) / CPR & 63);
         __builtin_amdgcn_sched_barrier(0);                     // one trip to the other lanes for all of them
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int id = tid + 256 * i;
+            const int id = tid + NT * i;
             const int row = id / CPR, c = id - row * CPR;
             const uint64_t at = (uint64_t)ro[i] * 16 + 16 * c;
             if (RAGGED && id >= KT * CPR) continue;
@@ -672,7 +650,8 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
             asm volatile("");
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const int id = tid + 256 * i, row = id / CPR;
+                const int id = tid + NT * i, row = id / CPR;
+                if (RAGGED && id >= KT * CPR) continue;
                 const uint32_t is = 0u - (uint32_t)((there >> (row & 63)) & 1);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -685,7 +664,7 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int id = tid + 256 * i;
+            const int id = tid + NT * i;
             if (RAGGED && id >= KT * CPR) continue;
             const int row = id / CPR, c = id - row * CPR;
             if constexpr (F8) {
@@ -709,15 +688,12 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     };
     auto next_tile = [&](int32_t t) __attribute__((always_inline)) { return t + 1 == kt.sink ? kt.first : t + 1; };
 
-    f32x16_t o[RT][ND];
-    float m[RT], l[RT];
+    f32x16_t o[ND];
+    float m, l;
+    m = -HUGE_VALF;
+    l = 0.f;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        m[rt] = -HUGE_VALF;
-        l[rt] = 0.f;
-#pragma unroll
-        for (int q = 0; q < ND; ++q) o[rt][q] = f32x16_t{};
-    }
+    for (int q = 0; q < ND; ++q) o[q] = f32x16_t{};
     // V^T operand: keys 16 kk + 4 h + {0 .. 3} and + 8, channel 32 q + (lane & 31)
     const int vt = (4 * h + ((lane >> 2) & 3)) * VS + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
 
@@ -749,91 +725,73 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
         if (v + 1 < v1) load(place(there_n));
         if (v + 2 < v1) look_up(t2);
         const char *ks = lds + st * STAGE, *vs = ks + KT * KS;
-        f32x16_t s[RT][2];
-#if CB_PRIO
+        f32x16_t s[2];
         __builtin_amdgcn_s_setprio(1);
-#endif
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x16_t{};
+        s[0] = s[1] = f32x16_t{};
 #pragma unroll
         for (int q = 0; q < NS; ++q) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const bf16x8_t kf = *(const bf16x8_t *)(ks + (32 * t + n) * KS + 32 * q + 16 * h);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    s[rt][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[rt][q], s[rt][t], 0, 0, 0);
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[q], s[t], 0, 0, 0);
             }
         }
-#if CB_SCHED & 1
         __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
         for (int i = 0; i < 2 * NS - 4; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, RT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, 4 * RT, 0);
-#endif
-#if CB_PRIO
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
         __builtin_amdgcn_s_setprio(0);
-#endif
         if (!seen(k0, there, s_lo, s_hi)) {
             asm volatile("");                                  // a branch, not selects on every tile
+            // key k0 + 4 h + c is register e's, c = 32 (e >> 4) + acc_key(e & 15, 0)
+            const int32_t p = pos - k0 - 4 * h;
+            const uint64_t bits = there >> (4 * h);
+            const uint32_t vis[2] = {visible(p, (uint32_t)bits, a.window, a.n_sinks - k0 - 4 * h),
+                                     visible(p - 32, (uint32_t)(bits >> 32), a.window, a.n_sinks - k0 - 4 * h - 32)};
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                // key k0 + 4 h + c is register e's, c = 32 (e >> 4) + acc_key(e & 15, 0)
-                const int32_t p = pos[rt] - k0 - 4 * h;
-                const uint64_t bits = there >> (4 * h);
-                const uint32_t vis[2] = {visible(p, (uint32_t)bits, a.window, a.n_sinks - k0 - 4 * h),
-                                         visible(p - 32, (uint32_t)(bits >> 32), a.window, a.n_sinks - k0 - 4 * h - 32)};
-#pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    s[rt][e >> 4][e & 15] = keep_if(vis[e >> 4], acc_key(e & 15, 0), s[rt][e >> 4][e & 15]);
-            }
+            for (int e = 0; e < 32; ++e)
+                s[e >> 4][e & 15] = keep_if(vis[e >> 4], acc_key(e & 15, 0), s[e >> 4][e & 15]);
         }
         bf16x8_t vf[2][ND];
         read_v(vs, 0, vf[0]);
         __builtin_amdgcn_sched_barrier(0);
-        uint32_t pk[RT][16];
+        uint32_t pk[16];
+        float mx = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float mx = max3(s[rt][0][0], s[rt][0][1], s[rt][0][2]);
+        for (int e = 3; e < 31; e += 2) mx = max3(mx, s[e >> 4][e & 15], s[(e + 1) >> 4][(e + 1) & 15]);
+        mx = max3(mx, s[1][15], s[1][15]);
+        mx = both_halves_max(mx) * c2;
+        // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
+        if (__any(mx > m + kLag)) {
+            const float mn = fmaxf(m, mx);
+            const float al = __builtin_amdgcn_exp2f(m - (mn == -HUGE_VALF ? 0.f : mn));
+            m = mn;
+            l *= al;
 #pragma unroll
-            for (int e = 3; e < 31; e += 2) mx = max3(mx, s[rt][e >> 4][e & 15], s[rt][(e + 1) >> 4][(e + 1) & 15]);
-            mx = max3(mx, s[rt][1][15], s[rt][1][15]);
-            mx = both_halves_max(mx) * c2;
-            // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
-            if (__any(mx > m[rt] + kLag)) {
-                const float mn = fmaxf(m[rt], mx);
-                const float al = __builtin_amdgcn_exp2f(m[rt] - (mn == -HUGE_VALF ? 0.f : mn));
-                m[rt] = mn;
-                l[rt] *= al;
-#pragma unroll
-                for (int q = 0; q < ND; ++q) o[rt][q] *= al;
-            }
-            const float ref = m[rt] == -HUGE_VALF ? 0.f : m[rt];
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e >> 3][2 * e & 15], c2, -ref));
-                const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e >> 3][(2 * e & 15) + 1], c2, -ref));
-                sum += x0;
-                sum += x1;
-                pk[rt][e] = pack_bf16(x0, x1);
-            }
-            l[rt] += sum;
+            for (int q = 0; q < ND; ++q) o[q] *= al;
         }
-#if CB_IL
+        const float ref = m == -HUGE_VALF ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 3][2 * e & 15], c2, -ref));
+            const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 3][(2 * e & 15) + 1], c2, -ref));
+            sum += x0;
+            sum += x1;
+            pk[e] = pack_bf16(x0, x1);
+        }
+        l += sum;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
             if (kk < 3) read_v(vs, kk + 1, vf[(kk + 1) & 1]);
 #pragma unroll
             for (int q = 0; q < ND; ++q)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    o[rt][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        vf[kk & 1][q], frag(pk[rt][4 * kk], pk[rt][4 * kk + 1], pk[rt][4 * kk + 2], pk[rt][4 * kk + 3]),
-                        o[rt][q], 0, 0, 0);
+                o[q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    vf[kk & 1][q], frag(pk[4 * kk], pk[4 * kk + 1], pk[4 * kk + 2], pk[4 * kk + 3]),
+                    o[q], 0, 0, 0);
         }
         // a quarter of the weights, then its products beside the next quarter's
         __builtin_amdgcn_sched_group_barrier(0x406, 28, 1);
@@ -842,33 +800,11 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
             if (kk < 3) __builtin_amdgcn_sched_group_barrier(0x100, 2 * ND, 1);
 #pragma unroll
             for (int q = 0; q < ND; ++q) {
-                __builtin_amdgcn_sched_group_barrier(0x008, RT, 1);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
                 if (kk < 3) __builtin_amdgcn_sched_group_barrier(0x406, (28 + ND - 1) / ND, 1);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-#else
-#if CB_PRIO
-        __builtin_amdgcn_s_setprio(1);
-#endif
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            // the next step's operands are requested before this step's products
-            if (kk < 3) read_v(vs, kk + 1, vf[(kk + 1) & 1]);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int q = 0; q < ND; ++q)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    o[rt][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        vf[kk & 1][q], frag(pk[rt][4 * kk], pk[rt][4 * kk + 1], pk[rt][4 * kk + 2], pk[rt][4 * kk + 3]),
-                        o[rt][q], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#endif
-#if CB_PRIO
-        __builtin_amdgcn_s_setprio(0);
-#endif
         if (v + 1 < v1) store(st ^ 1, there_n, !seen(t1 * KT, there_n, p_lo, p_hi));
         there = there_n;
         t0 = t1;
@@ -890,58 +826,52 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
                 if (!((there >> kk) & 1)) continue;
                 const char *vrow = vp + (uint64_t)(uint32_t)__shfl((int)off, kk) * 16;
                 const int32_t key = k0 + kk;
+                const bool see = key <= pos && (a.window == 0 || key > pos - a.window || key < a.n_sinks);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const bool see = key <= pos[rt] && (a.window == 0 || key > pos[rt] - a.window || key < a.n_sinks);
+                for (int q = 0; q < ND; ++q)
 #pragma unroll
-                    for (int q = 0; q < ND; ++q)
-#pragma unroll
-                        for (int r = 0; r < 16; r += 2) {
-                            const int c = 32 * q + acc_key(r, h);
-                            const uint32_t u = F8 ? e4m3_pair<false>(*(const uint16_t *)(vrow + c)) : *(const uint32_t *)(vrow + 2 * c);
-                            if (see && not_finite(u & 0xffffu)) o[rt][q][r] += bf_lo(u);
-                            if (see && not_finite(u & 0xffff0000u)) o[rt][q][r + 1] += bf_hi(u);
-                        }
-                }
+                    for (int r = 0; r < 16; r += 2) {
+                        const int c = 32 * q + acc_key(r, h);
+                        const uint32_t u = F8 ? e4m3_pair<false>(*(const uint16_t *)(vrow + c)) : *(const uint32_t *)(vrow + 2 * c);
+                        if (see && not_finite(u & 0xffffu)) o[q][r] += bf_lo(u);
+                        if (see && not_finite(u & 0xffff0000u)) o[q][r + 1] += bf_hi(u);
+                    }
             }
         }
     }
 
     const float vsc = F8 ? a.vscale[head] : 1.f;
+    const int rr = w0 + n;
+    const float lr = l + __shfl_xor(l, 32);
+    if (rr >= n_rows) return;
+    if (it.parts > 1) {
+        float *w = cl.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int rr = w0 + 32 * rt + n;
-        const float lr = l[rt] + __shfl_xor(l[rt], 32);
-        if (rr >= n_rows) continue;
-        if (it.parts > 1) {
-            float *w = cl.ws + ((int64_t)(it.slot + it.part) * a.n_heads + head) * (M * (D + 2));
+        for (int q = 0; q < ND; ++q)
 #pragma unroll
-            for (int q = 0; q < ND; ++q)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4)
-                    *(float4 *)(w + rr * D + 32 * q + acc_key(r, h)) =
-                        make_float4(o[rt][q][r], o[rt][q][r + 1], o[rt][q][r + 2], o[rt][q][r + 3]);
-            if (h == 0) {
-                w[M * D + rr] = m[rt];
-                w[M * D + M + rr] = lr;
-            }
-        } else {
-            const int32_t tok = (int32_t)fast_div((uint32_t)(row0 + rr), a.G), u = row0 + rr - tok * G;
-            uint16_t *out = a.out + (int64_t)(rq.row0 + tok) * a.o_tok + (int64_t)(head * G + u) * a.o_head;
-            const float inv = vsc / lr;
-#pragma unroll
-            for (int q = 0; q < ND; ++q)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    uint2 y = make_uint2(pack_bf16(o[rt][q][r] * inv, o[rt][q][r + 1] * inv),
-                                         pack_bf16(o[rt][q][r + 2] * inv, o[rt][q][r + 3] * inv));
-                    if (lr == 0.f) y = make_uint2(0u, 0u);
-                    *(uint2 *)(out + 32 * q + acc_key(r, h)) = y;
-                }
-            if (a.lse && h == 0)
-                a.lse[(int64_t)(rq.row0 + tok) * (a.n_heads * G) + head * G + u] =
-                    lr == 0.f ? -HUGE_VALF : 0.6931471805599453f * (m[rt] + __log2f(lr));
+            for (int r = 0; r < 16; r += 4)
+                *(float4 *)(w + rr * D + 32 * q + acc_key(r, h)) =
+                    make_float4(o[q][r], o[q][r + 1], o[q][r + 2], o[q][r + 3]);
+        if (h == 0) {
+            w[M * D + rr] = m;
+            w[M * D + M + rr] = lr;
         }
+    } else {
+        const int32_t tok = (int32_t)fast_div((uint32_t)(row0 + rr), a.G), u = row0 + rr - tok * G;
+        uint16_t *out = a.out + (int64_t)(rq.row0 + tok) * a.o_tok + (int64_t)(head * G + u) * a.o_head;
+        const float inv = vsc / lr;
+#pragma unroll
+        for (int q = 0; q < ND; ++q)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                uint2 y = make_uint2(pack_bf16(o[q][r] * inv, o[q][r + 1] * inv),
+                                     pack_bf16(o[q][r + 2] * inv, o[q][r + 3] * inv));
+                if (lr == 0.f) y = make_uint2(0u, 0u);
+                *(uint2 *)(out + 32 * q + acc_key(r, h)) = y;
+            }
+        if (a.lse && h == 0)
+            a.lse[(int64_t)(rq.row0 + tok) * (a.n_heads * G) + head * G + u] =
+                lr == 0.f ? -HUGE_VALF : 0.6931471805599453f * (m + __log2f(lr));
     }
 }
 
@@ -1005,11 +935,11 @@ __device__ __forceinline__ void join_row(const PagedArgs &a, const PagedClass &c
 // Four rows a time; blocks go round while there are more of them.
 template <int D, int M, int KT, bool F8>
 __device__ __forceinline__ void join_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, uint32_t blocks,
-                                          SchedLds &sched) {
+                                          SchedLds<4> &sched) {
     for (uint32_t b = block;; b += blocks) {
         const uint32_t idx = b / (uint32_t)a.n_heads;
         Item it;
-        if (!find_item<M, KT, true>(a, cl, idx, sched, it)) return;
+        if (!find_item<M, KT, true, 4>(a, cl, idx, sched, it)) return;
         join_row<D, M, KT, F8>(a, cl, it, (int)(b - idx * a.n_heads), 4 * it.part + (threadIdx.x >> 6));
         __syncthreads();                                       // the item has been read
     }
@@ -1017,34 +947,32 @@ __device__ __forceinline__ void join_body(const PagedArgs &a, const PagedClass &
 
 // ------------------------------------------------------------------ kernels
 
-constexpr int kTileM = 128;
-
 template <int D, bool F8>
 __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
-    __shared__ SchedLds sched;
-    __shared__ __attribute__((aligned(16))) RowsLds<D> lds;
-    rows_body<D, 1, F8>(a, a.rows, blockIdx.x, sched, lds);
+    __shared__ SchedLds<4> sched;
+    __shared__ __attribute__((aligned(16))) RowsLds<D, 4> lds;
+    rows_body<D, F8, 4>(a, a.rows, blockIdx.x, sched, lds);
 }
 
 // The requests with few rows and the others in one launch: the tiles, which take longer, first.
-template <int D, bool F8>
-__global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedArgs a) {
-    __shared__ SchedLds sched;
-    __shared__ __attribute__((aligned(16))) union { RowsLds<D> rows; TileLds<D> tile; } lds;
-    if (blockIdx.x < a.tile.blocks) tile_body<D, 1, F8>(a, a.tile, blockIdx.x, sched, lds.tile);
-    else rows_body<D, 1, F8>(a, a.rows, blockIdx.x - a.tile.blocks, sched, lds.rows);
+template <int D, bool F8, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(PagedArgs a) {
+    __shared__ SchedLds<NW> sched;
+    __shared__ __attribute__((aligned(16))) union { RowsLds<D, NW> rows; TileLds<D> tile; } lds;
+    if (blockIdx.x < a.tile.blocks) tile_body<D, F8, NW>(a, a.tile, blockIdx.x, sched, lds.tile);
+    else rows_body<D, F8, NW>(a, a.rows, blockIdx.x - a.tile.blocks, sched, lds.rows);
 }
 
-template <int D, bool F8>
+template <int D, bool F8, int NW>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
-    __shared__ SchedLds sched;
-    if (blockIdx.x < a.tile.join_blocks) join_body<D, kTileM, kTileKT, F8>(a, a.tile, blockIdx.x, a.tile.join_blocks, sched);
+    __shared__ SchedLds<4> sched;
+    if (blockIdx.x < a.tile.join_blocks) join_body<D, 32 * NW, kTileKT, F8>(a, a.tile, blockIdx.x, a.tile.join_blocks, sched);
     else join_body<D, 16, kKT, F8>(a, a.rows, blockIdx.x - a.tile.join_blocks, a.rows.join_blocks, sched);
 }
 
 constexpr int kSmallRows = 16;          // rows of a request up to which rows_body takes it beside tile_body
 constexpr int kFewRows = 32;            // and alone, when no request is said to have more
-constexpr int kTileTarget = 512;        // workgroups of tile_body that long rows are divided into
+constexpr int kTileTarget = 512;        // workgroups of tile_body (of 128 rows) that long rows are divided into
 constexpr int kJoinBlocks = 2048;
 
 // The blocks of a class of requests and its part of the workspace.
@@ -1069,29 +997,46 @@ bool prepare_class(const PagedArgs &a, PagedClass &c, int target, int64_t row_mi
     return true;
 }
 
+template <int D, bool F8, int NW>
+hipError_t launch_tiles(PagedArgs a, char *w, int64_t ws_bytes, hipStream_t s) {
+    constexpr int M = 32 * NW;
+    const int64_t least = a.G.d <= kSmallRows && a.n_reqs > 1 ? kSmallRows : 0;
+    if (least > 0 && !prepare_class<D, 16, kKT>(a, a.rows, kTarget, 0, least, w, ws_bytes)) return hipErrorInvalidValue;
+    if (!prepare_class<D, M, kTileKT>(a, a.tile, kTileTarget * 4 / NW, least, INT64_MAX, w, ws_bytes)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((attn_tile_kernel<D, F8, NW>), dim3(a.tile.blocks + a.rows.blocks), dim3(64 * NW), 0, s, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    const uint32_t join = a.tile.join_blocks + a.rows.join_blocks;
+    if (join > 0) hipLaunchKernelGGL((attn_join_kernel<D, F8, NW>), dim3(join), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
 template <int D, bool F8>
 hipError_t launch(PagedArgs a, int32_t max_q_len, void *ws, int64_t ws_bytes, hipStream_t s) {
     char *w = (char *)ws;
-    if ((int64_t)max_q_len * a.G.d <= kFewRows) {
-        // few rows everywhere: rows_body alone, whatever the lengths turn out to be
-        if (!prepare_class<D, 16, kKT>(a, a.rows, kTarget, 0, INT64_MAX, w, ws_bytes)) return hipErrorInvalidValue;
-        hipLaunchKernelGGL((attn_rows_kernel<D, F8>), dim3(a.rows.blocks), dim3(256), 0, s, a);
-    } else {
-        const int64_t least = a.G.d <= kSmallRows && a.n_reqs > 1 ? kSmallRows : 0;
-        if (least > 0 && !prepare_class<D, 16, kKT>(a, a.rows, kTarget, 0, least, w, ws_bytes)) return hipErrorInvalidValue;
-        if (!prepare_class<D, kTileM, kTileKT>(a, a.tile, kTileTarget, least, INT64_MAX, w, ws_bytes)) return hipErrorInvalidValue;
-        hipLaunchKernelGGL((attn_tile_kernel<D, F8>), dim3(a.tile.blocks + a.rows.blocks), dim3(256), 0, s, a);
+    const int64_t rows = (int64_t)max_q_len * a.G.d;
+    if constexpr (D != 96) {
+        // 256 rows share a tile's way to LDS where there are two such workgroups for every compute unit
+        // and the requests are alike (their tokens fill three quarters of n_reqs x max_q_len).  A chunk
+        // of 2,048 x 8 rows in 8 heads over 32,768 keys: 2.09 ms, 2.20 with 128 rows; three chunks of
+        // 515 x 4 beside 24 single tokens: 64 us, 54 with 128 rows.  Heads of 96, whose 1.5 pieces a
+        // thread leave half the loads of the second empty: 1.93 and 1.77 ms.
+        if (rows >= 256 && (int64_t)a.n_tokens * a.G.d * a.n_heads >= 2 * 256 * 256 &&
+            4 * (int64_t)a.n_tokens >= 3 * (int64_t)a.n_reqs * max_q_len)
+            return launch_tiles<D, F8, 8>(a, w, ws_bytes, s);
     }
+    if (rows > kFewRows) return launch_tiles<D, F8, 4>(a, w, ws_bytes, s);
+    // few rows everywhere: rows_body alone, whatever the lengths turn out to be
+    if (!prepare_class<D, 16, kKT>(a, a.rows, kTarget, 0, INT64_MAX, w, ws_bytes)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((attn_rows_kernel<D, F8>), dim3(a.rows.blocks), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
-    const uint32_t join = a.tile.join_blocks + a.rows.join_blocks;
-    if (join > 0) hipLaunchKernelGGL((attn_join_kernel<D, F8>), dim3(join), dim3(256), 0, s, a);
+    if (a.rows.join_blocks > 0) hipLaunchKernelGGL((attn_join_kernel<D, F8, 4>), dim3(a.rows.join_blocks), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_tokens, int32_t n_reqs, int32_t max_q_len) {
-    const int64_t rows = (int64_t)2 * kTarget * 16 * (d + 2) * 4, tile = (int64_t)2 * kTileTarget * kTileM * (d + 2) * 4;
+    const int64_t rows = (int64_t)2 * kTarget * 16 * (d + 2) * 4, tile = (int64_t)2 * kTileTarget * 128 * (d + 2) * 4;
     return (int64_t)max_q_len * G <= kFewRows ? rows : rows + tile;
 }
 

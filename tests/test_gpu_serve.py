@@ -733,3 +733,55 @@ def test_calls_on_a_stream_object_and_a_handle(cb, serve):
     with torch.cuda.stream(st):
         s.run()
     assert torch.equal(s.out, want)
+
+
+def check_tokens(serve, s, tokens, heads, window=0, sinks=0):
+    """Some tokens (request, new token) and KV heads of a large step against the plain form, each as its request's last."""
+    got, gl, qd, G, d = f64(s.out), f64(s.lse), f64(s.q), s.G, s.d
+    for r, i in tokens:
+        nq, kv = s.lens[r]
+        t, p = s.starts[r] + i, kv - nq + i
+        for h in heads:
+            hs = slice(h * G, (h + 1) * G)
+            o, l, mag, smag = serve.attention(qd[t:t + 1, hs], s.K[r][h], s.V[r][h], p + 1, d ** -0.5, window, sinks)
+            es, few = (d + 8) * 2 * F32 * smag, (kv + 64) * 2 * F32
+            tol = BF * np.abs(o) * 1.01 + mag * (BF * 1.01 + (2 * es + few)[..., None])
+            assert (np.abs(got[t:t + 1, hs] - o) <= tol).all(), (r, i, h)
+            assert (np.abs(gl[t:t + 1, hs] - l) <= es + few + 8 * F32 * (np.abs(l) + 1)).all(), (r, i, h)
+
+
+@pytest.mark.parametrize("d,f8", [(128, False), (128, True), (64, False), (64, True), (96, False)])
+def test_attention_large_alike_chunks(cb, serve, d, f8):
+    """Chunks that fill the chip with 256 rows a workgroup (heads of 96: 128), a single token among them, with and
+    without a window, a value of V that only the later rows see, and rows in parts."""
+    s = Step(cb, [(512, 600), (512, 1500), (1, 700), (512, 512), (513, 513)], 8, 8, d, 16, f8, pad=2, seed=70, layers=1, layer=0)
+    some = [(0, 0), (0, 511), (1, 100), (1, 255), (1, 256), (2, 0), (3, 0), (3, 31), (3, 32), (3, 300), (4, 1), (4, 512)]
+    s.run()
+    check_tokens(serve, s, some, [0, 5])
+    assert (s.out[-2:] == 9.0).all()
+    clean = f64(s.out)
+    s.run(300, 4)
+    check_tokens(serve, s, some, [2, 7], 300, 4)
+    s.run(max_q=100)                                            # the same with 128 rows a workgroup
+    check_tokens(serve, s, some, [0, 5])
+    j = 200                                                     # of request 3: its rows from 200 on see it
+    at = (0, 1, int(s.table[3, j // 16]), 5, j % 16, 9)
+    if f8:
+        s.pool.view(torch.uint8)[at] = 0x7f
+    else:
+        s.pool[at] = float("inf")
+    s.run()
+    got = f64(s.out)
+    t0, hs = s.starts[3], slice(40, 48)
+    assert not np.isfinite(got[t0 + 200:t0 + 512, hs, 9]).any()
+    got[t0 + 200:t0 + 512, hs, 9] = clean[t0 + 200:t0 + 512, hs, 9]
+    assert np.array_equal(got, clean)
+
+
+def test_attention_large_chunk_in_parts(cb, serve):
+    """One chunk of 256-row tiles over a long context in few heads: its keys in parts."""
+    s = Step(cb, [(2050, 9000)], 1, 64, 64, 64, seed=71, layers=1, layer=0)
+    s.run()
+    check_tokens(serve, s, [(0, 0), (0, 3), (0, 4), (0, 1025), (0, 2049)], [0])
+    s.run(ws=False)
+    check_tokens(serve, s, [(0, 0), (0, 2049)], [0])
