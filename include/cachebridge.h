@@ -677,7 +677,7 @@ typedef struct {
     int32_t style;              /* CB_ROPE_HALF_SPLIT or CB_ROPE_INTERLEAVED */
     int32_t n_axes;             /* 1 .. 4 */
     const int32_t *positions;   /* device, [n_axes][axis_stride] */
-    int64_t axis_stride;        /* >= tokens of the call */
+    int64_t axis_stride;        /* >= tokens of the call, or 0: every axis has the same positions */
     uint8_t axis[128];          /* axis of pair i, i < head_dim / 2 */
 } cb_rope_axes_spec;
 
@@ -751,7 +751,7 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
  *   q, out: n_tokens rows of n_qheads = G * n_heads heads; they must not overlap.
  *   q_starts must not decrease; kv_lens beyond table_width * page_size count as that.
  *   max_q_len: the largest number of new tokens of any request, a hint that
- *     picks the kernels; results do not depend on its being right.
+ *     picks the kernels; a wrong one costs time and changes roundings only.
  *   scale: finite.  window, n_sinks >= 0.
  *   lse: fp32 [n_tokens][n_qheads], or NULL.
  *   workspace: device memory, 16-byte aligned, for the partial results of long
@@ -760,10 +760,10 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
  *     leaves nothing in it that another reads; calls that overlap in time need
  *     one each.
  * Scores and sums are fp32 from exact products; the weights exp(s_j - m) are
- * rounded to bf16 for their product with V (m the running maximum) and summed
- * unrounded.  Results do not depend on the other requests but for the order of
- * fp32 sums (where a row is split), and are bitwise reproducible.  head_dim in
- * {64, 96, 128}.
+ * rounded to bf16 for their product with V (m: the running maximum, or up to 8
+ * less in powers of two) and summed unrounded.  Results depend on the other
+ * requests only in the order of fp32 sums (where a row is split), and are
+ * bitwise reproducible.  head_dim in {64, 96, 128}.
  */
 cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,
                         const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,

@@ -30,6 +30,14 @@ current HIP stream.  The functions keep the C names:
 * :func:`cb_plan_create_multi`, :func:`cb_ridge_solve_ws` -- maps over the
   multi-layer feature of k selected source layers (Sec. 3.2, Eq. localfeature)
   and the blocked solve of their P = k d_s + 1 systems
+* serving a receiver from its decode-ready cache (Sec. 1: it decodes from the
+  handed-off rows): :func:`cb_page_tables` -- block tables, slot map and positions
+  of a step from the requests' lengths; :func:`cb_rope_axes` -- rotary positions
+  with several axes (:func:`rope_axes_spec`); :func:`cb_page_write` -- rows of a
+  cache, or a step's new rows, into the pages of a pool (:func:`page_pool`,
+  bfloat16 or e4m3), keys and queries turned on the way; :func:`cb_attn_paged` --
+  attention of every request's new tokens over its pages, whole or with a
+  sliding window and first tokens that stay visible
 
 Caches are bfloat16 tensors indexed ``[layer][kv][seq][head][tok][dim]`` (any
 strides with a unit channel stride).  Importing this package fails if the
@@ -242,19 +250,14 @@ def _check_weights(plan: "Plan", weights: torch.Tensor, row_stride: int, src: to
 
 def cache_view(t: Optional[torch.Tensor], n_layers=None, n_heads=None, head_dim=None) -> CbCache:
     """Describe a [layer][kv][seq][head][tok][dim] bfloat16 tensor (any strides, unit channel stride)."""
-    c = CbCache()
     if t is None:
-        c.n_layers, c.n_heads, c.head_dim = n_layers, n_heads, head_dim
-        return c
+        return CbCache(None, n_layers, n_heads, head_dim)
     if t.dtype != torch.bfloat16 or t.dim() != 6 or t.shape[1] != 2:
         raise ValueError("cache tensors are bfloat16 [layer][2][seq][head][tok][dim]")
     if t.shape[5] > 1 and t.stride(5) != 1:
         raise ValueError("cache channel stride must be 1")
     L, _, B, H, T, d = t.shape
-    c.data = t.data_ptr()
-    c.n_layers, c.n_heads, c.head_dim, c.n_seqs, c.seq_len = L, H, d, B, T
-    c.s_layer, c.s_kv, c.s_seq, c.s_head, c.s_tok = t.stride(0), t.stride(1), t.stride(2), t.stride(3), t.stride(4)
-    return c
+    return CbCache(t.data_ptr(), L, H, d, B, T, *t.stride()[:5])
 
 
 class Plan:
@@ -693,7 +696,7 @@ _lib.cb_attn_paged_workspace_bytes.argtypes = [_i32] * 6
 
 
 def _ints(t: torch.Tensor, n: int, name: str):
-    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements, got {t.dtype} {tuple(t.shape)}")
 
 
@@ -701,7 +704,11 @@ def _on_current_device(names: str, *tensors) -> int:
     """The library works on the current device: tensors of another (or of the host) are refused here.  Returns the
     device's index."""
     device = tensors[0].get_device()
-    if device < 0 or device != torch.cuda.current_device() or any(t is not None and t.get_device() != device for t in tensors):
+    good = device >= 0 and device == torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            good = False
+    if not good:
         where = ", ".join(f"{n} on {t.device}" for n, t in zip(names.split(), tensors) if t is not None)
         raise ValueError(f"every tensor must be on the current CUDA device: {where}")
     return device
@@ -767,9 +774,15 @@ def rope_axes_spec(table: torch.Tensor, positions: torch.Tensor, axis=None,
     return sp
 
 
+def _kept(described) -> tuple:
+    """The tensors behind a page_pool or rope_axes_spec (none for a structure filled by hand)."""
+    return getattr(described, "_keep", (None, None))
+
+
 def _check_axes_tokens(rope: Optional[CbRopeAxesSpec], n_tokens: int):
-    if rope is not None and rope._keep[1].shape[-1] < n_tokens:
-        raise ValueError(f"positions hold {rope._keep[1].shape[-1]} tokens, the call has {n_tokens}")
+    positions = _kept(rope)[1]
+    if positions is not None and positions.shape[-1] < n_tokens:
+        raise ValueError(f"positions hold {positions.shape[-1]} tokens, the call has {n_tokens}")
 
 
 def cb_page_tables(ctx_lens: torch.Tensor, q_lens: torch.Tensor, free_pages: torch.Tensor, page_size: int,
@@ -803,7 +816,7 @@ def cb_rope_axes(cache_in: torch.Tensor, cache_out: torch.Tensor, rope: CbRopeAx
     (:func:`rope_axes_spec`) into cache_out (may be cache_in); V rows copied."""
     iv, ov = cache_view(cache_in), cache_view(cache_out)
     _check_axes_tokens(rope, cache_in.shape[2] * cache_in.shape[4])
-    dev = _on_current_device("cache_in cache_out table positions", cache_in, cache_out, *rope._keep)
+    dev = _on_current_device("cache_in cache_out table positions", cache_in, cache_out, *_kept(rope))
     _check(_lib.cb_rope_axes(ctypes.byref(iv), ctypes.byref(ov), ctypes.byref(rope), int(bool(inverse)),
                              _stream_on(dev, stream)))
 
@@ -820,8 +833,8 @@ def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer
     _check_axes_tokens(rope, n)
     qv = None if q is None else _rows_view(q, "q")
     ov = None if q_out is None else _rows_view(q_out, "q_out")
-    dev = _on_current_device("rows slots q q_out pages scales table positions", rows, slots, q, q_out, *pages._keep,
-                             *(() if rope is None else rope._keep))
+    dev = _on_current_device("rows slots q q_out pages scales table positions", rows, slots, q, q_out, *_kept(pages),
+                             *_kept(rope))
     _check(_lib.cb_page_write(ctypes.byref(rv), ctypes.byref(pages), int(layer), _ptr(slots),
                               None if rope is None else ctypes.byref(rope), None if qv is None else ctypes.byref(qv),
                               None if ov is None else ctypes.byref(ov), _stream_on(dev, stream)))
@@ -851,7 +864,7 @@ def cb_attn_paged(q: torch.Tensor, pages: CbPages, layer: int, q_starts: torch.T
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     dev = _on_current_device("q q_starts kv_lens block_table out lse workspace pages scales", q, q_starts, kv_lens,
-                             block_table, out, lse, workspace, *pages._keep)
+                             block_table, out, lse, workspace, *_kept(pages))
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_lib.cb_attn_paged(ctypes.byref(qv), ctypes.byref(pages), int(layer), n, _ptr(q_starts), _ptr(kv_lens),
                               _ptr(block_table), block_table.stride(0), block_table.shape[1], ctypes.byref(ov),

@@ -6,10 +6,13 @@
 // exp(m - m').  In log2 units throughout (scale carries log2 e).
 //
 // Rows of one request and KV head are (token, head of its group) pairs, so the
-// group's query heads share every K and V row read.  Row tiles of 16 rows.
+// group's query heads share every K and V row read.  The weights exp(s_j - m)
+// are rounded to bf16 as the matrix cores' operand (2^-8 of a weight, below the
+// output's own rounding where the values do not cancel) and summed unrounded;
+// scores, sums and outputs are fp32.
 //
-// attn_rows_kernel: four waves, each with its own key tiles of 32 keys, from
-//   memory straight into matrix-core operands:
+// rows_body: requests of few rows, 16 of them a workgroup.  Each wave has its
+//   own key tiles of 32 keys, from memory straight into matrix-core operands:
 //   S^T = K Q^T (16x16x32): lane l holds row n = l & 15 and, of key subtile t,
 //     keys 16 t + 4 g + r, g = l >> 4, r = 0 .. 3: the statistics of a row are
 //     per-lane numbers.
@@ -18,12 +21,37 @@
 //     operand (eight keys of one channel) comes from eight 16-byte pieces of
 //     eight rows, transposed in registers (v_perm); channel E c + i goes to
 //     output row c of product i, so a lane ends with E consecutive channels.
-//   No LDS and no barrier until the waves' results are joined.
+//   No LDS and no barrier until the waves' results are joined.  K of the next
+//   tile is requested when K of this one has met the queries, V when V has
+//   become operands, table entries a tile earlier.  Bound by memory: 64 single
+//   tokens over 512 .. 16,384 keys (8 heads of 128, 8 query heads each, 1.36 GB)
+//   250 us, 5.4 TB/s; in e4m3 pages, 8 over 65,536 .. 131,072 (1.57 GB), 320 us,
+//   4.9 TB/s (a copy of 2 GiB runs at 4.9 TB/s here, both directions counted).
+//   Two waves per SIMD are enough: with registers for three the calls took 274
+//   and 344 us, 252 and 336 with two.  Requested at the top of a tile instead of
+//   a tile ahead, K and V took the kernel from 245 and 319 to 270 and 375 us.
+//
+// tile_body: the other requests, 32 rows a wave, 128 or 256 a workgroup, K and
+//   V tiles of 64 keys in LDS, two of them.
+//   S^T = K Q^T (32x32x16): lane l holds row l & 31 and, of each 32 keys, those
+//     with bit 2 = l >> 5.  O^T = V^T P^T takes P from these registers as
+//     above; its V operand comes out of LDS transposed (ds_read_b64_tr_b16).
+//   While a tile is worked on the next is on its way to registers and the
+//   table entries of the one after are on theirs; a tile's products with V run
+//   beside the weights of its next 16 keys.  Bound by the vector and the matrix
+//   units in turn (43% and 47% busy; 32 exponentials of 16 cycles and 100 other
+//   vector instructions stand against 32 products of 32 cycles): 2,048 tokens
+//   x 64 query heads over 32,768 keys in 8 heads of 128: 2.10 ms, 1.01 PFLOP/s
+//   (a bf16 matrix product of 8192^3: 1.21).  Without the way of K and V to LDS
+//   the same would take 1.6 ms.  Bytes between LDS rows are chosen so that no
+//   bank meets twice (with 32 bytes less between V's rows a quarter of the LDS
+//   cycles were conflicts).
 //
 // Division of work: a row tile's keys go in `parts` to workgroups of their own
 //   (cb_paged_rules.h), whose partial sums attn_join_kernel adds in the order
 //   of the parts.  Every workgroup finds its row tile and part from the
-//   requests' lengths by itself.
+//   requests' lengths by itself: sums over the requests by data-parallel moves,
+//   about 2 us, instead of a plan that a caller would have to keep in step.
 #include "cb_internal.h"
 #include "cb_paged_rules.h"
 
@@ -39,10 +67,15 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 
 constexpr int kKT = 32;                 // keys of a tile
 constexpr int kTileKT = 64;             // keys of a tile of the tile kernel
-constexpr int kPartMin = 24;            // least key tiles of a part of rows_body: six for each of the four waves
-constexpr int kTilePartMin = 16;        // and of tile_body
+// Least key tiles of a part, for rows_body (768 keys) and tile_body (1,024): what a part saves must be
+// worth the joining, a launch of about 8 us.  24 single tokens and three chunks with windows of 1,024
+// keys, one part each: 49 us; with parts of 256 keys and more: 61 us.
+constexpr int kPartMin = 24, kTilePartMin = 16;
 constexpr float kLag = 8.f;              // log2 by which the maximum in use may lag the true one
-constexpr int kTarget = 2048;           // workgroups that long rows are divided into
+// Workgroups that long rows are divided into: four for each of the 512 that are resident, so that
+// requests of different lengths end together (64 requests of 512 .. 16,384 keys: 262 us with 1,024,
+// 268 with 4,096, 259 with 2,048).
+constexpr int kTarget = 2048;
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     f32x2_t v = {lo, hi};
@@ -971,7 +1004,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
 }
 
 constexpr int kSmallRows = 16;          // rows of a request up to which rows_body takes it beside tile_body
-constexpr int kFewRows = 32;            // and alone, when no request is said to have more
+// ... and alone, when no request is said to have more: 64 requests of 2 tokens x 8 query heads take it
+// 235 us, 4 x 8 tile_body 282.
+constexpr int kFewRows = 32;
 constexpr int kTileTarget = 512;        // workgroups of tile_body (of 128 rows) that long rows are divided into
 constexpr int kJoinBlocks = 2048;
 

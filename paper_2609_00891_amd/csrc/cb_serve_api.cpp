@@ -70,7 +70,7 @@ cb_status check_rope_axes(const cb_rope_axes_spec *r, int d, int64_t n_tokens, c
     if (r->head_dim != d) return fail(CB_ERR_SHAPE, "rope was built for head_dim %d, the rows have %d", r->head_dim, d);
     if (r->n_pos < 0) return fail(CB_ERR_INVALID_ARGUMENT, "rope: n_pos is negative");
     if (r->n_axes < 1 || r->n_axes > 4) return fail(CB_ERR_INVALID_ARGUMENT, "rope: n_axes must be in 1..4 (got %d)", r->n_axes);
-    if (r->axis_stride < n_tokens && r->n_axes > 1)
+    if (r->axis_stride != 0 && r->axis_stride < n_tokens && r->n_axes > 1)
         return fail(CB_ERR_SHAPE, "rope: axis_stride (%lld) < tokens of the call (%lld)", (long long)r->axis_stride,
                     (long long)n_tokens);
     if (((uintptr_t)r->table) % 16 || ((uintptr_t)r->positions) % 4)
