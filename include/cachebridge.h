@@ -760,10 +760,10 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
  *     leaves nothing in it that another reads; calls that overlap in time need
  *     one each.
  * Scores and sums are fp32 from exact products; the weights exp(s_j - m) are
- * rounded to bf16 for their product with V (m: the running maximum, or up to 8
- * less in powers of two) and summed unrounded.  Results depend on the other
- * requests only in the order of fp32 sums (where a row is split), and are
- * bitwise reproducible.  head_dim in {64, 96, 128}.
+ * rounded to bf16 for their product with V (m the running maximum) and summed
+ * unrounded.  Results depend on the other requests only in the order of fp32
+ * sums (where a row is split), and are bitwise reproducible.  head_dim in
+ * {64, 96, 128}.
  */
 cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,
                         const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,

@@ -9,7 +9,10 @@
 // group's query heads share every K and V row read.  The weights exp(s_j - m)
 // are rounded to bf16 as the matrix cores' operand (2^-8 of a weight, below the
 // output's own rounding where the values do not cancel) and summed unrounded;
-// scores, sums and outputs are fp32.
+// scores, sums and outputs are fp32.  m is the running maximum itself, so the
+// largest weight is 1, which no rounding touches: with a maximum that may lag by
+// 2^8, which spares rescaling, a 2,048-token chunk took 1.3% less and its outputs
+// were off by 0.22% instead of 0.18% (0.17% is their own rounding).
 //
 // rows_body: requests of few rows, 16 of them a workgroup.  Each wave has its
 //   own key tiles of 32 keys, from memory straight into matrix-core operands:
@@ -71,7 +74,6 @@ constexpr int kTileKT = 64;             // keys of a tile of the tile kernel
 // worth the joining, a launch of about 8 us.  24 single tokens and three chunks with windows of 1,024
 // keys, one part each: 49 us; with parts of 256 keys and more: 61 us.
 constexpr int kPartMin = 24, kTilePartMin = 16;
-constexpr float kLag = 8.f;              // log2 by which the maximum in use may lag the true one
 // Workgroups that long rows are divided into: four for each of the 512 that are resident, so that
 // requests of different lengths end together (64 requests of 512 .. 16,384 keys: 262 us with 1,024,
 // 268 with 4,096, 259 with 2,048).
@@ -407,8 +409,8 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
         float mx = x[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
-        // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
-        if (__any(mx > m + kLag)) {
+        // sums are rescaled only where some row's maximum grows
+        if (__any(mx > m)) {
             mx = fmaxf(mx, __shfl_xor(mx, 16));
             mx = fmaxf(mx, __shfl_xor(mx, 32));
             mx = fmaxf(mx, m);
@@ -797,8 +799,8 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
         for (int e = 3; e < 31; e += 2) mx = max3(mx, s[e >> 4][e & 15], s[(e + 1) >> 4][(e + 1) & 15]);
         mx = max3(mx, s[1][15], s[1][15]);
         mx = both_halves_max(mx) * c2;
-        // the maximum in use may lag the true one by 2^kLag in weight: sums are rescaled seldom
-        if (__any(mx > m + kLag)) {
+        // sums are rescaled only where some row's maximum grows
+        if (__any(mx > m)) {
             const float mn = fmaxf(m, mx);
             const float al = __builtin_amdgcn_exp2f(m - (mn == -HUGE_VALF ? 0.f : mn));
             m = mn;
