@@ -581,6 +581,16 @@ __device__ __forceinline__ float both_halves_max(float x) {
     return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+typedef __attribute__((address_space(3))) char lds_char_t;
+// 16 bytes per lane from memory to LDS at m0 + 16 lane, counted by vmcnt; M0 is saved and restored.
+__device__ __forceinline__ void copy16(const void *from, uint32_t m0) {
+    uint32_t keep;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep)
+                 : "v"(from), "s"(m0)
+                 : "memory");
+}
+
 template <int D> struct TileLds {
     // bytes between rows of K and V: 16 rows' 16-byte pieces, and 4 rows' 64 bytes, in 64 banks each
     static constexpr int KS = 2 * D + 16, VS = D == 96 ? 192 : 2 * D + 64;
@@ -592,7 +602,8 @@ template <int D, bool F8, int NW>
 __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds<NW> &sched,
                                           TileLds<D> &tl) {
     constexpr int M = 32 * NW, NT = 64 * NW, KT = kTileKT, NS = D / 16, ND = D / 32;
-    constexpr int KS = TileLds<D>::KS, VS = TileLds<D>::VS;
+    constexpr bool DMA = !F8 && D != 96;                       // rows go to LDS as they are, by its own loads
+    constexpr int KS = DMA ? 2 * D : TileLds<D>::KS, VS = DMA ? 2 * D : TileLds<D>::VS;
     constexpr int CPR = F8 ? D / 16 : D / 8;                   // 16-byte pieces of a row in memory
     constexpr int NP = (KT * CPR + NT - 1) / NT;                 // pieces of a thread, for each of K and V
     constexpr bool RAGGED = KT * CPR % NT != 0;
@@ -659,12 +670,28 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
         there = __ballot(ok);
         return (ok ? (uint32_t)page : 0u) * a.s_page + (ok ? in_page : 0u) * a.s_tok;
     };
+    // By LDS's own loads piece p of a tile lands in place p: rows without gaps, their 16-byte pieces in
+    // an order of their own, so that the operands' reads meet no bank twice.  Row r has K's piece c in
+    // place c ^ f(r), f = r mod 16 (64 channels: r / 2 mod 8), and V's in place c ^ 4 (r mod 4) (64
+    // channels: c ^ 4 (r / 2 mod 2)).
+    const int my_row = tid / CPR, my_c = tid - my_row * CPR;
+    const int k_piece = 16 * (my_c ^ (D == 128 ? my_row & 15 : my_row >> 1 & 7));
+    const int v_piece = 16 * (my_c ^ (D == 128 ? 4 * (my_row & 3) : 4 * (my_row >> 1 & 1)));
     u32x4_t kr[NP], vr[NP];
-    auto load = [&](uint32_t off) __attribute__((always_inline)) {
+    auto load = [&](uint32_t off, int st) __attribute__((always_inline)) {
         uint32_t ro[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) ro[i] = (uint32_t)__shfl((int)off, (tid + NT * i) / CPR & 63);
         __builtin_amdgcn_sched_barrier(0);                     // one trip to the other lanes for all of them
+        if constexpr (DMA) {
+            const uint32_t to = (uint32_t)(uintptr_t)(lds_char_t *)(lds + st * STAGE) + 1024 * wave;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                copy16(kp + (uint64_t)ro[i] * 16 + k_piece, __builtin_amdgcn_readfirstlane(to + 16 * NT * i));
+                copy16(vp + (uint64_t)ro[i] * 16 + v_piece, __builtin_amdgcn_readfirstlane(to + 16 * NT * i + KT * KS));
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int id = tid + NT * i;
@@ -680,6 +707,12 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     // that are not there become zeros as well.
     auto store = [&](int st, uint64_t there, bool edge) __attribute__((always_inline)) {
         char *ks = lds + st * STAGE, *vs = ks + KT * KS;
+        if constexpr (DMA) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's pieces have landed
+            if (!edge) return;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) vr[i] = *(const u32x4_t *)(vs + 16 * (tid + NT * i));
+        }
         if (edge) {
             uint32_t found = 0;
             asm volatile("");
@@ -696,6 +729,11 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
                 }
             }
             if (found) odd = 1;
+        }
+        if constexpr (DMA) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) *(u32x4_t *)(vs + 16 * (tid + NT * i)) = vr[i];
+            return;
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -729,13 +767,19 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     l = 0.f;
 #pragma unroll
     for (int q = 0; q < ND; ++q) o[q] = f32x16_t{};
-    // V^T operand: keys 16 kk + 4 h + {0 .. 3} and + 8, channel 32 q + (lane & 31)
-    const int vt = (4 * h + ((lane >> 2) & 3)) * VS + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    // K operand: key n, channels 16 q + 8 h .. + 7, at k_at ^ 32 q (rows without gaps) or k_at + 32 q.
+    // V^T operand: keys 16 kk + 4 h + {0 .. 3} and + 8, channel 32 q + (lane & 31), at v_at ^ 64 q or
+    // v_at + 64 q.
+    const int r4 = (lane >> 2) & 3, f_n = D == 128 ? n & 15 : n >> 1 & 7;
+    const int k_at = n * KS + (DMA ? 16 * (h ^ f_n) : 16 * h);
+    const int v_at = (4 * h + r4) * VS + 32 * ((lane >> 4) & 1) + 8 * (lane & 3) + (DMA ? (D == 128 ? 64 * r4 : 64 * (r4 >> 1)) : 0);
+    auto k_place = [&](int q) __attribute__((always_inline)) { return DMA ? k_at ^ 32 * q : k_at + 32 * q; };
+    auto v_place = [&](int q) __attribute__((always_inline)) { return DMA ? v_at ^ 64 * q : v_at + 64 * q; };
 
     auto read_v = [&](const char *vs, int kk, bf16x8_t *f) __attribute__((always_inline)) {
 #pragma unroll
         for (int q = 0; q < ND; ++q) {
-            const char *pp = vs + vt + 16 * kk * VS + 64 * q;
+            const char *pp = vs + v_place(q) + 16 * kk * VS;
             const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)pp);
             const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(pp + 8 * VS));
             typedef __attribute__((ext_vector_type(8))) short s16x8_t;
@@ -748,8 +792,9 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     int32_t t0 = kt.tile(v0), t1 = next_tile(t0), t2 = next_tile(t1);   // this tile and the two behind it
     if (v0 < v1) {
         look_up(t0);
-        load(place(there));
+        const uint32_t off = place(there);
         if (v0 + 1 < v1) look_up(t1);
+        load(off, 0);
         __syncthreads();                                       // odd is set
         store(0, there, !seen(t0 * KT, there, p_lo, p_hi));
     }
@@ -757,8 +802,11 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     for (int32_t v = v0; v < v1; ++v) {
         const int st = (v - v0) & 1;
         const int32_t k0 = t0 * KT;
-        if (v + 1 < v1) load(place(there_n));
+        // (the table entries first: what waits for them later does not wait for the rows)
+        uint32_t off = 0;
+        if (v + 1 < v1) off = place(there_n);
         if (v + 2 < v1) look_up(t2);
+        if (v + 1 < v1) load(off, st ^ 1);
         const char *ks = lds + st * STAGE, *vs = ks + KT * KS;
         f32x16_t s[2];
         __builtin_amdgcn_s_setprio(1);
@@ -767,7 +815,7 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
         for (int q = 0; q < NS; ++q) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const bf16x8_t kf = *(const bf16x8_t *)(ks + (32 * t + n) * KS + 32 * q + 16 * h);
+                const bf16x8_t kf = *(const bf16x8_t *)(ks + k_place(q) + 32 * t * KS);
                 s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[q], s[t], 0, 0, 0);
             }
         }
