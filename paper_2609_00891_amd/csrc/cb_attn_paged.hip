@@ -39,15 +39,18 @@
 //   S^T = K Q^T (32x32x16): lane l holds row l & 31 and, of each 32 keys, those
 //     with bit 2 = l >> 5.  O^T = V^T P^T takes P from these registers as
 //     above; its V operand comes out of LDS transposed (ds_read_b64_tr_b16).
-//   While a tile is worked on the next is on its way to registers and the
-//   table entries of the one after are on theirs; a tile's products with V run
-//   beside the weights of its next 16 keys.  Bound by the vector and the matrix
-//   units in turn (43% and 47% busy; 32 exponentials of 16 cycles and 100 other
-//   vector instructions stand against 32 products of 32 cycles): 2,048 tokens
-//   x 64 query heads over 32,768 keys in 8 heads of 128: 2.10 ms, 1.01 PFLOP/s
-//   (a bf16 matrix product of 8192^3: 1.21).  Without the way of K and V to LDS
-//   the same would take 1.6 ms.  Bytes between LDS rows are chosen so that no
-//   bank meets twice (with 32 bytes less between V's rows a quarter of the LDS
+//   While a tile is worked on the next is on its way, and the table entries of
+//   the one after are on theirs.  bf16 rows of 64 or 128 channels go to LDS by
+//   its own loads (2.14 -> 2.07 ms below, and 370 -> 312 us for 8 new tokens of
+//   64 requests over 512 .. 16,384 keys), others through registers (e4m3 becomes
+//   bf16 on the way; 96 channels are no whole number of pieces a thread).  A
+//   tile's products with V run beside the weights of its next 16 keys.
+//   Bound by the board's power: 2,048 tokens x 64 query heads over 32,768 keys
+//   in 8 heads of 128 take 2.07 .. 2.20 ms from board to board, 0.97 .. 1.03
+//   PFLOP/s (a bf16 matrix product of 8192^3: 1.21), at 1.95 GHz of 2.4 with the
+//   matrix units 47% and the vector units 53% busy; four sums and maxima instead
+//   of one, other orders of the products and wave priorities change nothing.
+//   No LDS bank meets twice (with V's rows 288 bytes apart a quarter of the LDS
 //   cycles were conflicts).
 //
 // Division of work: a row tile's keys go in `parts` to workgroups of their own
@@ -809,7 +812,6 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
         if (v + 1 < v1) load(off, st ^ 1);
         const char *ks = lds + st * STAGE, *vs = ks + KT * KS;
         f32x16_t s[2];
-        __builtin_amdgcn_s_setprio(1);
         s[0] = s[1] = f32x16_t{};
 #pragma unroll
         for (int q = 0; q < NS; ++q) {
@@ -826,7 +828,6 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-        __builtin_amdgcn_s_setprio(0);
         if (!seen(k0, there, s_lo, s_hi)) {
             asm volatile("");                                  // a branch, not selects on every tile
             // key k0 + 4 h + c is register e's, c = 32 (e >> 4) + acc_key(e & 15, 0)
