@@ -20,6 +20,7 @@
 
 #include "cb_internal.h"
 #include "cb_rules.h"
+#include "cb_serve_internal.h"
 
 struct cb_plan {
     int device = 0;

@@ -58,7 +58,7 @@
 //   of the parts.  Every workgroup finds its row tile and part from the
 //   requests' lengths by itself: sums over the requests by data-parallel moves,
 //   about 2 us, instead of a plan that a caller would have to keep in step.
-#include "cb_internal.h"
+#include "cb_serve_internal.h"
 #include "cb_paged_rules.h"
 
 namespace cb {
@@ -1121,7 +1121,7 @@ hipError_t launch(PagedArgs a, int32_t max_q_len, void *ws, int64_t ws_bytes, hi
 
 }  // namespace
 
-int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_tokens, int32_t n_reqs, int32_t max_q_len) {
+int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t max_q_len) {
     const int64_t rows = (int64_t)2 * kTarget * 16 * (d + 2) * 4, tile = (int64_t)2 * kTileTarget * 128 * (d + 2) * 4;
     return (int64_t)max_q_len * G <= kFewRows ? rows : rows + tile;
 }

@@ -19,7 +19,7 @@
 //   cache of 64 layers x 4,096 tokens into 16-bit pages (2.1 GB) 0.41 ms, 5.2
 //   TB/s; four of up to 2,048 tokens into 8-bit pages, keys turned (2.4 GB),
 //   0.51 ms, 4.6 TB/s.
-#include "cb_internal.h"
+#include "cb_serve_internal.h"
 
 namespace cb {
 namespace {
