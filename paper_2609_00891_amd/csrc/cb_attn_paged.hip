@@ -47,9 +47,10 @@
 //   tile's products with V run beside the weights of its next 16 keys.
 //   Bound by the board's power: 2,048 tokens x 64 query heads over 32,768 keys
 //   in 8 heads of 128 take 2.07 .. 2.20 ms from board to board, 0.97 .. 1.03
-//   PFLOP/s (a bf16 matrix product of 8192^3: 1.21), at 1.95 GHz of 2.4 with the
-//   matrix units 47% and the vector units 53% busy; four sums and maxima instead
-//   of one, other orders of the products and wave priorities change nothing.
+//   PFLOP/s (a bf16 matrix product of 8192^3: 1.21), at 1.32 kW and 2.01 GHz of
+//   2.4 with the matrix units busy in 49% of the cycles; four sums and maxima
+//   instead of one, other orders of the products and wave priorities change
+//   nothing.
 //   No LDS bank meets twice (with V's rows 288 bytes apart a quarter of the LDS
 //   cycles were conflicts).
 //
@@ -163,8 +164,8 @@ template <typename T> __device__ __forceinline__ T wave_sums(T x) {
 }
 
 // The row tile and part of index `idx`, or false behind the last.  JOIN: of the rows of all tiles in
-// more than one part, four at a time, the idx-th four (it.part: which four of the tile).  The work of all requests is summed in fp64: whole numbers, exact below 2^53, and
-// the same in every workgroup.
+// more than one part, four at a time, the idx-th four (it.part: which four of the tile).  The work of
+// all requests is summed in fp64: whole numbers, exact below 2^53, and the same in every workgroup.
 template <int M, int KT, bool JOIN, int NW>
 __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &cl, uint32_t idx, SchedLds<NW> &sh, Item &out) {
     constexpr int NT = 64 * NW;
@@ -190,7 +191,9 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &
     W = 0.0;
 #pragma unroll
     for (int v = 0; v < NW; ++v) W += sh.work[v];
-    const int64_t c = part_tiles((int64_t)W, a.n_heads, cl.target, KT == kKT ? kPartMin : kTilePartMin);
+    // (only starts that decrease, each request claiming the same rows, could reach the limit)
+    const int64_t c = W * a.n_heads < 4e18 ? part_tiles((int64_t)W, a.n_heads, cl.target, KT == kKT ? kPartMin : kTilePartMin)
+                                           : INT64_MAX;
     uint32_t n_before = 0, s_before = 0;
     for (int r0 = 0; r0 < a.n_reqs; r0 += NT) {
         const RequestWork w = r0 == 0 ? w0 : work_of(r0 + tid);
@@ -608,7 +611,7 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     constexpr bool DMA = !F8 && D != 96;                       // rows go to LDS as they are, by its own loads
     constexpr int KS = DMA ? 2 * D : TileLds<D>::KS, VS = DMA ? 2 * D : TileLds<D>::VS;
     constexpr int CPR = F8 ? D / 16 : D / 8;                   // 16-byte pieces of a row in memory
-    constexpr int NP = (KT * CPR + NT - 1) / NT;                 // pieces of a thread, for each of K and V
+    constexpr int NP = (KT * CPR + NT - 1) / NT;               // pieces of a thread, for each of K and V
     constexpr bool RAGGED = KT * CPR % NT != 0;
     constexpr int STAGE = KT * (KS + VS);
     char *lds = tl.kv[0];
