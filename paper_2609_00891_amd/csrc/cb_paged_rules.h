@@ -30,7 +30,7 @@ CB_HD KeyTiles key_tiles(int32_t p_lo, int32_t p_hi, int32_t window, int32_t n_s
     KeyTiles k = {0, 0, 0};
     if (p_hi < 0) return k;
     const int32_t end = p_hi / KT + 1;
-    if (window > 0 && p_lo - window + 1 > 0) {
+    if (window > 0 && p_lo >= window) {                        // (p_lo - window may be below the least number)
         const int32_t lo = p_lo - window + 1;
         k.first = lo / KT;
         const int32_t s = n_sinks < lo ? n_sinks : lo;

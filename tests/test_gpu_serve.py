@@ -426,6 +426,20 @@ def test_attention_more_new_tokens_than_keys(cb, serve):
     assert (np.abs(got[3:5, :2] - o) <= 2 * BF * 1.02 * (mag + np.abs(o))).all()
 
 
+@pytest.mark.parametrize("G,q", [(2, 5), (4, 70)])
+def test_attention_largest_window_with_more_new_tokens_than_keys(cb, serve, G, q):
+    s = Step(cb, [(q, q), (3, 40)], 2, G, 64, 16, seed=9)
+    whole = s.run(kv=[q - 3, 40])
+    wide = s.run(kv=[q - 3, 40], window=2 ** 31 - 1)
+    assert torch.equal(wide[0], whole[0]) and torch.equal(wide[1], whole[1])
+    got = f64(s.out)
+    assert (got[:3] == 0).all()
+    for h in range(2):
+        hs = slice(h * G, (h + 1) * G)
+        o, _, mag, _ = serve.attention(f64(s.q)[3:q, hs], s.K[0][h], s.V[0][h], q - 3, 64 ** -0.5)
+        assert (np.abs(got[3:q, hs] - o) <= 2 * BF * 1.02 * (mag + np.abs(o))).all()
+
+
 def test_attention_lengths_out_of_range_stay_in_bounds(cb, serve):
     """Lengths beyond the table and starts beyond the rows are cut to them; negative ones are none."""
     s = Step(cb, [(1, 60), (1, 30)], 1, 2, 64, 16, seed=10)

@@ -70,6 +70,21 @@ def test_key_tiles_are_those_with_a_visible_key(rules, KT):
         assert set(got) - want <= {t for t in range(max(p_lo, 0) // KT + 1)} if p_lo < 0 else set(got) == want
 
 
+def test_key_tiles_with_the_largest_window_and_rows_before_the_first_key(tmp_path):
+    """Sums that wrap, as a compiler may form them, must not turn the largest window into a small one."""
+    (tmp_path / "rules.cpp").write_text(SOURCE)
+    so = str(tmp_path / "librules.so")
+    subprocess.run(["g++", "-O2", "-fwrapv", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, str(tmp_path / "rules.cpp"), "-o", so],
+                   check=True)
+    lib = ctypes.CDLL(so)
+    for window in (2 ** 31 - 1, 2 ** 31 - 40):
+        for p_lo, p_hi in ((-100, 70), (-41, 0), (-40, 200), (-2, 1), (0, 33), (2 ** 31 - 70, 2 ** 31 - 60)):
+            out = (ctypes.c_int * 3)()
+            lib.tiles(p_lo, p_hi, window, 0, 32, out)
+            hidden = max(0, p_lo - window + 1)                  # keys before this one are seen by no row
+            assert tuple(out) == (p_hi // 32 + 1 - hidden // 32, 0, hidden // 32), (window, p_lo, p_hi, tuple(out))
+
+
 def test_every_key_tile_of_every_row_tile_has_one_part(rules):
     """The workgroups' division, evaluated as they do: every (request, row tile, key tile) once, partial results and
     workgroups within what the host provides."""
