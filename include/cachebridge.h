@@ -727,9 +727,10 @@ cb_status cb_rope_axes(const cb_cache *in, const cb_cache *out, const cb_rope_ax
  * E4M3 pages hold x * (1 / scale) rounded to nearest even, clamped to +-448 (NaN
  * stays NaN).  q, q_out (both or neither, only with rope): query rows
  * turned in the same launch, token t of q into token t of q_out (q_out may be
- * q; q->n_tokens = the tokens of rows).  A token whose slot is outside the pool
- * (-1: padding) is skipped, its query too.  Two tokens must not name one slot;
- * rows, q and the pool must not overlap.  head_dim a multiple of 16 up to 256.
+ * q; its rows must not overlap; q->n_tokens = the tokens of rows).  A token
+ * whose slot is outside the pool (-1: padding) is skipped, its query too.  Two
+ * tokens must not name one slot; rows, q and the pool must not overlap.
+ * head_dim a multiple of 16 up to 256.
  */
 cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t layer0, const int32_t *slots,
                         const cb_rope_axes_spec *rope, const cb_rows *q, const cb_rows *q_out, void *stream);
@@ -748,11 +749,12 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
  * masked or unwritten places hold, NaN and infinities among it, does not reach
  * a row that does not see them.  Rows of no request, such as those behind
  * q_starts[n_reqs], are left as they were.
- *   q, out: n_tokens rows of n_qheads = G * n_heads heads; they must not overlap.
+ *   q, out: n_tokens rows of n_qheads = G * n_heads heads; out's rows must not
+ *     overlap q's or one another.
  *   q_starts must not decrease; kv_lens beyond table_width * page_size count as that.
  *   max_q_len: the largest number of new tokens of any request, a hint that
  *     picks the kernels; a wrong one costs time and changes roundings only.
- *   scale: finite.  window, n_sinks >= 0.
+ *   scale: finite, also times log2 e.  window, n_sinks >= 0.
  *   lse: fp32 [n_tokens][n_qheads], or NULL.
  *   workspace: device memory, 16-byte aligned, for the partial results of long
  *     rows that several workgroups share; cb_attn_paged_workspace_bytes gives

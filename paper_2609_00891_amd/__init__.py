@@ -700,6 +700,12 @@ def _ints(t: torch.Tensor, n: int, name: str):
         raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements, got {t.dtype} {tuple(t.shape)}")
 
 
+def _fit_int32(*values):
+    """The C calls take these as 32-bit numbers: a larger one would wrap."""
+    if not all(-(1 << 31) <= v < 1 << 31 for v in values):
+        raise ValueError(f"outside the range of 32-bit numbers: {values}")
+
+
 def _on_current_device(names: str, *tensors) -> int:
     """The library works on the current device: tensors of another (or of the host) are refused here.  Returns the
     device's index."""
@@ -797,6 +803,7 @@ def cb_page_tables(ctx_lens: torch.Tensor, q_lens: torch.Tensor, free_pages: tor
                        (positions, slots.numel(), "positions"), (info, n, "info"), (n_used, 1, "n_used")):
         _ints(t, m, name)
     _check_table(block_table, n)
+    _fit_int32(page_size)
     dev = _on_current_device("ctx_lens q_lens free_pages block_table q_starts kv_lens slots positions info n_used", ctx_lens,
                              q_lens, free_pages, block_table, q_starts, kv_lens, slots, positions, info, n_used)
     _check(_lib.cb_page_tables(n, _ptr(ctx_lens), _ptr(q_lens), _ptr(free_pages), free_pages.numel(), int(page_size),
@@ -830,6 +837,7 @@ def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer
     n = rows.shape[2] * rows.shape[4] if rows.dim() == 6 else 0
     rv = cache_view(rows)
     _ints(slots, n, "slots")
+    _fit_int32(layer)
     _check_axes_tokens(rope, n)
     qv = None if q is None else _rows_view(q, "q")
     ov = None if q_out is None else _rows_view(q_out, "q_out")
@@ -859,6 +867,7 @@ def cb_attn_paged(q: torch.Tensor, pages: CbPages, layer: int, q_starts: torch.T
     _ints(q_starts, n + 1, "q_starts")
     _ints(kv_lens, n, "kv_lens")
     _check_table(block_table, n)
+    _fit_int32(layer, max_q_len, window, sinks)
     if lse is not None:
         _need(lse, (q.shape[0], q.shape[1]), torch.float32, "lse")
     if workspace is not None and not workspace.is_contiguous():

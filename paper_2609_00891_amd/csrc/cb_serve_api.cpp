@@ -63,6 +63,14 @@ cb_status check_rows(const char *name, const cb_rows *r, int d) {
     return CB_OK;
 }
 
+// Rows that a call writes: no two may share an element.
+cb_status check_rows_written(const char *name, const cb_rows *r, int d) {
+    if (cb_status s = check_rows(name, r, d)) return s;
+    if ((r->n_tokens > 1 && r->s_tok < d) || (r->n_heads > 1 && r->s_head < d))
+        return fail(CB_ERR_SHAPE, "%s is written: its rows must not overlap", name);
+    return CB_OK;
+}
+
 cb_status check_rope_axes(const cb_rope_axes_spec *r, int d, int64_t n_tokens, cb::RopeAxes *out) {
     if (!r->table || !r->positions) return fail(CB_ERR_INVALID_ARGUMENT, "rope: table and positions must be non-NULL");
     if (r->style != CB_ROPE_HALF_SPLIT && r->style != CB_ROPE_INTERLEAVED)
@@ -192,7 +200,7 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
         if (cb_status s = check_rope_axes(rope, rows->head_dim, a.n_tokens, &a.rope)) return s;
     if (q) {
         if (cb_status s = check_rows("q", q, rows->head_dim)) return s;
-        if (cb_status s = check_rows("q_out", q_out, rows->head_dim)) return s;
+        if (cb_status s = check_rows_written("q_out", q_out, rows->head_dim)) return s;
         if (q->n_tokens != a.n_tokens || q_out->n_tokens != a.n_tokens || q->n_heads != q_out->n_heads)
             return fail(CB_ERR_SHAPE, "q and q_out must have the tokens of rows and equal heads");
         if (q->n_heads > (1 << 24)) return fail(CB_ERR_UNSUPPORTED, "too many query heads");
@@ -240,7 +248,7 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
     if (d != 64 && d != 96 && d != 128) return fail(CB_ERR_UNSUPPORTED, "head_dim must be 64, 96 or 128 (got %d)", d);
     if (layer < 0 || layer >= c.n_layers) return fail(CB_ERR_INVALID_ARGUMENT, "layer %d is outside the pool's %d", layer, c.n_layers);
     if (cb_status s = check_rows("q", q, d)) return s;
-    if (cb_status s = check_rows("out", out, d)) return s;
+    if (cb_status s = check_rows_written("out", out, d)) return s;
     if (out->n_tokens != q->n_tokens || out->n_heads != q->n_heads) return fail(CB_ERR_SHAPE, "q and out disagree on tokens or heads");
     if (q->n_heads % c.n_heads) return fail(CB_ERR_SHAPE, "%d query heads are no multiple of %d KV heads", q->n_heads, c.n_heads);
     if (n_reqs < 0) return fail(CB_ERR_INVALID_ARGUMENT, "n_reqs is negative");
@@ -250,7 +258,8 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
     if ((int64_t)table_width * c.seq_len > INT32_MAX)
         return fail(CB_ERR_UNSUPPORTED, "table_width * page size must be below 2^31");
     if (max_q_len < 0) return fail(CB_ERR_INVALID_ARGUMENT, "max_q_len is negative");
-    if (!std::isfinite(scale)) return fail(CB_ERR_INVALID_ARGUMENT, "scale must be finite");
+    const float scale_log2 = scale * 1.4426950408889634f;
+    if (!std::isfinite(scale_log2)) return fail(CB_ERR_INVALID_ARGUMENT, "scale must be finite (and so scale * log2 e)");
     if (window < 0 || n_sinks < 0) return fail(CB_ERR_INVALID_ARGUMENT, "window and n_sinks must be >= 0");
     if (workspace_bytes < 0) return fail(CB_ERR_INVALID_ARGUMENT, "workspace_bytes is negative");
     if (((uintptr_t)workspace) % 16 || ((uintptr_t)lse) % 4 || ((uintptr_t)q_starts) % 4 || ((uintptr_t)kv_lens) % 4 ||
@@ -284,7 +293,7 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
     a.n_reqs = n_reqs;
     a.n_heads = c.n_heads;
     a.G = cb::make_fastdiv((uint32_t)(q->n_heads / c.n_heads));
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_log2 = scale_log2;
     if (el == 1) {
         a.kscale = pages->scales + (int64_t)layer * 2 * c.n_heads;
         a.vscale = a.kscale + c.n_heads;

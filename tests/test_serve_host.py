@@ -206,6 +206,9 @@ def attn(cb, **kw):
     (dict(scale=float("inf")), ARG), (dict(window=-1), ARG), (dict(sinks=-1), ARG), (dict(ws=P + 4, ws_bytes=64), ALIGN),
     (dict(ws_bytes=-1), ARG), (dict(lse=P + 1), ALIGN),
     (dict(q=dict(n_tokens=0), out=dict(n_tokens=0)), OK), (dict(n_reqs=0), OK),
+    (dict(out=dict(data=3 * P, s_tok=0)), SHAPE), (dict(out=dict(data=3 * P, s_head=32)), SHAPE), (dict(scale=3e38), ARG),
+    (dict(q=dict(s_tok=0, s_head=0), n_reqs=0), OK),
+    (dict(q=dict(n_tokens=1, n_heads=2), out=dict(data=3 * P, n_tokens=1, n_heads=2, s_tok=0), n_reqs=0), OK),
 ])
 def test_attention_refuses(cb, kw, status):
     assert attn(cb, **kw) == status, cb.cb_last_error()
@@ -235,6 +238,8 @@ def write(cb, **kw):
     (dict(rope={}, q=dict(n_tokens=5), qo=dict(n_tokens=5, n_heads=2)), SHAPE),
     (dict(rope={}, q=dict(n_tokens=5), qo=dict(n_tokens=5, s_tok=512)), ARG),
     (dict(rows=dict(n_seqs=1, seq_len=0)), OK),
+    (dict(rope={}, q=dict(n_tokens=5), qo=dict(n_tokens=5, data=3 * P, s_tok=0)), SHAPE),
+    (dict(rope={}, q=dict(n_tokens=5), qo=dict(n_tokens=5, data=3 * P, s_head=0)), SHAPE),
 ])
 def test_page_write_refuses(cb, kw, status):
     assert write(cb, **kw) == status, cb.cb_last_error()
@@ -288,6 +293,13 @@ def test_binding_refuses_wrong_tensors(cb):
                        (dict(block_table=i(3, 3)), "block_table"), (dict(lse=z(2, 4)), "lse"), (dict(), "current CUDA device")):
         with pytest.raises(ValueError, match=match):
             cb.cb_attn_paged(**dict(good, **bad))
+    for name in ("layer", "max_q_len", "window", "sinks"):
+        with pytest.raises(ValueError, match="32-bit"):
+            cb.cb_attn_paged(**dict(good, **{name: 2 ** 32 + 1}))
+    with pytest.raises(ValueError, match="32-bit"):
+        cb.cb_page_write(z(1, 2, 1, 2, 9, 64), pg, i(9), layer=2 ** 32)
+    with pytest.raises(ValueError, match="32-bit"):
+        cb.cb_page_tables(i(2), i(2), i(4), 2 ** 32 + 16, i(2, 3), i(3), i(2), i(8), i(8), i(2), i(1))
     table = z(10, 32, 2, t=torch.float32)
     with pytest.raises(ValueError, match="axis"):
         cb.rope_axes_spec(table, i(3, 8), axis=[0] * 31)
