@@ -28,8 +28,8 @@
 //   tile is requested when K of this one has met the queries, V when V has
 //   become operands, table entries a tile earlier.  Bound by memory: 64 single
 //   tokens over 512 .. 16,384 keys (8 heads of 128, 8 query heads each, 1.36 GB)
-//   250 us, 5.4 TB/s; in e4m3 pages, 8 over 65,536 .. 131,072 (1.57 GB), 320 us,
-//   4.9 TB/s (a copy of 2 GiB runs at 4.9 TB/s here, both directions counted).
+//   250 us, 5.4 TB/s; in e4m3 pages, 8 over 65,536 .. 131,072 (1.57 GB), 312 us,
+//   5.0 TB/s (a copy of 2 GiB runs at 4.9 TB/s here, both directions counted).
 //   Two waves per SIMD are enough: with registers for three the calls took 274
 //   and 344 us, 252 and 336 with two.  Requested at the top of a tile instead of
 //   a tile ahead, K and V took the kernel from 245 and 319 to 270 and 375 us.
@@ -55,8 +55,8 @@
 //   cycles were conflicts).
 //
 // Division of work: a row tile's keys go in `parts` to workgroups of their own
-//   (cb_paged_rules.h), whose partial sums attn_join_kernel adds in the order
-//   of the parts.  Every workgroup finds its row tile and part from the
+//   (cb_paged_rules.h), whose partial sums attn_join_kernel adds in an order that
+//   depends on their number alone.  Every workgroup finds its row tile and part from the
 //   requests' lengths by itself: sums over the requests by data-parallel moves,
 //   about 2 us, instead of a plan that a caller would have to keep in step.
 #include "cb_serve_internal.h"
@@ -74,10 +74,17 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 
 constexpr int kKT = 32;                 // keys of a tile
 constexpr int kTileKT = 64;             // keys of a tile of the tile kernel
-// Least key tiles of a part, for rows_body (768 keys) and tile_body (1,024): what a part saves must be
-// worth the joining, a launch of about 8 us.  24 single tokens and three chunks with windows of 1,024
-// keys, one part each: 49 us; with parts of 256 keys and more: 61 us.
-constexpr int kPartMin = 24, kTilePartMin = 16;
+// Key tiles from which a row tile may be divided and the least of a part, for rows_body (1,152 and 512
+// keys) and tile_body (1,536 and 512): what dividing saves must be worth the joining, a launch of about
+// 8 us, and every part costs it something.  24 single tokens and three chunks with windows of 1,024 keys,
+// undivided: 49 us; with parts of 256 keys and more: 61 us.  One single token (8 heads of 128) over 8,192
+// and 131,072 keys: 18.5 and 113 us; with parts of at least 256 keys 18.0 and 113, of 768 21.3 and 111;
+// over 131,072 keys of one head: 26.5, 33.9 and 25.4.
+constexpr int part_min(int KT) { return KT == kKT ? 16 : 8; }
+constexpr int split_min(int KT) { return KT == kKT ? 36 : 24; }
+// Parts above which a row is joined by a workgroup instead of a wave: one single token over 131,072 keys
+// (256 parts) 113 us, 121 by a wave.
+constexpr int kWideParts = 16;
 // Workgroups that long rows are divided into: four for each of the 512 that are resident, so that
 // requests of different lengths end together (64 requests of 512 .. 16,384 keys: 262 us with 1,024,
 // 268 with 4,096, 259 with 2,048).
@@ -164,8 +171,9 @@ template <typename T> __device__ __forceinline__ T wave_sums(T x) {
 }
 
 // The row tile and part of index `idx`, or false behind the last.  JOIN: of the rows of all tiles in
-// more than one part, four at a time, the idx-th four (it.part: which four of the tile).  The work of
-// all requests is summed in fp64: whole numbers, exact below 2^53, and the same in every workgroup.
+// more than one part, four at a time (in more than kWideParts: one), the idx-th (it.part: which of the
+// tile).  The work of all requests is summed in fp64: whole numbers, exact below 2^53, and the same in
+// every workgroup.
 template <int M, int KT, bool JOIN, int NW>
 __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &cl, uint32_t idx, SchedLds<NW> &sh, Item &out) {
     constexpr int NT = 64 * NW;
@@ -192,13 +200,13 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &
 #pragma unroll
     for (int v = 0; v < NW; ++v) W += sh.work[v];
     // (only starts that decrease, each request claiming the same rows, could reach the limit)
-    const int64_t c = W * a.n_heads < 4e18 ? part_tiles((int64_t)W, a.n_heads, cl.target, KT == kKT ? kPartMin : kTilePartMin)
-                                           : INT64_MAX;
+    const int64_t c = W * a.n_heads < 4e18 ? part_tiles((int64_t)W, a.n_heads, cl.target, part_min(KT)) : INT64_MAX;
     uint32_t n_before = 0, s_before = 0;
     for (int r0 = 0; r0 < a.n_reqs; r0 += NT) {
         const RequestWork w = r0 == 0 ? w0 : work_of(r0 + tid);
-        const int32_t parts = parts_of(w.bound, c);
-        const uint32_t n = JOIN ? (parts > 1 ? (w.rows + 3) / 4 : 0) : (uint32_t)w.tiles * parts;
+        const int32_t parts = parts_of(w.bound, c, split_min(KT));
+        const bool wide = JOIN && parts > kWideParts;
+        const uint32_t n = JOIN ? (parts > 1 ? (wide ? w.rows : (w.rows + 3) / 4) : 0) : (uint32_t)w.tiles * parts;
         const uint32_t s = parts > 1 ? (uint32_t)w.tiles * parts : 0;
         uint32_t ni = wave_sums(n), si = wave_sums(s);
         if (r0 > 0) __syncthreads();                          // the last round's sums have been read
@@ -216,8 +224,11 @@ __device__ __forceinline__ bool find_item(const PagedArgs &a, const PagedClass &
         }
         const uint32_t first = n_before + ni - n;
         if (idx - first < n) {
-            const uint32_t k = idx - first, per = JOIN ? M / 4 : (uint32_t)parts, tile = k / per;
-            sh.item = {r0 + tid, (int32_t)tile, (int32_t)(k - tile * per), parts, (int32_t)(s_before + si - s + tile * parts)};
+            // the last row tile, with the most keys, first: 2,048 tokens over themselves (8 heads of 128,
+            // 8 query heads each) 97 us, 115 with the first one first
+            const uint32_t k = idx - first, per = JOIN ? (wide ? M : M / 4) : (uint32_t)parts;
+            const uint32_t tile = JOIN ? k / per : w.tiles - 1 - k / per;
+            sh.item = {r0 + tid, (int32_t)tile, (int32_t)(k % per), parts, (int32_t)(s_before + si - s + tile * parts)};
             sh.found = 1;
         }
         n_before += total;
@@ -964,31 +975,27 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
 
 // ------------------------------------------------------------------ joining parts
 
-// A row of a row tile that went in parts, by one wave: the partial sums, brought to the common maximum.
-// Lane p holds the weight of part p (64 parts at a time); 4 D bytes of a part are D / 4 lanes' loads,
+// The partial sums of parts p0 .. p1 - 1 of a row, by one wave, brought to the maximum of all parts: lane
+// l < D / 4 gets four channels' sum in t, every lane the weights' sum in lt and the maximum in mx.  Lane p
+// holds the weight of part p (64 parts at a time); 4 D bytes of a part are D / 4 lanes' loads,
 // so NP parts are added at once, slot p0 takes parts p0, p0 + NP, ..., and the slots are added at the
 // end: always the same order.
-template <int D, int M, int KT, bool F8>
-__device__ __forceinline__ void join_row(const PagedArgs &a, const PagedClass &cl, const Item &it, int head, int rr) {
-    constexpr int LP = D / 4, NP = 64 / LP;
+// Eight loads on their way together: one single token over 131,072 keys in 171 parts 117 us instead of 136.
+template <int D, int M>
+__device__ __forceinline__ void join_parts(const float *w0, int64_t step, int rr, int parts, int p0, int p1, f32x4_t &t, float &lt,
+                                           float &mx) {
+    constexpr int LP = D / 4, NP = 64 / LP, U = 8;
     const int lane = threadIdx.x & 63;
-    const Request rq = request(a, it.req);
-    const int32_t G = (int32_t)a.G.d;
-    const int32_t row0 = it.tile * M;
-    const int32_t n_rows = (int32_t)min((int64_t)rq.q_len * G - row0, (int64_t)M);
-    if (rr >= n_rows) return;
-    const int ch = lane % LP * 4, p0 = lane / LP;
-    const float *w0 = cl.ws + ((int64_t)it.slot * a.n_heads + head) * (M * (D + 2));
-    const int64_t step = (int64_t)a.n_heads * (M * (D + 2));
-    float mx = -HUGE_VALF;
-    for (int p = lane; p < it.parts; p += 64) mx = fmaxf(mx, w0[p * step + M * D + rr]);
+    const int ch = lane % LP * 4, slot = lane / LP;
+    mx = -HUGE_VALF;
+    for (int p = lane; p < parts; p += 64) mx = fmaxf(mx, w0[p * step + M * D + rr]);
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) mx = fmaxf(mx, __shfl_xor(mx, s));
     const float ref = mx == -HUGE_VALF ? 0.f : mx;
-    float lt = 0.f;
+    lt = 0.f;
     f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-    for (int pb = 0; pb < it.parts; pb += 64) {
-        const int np = min(64, it.parts - pb);
+    for (int pb = p0; pb < p1; pb += 64) {
+        const int np = min(64, p1 - pb);
         float f = 0.f;
         if (lane < np) {
             const float *w = w0 + (pb + lane) * step + M * D + rr;
@@ -996,39 +1003,82 @@ __device__ __forceinline__ void join_row(const PagedArgs &a, const PagedClass &c
             lt += w[M] * f;
         }
         const float *x0 = w0 + pb * step + rr * D + ch;
-#pragma unroll 8
-        for (int q = 0; q < np; q += NP) {
-            const float fq = __shfl(f, min(q + p0, 63));
-            if (p0 < NP && q + p0 < np) y += *(const f32x4_t *)(x0 + (q + p0) * step) * fq;
+        for (int q = 0; q < np; q += U * NP) {
+            f32x4_t x[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) x[i] = *(const f32x4_t *)(x0 + min(q + i * NP + slot, np - 1) * step);
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int p = q + i * NP + slot;
+                const float fq = __shfl(f, min(p, 63));
+                if (slot < NP && p < np) y += x[i] * fq;
+            }
         }
     }
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) lt += __shfl_xor(lt, s);
-    f32x4_t t = {0.f, 0.f, 0.f, 0.f};
+    t = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < NP; ++s)
 #pragma unroll
         for (int e = 0; e < 4; ++e) t[e] += __shfl(y[e], s * LP + lane % LP);
-    if (lane >= LP) return;
+}
+
+template <int D> struct JoinLds { f32x4_t t[4][D / 4]; float lt[4]; };
+
+// The rows of one item: four, a wave each, or, of a tile in many parts, one, whose parts the waves share.
+template <int D, int M, bool F8>
+__device__ __forceinline__ void join_rows(const PagedArgs &a, const PagedClass &cl, const Item &it, int head, JoinLds<D> &lds) {
+    constexpr int LP = D / 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool wide = it.parts > kWideParts;
+    const int rr = wide ? it.part : 4 * it.part + wave;
+    const Request rq = request(a, it.req);
+    const int32_t G = (int32_t)a.G.d;
+    const int32_t row0 = it.tile * M;
+    const int32_t n_rows = (int32_t)min((int64_t)rq.q_len * G - row0, (int64_t)M);
+    const float *w0 = cl.ws + ((int64_t)it.slot * a.n_heads + head) * (M * (D + 2));
+    const int64_t step = (int64_t)a.n_heads * (M * (D + 2));
+    f32x4_t t = {0.f, 0.f, 0.f, 0.f};
+    float lt = 0.f, mx = 0.f;
+    if (rr < n_rows) {
+        const int p0 = wide ? it.parts * wave / 4 : 0, p1 = wide ? it.parts * (wave + 1) / 4 : it.parts;
+        join_parts<D, M>(w0, step, rr, it.parts, p0, p1, t, lt, mx);
+    }
+    if (wide) {                                                // the waves' sums, in their order
+        if (lane < LP) lds.t[wave][lane] = t;
+        if (lane == 0) lds.lt[wave] = lt;
+        __syncthreads();
+        if (wave > 0) return;
+        const int l = lane < LP ? lane : 0;
+        t = lds.t[0][l];
+        lt = lds.lt[0];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+            t += lds.t[w][l];
+            lt += lds.lt[w];
+        }
+    }
+    if (rr >= n_rows || lane >= LP) return;
     const float inv = (F8 ? a.vscale[head] : 1.f) / lt;
     const int32_t tok = (int32_t)fast_div((uint32_t)(row0 + rr), a.G), u = row0 + rr - tok * G;
-    uint16_t *out = a.out + (int64_t)(rq.row0 + tok) * a.o_tok + (int64_t)(head * G + u) * a.o_head + ch;
+    uint16_t *out = a.out + (int64_t)(rq.row0 + tok) * a.o_tok + (int64_t)(head * G + u) * a.o_head + 4 * lane;
     *(u32x2_t *)out = lt == 0.f ? u32x2_t{0u, 0u} : u32x2_t{pack_bf16(t[0] * inv, t[1] * inv), pack_bf16(t[2] * inv, t[3] * inv)};
-    if (a.lse && ch == 0)
+    if (a.lse && lane == 0)
         a.lse[(int64_t)(rq.row0 + tok) * (a.n_heads * G) + head * G + u] =
             lt == 0.f ? -HUGE_VALF : 0.6931471805599453f * (mx + __log2f(lt));
 }
 
-// Four rows a time; blocks go round while there are more of them.
+// Blocks go round while there are more items.
 template <int D, int M, int KT, bool F8>
 __device__ __forceinline__ void join_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, uint32_t blocks,
-                                          SchedLds<4> &sched) {
+                                          SchedLds<4> &sched, JoinLds<D> &lds) {
     for (uint32_t b = block;; b += blocks) {
         const uint32_t idx = b / (uint32_t)a.n_heads;
         Item it;
         if (!find_item<M, KT, true, 4>(a, cl, idx, sched, it)) return;
-        join_row<D, M, KT, F8>(a, cl, it, (int)(b - idx * a.n_heads), 4 * it.part + (threadIdx.x >> 6));
-        __syncthreads();                                       // the item has been read
+        join_rows<D, M, F8>(a, cl, it, (int)(b - idx * a.n_heads), lds);
+        __syncthreads();                                       // the item and the sums have been read
     }
 }
 
@@ -1053,8 +1103,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(PagedArgs a) {
 template <int D, bool F8, int NW>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
     __shared__ SchedLds<4> sched;
-    if (blockIdx.x < a.tile.join_blocks) join_body<D, 32 * NW, kTileKT, F8>(a, a.tile, blockIdx.x, a.tile.join_blocks, sched);
-    else join_body<D, 16, kKT, F8>(a, a.rows, blockIdx.x - a.tile.join_blocks, a.rows.join_blocks, sched);
+    __shared__ JoinLds<D> lds;
+    if (blockIdx.x < a.tile.join_blocks) join_body<D, 32 * NW, kTileKT, F8>(a, a.tile, blockIdx.x, a.tile.join_blocks, sched, lds);
+    else join_body<D, 16, kKT, F8>(a, a.rows, blockIdx.x - a.tile.join_blocks, a.rows.join_blocks, sched, lds);
 }
 
 constexpr int kSmallRows = 16;          // rows of a request up to which rows_body takes it beside tile_body
@@ -1073,13 +1124,13 @@ bool prepare_class(const PagedArgs &a, PagedClass &c, int target, int64_t row_mi
     c.target = (int32_t)std::min<int64_t>(target, ws_bytes / (2 * slot));
     // no row is long enough to be divided
     const int32_t most = (int32_t)std::min<int64_t>((int64_t)a.table_width * a.page_size.d, INT32_MAX);
-    if (parts_of(key_tiles_bound(most, M, a.window, a.n_sinks, KT), KT == kKT ? kPartMin : kTilePartMin) == 1) c.target = 0;
+    if (parts_of(key_tiles_bound(most, M, a.window, a.n_sinks, KT), part_min(KT), split_min(KT)) == 1) c.target = 0;
     c.ws = (float *)ws;
     ws += 2 * slot * c.target;
     ws_bytes -= 2 * slot * c.target;
     const int64_t tiles = row_tiles_bound(a.n_tokens, a.n_reqs, a.G.d, M, row_max);
     const int64_t blocks = (tiles + c.target / a.n_heads) * a.n_heads;
-    const int64_t join = std::min<int64_t>(tiles, c.target / a.n_heads) * (M / 4) * a.n_heads;
+    const int64_t join = std::min<int64_t>(tiles, c.target / a.n_heads) * M * a.n_heads;
     if (blocks > INT32_MAX / 2 || join > INT32_MAX / 2) return false;
     c.blocks = (uint32_t)blocks;
     c.join_blocks = (uint32_t)std::min<int64_t>(join, kJoinBlocks);

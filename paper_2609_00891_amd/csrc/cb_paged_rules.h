@@ -68,6 +68,9 @@ CB_HD int32_t parts_of(int64_t bound, int64_t c) {
     return bound <= c ? 1 : (int32_t)(bound / c + (bound % c >= c - c / 2 ? 1 : 0));
 }
 
+// ... and with fewer than `least` key tiles always one.
+CB_HD int32_t parts_of(int64_t bound, int64_t c, int32_t least) { return bound < least ? 1 : parts_of(bound, c); }
+
 // Part s of `parts` of a list of n key tiles: v in [begin, end).
 CB_HD int32_t part_begin(int32_t n, int32_t s, int32_t parts) { return (int32_t)((int64_t)n * s / parts); }
 

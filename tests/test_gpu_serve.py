@@ -364,6 +364,19 @@ def test_attention_long_rows_in_parts(cb, serve, f8):
         s.check(serve, rows=[0, 1, 2])
 
 
+@pytest.mark.parametrize("d,f8", [(64, False), (96, False), (128, False), (64, True), (96, True), (128, True)])
+def test_attention_rows_in_many_parts(cb, serve, d, f8):
+    """Rows in dozens of parts, of single tokens and of chunks, joined by a workgroup each; the same bits every time."""
+    s = Step(cb, [(1, 20000), (40, 12000), (3, 5000), (2, 300)], 2, 2, d, 16, f8, pad=1, seed=80)
+    s.run()
+    s.check(serve)
+    a, al = s.out.clone(), s.lse.clone()
+    s.run()
+    assert torch.equal(a, s.out) and torch.equal(al, s.lse)
+    s.run(max_q=1)
+    s.check(serve)
+
+
 def test_attention_chunk_in_parts(cb, serve):
     s = Step(cb, [(70, 2100), (1, 50)], 1, 2, 64, 16, seed=4)
     s.run()

@@ -19,6 +19,7 @@ int tile_at(int n, int sink, int first, int v) { cb::KeyTiles k = {n, sink, firs
 int64_t bound(int kv, int tokens, int window, int sinks, int KT) { return cb::key_tiles_bound(kv, tokens, window, sinks, KT); }
 int64_t part_tiles(int64_t W, int H, int target, int c_min) { return cb::part_tiles(W, H, target, c_min); }
 int parts_of(int64_t b, int64_t c) { return cb::parts_of(b, c); }
+int parts_least(int64_t b, int64_t c, int least) { return cb::parts_of(b, c, least); }
 int part_begin(int n, int s, int parts) { return cb::part_begin(n, s, parts); }
 void work(int q, int kv, int G, int M, int KT, int64_t lo, int64_t hi, int window, int sinks, int64_t *out) {
     cb::RequestWork w = cb::request_work(q, kv, G, M, KT, lo, hi, window, sinks);
@@ -126,6 +127,13 @@ def test_every_key_tile_of_every_row_tile_has_one_part(rules):
         assert 3 * slots * H <= 4 * target
         assert joined <= min(tiles_bound, target // H)
         assert slots < 1 << 24
+
+
+def test_short_rows_have_one_part(rules):
+    rules.parts_least.restype, rules.parts_least.argtypes = ctypes.c_int, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int]
+    for b in range(0, 200):
+        for c in (8, 16, 50, 2 ** 63 - 1):
+            assert rules.parts_least(b, c, 36) == (1 if b < 36 else rules.parts_of(b, c))
 
 
 # ------------------------------------------------------------------ refusals (nothing is enqueued: no GPU needed)
