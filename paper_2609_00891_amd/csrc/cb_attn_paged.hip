@@ -46,7 +46,7 @@
 //   bf16 on the way; 96 channels are no whole number of pieces a thread).  A
 //   tile's products with V run beside the weights of its next 16 keys.
 //   Bound by the board's power: 2,048 tokens x 64 query heads over 32,768 keys
-//   in 8 heads of 128 take 2.07 .. 2.20 ms from board to board, 0.97 .. 1.03
+//   in 8 heads of 128 take 2.01 .. 2.20 ms from board to board, 0.97 .. 1.06
 //   PFLOP/s (a bf16 matrix product of 8192^3: 1.21), at 1.32 kW and 2.01 GHz of
 //   2.4 with the matrix units busy in 49% of the cycles; four sums and maxima
 //   instead of one, other orders of the products and wave priorities change
@@ -85,6 +85,8 @@ constexpr int split_min(int KT) { return KT == kKT ? 36 : 24; }
 // Parts above which a row is joined by a workgroup instead of a wave: one single token over 131,072 keys
 // (256 parts) 113 us, 121 by a wave.
 constexpr int kWideParts = 16;
+// Blocks of one kind in turn, one for every compute unit, where a launch has both.
+constexpr uint32_t kRun = 256;
 // Workgroups that long rows are divided into: four for each of the 512 that are resident, so that
 // requests of different lengths end together (64 requests of 512 .. 16,384 keys: 262 us with 1,024,
 // 268 with 4,096, 259 with 2,048).
@@ -1091,13 +1093,27 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
     rows_body<D, F8, 4>(a, a.rows, blockIdx.x, sched, lds);
 }
 
-// The requests with few rows and the others in one launch: the tiles, which take longer, first.
+// The requests with few rows and the others in one launch, runs of the two in turn, so that a compute
+// unit has products of the one beside loads of the other; a tile, which takes longer, first.  64 single
+// tokens over 1,024 .. 8,192 keys beside a chunk of 512 (8 heads of 128, 8 query heads each): 252 us, 272
+// with all tiles first, 272 with runs of 8; 24 beside three chunks of 515 with windows of 1,024: 53, 54, 72.
 template <int D, bool F8, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(PagedArgs a) {
     __shared__ SchedLds<NW> sched;
     __shared__ __attribute__((aligned(16))) union { RowsLds<D, NW> rows; TileLds<D> tile; } lds;
-    if (blockIdx.x < a.tile.blocks) tile_body<D, F8, NW>(a, a.tile, blockIdx.x, sched, lds.tile);
-    else rows_body<D, F8, NW>(a, a.rows, blockIdx.x - a.tile.blocks, sched, lds.rows);
+    const uint32_t pairs = min(a.tile.blocks, a.rows.blocks) / kRun, run = blockIdx.x / kRun;
+    uint32_t b;
+    bool tile;
+    if (run < 2 * pairs) {
+        tile = !(run & 1);
+        b = run / 2 * kRun + blockIdx.x % kRun;
+    } else {
+        b = blockIdx.x - pairs * kRun;
+        tile = b < a.tile.blocks;
+        if (!tile) b -= a.tile.blocks - pairs * kRun;
+    }
+    if (tile) tile_body<D, F8, NW>(a, a.tile, b, sched, lds.tile);
+    else rows_body<D, F8, NW>(a, a.rows, b, sched, lds.rows);
 }
 
 template <int D, bool F8, int NW>
