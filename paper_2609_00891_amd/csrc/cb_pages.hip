@@ -15,7 +15,7 @@
 //   and angles are read once for the group; products in fp32 from the exact
 //   bf16 values and the fp32 table, one rounding to the output's type.
 //   HBM-bound: every row is read once and written once.  40 layers of 12,282
-//   tokens turned back (8 heads of 128, 4.0 GB) 0.80 ms, 5.0 TB/s; a mapped
+//   tokens turned back (8 heads of 128, 4.0 GB) 0.78 .. 0.80 ms, 5.0 TB/s; a mapped
 //   cache of 64 layers x 4,096 tokens into 16-bit pages (2.1 GB) 0.41 ms, 5.2
 //   TB/s; four of up to 2,048 tokens into 8-bit pages, keys turned (2.4 GB),
 //   0.51 ms, 4.6 TB/s.
@@ -229,42 +229,73 @@ __device__ __forceinline__ uint2 pack8_e4m3(const float y[8], float inv) {
     return make_uint2((uint32_t)r[0], (uint32_t)r[1]);
 }
 
+// The value of another lane.
+__device__ __forceinline__ uint4 exchange(const uint4 &v, int lane) {
+    return make_uint4((uint32_t)__shfl((int)v.x, lane), (uint32_t)__shfl((int)v.y, lane), (uint32_t)__shfl((int)v.z, lane),
+                      (uint32_t)__shfl((int)v.w, lane));
+}
+
 // Rows of a token, in this order: K rows (layer, head), then query rows, then V rows.  blockIdx.y takes
-// a.group of them; blockIdx.x takes a.tok_per_block tokens.
-template <bool ROPE, bool F8>
+// a.group of them; a wave takes a.tok_per_wave tokens.
+// PAIRS: where half a row is no whole number of 128-byte lines, the lanes of two neighbouring tokens read
+// and write one row of the two at a time and exchange the halves in registers.  12,282 tokens of 40 layers
+// of 4 heads turned back: 96 channels 394 -> 297 us, 64 channels 246 -> 200.  A short call it makes longer
+// (2,048 tokens of 4 layers of 8 heads of 96: 14.3 -> 15.6 us, a group of 1; 4,096 of 8 layers of 64: 25.2
+// -> 24.0, a group of 4), so only groups of 4 rows or more take it.  8-bit pages do not (128 channels: 514
+// -> 520 us, 64: 284 -> 296, 96: 428 -> 420).
+constexpr int kPairsGroup = 4;
+template <bool ROPE, bool F8, bool PAIRS>
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
-    const int nc2 = (int)a.nc2.d;
-    const uint32_t tl = fast_div(threadIdx.x, a.nc2);
-    const int c = (int)(threadIdx.x - tl * nc2);
-    const int64_t tok = (int64_t)blockIdx.x * a.tok_per_block + tl;
-    if ((int)tl >= a.tok_per_block || tok >= a.n_tokens) return;
-    // where the token's rows go
-    int64_t out_tok = 0;
-    const uint32_t seq = fast_div((uint32_t)tok, a.seq_len);
-    const uint32_t in_seq = (uint32_t)tok - seq * a.seq_len.d;
-    if (a.slots) {
-        const int32_t slot = a.slots[tok];
-        if (slot < 0 || slot >= a.n_slots) return;
-        const uint32_t page = fast_div((uint32_t)slot, a.page_size);
-        out_tok = page * a.os.seq + (int64_t)((uint32_t)slot - page * a.page_size.d) * a.os.tok;
-    } else {
-        out_tok = seq * a.os.seq + (int64_t)in_seq * a.os.tok;
+    static_assert(!(F8 && PAIRS), "8-bit pages have no pairs");
+    const int nc2 = (int)a.nc2.d, lane = threadIdx.x & 63;
+    const int tl = (int)fast_div((uint32_t)lane, a.nc2), c = lane - tl * nc2;
+    if (tl >= a.tok_per_wave) return;                          // (an even number: of a pair both stay)
+    const int64_t tok = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * a.tok_per_wave + tl;
+    const int odd = PAIRS ? tl & 1 : 0, other = lane + (odd ? -nc2 : nc2);
+    // where the rows of the lane's token, or of the pair's two, come from and go
+    constexpr int NT = PAIRS ? 2 : 1;
+    int64_t in_tok[NT], out_tok[NT];
+    bool ok[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int64_t t = tok - odd + i;
+        ok[i] = t < a.n_tokens;
+        in_tok[i] = out_tok[i] = 0;
+        if (!ok[i]) continue;
+        const uint32_t seq = fast_div((uint32_t)t, a.seq_len);
+        const uint32_t in_seq = (uint32_t)t - seq * a.seq_len.d;
+        in_tok[i] = seq * a.is.seq + (int64_t)in_seq * a.is.tok;
+        if (a.slots) {
+            const int32_t slot = a.slots[t];
+            ok[i] = slot >= 0 && slot < a.n_slots;
+            const uint32_t page = fast_div((uint32_t)slot, a.page_size);
+            out_tok[i] = page * a.os.seq + (int64_t)((uint32_t)slot - page * a.page_size.d) * a.os.tok;
+        } else {
+            out_tok[i] = seq * a.os.seq + (int64_t)in_seq * a.os.tok;
+        }
     }
-    const int64_t in_tok = seq * a.is.seq + (int64_t)in_seq * a.is.tok;
+    if (!ok[0] && !ok[NT - 1]) return;                         // both lanes of a pair
     const int row0 = blockIdx.y * a.group, row1 = min(row0 + a.group, a.n_rows);
     const int LH = a.n_lh, QH = a.n_qh;
-    Angles an;
-    if (ROPE && row0 < LH + QH) an = load_angles(a.rope, tok, c, nc2, a.sign);
+    Angles an = {};
+    if (ROPE && row0 < LH + QH && ok[odd]) an = load_angles(a.rope, tok, c, nc2, a.sign);
+    // the two 16-byte chunks of a row that the lane reads, or one of each of the pair's rows
+    const int p0 = PAIRS ? odd * nc2 + c : c, p1 = PAIRS ? p0 : c + nc2;
     for (int row = row0; row < row1; ++row) {
         const bool is_q = row >= LH && row < LH + QH;
         const int kv = row >= LH + QH;
         const int lh = kv ? row - LH - QH : row;
         const int l = is_q ? 0 : (int)fast_div((uint32_t)lh, a.n_heads), h = is_q ? 0 : lh - l * (int)a.n_heads.d;
-        const uint16_t *x = is_q ? a.q + tok * a.q_tok + (row - LH) * a.q_head
-                                 : a.in + l * a.is.layer + kv * a.is.kv + h * a.is.head + in_tok;
-        ChunkPair v;
-        v.a = *(const uint4 *)(x + 8 * c);
-        v.b = *(const uint4 *)(x + 8 * (c + nc2));
+        const uint16_t *x = is_q ? a.q + (tok - odd) * a.q_tok + (row - LH) * a.q_head
+                                 : a.in + l * a.is.layer + kv * a.is.kv + h * a.is.head;
+        const uint16_t *x0 = x + (is_q ? 0 : in_tok[0]), *x1 = x + (is_q ? (PAIRS ? a.q_tok : 0) : in_tok[NT - 1]);
+        ChunkPair v = {};
+        if (ok[0]) v.a = *(const uint4 *)(x0 + 8 * p0);
+        if (ok[NT - 1]) v.b = *(const uint4 *)(x1 + 8 * p1);
+        if constexpr (PAIRS) {
+            const uint4 got = exchange(odd ? v.a : v.b, other);
+            if (odd) v.a = got; else v.b = got;
+        }
         float y0[8], y1[8];
         const bool turned = ROPE && !kv;
         if (turned) {
@@ -275,14 +306,20 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
         }
         if (F8 && !is_q) {
             const float inv = 1.0f / a.scales[((a.layer0 + l) * 2 + kv) * (int)a.n_heads.d + h];
-            uint8_t *o = (uint8_t *)a.out + l * a.os.layer + kv * a.os.kv + h * a.os.head + out_tok;
-            *(uint2 *)(o + 8 * c) = pack8_e4m3(y0, inv);
-            *(uint2 *)(o + 8 * (c + nc2)) = pack8_e4m3(y1, inv);
+            uint8_t *o = (uint8_t *)a.out + l * a.os.layer + kv * a.os.kv + h * a.os.head;
+            *(uint2 *)(o + out_tok[0] + 8 * c) = pack8_e4m3(y0, inv);
+            *(uint2 *)(o + out_tok[0] + 8 * (c + nc2)) = pack8_e4m3(y1, inv);
         } else {
-            uint16_t *o = is_q ? a.q_out + tok * a.qo_tok + (row - LH) * a.qo_head
-                               : (uint16_t *)a.out + l * a.os.layer + kv * a.os.kv + h * a.os.head + out_tok;
-            *(uint4 *)(o + 8 * c) = turned ? pack8(y0) : v.a;
-            *(uint4 *)(o + 8 * (c + nc2)) = turned ? pack8(y1) : v.b;
+            uint16_t *o = is_q ? a.q_out + (tok - odd) * a.qo_tok + (row - LH) * a.qo_head
+                               : (uint16_t *)a.out + l * a.os.layer + kv * a.os.kv + h * a.os.head;
+            uint16_t *o0 = o + (is_q ? 0 : out_tok[0]), *o1 = o + (is_q ? (PAIRS ? a.qo_tok : 0) : out_tok[NT - 1]);
+            uint4 w0 = turned ? pack8(y0) : v.a, w1 = turned ? pack8(y1) : v.b;
+            if constexpr (PAIRS) {
+                const uint4 got = exchange(odd ? w0 : w1, other);
+                if (odd) w0 = got; else w1 = got;
+            }
+            if (ok[0]) *(uint4 *)(o0 + 8 * p0) = w0;
+            if (ok[NT - 1]) *(uint4 *)(o1 + 8 * p1) = w1;
         }
     }
 }
@@ -301,18 +338,19 @@ hipError_t launch_page_tables(const PageTablesArgs &a, hipStream_t s) {
 
 hipError_t launch_rows(RowsArgs a, bool rope, bool f8, hipStream_t s) {
     if (a.n_tokens == 0 || a.n_rows == 0) return hipSuccess;
-    a.tok_per_block = 256 / (int)a.nc2.d;
-    const int64_t bx = (a.n_tokens + a.tok_per_block - 1) / a.tok_per_block;
+    a.tok_per_wave = 64 / (int)a.nc2.d & ~1;
+    const int64_t tok_per_block = 4 * a.tok_per_wave, bx = (a.n_tokens + tok_per_block - 1) / tok_per_block;
     // up to 16 rows share a token's slot and angles while the launch still fills the chip
     int group = 16;
     while (group > 1 && bx * ((a.n_rows + group - 1) / group) < 2048) group /= 2;
     while ((a.n_rows + group - 1) / group > 65535) group *= 2;
     a.group = group;
     const dim3 grid((unsigned)bx, (unsigned)((a.n_rows + group - 1) / group));
-    if (rope && f8) hipLaunchKernelGGL((rows_kernel<true, true>), grid, dim3(256), 0, s, a);
-    else if (rope) hipLaunchKernelGGL((rows_kernel<true, false>), grid, dim3(256), 0, s, a);
-    else if (f8) hipLaunchKernelGGL((rows_kernel<false, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((rows_kernel<false, false>), grid, dim3(256), 0, s, a);
+    const bool pairs = !f8 && a.nc2.d % 8 != 0 && group >= kPairsGroup;
+    const auto kernel = f8 ? rope ? rows_kernel<true, true, false> : rows_kernel<false, true, false>
+                        : pairs ? rope ? rows_kernel<true, false, true> : rows_kernel<false, false, true>
+                                : rope ? rows_kernel<true, false, false> : rows_kernel<false, false, false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

@@ -47,7 +47,7 @@ struct RowsArgs {
     int32_t n_lh, n_qh;       // (layer, head) rows and query rows of a token
     int32_t n_rows;           // K, then query, then V rows that are worked on
     int32_t group;            // rows of a token that one thread takes
-    int32_t tok_per_block;
+    int32_t tok_per_wave;
     int32_t layer0;           // the scales' layer of in's first
     const float *scales;      // e4m3 pages
     RopeAxes rope;

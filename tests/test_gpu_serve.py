@@ -141,6 +141,50 @@ def test_rope_axes(cb, serve, d, axes, style, L, H, B, T, token_major, inverse):
     assert torch.equal(inplace[:, 0].nan_to_num(3.0), out[:, 0].nan_to_num(3.0)) and torch.equal(inplace[:, 1], x[:, 1])
 
 
+@pytest.mark.parametrize("d", [16, 48, 64, 80, 96, 112, 176, 240])
+def test_long_calls_of_narrow_rows(cb, serve, d):
+    """Rows whose halves are no whole lines, in calls of many (layer, head) rows: an odd number of tokens, some of them
+    without a slot, some positions outside the table; in place, out of place and into pages are the same."""
+    L, H, B, T = 10, 8, 3, 401
+    g, n = gen(d), 3 * 401
+    x = randn(g, L, 2, B, H, T, d).cuda()
+    table, pos, axis = make_rope(cb, d, 2, n, seed=d, bad=(7, n - 1))
+    rope = cb.rope_axes_spec(table, i32(pos), axis)
+
+    def same(u, v):
+        return torch.equal(u.isnan(), v.isnan()) and torch.equal(u.nan_to_num(1.0), v.nan_to_num(1.0))
+
+    out = torch.full_like(x, 3.0)
+    cb.cb_rope_axes(x, out, rope)
+    y = x.clone()
+    cb.cb_rope_axes(y, y, rope)
+    assert same(y, out) and torch.equal(out[:, 1], x[:, 1])
+    rows = f64(x).transpose(2, 4, 0, 1, 3, 5).reshape(n, L, 2, H, d)
+    want, mag = serve.turn(rows[:, :2, 0], table.cpu().numpy(), pos, axis, 0)
+    got = f64(out).transpose(2, 4, 0, 1, 3, 5).reshape(n, L, 2, H, d)[:, :2, 0]
+    check_turned(got, want, mag, "keys")
+    pool = torch.full((L, 2, n, H, 1, d), 5.0, dtype=torch.bfloat16, device="cuda")
+    slots = torch.randperm(n, generator=g).int()
+    slots[[0, 5, 6, 7, 400, n - 2]] = -1
+    q = randn(g, n, 5, d).cuda()
+    q_out, q_ref = torch.full_like(q, 7.0), torch.empty((1, 2, 1, 5, n, d), dtype=torch.bfloat16, device="cuda")
+    cb.cb_page_write(x, cb.page_pool(pool), slots.cuda(), rope=rope, q=q, q_out=q_out)
+    cb.cb_rope_axes(q.transpose(0, 1)[None, None, None].expand(1, 2, 1, 5, n, d), q_ref, rope)
+    keep = slots >= 0
+    flat = out.permute(2, 4, 0, 1, 3, 5).reshape(n, L, 2, H, d).cpu()
+    moved = pool.permute(2, 4, 0, 1, 3, 5).reshape(n, L, 2, H, d).cpu()
+    assert same(moved[slots[keep].long()], flat[keep])
+    left = torch.ones(n, dtype=torch.bool)
+    left[slots[keep].long()] = False
+    assert (moved[left] == 5.0).all()
+    assert same(q_out.cpu()[keep], q_ref[0, 0, 0].transpose(0, 1).cpu()[keep])
+    assert (q_out.cpu()[~keep] == 7.0).all()
+    z = torch.full_like(pool, 5.0)                              # without a turn: the rows themselves
+    cb.cb_page_write(x, cb.page_pool(z), slots.cuda())
+    plain = x.permute(2, 4, 0, 1, 3, 5).reshape(n, L, 2, H, d).cpu()
+    assert torch.equal(z.permute(2, 4, 0, 1, 3, 5).reshape(n, L, 2, H, d).cpu()[slots[keep].long()], plain[keep])
+
+
 def test_rope_axes_with_one_axis_is_rope(cb):
     """Positions 3 .. 3 + T - 1 in one axis: the transform that cb_rope makes from an offset, bit for bit."""
     x = randn(gen(1), 2, 2, 1, 3, 40, 128).cuda()
