@@ -1,0 +1,85 @@
+"""Host analysis (no GPU) of the compiled kernels that load to LDS from inline statements: the wait states that such a
+load needs behind the writes of what it reads, which the compiler puts in for its own instructions and cannot put into
+an inline statement.
+
+  a scalar write of M0, which says where in LDS the data go    one wait state
+
+Every instruction is a wait state, s_nop n is n + 1 of them."""
+import concurrent.futures
+import glob
+import os
+import re
+import subprocess
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2609_00891_amd", "csrc")
+READS_M0 = re.compile(r"^(global_load_lds_|buffer_load_.*\blds\b|s_movrel|v_movrel|s_sendmsg|ds_\w*(gws|addtid))")
+
+
+def missing_waits(asm):
+    """(instructions that read M0, those too close behind a write of what they read) of an assembly."""
+    readers, bad, since_m0 = 0, [], 99
+    for line in asm.split("\n"):
+        s = line.split(";")[0].strip()
+        if not s or s[0] in ".#" or s.endswith(":"):
+            continue
+        op, _, operands = s.partition(" ")
+        if READS_M0.match(s):
+            readers += 1
+            if since_m0 < 1:
+                bad.append(s)
+        since_m0 += 1 + int(operands) if op == "s_nop" else 1
+        if op.startswith("s_") and re.match(r"m0\b", operands.strip()) and not op.startswith("s_cmp"):
+            since_m0 = 0
+    return readers, bad
+
+
+def test_analysis_counts_wait_states():
+    load = "\tglobal_load_lds_dwordx4 v2, s[4:5] nt"
+    for lines, wrong in ((["\ts_mov_b32 m0, s3", load], 1), (["\ts_mov_b32 m0, s3", "\ts_nop 0", load], 0),
+                         (["\ts_mov_b32 m0, s3", ".LBB0_1:", "\t; a comment", load], 1),
+                         (["\ts_add_u32 m0, m0, 0x400", load], 1), (["\ts_mov_b32 s3, m0", load], 0),
+                         (["\ts_mov_b32 m0, s3", "\ts_mov_b64 exec, 15", load, "\ts_mov_b32 m0, s6"], 0)):
+        readers, bad = missing_waits("\n".join(lines))
+        assert readers == 1 and len(bad) == wrong, lines
+
+
+def loads_to_lds(path):
+    text = open(path).read()
+    return "global_load_lds" in text or any(loads_to_lds(os.path.join(CSRC, h)) for h in re.findall(r'#include "(cb_\w+\.h)"', text))
+
+
+SOURCES = sorted(os.path.basename(s) for s in glob.glob(os.path.join(CSRC, "*.hip")) if loads_to_lds(s))
+
+
+@pytest.fixture(scope="module")
+def assemblies(tmp_path_factory):
+    sys.path.insert(0, os.path.dirname(CSRC))
+    try:
+        import build as lib_build
+    finally:
+        sys.path.pop(0)
+    out = tmp_path_factory.mktemp("asm")
+
+    def compile_one(name):
+        s = str(out / (name + ".s"))
+        subprocess.run([lib_build._hipcc()] + lib_build.COMMON + ["-x", "hip", "-S", "--cuda-device-only",
+                       os.path.join(CSRC, name), "-o", s], check=True, capture_output=True)
+        return open(s).read()
+
+    with concurrent.futures.ThreadPoolExecutor(max_workers=8) as ex:
+        return dict(zip(SOURCES, ex.map(compile_one, SOURCES)))
+
+
+def test_every_source_with_such_loads_is_looked_at():
+    assert {"cb_apply.hip", "cb_apply_multi.hip", "cb_attn.hip", "cb_attn_paged.hip", "cb_stats.hip", "cb_stats_centered.hip",
+            "cb_stats_multi.hip", "cb_stats_rope.hip"} <= set(SOURCES)
+
+
+@pytest.mark.parametrize("name", SOURCES)
+def test_loads_to_lds_wait_for_what_they_read(assemblies, name):
+    readers, bad = missing_waits(assemblies[name])
+    assert readers > 0 and not bad, (len(bad), bad[:3])
