@@ -476,12 +476,12 @@ __device__ __forceinline__ PairTask pair_task(const ApplyMultiArgs &a, int task)
 // Eight 16-byte copies global -> LDS under one save of M0: copy j reads
 // base + off[J + j] per lane and writes lane l's chunk at m0 + 1024 j + 16 l.
 // The compiler does not count these loads in its own vmcnt waits, nor does it see
-// the wait state that a load to LDS needs behind a write of M0: the statement has
-// it.
+// the wait states that a load to LDS needs: one behind a write of M0, five behind a
+// vector instruction that wrote its scalar address.  The statement has them.
 template <int J>
 __device__ __forceinline__ void dma8(const uint32_t (&off)[16], const void *base, uint32_t m0) {
     uint32_t keep_m0;
-    asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
+    asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 2\n\t"
                  "global_load_lds_dwordx4 %[v0], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v1], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v2], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
@@ -500,7 +500,7 @@ __device__ __forceinline__ void dma8(const uint32_t (&off)[16], const void *base
 
 __device__ __forceinline__ void dma2(uint32_t off0, uint32_t off1, const void *base, uint32_t m0) {
     uint32_t keep_m0;
-    asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
+    asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 2\n\t"
                  "global_load_lds_dwordx4 %[v0], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v1], %[sb]\n\t"
                  "s_mov_b32 m0, %[km]"

@@ -150,12 +150,13 @@ template <> struct Own<2, 1> {
 // other ring stages; completion is tracked with explicit vmcnt waits below.
 // M0 (and EXEC, where a copy is limited to some lanes) is saved and restored
 // inside the statement, so the compiler's own use of them is unaffected.  A load to
-// LDS may follow a write of M0 one wait state later at the earliest, and the
-// compiler does not see into the statements: they wait themselves.  The
+// LDS may follow a write of M0 one wait state later at the earliest, and a vector
+// instruction that wrote its scalar address (v_readfirstlane) five, and the compiler
+// does not see into the statements: they wait themselves.  The
 // row copies carry the non-temporal hint: every row is read once per call.
 __device__ __forceinline__ void dma16_sbase(uint32_t voff, const void *sbase, uint32_t m0) {
     uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b32 m0, %0"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b32 m0, %0"
                  : "=&s"(keep)
                  : "v"(voff), "s"(sbase), "s"(m0)
                  : "memory");
@@ -163,7 +164,7 @@ __device__ __forceinline__ void dma16_sbase(uint32_t voff, const void *sbase, ui
 // Two copies into LDS destinations m0 and m0 + 4096 under one M0 save/restore.
 __device__ __forceinline__ void dma16_pair(uint32_t va, const void *sa, uint32_t vb, const void *sb, uint32_t m0) {
     uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\t"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\t"
                  "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4 nt\n\ts_mov_b32 m0, %0"
                  : "=&s"(keep)
                  : "v"(va), "s"(sa), "v"(vb), "s"(sb), "s"(m0)

@@ -2,7 +2,8 @@
 load needs behind the writes of what it reads, which the compiler puts in for its own instructions and cannot put into
 an inline statement.
 
-  a scalar write of M0, which says where in LDS the data go    one wait state
+  a scalar write of M0, which says where in LDS the data go                   one wait state
+  a vector instruction's write of the scalar registers that hold an address    five
 
 Every instruction is a wait state, s_nop n is n + 1 of them."""
 import concurrent.futures
@@ -19,9 +20,21 @@ CSRC = os.path.join(ROOT, "paper_2609_00891_amd", "csrc")
 READS_M0 = re.compile(r"^(global_load_lds_|buffer_load_.*\blds\b|s_movrel|v_movrel|s_sendmsg|ds_\w*(gws|addtid))")
 
 
+VECTOR_MEMORY = re.compile(r"^(global_|buffer_|flat_|scratch_)")
+SCALAR_SECOND = re.compile(r"^v_((add|sub|subrev|addc|subb|subbrev)_co_|div_scale|mad_[ui]64)")
+
+
+def scalar_regs(text):
+    out = set()
+    for a, b, c in re.findall(r"\bs\[(\d+):(\d+)\]|\bs(\d+)\b", text):
+        out |= {int(c)} if c else set(range(int(a), int(b) + 1))
+    return out
+
+
 def missing_waits(asm):
-    """(instructions that read M0, those too close behind a write of what they read) of an assembly."""
-    readers, bad, since_m0 = 0, [], 99
+    """(instructions that read M0, vector memory instructions and those too close behind a write of what they read) of an
+    assembly."""
+    readers, bad, since_m0, written = 0, [], 99, {}            # written: states since a vector write of a scalar register
     for line in asm.split("\n"):
         s = line.split(";")[0].strip()
         if not s or s[0] in ".#" or s.endswith(":"):
@@ -31,9 +44,18 @@ def missing_waits(asm):
             readers += 1
             if since_m0 < 1:
                 bad.append(s)
-        since_m0 += 1 + int(operands) if op == "s_nop" else 1
-        if op.startswith("s_") and re.match(r"m0\b", operands.strip()) and not op.startswith("s_cmp"):
-            since_m0 = 0
+        if VECTOR_MEMORY.match(s) and any(written.get(r, 99) < 5 for r in scalar_regs(operands)):
+            bad.append(s)
+        states = 1 + int(operands) if op == "s_nop" else 1
+        since_m0 += states
+        written = {r: n + states for r, n in written.items() if n + states < 5}
+        dst = operands.split(",")[:2 if SCALAR_SECOND.match(op) else 1]
+        if op.startswith("s_"):
+            if re.match(r"m0\b", operands.strip()) and not op.startswith("s_cmp"):
+                since_m0 = 0
+            written = {r: n for r, n in written.items() if r not in scalar_regs(dst[0])}
+        elif op.startswith("v_"):
+            written.update({r: 0 for d in dst for r in scalar_regs(d)})
     return readers, bad
 
 
@@ -42,7 +64,12 @@ def test_analysis_counts_wait_states():
     for lines, wrong in ((["\ts_mov_b32 m0, s3", load], 1), (["\ts_mov_b32 m0, s3", "\ts_nop 0", load], 0),
                          (["\ts_mov_b32 m0, s3", ".LBB0_1:", "\t; a comment", load], 1),
                          (["\ts_add_u32 m0, m0, 0x400", load], 1), (["\ts_mov_b32 s3, m0", load], 0),
-                         (["\ts_mov_b32 m0, s3", "\ts_mov_b64 exec, 15", load, "\ts_mov_b32 m0, s6"], 0)):
+                         (["\ts_mov_b32 m0, s3", "\ts_mov_b64 exec, 15", load, "\ts_mov_b32 m0, s6"], 0),
+                         (["\tv_readfirstlane_b32 s5, v9", "\ts_mov_b32 m0, s3", "\ts_nop 2", load], 1),
+                         (["\tv_readfirstlane_b32 s5, v9", "\ts_mov_b32 m0, s3", "\ts_nop 3", load], 0),
+                         (["\tv_readfirstlane_b32 s3, v9", "\ts_mov_b32 m0, s3", "\ts_nop 0", load], 0),
+                         (["\tv_cmp_lt_u32_e64 s[4:5], v1, v2", "\ts_mov_b64 s[4:5], s[8:9]", load], 0),
+                         (["\tv_cmp_lt_u32_e64 s[4:5], v1, v2", load], 1)):
         readers, bad = missing_waits("\n".join(lines))
         assert readers == 1 and len(bad) == wrong, lines
 
