@@ -117,14 +117,10 @@ __device__ __forceinline__ uint32_t xoff(uint32_t t, uint32_t cb) {
 }
 
 // HBM -> LDS copy of 16 bytes per lane to M0 + 16 lane (direct-to-LDS load).
-// M0 is saved and restored inside the statement, which also holds the wait state
-// that a load to LDS needs behind a write of M0 (the compiler does not see it).
+// The statement holds the wait state that a load to LDS needs behind a write of M0
+// (the compiler does not see into it); the compiler keeps nothing in M0 here.
 __device__ __forceinline__ void dma16(const void *gaddr, uint32_t m0) {
-    uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep)
-                 : "v"(gaddr), "s"(m0)
-                 : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gaddr), "s"(m0) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_vm() {

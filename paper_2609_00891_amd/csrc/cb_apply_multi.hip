@@ -473,15 +473,15 @@ __device__ __forceinline__ PairTask pair_task(const ApplyMultiArgs &a, int task)
     return t;
 }
 
-// Eight 16-byte copies global -> LDS under one save of M0: copy j reads
+// Eight 16-byte copies global -> LDS: copy j reads
 // base + off[J + j] per lane and writes lane l's chunk at m0 + 1024 j + 16 l.
 // The compiler does not count these loads in its own vmcnt waits, nor does it see
-// the wait states that a load to LDS needs: one behind a write of M0, five behind a
-// vector instruction that wrote its scalar address.  The statement has them.
+// the wait state that a load to LDS needs behind a write of M0: the statement has
+// it.  It keeps nothing in M0 here, and base is a kernel argument's sum, written by
+// scalar instructions.
 template <int J>
 __device__ __forceinline__ void dma8(const uint32_t (&off)[16], const void *base, uint32_t m0) {
-    uint32_t keep_m0;
-    asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 2\n\t"
+    asm volatile("s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v0], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v1], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v2], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
@@ -489,23 +489,16 @@ __device__ __forceinline__ void dma8(const uint32_t (&off)[16], const void *base
                  "global_load_lds_dwordx4 %[v4], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v5], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v6], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %[v7], %[sb]\n\t"
-                 "s_mov_b32 m0, %[km]"
-                 : [km] "=&s"(keep_m0)
-                 : [m0] "s"(m0), [sb] "s"(base), [v0] "v"(off[J + 0]), [v1] "v"(off[J + 1]), [v2] "v"(off[J + 2]),
-                   [v3] "v"(off[J + 3]), [v4] "v"(off[J + 4]), [v5] "v"(off[J + 5]), [v6] "v"(off[J + 6]),
-                   [v7] "v"(off[J + 7])
+                 "global_load_lds_dwordx4 %[v7], %[sb]" ::[m0] "s"(m0), [sb] "s"(base),
+                 [v0] "v"(off[J + 0]), [v1] "v"(off[J + 1]), [v2] "v"(off[J + 2]), [v3] "v"(off[J + 3]),
+                 [v4] "v"(off[J + 4]), [v5] "v"(off[J + 5]), [v6] "v"(off[J + 6]), [v7] "v"(off[J + 7])
                  : "memory", "scc");
 }
 
 __device__ __forceinline__ void dma2(uint32_t off0, uint32_t off1, const void *base, uint32_t m0) {
-    uint32_t keep_m0;
-    asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 2\n\t"
+    asm volatile("s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %[v0], %[sb]\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %[v1], %[sb]\n\t"
-                 "s_mov_b32 m0, %[km]"
-                 : [km] "=&s"(keep_m0)
-                 : [m0] "s"(m0), [sb] "s"(base), [v0] "v"(off0), [v1] "v"(off1)
+                 "global_load_lds_dwordx4 %[v1], %[sb]" ::[m0] "s"(m0), [sb] "s"(base), [v0] "v"(off0), [v1] "v"(off1)
                  : "memory", "scc");
 }
 

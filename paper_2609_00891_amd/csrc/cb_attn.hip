@@ -66,15 +66,11 @@ __device__ __forceinline__ void split8(const float *v, bf16x8_t &hi, bf16x8_t &l
 }
 
 // 16 bytes per lane HBM -> LDS at M0 + 16 lane (global_load_lds_dwordx4),
-// tracked by vmcnt; M0 is saved and restored inside the statement, which also holds
-// the wait states that the load needs behind what it reads: one behind the write of
-// M0, five behind a vector instruction that wrote the address in scalar registers.
+// tracked by vmcnt.  The statement holds the wait state that the load needs behind
+// the write of M0; the address in scalar registers was written five or more states
+// before.  The compiler keeps nothing in M0 here.
 __device__ __forceinline__ void copy16(uint32_t voff, const void *sbase, uint32_t m0) {
-    uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep)
-                 : "v"(voff), "s"(sbase), "s"(m0)
-                 : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(m0) : "memory");
 }
 
 // Key index of accumulator register v in lane half hh of a 32x32 tile whose

@@ -601,15 +601,11 @@ __device__ __forceinline__ float both_halves_max(float x) {
 }
 
 typedef __attribute__((address_space(3))) char lds_char_t;
-// 16 bytes per lane from memory to LDS at m0 + 16 lane, counted by vmcnt; M0 is saved and restored.
-// A load to LDS may follow a write of M0 one wait state later at the earliest, and the compiler does not see
-// into the statement: it waits itself.
+// 16 bytes per lane from memory to LDS at m0 + 16 lane, counted by vmcnt.  A load to LDS may follow a write of M0
+// one wait state later at the earliest, and the compiler does not see into the statement: it waits itself.
+// The compiler keeps nothing in M0 here.
 __device__ __forceinline__ void copy16(const void *from, uint32_t m0) {
-    uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep)
-                 : "v"(from), "s"(m0)
-                 : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(m0) : "memory");
 }
 
 template <int D> struct TileLds {

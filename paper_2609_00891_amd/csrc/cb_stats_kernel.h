@@ -148,42 +148,38 @@ template <> struct Own<2, 1> {
 // dword form).  They are issued through inline assembly so that the compiler
 // does not add its own conservative waits between them and the LDS reads of
 // other ring stages; completion is tracked with explicit vmcnt waits below.
-// M0 (and EXEC, where a copy is limited to some lanes) is saved and restored
-// inside the statement, so the compiler's own use of them is unaffected.  A load to
-// LDS may follow a write of M0 one wait state later at the earliest, and a vector
-// instruction that wrote its scalar address (v_readfirstlane) five, and the compiler
-// does not see into the statements: they wait themselves.  The
-// row copies carry the non-temporal hint: every row is read once per call.
+// EXEC, where a copy is limited to some lanes, is saved and restored inside the
+// statement; the compiler keeps nothing in M0 here.  A load to LDS may follow a
+// write of M0 one wait state later at the earliest, and a vector instruction that
+// wrote its scalar address (v_readfirstlane) five, and the compiler does not see
+// into the statements: they wait themselves, s_nop WAIT.  WAIT = 0 where the address
+// comes from scalar instructions, 3 where it may come from vector ones: four more
+// states in every statement took the statistics 3.3% longer.  The row copies carry
+// the non-temporal hint: every row is read once per call.
+template <int WAIT>
 __device__ __forceinline__ void dma16_sbase(uint32_t voff, const void *sbase, uint32_t m0) {
-    uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep)
-                 : "v"(voff), "s"(sbase), "s"(m0)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop %3\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(sbase),
+                 "s"(m0), "n"(WAIT)
                  : "memory");
 }
-// Two copies into LDS destinations m0 and m0 + 4096 under one M0 save/restore.
+// Two copies into LDS destinations m0 and m0 + 4096.
+template <int WAIT>
 __device__ __forceinline__ void dma16_pair(uint32_t va, const void *sa, uint32_t vb, const void *sb, uint32_t m0) {
-    uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\t"
-                 "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4 nt\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep)
-                 : "v"(va), "s"(sa), "v"(vb), "s"(sb), "s"(m0)
+    asm volatile("s_mov_b32 m0, %4\n\ts_nop %5\n\tglobal_load_lds_dwordx4 %0, %1 nt\n\t"
+                 "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 nt" ::"v"(va),
+                 "s"(sa), "v"(vb), "s"(sb), "s"(m0), "n"(WAIT)
                  : "memory", "scc");
 }
 // Dword copy by the lanes set in `lanes` only (the wave is otherwise fully active).
 __device__ __forceinline__ void dma4_lanes(const void *gaddr, uint32_t m0, uint64_t lanes) {
     uint64_t keep_exec;
-    uint32_t keep_m0;
     asm volatile(
         "s_mov_b64 %0, exec\n\t"
-        "s_mov_b64 exec, %3\n\t"
-        "s_mov_b32 %1, m0\n\t"
-        "s_mov_b32 m0, %4\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dword %2, off\n\t"
-        "s_mov_b32 m0, %1\n\t"
+        "s_mov_b32 m0, %3\n\t"
+        "s_mov_b64 exec, %2\n\t"
+        "global_load_lds_dword %1, off\n\t"
         "s_mov_b64 exec, %0"
-        : "=&s"(keep_exec), "=&s"(keep_m0)
+        : "=&s"(keep_exec)
         : "v"(gaddr), "s"(lanes), "s"(m0)
         : "memory");
 }
@@ -453,18 +449,19 @@ __device__ __forceinline__ void stats_wave(const StatsArgs &a, const StatsCtx c,
     // tensor copies 2 part and 2 part + 1 (all of them in part 0 when the
     // schedule is not static), and the weights in part 3.
     auto issue_part = [&](const TilePos &q, int st, int part) {
+        constexpr int WAIT = CENTER ? 3 : 0;                 // centered: the cursor is in vector registers
         const uint32_t stage = lds_base + st * K::STAGE;
         const uint32_t mw = __builtin_amdgcn_readfirstlane(stage + wave * 1024);
         auto src = [&](int i) { return uniform_ptr(cbase[i] + (cisx[i] ? q.offx : q.offy)); };
         auto voff = [&](int i) { return RAGGED ? min(ctok[i], q.tmax) * cstk[i] + cvo[i] : cvo[i]; };
         if constexpr (CP::STATIC) {
             const int i = 2 * part;
-            if (i + 1 < L) dma16_pair(voff(i), src(i), voff(i + 1), src(i + 1), mw + i * 4096);
-            else if (i < L) dma16_sbase(voff(i), src(i), mw + i * 4096);
+            if (i + 1 < L) dma16_pair<WAIT>(voff(i), src(i), voff(i + 1), src(i + 1), mw + i * 4096);
+            else if (i < L) dma16_sbase<WAIT>(voff(i), src(i), mw + i * 4096);
         } else if (part == 0) {
 #pragma unroll
             for (int i = 0; i < L; ++i)
-                if (i < n_copies) dma16_sbase(voff(i), src(i), mw + i * 4096);
+                if (i < n_copies) dma16_sbase<WAIT>(voff(i), src(i), mw + i * 4096);
         }
         if (part == 3) {
             const bool ok = q.live && (!RAGGED || (uint32_t)(lane & 31) <= q.tmax);

@@ -74,57 +74,55 @@ struct MultiCtx {
     int64_t s_seq, t_seq;                    // elements between sequences
 };
 
-// All copies of one tile by one wave, under one save of M0 (and EXEC): NL
+// All copies of one tile by one wave, under one save of EXEC: NL
 // 16-byte copies into consecutive 4 KiB LDS slots starting at m0, then a
-// dword copy of the weights by lanes 0..3 into wm0 + 4 lane.  M0 and EXEC are
-// restored before the statement ends, so the compiler's use of them is
-// unaffected.  A load to LDS may follow a write of M0 one wait state later at the
-// earliest (an s_nop, or the instructions that set EXEC), and a vector instruction
-// that wrote its scalar address five: the first s_nop.
+// dword copy of the weights by lanes 0..3 into wm0 + 4 lane.  EXEC is restored
+// before the statement ends; the compiler keeps nothing in M0 here.  A load to LDS
+// may follow a write of M0 one wait state later at the earliest: an s_nop, or the
+// instructions that set EXEC.
 template <int NL>
 __device__ __forceinline__ void dma_tile(const uint32_t (&voff)[NL], const void *const (&base)[NL], uint32_t m0,
                                          const void *wg, uint32_t wm0) {
-    uint32_t keep_m0;
     uint64_t keep_exec;
 #define CB_CP(i) "global_load_lds_dwordx4 %" #i "_v, %" #i "_s\n\t"
     if constexpr (NL == 1) {
-        asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 2\n\t"
+        asm volatile("s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v0], %[s0]\n\t"
                      "s_mov_b32 m0, %[wm]\n\ts_mov_b64 %[ke], exec\n\ts_mov_b64 exec, 15\n\t"
-                     "global_load_lds_dword %[wg], off\n\ts_mov_b64 exec, %[ke]\n\ts_mov_b32 m0, %[km]"
-                     : [km] "=&s"(keep_m0), [ke] "=&s"(keep_exec)
+                     "global_load_lds_dword %[wg], off\n\ts_mov_b64 exec, %[ke]"
+                     : [ke] "=&s"(keep_exec)
                      : [m0] "s"(m0), [v0] "v"(voff[0]), [s0] "s"(base[0]), [wm] "s"(wm0), [wg] "v"(wg)
                      : "memory");
     } else if constexpr (NL == 2) {
-        asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 2\n\t"
+        asm volatile("s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v0], %[s0]\n\ts_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v1], %[s1]\n\t"
                      "s_mov_b32 m0, %[wm]\n\ts_mov_b64 %[ke], exec\n\ts_mov_b64 exec, 15\n\t"
-                     "global_load_lds_dword %[wg], off\n\ts_mov_b64 exec, %[ke]\n\ts_mov_b32 m0, %[km]"
-                     : [km] "=&s"(keep_m0), [ke] "=&s"(keep_exec)
+                     "global_load_lds_dword %[wg], off\n\ts_mov_b64 exec, %[ke]"
+                     : [ke] "=&s"(keep_exec)
                      : [m0] "s"(m0), [v0] "v"(voff[0]), [s0] "s"(base[0]), [v1] "v"(voff[1]), [s1] "s"(base[1]),
                        [wm] "s"(wm0), [wg] "v"(wg)
                      : "memory", "scc");
     } else if constexpr (NL == 3) {
-        asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 2\n\t"
+        asm volatile("s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v0], %[s0]\n\ts_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v1], %[s1]\n\ts_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v2], %[s2]\n\t"
                      "s_mov_b32 m0, %[wm]\n\ts_mov_b64 %[ke], exec\n\ts_mov_b64 exec, 15\n\t"
-                     "global_load_lds_dword %[wg], off\n\ts_mov_b64 exec, %[ke]\n\ts_mov_b32 m0, %[km]"
-                     : [km] "=&s"(keep_m0), [ke] "=&s"(keep_exec)
+                     "global_load_lds_dword %[wg], off\n\ts_mov_b64 exec, %[ke]"
+                     : [ke] "=&s"(keep_exec)
                      : [m0] "s"(m0), [v0] "v"(voff[0]), [s0] "s"(base[0]), [v1] "v"(voff[1]), [s1] "s"(base[1]),
                        [v2] "v"(voff[2]), [s2] "s"(base[2]), [wm] "s"(wm0), [wg] "v"(wg)
                      : "memory", "scc");
     } else {
-        asm volatile("s_mov_b32 %[km], m0\n\ts_mov_b32 m0, %[m0]\n\ts_nop 2\n\t"
+        asm volatile("s_mov_b32 m0, %[m0]\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v0], %[s0]\n\ts_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v1], %[s1]\n\ts_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v2], %[s2]\n\ts_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"
                      "global_load_lds_dwordx4 %[v3], %[s3]\n\t"
                      "s_mov_b32 m0, %[wm]\n\ts_mov_b64 %[ke], exec\n\ts_mov_b64 exec, 15\n\t"
-                     "global_load_lds_dword %[wg], off\n\ts_mov_b64 exec, %[ke]\n\ts_mov_b32 m0, %[km]"
-                     : [km] "=&s"(keep_m0), [ke] "=&s"(keep_exec)
+                     "global_load_lds_dword %[wg], off\n\ts_mov_b64 exec, %[ke]"
+                     : [ke] "=&s"(keep_exec)
                      : [m0] "s"(m0), [v0] "v"(voff[0]), [s0] "s"(base[0]), [v1] "v"(voff[1]), [s1] "s"(base[1]),
                        [v2] "v"(voff[2]), [s2] "s"(base[2]), [v3] "v"(voff[3]), [s3] "s"(base[3]),
                        [wm] "s"(wm0), [wg] "v"(wg)

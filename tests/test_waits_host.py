@@ -5,7 +5,8 @@ an inline statement.
   a scalar write of M0, which says where in LDS the data go                   one wait state
   a vector instruction's write of the scalar registers that hold an address    five
 
-Every instruction is a wait state, s_nop n is n + 1 of them."""
+Every instruction is a wait state, s_nop n is n + 1 of them.  The statements do not save M0: nothing outside of inline
+statements may use it in these kernels."""
 import concurrent.futures
 import glob
 import os
@@ -74,6 +75,17 @@ def test_analysis_counts_wait_states():
         assert readers == 1 and len(bad) == wrong, lines
 
 
+def outside_inline(asm):
+    """The instructions of an assembly that the compiler made itself."""
+    inline, out = False, []
+    for line in asm.split("\n"):
+        if "#ASMSTART" in line or "#ASMEND" in line:
+            inline = "#ASMSTART" in line
+        elif not inline:
+            out.append(line.split(";")[0].strip())
+    return out
+
+
 def loads_to_lds(path):
     text = open(path).read()
     return "global_load_lds" in text or any(loads_to_lds(os.path.join(CSRC, h)) for h in re.findall(r'#include "(cb_\w+\.h)"', text))
@@ -110,3 +122,10 @@ def test_every_source_with_such_loads_is_looked_at():
 def test_loads_to_lds_wait_for_what_they_read(assemblies, name):
     readers, bad = missing_waits(assemblies[name])
     assert readers > 0 and not bad, (len(bad), bad[:3])
+
+
+@pytest.mark.parametrize("name", SOURCES)
+def test_the_compiler_keeps_nothing_in_m0(assemblies, name):
+    used = [s for s in outside_inline(assemblies[name]) if re.search(r"\bm0\b", s) or READS_M0.match(s) or "set_gpr_idx" in s]
+    assert not used, used[:3]
+    assert "m0" not in "".join(outside_inline("\t;;#ASMSTART\n\ts_mov_b32 m0, s1\n\t;;#ASMEND\n\ts_nop 0"))
