@@ -784,6 +784,10 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
     l = 0.f;
 #pragma unroll
     for (int q = 0; q < ND; ++q) o[q] = f32x16_t{};
+    // The exponent is fma(s, c2, -m) with m = c2 max s rounded: off by up to half an ulp of m, alike for every
+    // key of a row, so it cancels against the sum of the weights as long as it is small.  Where some row's |m| passes 2^24 it
+    // is not (2^32 would overflow the weights): from there the scores take c2, rounded, before.
+    bool far = false;
     // K operand: key n, channels 16 q + 8 h .. + 7, at k_at ^ 32 q (rows without gaps) or k_at + 32 q.
     // V^T operand: keys 16 kk + 4 h + {0 .. 3} and + 8, channel 32 q + (lane & 31), at v_at ^ 64 q or
     // v_at + 64 q.
@@ -870,13 +874,20 @@ __device__ __forceinline__ void tile_body(const PagedArgs &a, const PagedClass &
             l *= al;
 #pragma unroll
             for (int q = 0; q < ND; ++q) o[q] *= al;
+            far = __any(fabsf(m == -HUGE_VALF ? 0.f : m) > 16777216.f);
         }
         const float ref = m == -HUGE_VALF ? 0.f : m;
+        float ce = c2;
+        if (far) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] *= c2;
+            ce = 1.f;
+        }
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 3][2 * e & 15], c2, -ref));
-            const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 3][(2 * e & 15) + 1], c2, -ref));
+            const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 3][2 * e & 15], ce, -ref));
+            const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 3][(2 * e & 15) + 1], ce, -ref));
             sum += x0;
             sum += x1;
             pk[e] = pack_bf16(x0, x1);

@@ -856,3 +856,58 @@ def test_attention_large_chunk_in_parts(cb, serve):
     check_tokens(serve, s, [(0, 0), (0, 3), (0, 4), (0, 1025), (0, 2049)], [0])
     s.run(ws=False)
     check_tokens(serve, s, [(0, 0), (0, 2049)], [0])
+
+
+def one_hot(cb, lens, G, d, f8, exponent, sign=1.0, scale=None):
+    """A step whose scores are exact and so far apart that a row's largest visible one takes all the weight: key j is
+    c_j in every channel, c_j whole numbers that fit both types, queries 2^exponent in every channel."""
+    s = Step(cb, lens, 1, G, d, 16, f8, seed=90)
+    c = [np.random.default_rng(r).permutation(kv) % 13 * 16 + 16.0 for r, (_, kv) in enumerate(lens)]
+    for r, (nq, kv) in enumerate(lens):
+        for j in range(kv):
+            s.pool[s.layer, 0, int(s.table[r, j // 16]), :, j % 16] = torch.full((1, d), c[r][j]).to(s.pool.dtype).cuda()
+    s.q = torch.full_like(s.q, sign * 2.0 ** exponent)
+    s.run(scale=scale)
+    sc = d ** -0.5 if scale is None else scale
+    kscale = 1.0 if not f8 else float(s.scales[s.layer, 0, 0])
+    for r, (nq, kv) in enumerate(lens):
+        for i in range(nq):
+            t, p = s.starts[r] + i, kv - nq + i
+            score = sc * kscale * d * sign * 2.0 ** exponent * c[r][:p + 1]
+            best = np.flatnonzero(score == score.max())
+            v = s.V[r][0][best]                                             # equal scores share the weight
+            got, l = f64(s.out)[t], f64(s.lse)[t]
+            tol = BF * 1.01 * np.abs(v.mean(0)) + (BF + (kv + 64) * 2 * F32) * np.abs(v).mean(0)
+            assert (np.abs(got - v.mean(0)) <= tol).all(), (r, i)
+            want = score.max() + math.log(len(best))
+            assert (np.abs(l - want) <= 8 * F32 * (np.abs(want) + 1)).all(), (r, i)
+
+
+@pytest.mark.parametrize("sign,scale", [(1.0, None), (-1.0, None), (1.0, -0.3)])
+@pytest.mark.parametrize("exponent", [12, 17, 20, 24, 27, 28, 40, 90])
+@pytest.mark.parametrize("f8", [False, True])
+def test_attention_scores_beyond_the_places_of_fp32(cb, f8, exponent, sign, scale):
+    """Scores of 2^20 .. 2^100: fp32 has no fractions there, but the differences are whole scores and the largest one's
+    weight is 1 in every kernel."""
+    for lens, G in (([(1, 70), (3, 40)], 4), ([(70, 200), (40, 40)], 2), ([(300, 300)], 1)):
+        one_hot(cb, lens, G, 128, f8, exponent, sign, scale)
+    one_hot(cb, [(40, 100), (1, 60)], 4, 96, f8, exponent, sign, scale)
+
+
+def test_attention_scores_beyond_the_places_of_fp32_in_large_chunks(cb):
+    for exponent in (20, 28):
+        s = Step(cb, [(520, 520)], 8, 64, 64, 16, seed=91, layers=1, layer=0)
+        c = torch.arange(520) % 251 + 1
+        pool = s.pool
+        for j in range(520):
+            pool[0, 0, int(s.table[0, j // 16]), :, j % 16] = float(c[j])
+        s.q = torch.full_like(s.q, 2.0 ** exponent)
+        s.run()
+        best = [int(max(range(i + 1), key=lambda j: (int(c[j]), j))) for i in range(520)]
+        got = f64(s.out)
+        for i in (0, 1, 63, 64, 200, 250, 251, 519):
+            rows = [j for j in range(i + 1) if c[j] == c[best[i]]]
+            for h in (0, 7):
+                v = s.V[0][h][rows]
+                tol = BF * 1.01 * np.abs(v.mean(0)) + (BF + 584 * 2 * F32) * np.abs(v).mean(0)
+                assert (np.abs(got[i, 64 * h:64 * h + 64] - v.mean(0)) <= tol).all(), (exponent, i, h)
