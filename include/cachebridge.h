@@ -653,7 +653,8 @@ typedef struct {
 /*
  * Packed token rows (queries, attention outputs): element (token, head, ch) at
  *   data[token * s_tok + head * s_head + ch]   (bfloat16, ch stride 1),
- * every row 16-byte aligned.
+ * every row 16-byte aligned.  Rows that a call writes may not overlap: the larger
+ * stride is at least what the smaller one spans with its count (CB_ERR_SHAPE).
  */
 typedef struct {
     void *data;

@@ -63,11 +63,29 @@ cb_status check_rows(const char *name, const cb_rows *r, int d) {
     return CB_OK;
 }
 
+// Rows of d elements at every combination of n indexes (counts, strides): false if two could share an
+// element.  The dimensions have to nest: each stride is at least what the smaller ones span together.
+bool rows_apart(int d, int n, const int64_t *count, const int64_t *stride) {
+    int order[5], m = 0;
+    for (int i = 0; i < n; ++i) {
+        if (count[i] <= 1) continue;
+        int j = m++;
+        for (; j > 0 && stride[order[j - 1]] > stride[i]; --j) order[j] = order[j - 1];
+        order[j] = i;
+    }
+    __int128 span = d;
+    for (int j = 0; j < m; ++j) {
+        if (stride[order[j]] < span) return false;
+        span += (__int128)(count[order[j]] - 1) * stride[order[j]];
+    }
+    return true;
+}
+
 // Rows that a call writes: no two may share an element.
 cb_status check_rows_written(const char *name, const cb_rows *r, int d) {
     if (cb_status s = check_rows(name, r, d)) return s;
-    if ((r->n_tokens > 1 && r->s_tok < d) || (r->n_heads > 1 && r->s_head < d))
-        return fail(CB_ERR_SHAPE, "%s is written: its rows must not overlap", name);
+    const int64_t count[2] = {r->n_tokens, r->n_heads}, stride[2] = {r->s_tok, r->s_head};
+    if (!rows_apart(d, 2, count, stride)) return fail(CB_ERR_SHAPE, "%s is written: its rows must not overlap", name);
     return CB_OK;
 }
 

@@ -333,3 +333,32 @@ def test_plain_tables_by_hand():
     assert r["block_table"].tolist() == [[7, 20, -1], [21, -1, -1], [9, 8, -1], [-1, -1, -1]]
     assert r["positions"].tolist() == [3, 4, 0] + [-1] * 6
     assert r["slots"].tolist() == [7 * 4 + 3, 80, 84] + [-1] * 6
+
+
+# ------------------------------------------------------------------ rows that are written
+
+@pytest.mark.parametrize("s_tok,s_head,ok", [
+    (64, 64, False), (64, 128, False), (128, 64, False), (192, 64, False), (256, 64, True), (264, 64, True), (64, 192, True),
+    (64, 184, False), (64, 0, False), (0, 64, False), (56, 256, False)])
+def test_rows_that_meet_are_refused_where_they_are_written(cb, s_tok, s_head, ok):
+    """Three tokens of four heads of 64: two (token, head) rows may not share an element in an output."""
+    at = sorted((t * s_tok + h * s_head) for t in range(3) for h in range(4))
+    assert ok == all(b - a >= 64 for a, b in zip(at, at[1:]))
+    r = dict(n_tokens=3, n_heads=4, s_tok=s_tok, s_head=s_head)
+    assert attn(cb, out=dict(r, data=3 * P), n_reqs=0) == (OK if ok else SHAPE)
+    # (rows without tokens: with good strides the call ends at the next check, that of the token counts)
+    q = dict(n_tokens=3, n_heads=4)
+    assert write(cb, rope={}, q=q, qo=dict(r, data=3 * P)) == SHAPE
+    assert ("must not overlap" in cb.cb_last_error()) == (not ok)
+    assert attn(cb, q=dict(r, data=3 * P), n_reqs=0) == OK                  # what is only read may meet
+
+
+def test_rows_that_interleave_without_nesting_are_refused(cb):
+    """Apart, but neither dimension's stride spans the other: refused as the header says."""
+    assert attn(cb, out=dict(data=3 * P, n_tokens=3, n_heads=4, s_tok=320, s_head=128), n_reqs=0) == SHAPE
+
+
+def test_rows_far_apart_do_not_wrap(cb):
+    for s_tok, s_head, ok in ((1 << 62, 1 << 61, False), (1 << 62, 1 << 60, True), (64, 1 << 62, True)):
+        out = dict(data=3 * P, n_tokens=3, n_heads=4, s_tok=s_tok, s_head=s_head)
+        assert attn(cb, out=out, n_reqs=0) == (OK if ok else SHAPE)
