@@ -713,7 +713,9 @@ cb_status cb_page_tables(int32_t n_reqs, const int32_t *ctx_lens, const int32_t 
  * cb_rope with explicit positions of several axes: every K row of `in` turned
  * by its token's positions (turned back when `inverse` is non-zero) into
  * `out`, in fp32 from the exact bf16 values with one rounding.  V rows, in
- * place use, geometry, widths and overlaps as in cb_rope.
+ * place use, geometry, widths and overlaps as in cb_rope.  The rows of `out`
+ * that are written may not overlap one another: its strides nest, each at least
+ * what the smaller ones span (CB_ERR_SHAPE).
  */
 cb_status cb_rope_axes(const cb_cache *in, const cb_cache *out, const cb_rope_axes_spec *rope, int32_t inverse,
                        void *stream);
@@ -730,7 +732,9 @@ cb_status cb_rope_axes(const cb_cache *in, const cb_cache *out, const cb_rope_ax
  * turned in the same launch, token t of q into token t of q_out (q_out may be
  * q; its rows must not overlap; q->n_tokens = the tokens of rows).  A token
  * whose slot is outside the pool (-1: padding) is skipped, its query too.  Two
- * tokens must not name one slot; rows, q and the pool must not overlap.
+ * tokens must not name one slot; rows, q and the pool must not overlap, nor the
+ * pool's rows one another (its strides nest, or CB_ERR_SHAPE; a pool that is
+ * only read may have any).
  * head_dim a multiple of 16 up to 256.
  */
 cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t layer0, const int32_t *slots,

@@ -89,6 +89,15 @@ cb_status check_rows_written(const char *name, const cb_rows *r, int d) {
     return CB_OK;
 }
 
+// A cache or pool that a call writes: the rows of all its dimensions, or without kv those of K.
+cb_status check_cache_written(const char *name, const cb_cache &c, bool kv) {
+    const int64_t count[5] = {c.n_layers, kv ? 2 : 1, c.n_seqs, c.n_heads, c.seq_len};
+    const int64_t stride[5] = {c.s_layer, c.s_kv, c.s_seq, c.s_head, c.s_tok};
+    if (!rows_apart(c.head_dim, 5, count, stride))
+        return fail(CB_ERR_SHAPE, "%s is written: its rows must not overlap", name);
+    return CB_OK;
+}
+
 cb_status check_rope_axes(const cb_rope_axes_spec *r, int d, int64_t n_tokens, cb::RopeAxes *out) {
     if (!r->table || !r->positions) return fail(CB_ERR_INVALID_ARGUMENT, "rope: table and positions must be non-NULL");
     if (r->style != CB_ROPE_HALF_SPLIT && r->style != CB_ROPE_INTERLEAVED)
@@ -193,6 +202,7 @@ cb_status cb_rope_axes(const cb_cache *in, const cb_cache *out, const cb_rope_ax
     if (same && (in->s_layer != out->s_layer || in->s_kv != out->s_kv || in->s_seq != out->s_seq ||
                  in->s_head != out->s_head || in->s_tok != out->s_tok))
         return fail(CB_ERR_INVALID_ARGUMENT, "an in-place transform needs out to have in's strides");
+    if (cb_status s = check_cache_written("out", *out, !same)) return s;
     a.out = out->data;
     a.os = strides_of(*out);
     a.n_rows = (same ? 1 : 2) * a.n_lh;
@@ -235,6 +245,7 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
     if (a.n_tokens == 0) return cb::api_ok();
     if (!slots) return fail(CB_ERR_INVALID_ARGUMENT, "slots is NULL");
     if (((uintptr_t)slots) % 4) return fail(CB_ERR_MISALIGNED, "slots must be 4-byte aligned");
+    if (cb_status s = check_cache_written("pages", c, true)) return s;
     a.out = (char *)c.data + (int64_t)layer0 * c.s_layer * (pages->dtype == CB_PAGES_E4M3 ? 1 : 2);
     a.os = strides_of(c);
     a.slots = slots;

@@ -362,3 +362,37 @@ def test_rows_far_apart_do_not_wrap(cb):
     for s_tok, s_head, ok in ((1 << 62, 1 << 61, False), (1 << 62, 1 << 60, True), (64, 1 << 62, True)):
         out = dict(data=3 * P, n_tokens=3, n_heads=4, s_tok=s_tok, s_head=s_head)
         assert attn(cb, out=out, n_reqs=0) == (OK if ok else SHAPE)
+
+
+# a cache of three layers, four sequences or pages, two heads, 16 tokens of 64 channels, every dimension beside the others
+NESTED = dict(n_layers=3, n_seqs=4, n_heads=2, seq_len=16, head_dim=64, s_layer=16384, s_kv=8192, s_seq=2048, s_head=1024,
+              s_tok=64)
+MEET = [dict(s_tok=0), dict(s_head=0), dict(s_seq=0), dict(s_kv=0), dict(s_layer=0), dict(s_tok=48), dict(s_head=64),
+        dict(s_seq=1024), dict(s_kv=2048), dict(s_layer=8192), dict(s_kv=8176), dict(s_layer=4096, s_kv=16384)]
+
+
+def refused_as_written(cb, status, name):
+    return status == SHAPE and f"{name} is written" in cb.cb_last_error()
+
+
+@pytest.mark.parametrize("kw", MEET)
+@pytest.mark.parametrize("dtype,scales", [(0, None), (1, P)])
+def test_a_pool_whose_rows_meet_is_refused_where_it_is_written(cb, kw, dtype, scales):
+    bad = {**NESTED, "dtype": dtype, "scales": scales, **kw}
+    r = dict(data=4 * P, n_layers=2, n_seqs=1, seq_len=5)
+    assert refused_as_written(cb, write(cb, rows=r, pages=bad), "pages"), cb.cb_last_error()
+    # without tokens nothing is written; what attention reads may meet (a broadcast pool)
+    assert write(cb, rows=dict(r, seq_len=0), pages=bad) == OK
+    assert attn(cb, pages=bad, n_reqs=0) == OK
+
+
+@pytest.mark.parametrize("kw", MEET)
+def test_a_turned_cache_whose_rows_meet_is_refused(cb, kw):
+    def turn(inn, out):
+        return cb.library().cb_rope_axes(ctypes.byref(cache(cb, **inn)), ctypes.byref(cache(cb, **out)),
+                                         ctypes.byref(rope(cb)), 0, None)
+    bad = {**NESTED, **kw}
+    assert refused_as_written(cb, turn(NESTED, dict(bad, data=8 * P)), "out"), cb.cb_last_error()
+    if "s_kv" not in kw and kw != dict(s_layer=8192):           # in place only keys are written, and those are apart
+        assert refused_as_written(cb, turn(bad, bad), "out"), cb.cb_last_error()
+    assert turn(dict(bad, n_seqs=0), dict(bad, n_seqs=0, data=8 * P)) == OK
