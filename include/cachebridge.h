@@ -767,10 +767,12 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
  *     leaves nothing in it that another reads; calls that overlap in time need
  *     one each.
  * Scores and sums are fp32 from exact products; the weights exp(s_j - m) are
- * rounded to bf16 for their product with V (m the running maximum) and summed
- * unrounded.  Results depend on the other requests only in the order of fp32
- * sums (where a row is split), and are bitwise reproducible.  head_dim in
- * {64, 96, 128}.
+ * rounded to bf16 for their product with V (m a running maximum) and summed
+ * unrounded.  max_q_len, the workspace's size and the other requests decide which
+ * kernel takes a row and how its keys are divided, and every part has a running
+ * maximum of its own: they change the order of the fp32 sums and, within its
+ * rounding, the bf16 number of a weight.  The same call gives the same bits
+ * again.  head_dim in {64, 96, 128}.
  */
 cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,
                         const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,

@@ -911,3 +911,39 @@ def test_attention_scores_beyond_the_places_of_fp32_in_large_chunks(cb):
                 v = s.V[0][h][rows]
                 tol = BF * 1.01 * np.abs(v.mean(0)) + (BF + 584 * 2 * F32) * np.abs(v).mean(0)
                 assert (np.abs(got[i, 64 * h:64 * h + 64] - v.mean(0)) <= tol).all(), (exponent, i, h)
+
+
+@pytest.mark.parametrize("d,f8", [(64, False), (96, True), (128, False), (128, True)])
+@pytest.mark.parametrize("nq,kv", [(1, 300), (2, 700), (4, 2600)])
+def test_attention_of_a_request_beside_others(cb, serve, d, f8, nq, kv):
+    """A request alone, beside a chunk (which picks the other kernel for it) and beside rows long enough to be divided:
+    other orders of sums and other bf16 weights, each within its roundings, the same bits for the same call.  Two results
+    differ by the two outputs' roundings and, for weights w whose bf16 numbers differ by up to 2^-8 w on either side, by
+    twice the weights' share."""
+    H, G = 2, 8
+    beside = ([], [(90, 400)], [(1, 30000)], [(300, 2000), (1, 9000), (2, 40)])
+    results, first = [], None
+    for others in beside:
+        s = Step(cb, [(nq, kv)] + others, H, G, d, 16, f8, seed=95, layers=1, layer=0)
+        if first is None:
+            first = s
+        else:                                                   # the request's own keys, values and queries are the first step's
+            s.K[0], s.V[0] = first.K[0], first.V[0]
+            s.scales = first.scales
+            s.q[:nq] = first.q[:nq]
+            for j in range(-(-kv // 16)):
+                s.pool[0, :, int(s.table[0, j])] = first.pool[0, :, int(first.table[0, j])]
+        s.run()
+        s.check(serve, rows=[0])
+        a, l = s.out[:nq].clone(), s.lse[:nq].clone()
+        s.run()
+        assert torch.equal(a, s.out[:nq]) and torch.equal(l, s.lse[:nq])
+        results.append((f64(a), f64(l)))
+    for h in range(H):
+        hs = slice(h * G, (h + 1) * G)
+        o, l, mag, smag = serve.attention(f64(first.q)[:nq, hs], first.K[0][h], first.V[0][h], kv, d ** -0.5)
+        es, few = (d + 8) * 2 * F32 * smag, (kv + 64) * 2 * F32
+        tol = 2 * (BF * 1.01 * np.abs(o) + mag * (BF * 1.01 + (2 * es + few)[..., None]))
+        for a, al in results[1:]:
+            assert (np.abs(a[:, hs] - results[0][0][:, hs]) <= tol).all()
+            assert (np.abs(al[:, hs] - results[0][1][:, hs]) <= 2 * (es + few + 8 * F32 * (np.abs(l) + 1))).all()
