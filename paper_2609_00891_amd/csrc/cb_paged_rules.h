@@ -1,8 +1,9 @@
-// cb_paged_rules.h -- how attention over pages is cut into workgroups: rules on
-// lengths that every workgroup evaluates for itself from the requests' lengths
+// cb_paged_rules.h -- how the serving calls are cut into workgroups, free of the
+// HIP runtime so that it can be checked on the CPU: attention over pages, by rules
+// on lengths that every workgroup evaluates for itself from the requests' lengths
 // on the device (so no plan has to be built or kept), shared with the host that
-// sizes grids and workspaces, and free of the HIP runtime so that they can be
-// checked on the CPU.
+// sizes grids and workspaces; and, on the host alone, the rows that are turned,
+// copied or written into pages.
 #pragma once
 #include <cstdint>
 
@@ -100,6 +101,35 @@ inline int64_t row_tiles_bound(int64_t n_tokens, int64_t n_reqs, int64_t G, int6
     const int64_t all = n_tokens * G / M + n_reqs;
     const int64_t each = row_max / M + (row_max % M != 0);
     return each <= all / n_reqs ? n_reqs * each : all;
+}
+
+// Host side: the launch that turns n_rows rows of head_dim channels of each of n_tokens tokens.
+// PAIRS: where half a row is no whole number of 128-byte lines, the lanes of two neighbouring tokens read
+// and write one row of the two at a time and exchange the halves in registers.  12,282 tokens of 40 layers
+// of 4 heads turned back: 96 channels 394 -> 297 us, 64 channels 246 -> 200.  A short call it makes longer
+// (2,048 tokens of 4 layers of 8 heads of 96: 14.3 -> 15.6 us, a group of 1; 4,096 of 8 layers of 64: 25.2
+// -> 24.0, a group of 4), so only groups of 4 rows or more take it.  8-bit pages do not (128 channels: 514
+// -> 520 us, 64: 284 -> 296, 96: 428 -> 420).
+constexpr int kPairsGroup = 4;
+struct RowsCut {
+    int32_t tok_per_wave;    // even
+    int32_t group;           // rows of a token that one thread takes
+    int64_t blocks, groups;  // the grid: workgroups of four waves, groups of rows
+    bool pairs;
+};
+inline RowsCut rows_cut(int64_t n_tokens, int32_t n_rows, int32_t head_dim, bool f8) {
+    RowsCut c;
+    const int nc2 = head_dim / 16;
+    c.tok_per_wave = (64 / nc2) & ~1;
+    const int64_t per = 4 * (int64_t)c.tok_per_wave;
+    c.blocks = (n_tokens + per - 1) / per;
+    // up to 16 rows share a token's slot and angles while the launch still fills the chip
+    c.group = 16;
+    while (c.group > 1 && c.blocks * ((n_rows + c.group - 1) / c.group) < 2048) c.group /= 2;
+    while ((n_rows + c.group - 1) / c.group > 65535) c.group *= 2;
+    c.groups = (n_rows + c.group - 1) / c.group;
+    c.pairs = !f8 && nc2 % 8 != 0 && c.group >= kPairsGroup;
+    return c;
 }
 
 }  // namespace cb

@@ -20,6 +20,7 @@
 //   TB/s; four of up to 2,048 tokens into 8-bit pages, keys turned (2.4 GB),
 //   0.51 ms, 4.6 TB/s.
 #include "cb_serve_internal.h"
+#include "cb_paged_rules.h"
 
 namespace cb {
 namespace {
@@ -237,13 +238,7 @@ __device__ __forceinline__ uint4 exchange(const uint4 &v, int lane) {
 
 // Rows of a token, in this order: K rows (layer, head), then query rows, then V rows.  blockIdx.y takes
 // a.group of them; a wave takes a.tok_per_wave tokens.
-// PAIRS: where half a row is no whole number of 128-byte lines, the lanes of two neighbouring tokens read
-// and write one row of the two at a time and exchange the halves in registers.  12,282 tokens of 40 layers
-// of 4 heads turned back: 96 channels 394 -> 297 us, 64 channels 246 -> 200.  A short call it makes longer
-// (2,048 tokens of 4 layers of 8 heads of 96: 14.3 -> 15.6 us, a group of 1; 4,096 of 8 layers of 64: 25.2
-// -> 24.0, a group of 4), so only groups of 4 rows or more take it.  8-bit pages do not (128 channels: 514
-// -> 520 us, 64: 284 -> 296, 96: 428 -> 420).
-constexpr int kPairsGroup = 4;
+// PAIRS: two tokens' lanes exchange halves of rows (rows_cut in cb_paged_rules.h, with what it measured).
 template <bool ROPE, bool F8, bool PAIRS>
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
     static_assert(!(F8 && PAIRS), "8-bit pages have no pairs");
@@ -338,15 +333,11 @@ hipError_t launch_page_tables(const PageTablesArgs &a, hipStream_t s) {
 
 hipError_t launch_rows(RowsArgs a, bool rope, bool f8, hipStream_t s) {
     if (a.n_tokens == 0 || a.n_rows == 0) return hipSuccess;
-    a.tok_per_wave = 64 / (int)a.nc2.d & ~1;
-    const int64_t tok_per_block = 4 * a.tok_per_wave, bx = (a.n_tokens + tok_per_block - 1) / tok_per_block;
-    // up to 16 rows share a token's slot and angles while the launch still fills the chip
-    int group = 16;
-    while (group > 1 && bx * ((a.n_rows + group - 1) / group) < 2048) group /= 2;
-    while ((a.n_rows + group - 1) / group > 65535) group *= 2;
-    a.group = group;
-    const dim3 grid((unsigned)bx, (unsigned)((a.n_rows + group - 1) / group));
-    const bool pairs = !f8 && a.nc2.d % 8 != 0 && group >= kPairsGroup;
+    const RowsCut cut = rows_cut(a.n_tokens, a.n_rows, 16 * (int)a.nc2.d, f8);
+    a.tok_per_wave = cut.tok_per_wave;
+    a.group = cut.group;
+    const dim3 grid((unsigned)cut.blocks, (unsigned)cut.groups);
+    const bool pairs = cut.pairs;
     const auto kernel = f8 ? rope ? rows_kernel<true, true, false> : rows_kernel<false, true, false>
                         : pairs ? rope ? rows_kernel<true, false, true> : rows_kernel<false, false, true>
                                 : rope ? rows_kernel<true, false, false> : rows_kernel<false, false, false>;

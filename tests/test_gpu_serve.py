@@ -8,7 +8,10 @@ Tolerances are the operators' own roundings, counted element by element:
   score's error (d fp32 sums of products of at most S = max_j sum_i |scale q_i k_i|: (d + 4) 2^-23 S, counted for the
   weight and for their sum), the sums over n keys take n 2^-24, exp2 and log2 a few ulps; the output rounds once more.
 """
+import ctypes
 import math
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -947,3 +950,88 @@ def test_attention_of_a_request_beside_others(cb, serve, d, f8, nq, kv):
         for a, al in results[1:]:
             assert (np.abs(a[:, hs] - results[0][0][:, hs]) <= tol).all()
             assert (np.abs(al[:, hs] - results[0][1][:, hs]) <= 2 * (es + few + 8 * F32 * (np.abs(l) + 1))).all()
+
+
+# ------------------------------------------------------------------ rows whose halves two tokens' lanes exchange
+
+@pytest.fixture(scope="module")
+def rows_cut(tmp_path_factory):
+    """The launch of a call on rows, from the library's own rule: (group, whether pairs of tokens exchange halves)."""
+    d = tmp_path_factory.mktemp("rows_cut")
+    (d / "cut.cpp").write_text('#include "cb_paged_rules.h"\nextern "C" int cut(int64_t n, int rows, int d, int f8) {\n'
+                               '    cb::RowsCut c = cb::rows_cut(n, rows, d, f8); return 2 * c.group + c.pairs; }\n')
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_00891_amd", "csrc")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(d / "cut.cpp"), "-o", str(d / "cut.so")],
+                   check=True)
+    lib = ctypes.CDLL(str(d / "cut.so"))
+    lib.cut.argtypes = [ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int]
+    return lambda n, rows, d, f8=False: divmod(lib.cut(n, rows, d, int(f8)), 2)
+
+
+@pytest.mark.parametrize("style", [0, 1])
+@pytest.mark.parametrize("d,L,H,B,T,token_major", [
+    (64, 54, 8, 3, 401, False), (96, 54, 8, 3, 401, True), (16, 103, 16, 3, 401, False), (112, 40, 8, 1, 801, False),
+    (240, 30, 8, 3, 401, True), (64, 80, 128, 1, 1, False), (96, 200, 8, 2, 150, False)])
+def test_rows_that_exchange_halves(cb, serve, rows_cut, d, L, H, B, T, token_major, style):
+    """Every form of the exchange, in calls that the rule gives to it: out of place and in place, forward and back, into
+    pages with tokens without a slot (of pairs one, the other or both) and query rows, turned or not.  The same bits as
+    layer by layer, calls that the rule gives to the other form, and the plain form in some layers."""
+    n, QH = B * T, 5
+    for rows in (L * H, 2 * L * H, 2 * L * H + QH):
+        group, pairs = rows_cut(n, rows, d)
+        assert pairs and group >= 4
+    assert not rows_cut(n, 2 * H, d)[1]
+    g = gen(d + T)
+    shape = (L, 2, B, T, H, d) if token_major else (L, 2, B, H, T, d)
+    x = torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(d + T), device="cuda").to(torch.bfloat16)
+    x = x.permute(0, 1, 2, 4, 3, 5) if token_major else x
+    table, pos, axis = make_rope(cb, d, 3, n, seed=d, bad=(n - 1, 7) if n > 8 else ())
+    rope = cb.rope_axes_spec(table, i32(pos), axis, style)
+
+    def same(u, v):
+        return torch.equal(u.isnan(), v.isnan()) and torch.equal(u.nan_to_num(1.0), v.nan_to_num(1.0))
+
+    for inverse in (False, True):
+        out = torch.full((L, 2, B, H, T, d), 3.0, dtype=torch.bfloat16, device="cuda")
+        cb.cb_rope_axes(x, out, rope, inverse=inverse)
+        one = torch.full_like(out, 3.0)
+        for l in range(L):
+            cb.cb_rope_axes(x[l:l + 1], one[l:l + 1], rope, inverse=inverse)
+        assert same(out, one)
+        y = x.clone(memory_format=torch.preserve_format)
+        cb.cb_rope_axes(y, y, rope, inverse=inverse)
+        assert same(y, one)
+        for l in (0, L - 1):
+            want, mag = serve.turn(f64(x[l, 0, :, :2]).transpose(0, 2, 1, 3).reshape(n, -1, d), table.cpu().numpy(), pos, axis,
+                                   style, inverse)
+            check_turned(f64(out[l, 0, :, :2]).transpose(0, 2, 1, 3).reshape(n, -1, d), want, mag, "keys")
+    slots = torch.randperm(n + 3, generator=g)[:n].int()
+    if n > 8:
+        slots[[0, 5, 6, 7, 10, 11, n // 2, n - 2]] = -1
+        slots[3] = n + 3
+    keep = ((slots >= 0) & (slots < n + 3)).cuda()
+    at = slots.cuda()[keep].long()
+    left = torch.ones(n + 3, dtype=torch.bool, device="cuda")
+    left[at] = False
+    q = randn(g, n, QH, d).cuda()
+    q_ref = torch.empty((1, 2, 1, QH, n, d), dtype=torch.bfloat16, device="cuda")
+    cb.cb_rope_axes(q.transpose(0, 1)[None, None, None].expand(1, 2, 1, QH, n, d), q_ref, rope)
+    for turned in (True, False):
+        ref = x
+        if turned:
+            ref = torch.full((L, 2, B, H, T, d), 3.0, dtype=torch.bfloat16, device="cuda")
+            cb.cb_rope_axes(x, ref, rope)
+        pool = torch.full((L, 2, n + 3, H, 1, d), 5.0, dtype=torch.bfloat16, device="cuda")
+        q_out = torch.full_like(q, 7.0)
+        kw = dict(rope=rope, q=q, q_out=q_out) if turned else {}
+        cb.cb_page_write(x, cb.page_pool(pool), slots.cuda(), **kw)
+        moved = pool.squeeze(4)                                 # [layer][kv][slot][head][d]
+        flat = ref.permute(0, 1, 2, 4, 3, 5).reshape(L, 2, n, H, d)
+        assert same(moved[:, :, at], flat[:, :, keep])
+        assert (moved[:, :, left] == 5.0).all()
+        if turned:
+            assert same(q_out[keep], q_ref[0, 0, 0].transpose(0, 1)[keep]) and (q_out[~keep] == 7.0).all()
+            cb.cb_page_write(x, cb.page_pool(pool), slots.cuda(), rope=rope, q=q_out, q_out=q_out)   # in place: once more
+            twice = torch.empty_like(q_ref)
+            cb.cb_rope_axes(q_ref, twice, rope)
+            assert same(q_out[keep], twice[0, 0, 0].transpose(0, 1)[keep]) and (q_out[~keep] == 7.0).all()

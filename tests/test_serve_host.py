@@ -396,3 +396,31 @@ def test_a_turned_cache_whose_rows_meet_is_refused(cb, kw):
     if "s_kv" not in kw and kw != dict(s_layer=8192):           # in place only keys are written, and those are apart
         assert refused_as_written(cb, turn(bad, bad), "out"), cb.cb_last_error()
     assert turn(dict(bad, n_seqs=0), dict(bad, n_seqs=0, data=8 * P)) == OK
+
+
+def test_the_launch_of_rows_covers_every_token_and_row(tmp_path):
+    """The rule that cuts a call on rows: every token in a wave, every row in a group, whole pairs of tokens, and the
+    exchange of halves only for long calls on 16-bit rows whose half is no whole number of lines."""
+    (tmp_path / "cut.cpp").write_text(
+        '#include "cb_paged_rules.h"\nextern "C" void cut(int64_t n, int rows, int d, int f8, int64_t *o) {\n'
+        '    cb::RowsCut c = cb::rows_cut(n, rows, d, f8);\n'
+        '    o[0] = c.tok_per_wave; o[1] = c.group; o[2] = c.blocks; o[3] = c.groups; o[4] = c.pairs; }\n')
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, str(tmp_path / "cut.cpp"), "-o",
+                    str(tmp_path / "cut.so")], check=True)
+    lib = ctypes.CDLL(str(tmp_path / "cut.so"))
+    lib.cut.argtypes = [ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p]
+    rng, out, seen = np.random.default_rng(2), (ctypes.c_int64 * 5)(), set()
+    for _ in range(3000):
+        d, f8 = 16 * int(rng.integers(1, 17)), int(rng.integers(2))
+        n, rows = int(np.exp(rng.uniform(0, 17))), int(np.exp(rng.uniform(0, 16)))
+        lib.cut(n, rows, d, f8, ctypes.addressof(out))
+        per_wave, group, blocks, groups, pairs = out
+        lanes = d // 16
+        assert per_wave % 2 == 0 and 2 <= per_wave and per_wave * lanes <= 64
+        assert (blocks - 1) * 4 * per_wave < n <= blocks * 4 * per_wave
+        assert (groups - 1) * group < rows <= groups * group and groups <= 65535
+        assert group <= 16 or groups * 2 > 65535
+        assert group == 1 or blocks * -(-rows // group) >= 2048 or -(-rows * 2 // group) > 65535
+        assert pairs == (not f8 and d % 128 != 0 and group >= 4)
+        seen.add((pairs, d))
+    assert {(1, 16 * k) for k in range(1, 17) if k % 8} <= seen
