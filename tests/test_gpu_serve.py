@@ -1035,3 +1035,37 @@ def test_rows_that_exchange_halves(cb, serve, rows_cut, d, L, H, B, T, token_maj
             twice = torch.empty_like(q_ref)
             cb.cb_rope_axes(q_ref, twice, rope)
             assert same(q_out[keep], twice[0, 0, 0].transpose(0, 1)[keep]) and (q_out[~keep] == 7.0).all()
+
+
+# ------------------------------------------------------------------ calls at once, captured steps
+
+def test_calls_on_two_streams_at_once(cb, serve):
+    """Divided rows and chunks on two streams, a workspace each, enqueued in turn without a wait between them: what one
+    leaves in a buffer the other could read, it would read here."""
+    steps = [Step(cb, [(1, 40000), (200, 6000), (1, 20000), (3, 50)], 2, 4, 128, 64, f8, seed=100 + f8, layers=1, layer=0)
+             for f8 in (False, True)]
+    st = [torch.cuda.Stream(), torch.cuda.Stream()]
+    want, args, ws, outs = [], [], [], []
+    for s in steps:
+        s.run()
+        check_tokens(serve, s, [(0, 0), (1, 0), (1, 199), (3, 2)], [1])
+        want.append((s.out.clone(), s.lse.clone()))
+        args.append((s.q, cb.page_pool(s.pool, s.scales), 0, i32(s.starts), i32([k for _, k in s.lens]), i32(s.table)))
+        need = cb.cb_attn_paged_workspace_bytes(s.n, len(s.lens), 8, 2, 128, s.max_q)
+        ws.append(torch.empty((need,), dtype=torch.uint8, device="cuda"))
+        outs.append([(torch.full_like(s.out, 5.0), torch.full_like(s.lse, 5.0)) for _ in range(20)])
+    first, last = ([torch.cuda.Event(enable_timing=True) for _ in st] for _ in range(2))
+    torch.cuda.synchronize()
+    for i in range(2):
+        first[i].record(st[i])
+    for rep in range(20):
+        for i in range(2):
+            o, l = outs[i][rep]
+            cb.cb_attn_paged(*args[i], o, steps[i].max_q, lse=l, workspace=ws[i], stream=st[i])
+    for i in range(2):
+        last[i].record(st[i])
+    torch.cuda.synchronize()
+    assert first[0].elapsed_time(last[1]) > 0 and first[1].elapsed_time(last[0]) > 0    # both were under way together
+    for i in range(2):
+        for o, l in outs[i]:
+            assert torch.equal(o, want[i][0]) and torch.equal(l, want[i][1])
