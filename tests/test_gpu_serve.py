@@ -1069,3 +1069,93 @@ def test_calls_on_two_streams_at_once(cb, serve):
     for i in range(2):
         for o, l in outs[i]:
             assert torch.equal(o, want[i][0]) and torch.equal(l, want[i][1])
+
+
+@pytest.mark.parametrize("max_q,G,window,sinks", [(3, 2, 0, 0), (40, 4, 0, 0), (40, 4, 3000, 40), (3, 2, 3000, 40), (40, 4, 700, 2)])
+def test_a_captured_step_of_long_requests(cb, serve, max_q, G, window, sinks):
+    """A step captured with a table of 12,000 keys and replayed with lengths that move requests between one part, several
+    and as many as a workgroup joins, between the kernels of short rows and of chunks, and out of the step.  Two graphs
+    with a workspace each take turns; every replay equals the eager call on its lengths and, in some tokens, the plain
+    form."""
+    H, d, ps, B, width, n = 2, 64, 16, 3, 750, 90
+    g = gen(110 + max_q)
+    P = B * width + 4
+    pool = torch.randn((1, 2, P, H, ps, d), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda").to(torch.bfloat16)
+    pages = cb.page_pool(pool)
+    rt = torch.empty((width * ps, d // 2, 2), dtype=torch.float32, device="cuda")
+    cb.cb_rope_table(THETA, d, width * ps, rt)
+    need = cb.cb_attn_paged_workspace_bytes(n, B, H * G, H, d, max_q)
+
+    def state():
+        z = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")
+        s = dict(ctx=i32([0] * B), q=i32([0] * B), free=i32([0] * 8), table=i32(np.full((B, width), -1)), q_starts=i32([0] * (B + 1)),
+                 kv=i32([0] * B), slots=i32([0] * n), pos=i32([0] * n), info=i32([0] * B), used=i32([0]), x=z(1, 2, 1, H, n, d),
+                 qin=z(n, H * G, d), qr=z(n, H * G, d), out=z(n, H * G, d),
+                 lse=torch.zeros((n, H * G), dtype=torch.float32, device="cuda"),
+                 ws=torch.empty((need,), dtype=torch.uint8, device="cuda"))
+        s["rope"] = cb.rope_axes_spec(rt, s["pos"])
+        return s
+
+    def step(s):
+        cb.cb_page_tables(s["ctx"], s["q"], s["free"], ps, s["table"], s["q_starts"], s["kv"], s["slots"], s["pos"], s["info"], s["used"])
+        cb.cb_page_write(s["x"], pages, s["slots"], rope=s["rope"], q=s["qin"], q_out=s["qr"])
+        cb.cb_attn_paged(s["qr"], pages, 0, s["q_starts"], s["kv"], s["table"], s["out"], max_q, window=window, sinks=sinks,
+                         lse=s["lse"], workspace=s["ws"])
+
+    graphs = []
+    for _ in range(2):
+        s = state()
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            step(s)
+        torch.cuda.current_stream().wait_stream(st)
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            step(s)
+        graphs.append((gr, s))
+    e = state()
+    # contexts and new tokens: short rows, one part, two, dozens (joined by a workgroup), a chunk of either, none
+    lengths = [([40, 300, 700], [1, 1, 1]), ([11900, 20, 0], [1, 2, 3]), ([1500, 11000, 9000], [3, 1, 2]),
+               ([9000, 30, 11500], [max_q, 1, 0]), ([100, 10000, 2000], [1, max_q, max_q]), ([0, 0, 0], [0, 0, 0]),
+               ([5000, 5000, 5000], [2, 1, 2]), ([11990, 3, 600], [1, max_q, 1])]
+    rng = np.random.default_rng(7)
+    for it, (ctx, q) in enumerate(lengths):
+        gr, s = graphs[it % 2]
+        x, qin = randn(g, 1, 2, 1, H, n, d).cuda(), randn(g, n, H * G, d).cuda()
+        perm = rng.permutation(P)
+        table, at = np.full((B, width), -1), 0
+        for b in range(B):
+            m = -(-ctx[b] // ps)
+            table[b, :m] = perm[at:at + m]
+            at += m
+        free = perm[at:at + 8]
+        assert len(free) == 8
+        for t in (s, e):
+            for k, v in (("ctx", ctx), ("q", q), ("free", free), ("table", table)):
+                t[k].copy_(i32(v))
+            t["x"].copy_(x); t["qin"].copy_(qin); t["out"].fill_(4.0); t["qr"].fill_(4.0); t["lse"].fill_(4.0)
+        torch.cuda.synchronize()
+        gr.replay()
+        torch.cuda.synchronize()
+        step(e)
+        torch.cuda.synchronize()
+        for k in ("q_starts", "kv", "slots", "pos", "info", "used", "table", "out", "qr", "lse"):
+            assert torch.equal(s[k], e[k]), (it, k)
+        total = sum(q)
+        assert s["info"].tolist() == [0] * B and (s["out"][total:] == 4.0).all() and (s["lse"][total:] == 4.0).all()
+        final, out, lse, qr = s["table"].cpu().numpy(), f64(s["out"]), f64(s["lse"]), f64(s["qr"])
+        start = 0
+        for b in range(B):
+            kv = ctx[b] + q[b]
+            ids = torch.tensor(final[b, :-(-kv // ps)].astype(np.int64), device="cuda")
+            for i in sorted({0, q[b] // 2, q[b] - 1} if q[b] else ()):
+                t, p, h = start + i, ctx[b] + i, (it + b) % H
+                rows = [f64(pool[0, z, ids, h].reshape(-1, d)[:p + 1]) for z in range(2)]
+                hs = slice(h * G, (h + 1) * G)
+                o, l, mag, smag = serve.attention(qr[t:t + 1, hs], *rows, p + 1, d ** -0.5, window, sinks)
+                es, few = (d + 8) * 2 * F32 * smag, (kv + 64) * 2 * F32
+                tol = BF * np.abs(o) * 1.01 + mag * (BF * 1.01 + (2 * es + few)[..., None])
+                assert (np.abs(out[t:t + 1, hs] - o) <= tol).all(), (it, b, i)
+                assert (np.abs(lse[t:t + 1, hs] - l) <= es + few + 8 * F32 * (np.abs(l) + 1)).all(), (it, b, i)
+            start += q[b]
