@@ -779,7 +779,12 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
                         const cb_rows *out, int32_t max_q_len, float scale, int32_t window, int32_t n_sinks, float *lse,
                         void *workspace, int64_t workspace_bytes, void *stream);
 
-/* Workspace bytes with which cb_attn_paged splits rows as far as it wants to (on any device). */
+/*
+ * Workspace bytes with which cb_attn_paged splits rows as far as it wants to (on
+ * any device), whatever the lengths: room for the parts of 2,048 workgroups of
+ * short rows, of 512 of chunks, or of both where a call of chunks has several
+ * requests.  Short conversations, whose rows are never split, need none (NULL).
+ */
 int64_t cb_attn_paged_workspace_bytes(int32_t n_tokens, int32_t n_reqs, int32_t n_qheads, int32_t n_heads,
                                       int32_t head_dim, int32_t max_q_len);
 

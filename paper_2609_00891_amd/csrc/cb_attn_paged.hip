@@ -1162,10 +1162,14 @@ bool prepare_class(const PagedArgs &a, PagedClass &c, int target, int64_t row_mi
     return true;
 }
 
+// Rows up to which a request goes to rows_body in a launch of tile_body: none where no other request could be
+// beside it, or where one token has more.
+int32_t least_rows(int32_t G, int32_t n_reqs) { return G <= kSmallRows && n_reqs > 1 ? kSmallRows : 0; }
+
 template <int D, bool F8, int NW>
 hipError_t launch_tiles(PagedArgs a, char *w, int64_t ws_bytes, hipStream_t s) {
     constexpr int M = 32 * NW;
-    const int64_t least = a.G.d <= kSmallRows && a.n_reqs > 1 ? kSmallRows : 0;
+    const int64_t least = least_rows((int32_t)a.G.d, a.n_reqs);
     if (least > 0 && !prepare_class<D, 16, kKT>(a, a.rows, kTarget, 0, least, w, ws_bytes)) return hipErrorInvalidValue;
     if (!prepare_class<D, M, kTileKT>(a, a.tile, kTileTarget * 4 / NW, least, INT64_MAX, w, ws_bytes)) return hipErrorInvalidValue;
     hipLaunchKernelGGL((attn_tile_kernel<D, F8, NW>), dim3(a.tile.blocks + a.rows.blocks), dim3(64 * NW), 0, s, a);
@@ -1200,9 +1204,10 @@ hipError_t launch(PagedArgs a, int32_t max_q_len, void *ws, int64_t ws_bytes, hi
 
 }  // namespace
 
-int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t max_q_len) {
+int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_reqs, int32_t max_q_len) {
     const int64_t rows = (int64_t)2 * kTarget * 16 * (d + 2) * 4, tile = (int64_t)2 * kTileTarget * 128 * (d + 2) * 4;
-    return (int64_t)max_q_len * G <= kFewRows ? rows : rows + tile;
+    if ((int64_t)max_q_len * G <= kFewRows) return rows;
+    return (least_rows(G, n_reqs) > 0 ? rows : 0) + tile;
 }
 
 hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, bool f8, int32_t max_q_len, void *ws, int64_t ws_bytes,

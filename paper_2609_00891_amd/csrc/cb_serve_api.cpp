@@ -264,7 +264,7 @@ int64_t cb_attn_paged_workspace_bytes(int32_t n_tokens, int32_t n_reqs, int32_t 
                                       int32_t head_dim, int32_t max_q_len) {
     if (n_tokens <= 0 || n_reqs <= 0 || n_heads <= 0 || n_qheads <= 0 || n_qheads % n_heads || head_dim <= 0 || max_q_len <= 0)
         return 0;
-    return cb::attn_paged_workspace_bytes(head_dim, n_qheads / n_heads, max_q_len);
+    return cb::attn_paged_workspace_bytes(head_dim, n_qheads / n_heads, n_reqs, max_q_len);
 }
 
 cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,

@@ -93,6 +93,6 @@ hipError_t launch_page_tables(const PageTablesArgs &a, hipStream_t s);
 hipError_t launch_rows(RowsArgs a, bool rope, bool f8, hipStream_t s);
 hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, bool f8, int32_t max_q_len, void *ws, int64_t ws_bytes,
                              hipStream_t s);
-int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t max_q_len);
+int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_reqs, int32_t max_q_len);
 
 }  // namespace cb

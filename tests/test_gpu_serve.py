@@ -1159,3 +1159,15 @@ def test_a_captured_step_of_long_requests(cb, serve, max_q, G, window, sinks):
                 assert (np.abs(out[t:t + 1, hs] - o) <= tol).all(), (it, b, i)
                 assert (np.abs(lse[t:t + 1, hs] - l) <= es + few + 8 * F32 * (np.abs(l) + 1)).all(), (it, b, i)
             start += q[b]
+
+
+def test_more_workspace_than_the_call_asks_for_changes_nothing(cb, serve):
+    """One chunk, and heads with more queries than a short row tile: the bits of a workspace of twice the size."""
+    for lens, H, G, d in (([(70, 9000)], 2, 2, 64), ([(1, 9000), (3, 5000)], 1, 40, 64), ([(1, 20000)], 1, 4, 96)):
+        s = Step(cb, lens, H, G, d, 16, seed=120, layers=1, layer=0)
+        need = cb.cb_attn_paged_workspace_bytes(s.n, len(lens), H * G, H, d, s.max_q)
+        s.run(ws=need)
+        a, l = s.out.clone(), s.lse.clone()
+        check_tokens(serve, s, [(0, 0)], [H - 1])
+        s.run(ws=2 * need)
+        assert torch.equal(a, s.out) and torch.equal(l, s.lse)

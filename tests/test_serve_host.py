@@ -424,3 +424,17 @@ def test_the_launch_of_rows_covers_every_token_and_row(tmp_path):
         assert pairs == (not f8 and d % 128 != 0 and group >= 4)
         seen.add((pairs, d))
     assert {(1, 16 * k) for k in range(1, 17) if k % 8} <= seen
+
+
+def test_workspace_holds_what_the_call_can_use(cb):
+    """Partial results of 16 rows (short rows: 4,096 slots) and of 128 (chunks: 1,024), both only in calls that can have
+    both: chunks in one request, or heads with more queries than a short row tile, have no short rows beside them."""
+    for d in (64, 96, 128):
+        short, chunk = 4096 * 16 * (d + 2) * 4, 1024 * 128 * (d + 2) * 4
+        for n_reqs, qheads, heads, max_q, want in ((5, 16, 2, 1, short), (1, 16, 2, 4, short), (1, 64, 2, 1, short),
+                                                   (5, 16, 2, 5, short + chunk), (1, 16, 2, 5, chunk), (1, 16, 1, 3, chunk),
+                                                   (9, 16, 1, 3, short + chunk), (9, 34, 2, 2, chunk), (9, 40, 1, 1, chunk)):
+            got = cb.cb_attn_paged_workspace_bytes(100, n_reqs, qheads, heads, d, max_q)
+            assert got == want, (n_reqs, qheads, heads, max_q)
+    for bad in ((0, 1, 8, 8, 64, 1), (1, 0, 8, 8, 64, 1), (1, 1, 8, 3, 64, 1), (1, 1, 8, 8, 64, 0)):
+        assert cb.cb_attn_paged_workspace_bytes(*bad) == 0
