@@ -851,6 +851,7 @@ def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer
 def cb_attn_paged_workspace_bytes(n_tokens: int, n_reqs: int, n_qheads: int, n_heads: int, head_dim: int,
                                   max_q_len: int) -> int:
     """Workspace bytes with which :func:`cb_attn_paged` splits long rows as far as it wants to."""
+    _fit_int32(n_tokens, n_reqs, n_qheads, n_heads, head_dim, max_q_len)
     return int(_lib.cb_attn_paged_workspace_bytes(int(n_tokens), int(n_reqs), int(n_qheads), int(n_heads), int(head_dim),
                                                   int(max_q_len)))
 

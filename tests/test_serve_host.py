@@ -438,3 +438,11 @@ def test_workspace_holds_what_the_call_can_use(cb):
             assert got == want, (n_reqs, qheads, heads, max_q)
     for bad in ((0, 1, 8, 8, 64, 1), (1, 0, 8, 8, 64, 1), (1, 1, 8, 3, 64, 1), (1, 1, 8, 8, 64, 0)):
         assert cb.cb_attn_paged_workspace_bytes(*bad) == 0
+
+
+def test_workspace_sizes_do_not_wrap(cb):
+    good = [100, 5, 16, 2, 64, 40]
+    assert cb.cb_attn_paged_workspace_bytes(*good) > 0
+    for i in range(6):
+        with pytest.raises(ValueError, match="32-bit"):
+            cb.cb_attn_paged_workspace_bytes(*(v + (2 ** 32 if i == j else 0) for j, v in enumerate(good)))
