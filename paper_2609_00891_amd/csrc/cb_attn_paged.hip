@@ -9,10 +9,13 @@
 // group's query heads share every K and V row read.  The weights exp(s_j - m)
 // are rounded to bf16 as the matrix cores' operand (2^-8 of a weight, below the
 // output's own rounding where the values do not cancel) and summed unrounded;
-// scores, sums and outputs are fp32.  m is the running maximum itself, so the
-// largest weight is 1, which no rounding touches: with a maximum that may lag by
-// 2^8, which spares rescaling, a 2,048-token chunk took 1.3% less and its outputs
-// were off by 0.22% instead of 0.18% (0.17% is their own rounding).
+// scores, sums and outputs are fp32.  Against 64 bits the outputs are off by 0.17%
+// (decode) to 0.19% (a 2,048-token chunk) in norm, 0.166% of it their own rounding:
+// weights in full would need a second product with V for what bf16 leaves out, half
+// of the matrix work again.  m is the running maximum itself, so the largest weight
+// is 1 (tile_body: to half an ulp of m), which the rounding hardly touches: with a
+// maximum that may lag by 2^8, which spares rescaling, a chunk took 1.3% less and
+// its outputs were off by 0.22%.
 //
 // rows_body: requests of few rows, 16 of them a workgroup.  Each wave has its
 //   own key tiles of 32 keys, from memory straight into matrix-core operands:
@@ -42,15 +45,16 @@
 //   While a tile is worked on the next is on its way, and the table entries of
 //   the one after are on theirs.  bf16 rows of 64 or 128 channels go to LDS by
 //   its own loads (2.14 -> 2.07 ms below, and 370 -> 312 us for 8 new tokens of
-//   64 requests over 512 .. 16,384 keys), others through registers (e4m3 becomes
-//   bf16 on the way; 96 channels are no whole number of pieces a thread).  A
-//   tile's products with V run beside the weights of its next 16 keys.
+//   64 requests over 512 .. 16,384 keys), others through registers: e4m3 becomes
+//   bf16 on the way, and rows of 96 channels get their padding there.  A tile's
+//   products with V run beside the weights of its next 16 keys.
 //   Bound by the board's power: 2,048 tokens x 64 query heads over 32,768 keys
 //   in 8 heads of 128 take 2.01 .. 2.20 ms from board to board, 0.97 .. 1.06
-//   PFLOP/s (a bf16 matrix product of 8192^3: 1.21), at 1.32 kW and 2.01 GHz of
-//   2.4 with the matrix units busy in 49% of the cycles; four sums and maxima
-//   instead of one, other orders of the products and wave priorities change
-//   nothing.
+//   PFLOP/s (a bf16 matrix product of 8192^3: 1.21 .. 1.45), e4m3 1.99; heads of 96
+//   1.82 ms, of 64 1.42 (the weights' work is the same, the products are half).  At
+//   128 channels 1.32 kW and 2.01 GHz of 2.4 with the matrix units busy in 47 - 49% of
+//   the cycles; four sums and maxima instead of one, other orders of the products
+//   and wave priorities change nothing.
 //   No LDS bank meets twice (with V's rows 288 bytes apart a quarter of the LDS
 //   cycles were conflicts).
 //
@@ -76,10 +80,15 @@ constexpr int kKT = 32;                 // keys of a tile
 constexpr int kTileKT = 64;             // keys of a tile of the tile kernel
 // Key tiles from which a row tile may be divided and the least of a part, for rows_body (1,152 and 512
 // keys) and tile_body (1,536 and 512): what dividing saves must be worth the joining, a launch of about
-// 8 us, and every part costs it something.  24 single tokens and three chunks with windows of 1,024 keys,
-// undivided: 49 us; with parts of 256 keys and more: 61 us.  One single token (8 heads of 128) over 8,192
-// and 131,072 keys: 18.5 and 113 us; with parts of at least 256 keys 18.0 and 113, of 768 21.3 and 111;
-// over 131,072 keys of one head: 26.5, 33.9 and 25.4.
+// 3 us where nothing is divided and 8 us where rows are, and every part costs it something.  24 single tokens
+// and three chunks with windows of 1,024 keys, undivided: 49 us; with parts of 256 keys and more: 61 us.
+// Single tokens (8 heads of 128, 8 query heads each) with windows of 1,056, 1,500 and 4,000 keys, divided
+// and not: one 18.9 / 16.4, 17.5 / 21.3 and 16.4 / 43.5 us, 8 of them 23.7 / 19.0, 20.7 / 24.7 and 34.3 /
+// 51.2.  Where the rows fill the chip undivided and are alike, dividing them only costs: 24 of them 27.0 /
+// 21.6, 41.6 / 27.9 and 84.4 / 74.9, 64 of them 56.4 / 45.9, 91.0 / 71.4 and 200.6 / 180.2 (such a caller
+// passes no workspace).  One single token (8 heads of 128) over 8,192 and 131,072 keys: 18.5 and 113 us;
+// with parts of at least 256 keys 18.0 and 113, of 768 21.3 and 111; over 131,072 keys of one head: 26.5,
+// 33.9 and 25.4.
 constexpr int part_min(int KT) { return KT == kKT ? 16 : 8; }
 constexpr int split_min(int KT) { return KT == kKT ? 36 : 24; }
 // Parts above which a row is joined by a workgroup instead of a wave: one single token over 131,072 keys
@@ -1103,9 +1112,10 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
 }
 
 // The requests with few rows and the others in one launch, runs of the two in turn, so that a compute
-// unit has products of the one beside loads of the other; a tile, which takes longer, first.  64 single
-// tokens over 1,024 .. 8,192 keys beside a chunk of 512 (8 heads of 128, 8 query heads each): 252 us, 272
-// with all tiles first, 272 with runs of 8; 24 beside three chunks of 515 with windows of 1,024: 53, 54, 72.
+// unit has products of the one beside loads of the other; a tile, which takes longer, first.  With fewer
+// than a run of either kind all tiles come first.  64 single tokens over 1,024 .. 8,192 keys beside a chunk
+// of 512 (8 heads of 128, 8 query heads each): 252 us, 272 with all tiles first, 272 with runs of 8; 24
+// beside three chunks of 515 with windows of 1,024, which have no whole run: 53, 72 with runs of 8.
 template <int D, bool F8, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(PagedArgs a) {
     __shared__ SchedLds<NW> sched;
@@ -1134,8 +1144,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedArgs a) {
 }
 
 constexpr int kSmallRows = 16;          // rows of a request up to which rows_body takes it beside tile_body
-// ... and alone, when no request is said to have more: 64 requests of 2 tokens x 8 query heads take it
-// 235 us, 4 x 8 tile_body 282.
+// ... and alone, when no request is said to have more.  64 requests over 512 .. 16,384 keys (8 heads of 128),
+// rows_body and tile_body: 16 rows each 228 and 231 us, 24 rows 276 and 298, 32 rows 281 and 300, 40 rows
+// 349 and 305, 64 rows 451 and 313; the same with 4 query heads a KV head as with 8.
 constexpr int kFewRows = 32;
 constexpr int kTileTarget = 512;        // workgroups of tile_body (of 128 rows) that long rows are divided into
 constexpr int kJoinBlocks = 2048;
