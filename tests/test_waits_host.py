@@ -32,32 +32,51 @@ def scalar_regs(text):
     return out
 
 
-def missing_waits(asm):
-    """(instructions that read M0, vector memory instructions and those too close behind a write of what they read) of an
-    assembly."""
-    readers, bad, since_m0, written = 0, [], 99, {}            # written: states since a vector write of a scalar register
-    for line in asm.split("\n"):
+def missing_waits(body):
+    """(instructions that read M0, those and vector memory instructions too close behind a write of what they read, on any
+    path) of one kernel's assembly."""
+    ins, labels = [], {}
+    for line in body.split("\n"):
         s = line.split(";")[0].strip()
-        if not s or s[0] in ".#" or s.endswith(":"):
+        label = re.match(r"^(\.LBB\S+):", s)
+        if label:
+            labels[label.group(1)] = len(ins)
+        elif s and s[0] not in ".#" and not s.endswith(":"):
+            ins.append(s)
+    # before each instruction: states since M0 was written, and since a vector instruction wrote a scalar register
+    state, work, bad = {0: (99, {})}, [0], set()
+    while work:
+        i = work.pop()
+        if i >= len(ins):
             continue
+        s, (since_m0, written) = ins[i], state[i]
         op, _, operands = s.partition(" ")
-        if READS_M0.match(s):
-            readers += 1
-            if since_m0 < 1:
-                bad.append(s)
+        if READS_M0.match(s) and since_m0 < 1:
+            bad.add(i)
         if VECTOR_MEMORY.match(s) and any(written.get(r, 99) < 5 for r in scalar_regs(operands)):
-            bad.append(s)
+            bad.add(i)
         states = 1 + int(operands) if op == "s_nop" else 1
-        since_m0 += states
+        since_m0 = min(99, since_m0 + states)
         written = {r: n + states for r, n in written.items() if n + states < 5}
         dst = operands.split(",")[:2 if SCALAR_SECOND.match(op) else 1]
-        if op.startswith("s_"):
-            if re.match(r"m0\b", operands.strip()) and not op.startswith("s_cmp"):
+        if op.startswith("s_") and not re.match(r"s_(bit)?cmp", op):
+            if re.match(r"m0\b", operands.strip()):
                 since_m0 = 0
             written = {r: n for r, n in written.items() if r not in scalar_regs(dst[0])}
         elif op.startswith("v_"):
             written.update({r: 0 for d in dst for r in scalar_regs(d)})
-    return readers, bad
+        branch = re.match(r"^s_(c?branch\S*)\s+(\.LBB\S+)", s)
+        if branch:
+            nxt = [labels[branch.group(2)]] + ([i + 1] if branch.group(1).startswith("cbranch") else [])
+        else:
+            nxt = [] if op == "s_endpgm" else [i + 1]
+        for t in nxt:
+            old = state.get(t, (99, {}))
+            new = (min(old[0], since_m0), {r: min(old[1].get(r, 99), written.get(r, 99)) for r in {*old[1], *written}})
+            if t not in state or new != old:
+                state[t] = new
+                work.append(t)
+    return sum(READS_M0.match(s) is not None for s in ins), [ins[i] for i in sorted(bad)]
 
 
 def test_analysis_counts_wait_states():
@@ -70,7 +89,12 @@ def test_analysis_counts_wait_states():
                          (["\tv_readfirstlane_b32 s5, v9", "\ts_mov_b32 m0, s3", "\ts_nop 3", load], 0),
                          (["\tv_readfirstlane_b32 s3, v9", "\ts_mov_b32 m0, s3", "\ts_nop 0", load], 0),
                          (["\tv_cmp_lt_u32_e64 s[4:5], v1, v2", "\ts_mov_b64 s[4:5], s[8:9]", load], 0),
-                         (["\tv_cmp_lt_u32_e64 s[4:5], v1, v2", load], 1)):
+                         (["\tv_cmp_lt_u32_e64 s[4:5], v1, v2", load], 1),
+                         (["\tv_readlane_b32 s4, v1, 3", "\ts_cmp_lg_u32 s4, 0", load], 1),
+                         (["\tv_readlane_b32 s4, v1, 3", "\ts_cbranch_scc1 .LBB0_2", "\ts_nop 7", ".LBB0_2:", load], 1),
+                         (["\ts_nop 0", ".LBB0_2:", load, "\ts_mov_b32 m0, s3", "\ts_cbranch_scc1 .LBB0_2"], 0),
+                         ([".LBB0_2:", load, "\ts_cbranch_scc0 .LBB0_3", "\tv_readlane_b32 s5, v1, 3", "\ts_branch .LBB0_2",
+                           ".LBB0_3:", "\ts_endpgm"], 1)):
         readers, bad = missing_waits("\n".join(lines))
         assert readers == 1 and len(bad) == wrong, lines
 
@@ -120,8 +144,12 @@ def test_every_source_with_such_loads_is_looked_at():
 
 @pytest.mark.parametrize("name", SOURCES)
 def test_loads_to_lds_wait_for_what_they_read(assemblies, name):
-    readers, bad = missing_waits(assemblies[name])
-    assert readers > 0 and not bad, (len(bad), bad[:3])
+    readers = 0
+    for kernel, body in re.findall(r"(?ms)^(_Z\S+):.*?\n(.*?)^\.Lfunc_end", assemblies[name]):
+        n, bad = missing_waits(body)
+        readers += n
+        assert not bad, (kernel, len(bad), bad[:3])
+    assert readers > 0
 
 
 @pytest.mark.parametrize("name", SOURCES)
