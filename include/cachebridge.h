@@ -633,6 +633,7 @@ cb_status cb_plan_feature_width(const cb_plan *plan, int32_t *P, int32_t *k);
 /* Element types of a pool. */
 #define CB_PAGES_BF16 0   /* bfloat16 */
 #define CB_PAGES_E4M3 1   /* 8-bit floats (4 exponent, 3 mantissa bits, largest 448, no infinities), with scales */
+#define CB_PAGES_E4M3_BLOCKS 2 /* the same 8-bit floats with a scale for every page and head, found as they are written */
 
 /*
  * A pool of pages, [layer][kv][page][head][tok][ch]: a cb_cache whose n_seqs
@@ -641,12 +642,16 @@ cb_status cb_plan_feature_width(const cb_plan *plan, int32_t *P, int32_t *k);
  * whose pages are its sequences.  E4M3: data holds bytes, strides count
  * elements, every row 16-byte aligned (multiples of 16 elements), and a stored
  * element e stands for e * scales[(layer * 2 + kv) * n_heads + head]
- * (fp32, device, positive and finite; NULL for CB_PAGES_BF16).  pages *
- * page_size < 2^31, and the pages of one (layer, kv) span less than 64 GiB.
+ * (fp32, device, positive and finite; NULL for CB_PAGES_BF16).  E4M3_BLOCKS:
+ * laid out as E4M3, but scales[((layer * pages + page) * n_heads + head) * 2 + kv],
+ * each a power of two from 2^-64 to 2^120 (of another number only the exponent
+ * counts); cb_page_quantize writes rows and scales, although the calls that only
+ * read take them as const.  pages * page_size < 2^31, and the pages of one (layer,
+ * kv) span less than 64 GiB.
  */
 typedef struct {
     cb_cache cache;
-    int32_t dtype;              /* CB_PAGES_BF16 or CB_PAGES_E4M3 */
+    int32_t dtype;              /* CB_PAGES_BF16, CB_PAGES_E4M3 or CB_PAGES_E4M3_BLOCKS */
     const float *scales;
 } cb_pages;
 
@@ -735,10 +740,57 @@ cb_status cb_rope_axes(const cb_cache *in, const cb_cache *out, const cb_rope_ax
  * tokens must not name one slot; rows, q and the pool must not overlap, nor the
  * pool's rows one another (its strides nest, or CB_ERR_SHAPE; a pool that is
  * only read may have any).
- * head_dim a multiple of 16 up to 256.
+ * head_dim a multiple of 16 up to 256.  CB_PAGES_E4M3_BLOCKS pools are written by
+ * cb_page_quantize.
  */
 cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t layer0, const int32_t *slots,
                         const cb_rope_axes_spec *rope, const cb_rows *q, const cb_rows *q_out, void *stream);
+
+/*
+ * Write rows into 8-bit pages and find the pages' scales (CB_PAGES_E4M3_BLOCKS).
+ * Request r's last q_lens[r] of its kv_lens[r] tokens are tokens row_starts[r],
+ * row_starts[r] + 1, ... of `rows` (numbered seq * seq_len + tok: the packed new
+ * tokens of one layer, with q_starts as row_starts, or a padded batch of mapped
+ * caches with seq_len * r), all its layers, into the pool's layers layer0,
+ * layer0 + 1, ...  Token position pos goes to page block_table[r * table_stride +
+ * pos / page_size], place pos % page_size.  For every page that gets rows, and every layer, head
+ * and K or V, M the largest finite magnitude of these rows as they are in `rows`:
+ *   2^e, e >= -64 least with M <= 448 2^e (keys that rope turns: 316 2^e, since a
+ *     turn can make a channel larger by sqrt 2), is the scale of a page whose first
+ *     place is among them; a page that holds earlier tokens of the request keeps
+ *     the larger of this and its own scale, and where it grows its earlier places
+ *     are rounded (nearest even) to the larger scale,
+ *   a row is stored as its bf16 value, K rows turned by rope in fp32, over the scale,
+ *     rounded once to e4m3, nearest even; infinities become NaN, NaN stays.
+ * Places behind a request's tokens stay as they were and stand for nothing.  A
+ * request with q_lens <= 0, kv_lens < q_lens or above table_width * page_size, or rows outside
+ * `rows`, takes no part (so with cb_page_tables' kv_lens, which are 0 for requests
+ * that it left out); tokens whose page is outside the pool are skipped, their queries too.
+ * rope, q and q_out as in cb_page_write (positions by token of `rows`).  No two requests may
+ * write one page.  Rows may serve several requests (a prompt that several go on from); q
+ * must then not be turned in place.  rows, q and the pool must not overlap, nor
+ * the pool's rows one another.  The same call gives the same bits again.  head_dim a multiple of 16
+ * up to 256, page_size <= 2^24.
+ */
+cb_status cb_page_quantize(const cb_cache *rows, const cb_pages *pages, int32_t layer0, int32_t n_reqs,
+                           const int32_t *row_starts, const int32_t *q_lens, const int32_t *kv_lens,
+                           const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                           const cb_rope_axes_spec *rope, const cb_rows *q, const cb_rows *q_out, void *stream);
+
+/*
+ * Read pages back into rows: the tokens that cb_page_quantize's arguments name,
+ * from a pool of any type into `rows` (bfloat16, n_layers of it from the pool's
+ * layer0 on), each element the number it stands for, formed in fp32 and rounded once.  rope, if not
+ * NULL, turns the K rows (inverse: turns them back, as a sender's keys are before
+ * cb_apply maps them) in fp32 before that rounding.  With q_lens = kv_lens whole requests are read.  Requests
+ * that take no part and tokens whose page is outside the pool leave their rows as
+ * they were, so do tokens of no request.  No two requests may have one row; rows
+ * and the pool must not overlap.  Widths, page_size and refusals as in cb_page_quantize.
+ */
+cb_status cb_page_read(const cb_pages *pages, int32_t layer0, const cb_cache *rows, int32_t n_reqs,
+                       const int32_t *row_starts, const int32_t *q_lens, const int32_t *kv_lens,
+                       const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                       const cb_rope_axes_spec *rope, int32_t inverse, void *stream);
 
 /*
  * Attention of every request's new tokens over its pages in one layer.  Row

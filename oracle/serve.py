@@ -87,3 +87,65 @@ def attention(q, K, V, kv_len, scale, window=0, sinks=0, hidden=()):
             mag[i, g] = w @ np.abs(v)
             smag[i, g] = (abs(scale) * (np.abs(k) @ np.abs(q[i, g]))).max()
     return out, lse, mag, smag
+
+
+# ------------------------------------------------------------------ pages whose scales belong to a page
+
+E_MIN = -64                          # exponent of the smallest scale
+
+
+def e4m3(x):
+    """x rounded to the nearest e4m3 number (ties to even); beyond the largest, and infinities: NaN."""
+    x = np.asarray(x, dtype=np.float64)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        e = np.where(x != 0, np.floor(np.log2(np.abs(np.where(x != 0, x, 1.0)))), -6)
+    step = 2.0 ** (np.clip(np.nan_to_num(e, nan=0.0, posinf=0.0), -6, 8) - 3)
+    y = np.round(x / step) * step
+    return np.where(np.abs(y) <= 448, y, np.nan)
+
+
+def block_exponent(rows, turned):
+    """The exponent of a block's scale from its rows (any shape)."""
+    a = np.abs(rows[np.isfinite(rows)])
+    m = float(a.max()) if a.size else 0.0
+    e = E_MIN
+    while m > (316.0 if turned else 448.0) * 2.0 ** e:
+        e += 1
+    return e
+
+
+def page_spans(row_starts, q_lens, kv_lens, page_size, n_rows, width):
+    """(request, entry, first place, tokens, first row) of every page that a request's last q tokens lie in."""
+    out = []
+    for r, (b, q, kv) in enumerate(zip(map(int, row_starts), map(int, q_lens), map(int, kv_lens))):
+        if q <= 0 or kv < q or kv > width * page_size or b < 0 or b + q > n_rows:
+            continue
+        pos = kv - q
+        while pos < kv:
+            n = min(kv - pos, page_size - pos % page_size)
+            out.append((r, pos // page_size, pos % page_size, n, b + pos - (kv - q)))
+            pos += n
+    return out
+
+
+def page_quantize(rows, turned, codes, exps, spans, block_table):
+    """rows, turned [row][layer][2][head][d] as they come and turned (K) float64; codes [layer][2][page][head][place][d]
+    and exps [layer][page][head][2] are updated, the new rows' codes before they are rounded.  turned None: nothing is
+    turned."""
+    y = rows if turned is None else turned
+    _, L, _, H, _ = rows.shape
+    for r, entry, at, n, t in spans:
+        page = int(block_table[r][entry])
+        if not 0 <= page < codes.shape[2]:
+            continue
+        for l in range(L):
+            for z in range(2):
+                for h in range(H):
+                    e = block_exponent(rows[t:t + n, l, z, h], turned is not None and z == 0)
+                    was = int(exps[l, page, h, z])
+                    if at > 0 and was >= e:
+                        e = was
+                    elif at > 0:
+                        codes[l, z, page, h, :at] = e4m3(codes[l, z, page, h, :at] * 2.0 ** (was - e))
+                    codes[l, z, page, h, at:at + n] = y[t:t + n, l, z, h] * 2.0 ** -e
+                    exps[l, page, h, z] = e

@@ -663,6 +663,7 @@ def cb_stats_accumulate_rope(plan: Plan, src: torch.Tensor, tgt: torch.Tensor, w
 
 CB_PAGES_BF16 = 0
 CB_PAGES_E4M3 = 1
+CB_PAGES_E4M3_BLOCKS = 2
 
 
 class CbPages(ctypes.Structure):
@@ -688,6 +689,13 @@ _lib.cb_rope_axes.argtypes = [ctypes.POINTER(CbCache), ctypes.POINTER(CbCache), 
 _lib.cb_page_write.restype = ctypes.c_int
 _lib.cb_page_write.argtypes = [ctypes.POINTER(CbCache), ctypes.POINTER(CbPages), _i32, _vp, ctypes.POINTER(CbRopeAxesSpec),
                                ctypes.POINTER(CbRows), ctypes.POINTER(CbRows), _vp]
+_SPANS = [_i32, _vp, _vp, _vp, _vp, _i64, _i32]          # n_reqs, row_starts, q_lens, kv_lens, block_table, stride, width
+_lib.cb_page_quantize.restype = ctypes.c_int
+_lib.cb_page_quantize.argtypes = [ctypes.POINTER(CbCache), ctypes.POINTER(CbPages), _i32] + _SPANS + [
+    ctypes.POINTER(CbRopeAxesSpec), ctypes.POINTER(CbRows), ctypes.POINTER(CbRows), _vp]
+_lib.cb_page_read.restype = ctypes.c_int
+_lib.cb_page_read.argtypes = [ctypes.POINTER(CbPages), _i32, ctypes.POINTER(CbCache)] + _SPANS + [
+    ctypes.POINTER(CbRopeAxesSpec), _i32, _vp]
 _lib.cb_attn_paged.restype = ctypes.c_int
 _lib.cb_attn_paged.argtypes = [ctypes.POINTER(CbRows), ctypes.POINTER(CbPages), _i32, _i32, _vp, _vp, _vp, _i64, _i32,
                                ctypes.POINTER(CbRows), _i32, ctypes.c_float, _i32, _i32, _vp, _vp, _i64, _vp]
@@ -726,8 +734,9 @@ def _stream_on(device: int, stream) -> int:
 
 def page_pool(t: torch.Tensor, scales: Optional[torch.Tensor] = None) -> CbPages:
     """Describe a pool of pages: a [layer][2][page][head][token][dim] tensor (any strides, unit dim stride) of
-    bfloat16, or of float8_e4m3fn with its float32 ``scales`` [layer][2][head].  A contiguous cache is a pool whose
-    pages are its sequences."""
+    bfloat16, or of float8_e4m3fn with its float32 ``scales``: [layer][2][head], or [layer][page][head][2], powers of
+    two, for pages whose scales are found as they are written (:func:`cb_page_quantize`).  A contiguous cache is a pool
+    whose pages are its sequences."""
     p = CbPages()
     if t.dtype == torch.bfloat16:
         if scales is not None:
@@ -736,12 +745,13 @@ def page_pool(t: torch.Tensor, scales: Optional[torch.Tensor] = None) -> CbPages
     elif t.dtype == torch.float8_e4m3fn:
         if t.dim() != 6 or t.shape[1] != 2 or (t.shape[5] > 1 and t.stride(5) != 1):
             raise ValueError("8-bit pages are float8_e4m3fn [layer][2][page][head][token][dim] with unit dim stride")
-        _need(scales, (t.shape[0], 2, t.shape[3]), torch.float32, "scales")
+        blocks = scales is not None and scales.dim() == 4
+        _need(scales, (t.shape[0], t.shape[2], t.shape[3], 2) if blocks else (t.shape[0], 2, t.shape[3]), torch.float32, "scales")
         c = p.cache
         c.data = t.data_ptr()
         c.n_layers, _, c.n_seqs, c.n_heads, c.seq_len, c.head_dim = t.shape
         c.s_layer, c.s_kv, c.s_seq, c.s_head, c.s_tok = (t.stride(i) for i in range(5))
-        p.dtype, p.scales = CB_PAGES_E4M3, scales.data_ptr()
+        p.dtype, p.scales = CB_PAGES_E4M3_BLOCKS if blocks else CB_PAGES_E4M3, scales.data_ptr()
     else:
         raise ValueError("pages are bfloat16 or float8_e4m3fn")
     p._keep = (t, scales)
@@ -846,6 +856,51 @@ def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer
     _check(_lib.cb_page_write(ctypes.byref(rv), ctypes.byref(pages), int(layer), _ptr(slots),
                               None if rope is None else ctypes.byref(rope), None if qv is None else ctypes.byref(qv),
                               None if ov is None else ctypes.byref(ov), _stream_on(dev, stream)))
+
+
+def _spans(row_starts: Optional[torch.Tensor], q_lens: torch.Tensor, kv_lens: torch.Tensor, block_table: torch.Tensor):
+    """The requests' arguments of the calls that find their tokens by lengths, as the C ABI takes them."""
+    n = kv_lens.numel()
+    for t, name in ((row_starts, "row_starts"), (q_lens, "q_lens"), (kv_lens, "kv_lens")):
+        if t is not None:
+            _ints(t, n, name)
+    _check_table(block_table, n)
+    return n, _ptr(row_starts), _ptr(q_lens), _ptr(kv_lens), _ptr(block_table), block_table.stride(0), block_table.shape[1]
+
+
+def cb_page_quantize(rows: torch.Tensor, pages: CbPages, row_starts: torch.Tensor, q_lens: torch.Tensor,
+                     kv_lens: torch.Tensor, block_table: torch.Tensor, layer: int = 0,
+                     rope: Optional[CbRopeAxesSpec] = None, q: Optional[torch.Tensor] = None,
+                     q_out: Optional[torch.Tensor] = None, stream=None):
+    """Write the K and V rows of a cache tensor into the 8-bit pages of the pool's layers ``layer`` ... and find the
+    scale of every page, head and K or V.  Request r's last ``q_lens[r]`` of ``kv_lens[r]`` tokens are tokens
+    ``row_starts[r]`` ... of rows; ``rope``, ``q`` and ``q_out`` as in :func:`cb_page_write`.  All int32 on the device."""
+    rv = cache_view(rows)
+    spans = _spans(row_starts, q_lens, kv_lens, block_table)
+    _fit_int32(layer)
+    _check_axes_tokens(rope, rows.shape[2] * rows.shape[4])
+    qv = None if q is None else _rows_view(q, "q")
+    ov = None if q_out is None else _rows_view(q_out, "q_out")
+    dev = _on_current_device("rows row_starts q_lens kv_lens block_table q q_out pages scales table positions", rows,
+                             row_starts, q_lens, kv_lens, block_table, q, q_out, *_kept(pages), *_kept(rope))
+    _check(_lib.cb_page_quantize(ctypes.byref(rv), ctypes.byref(pages), int(layer), *spans,
+                                 None if rope is None else ctypes.byref(rope), None if qv is None else ctypes.byref(qv),
+                                 None if ov is None else ctypes.byref(ov), _stream_on(dev, stream)))
+
+
+def cb_page_read(pages: CbPages, rows: torch.Tensor, row_starts: torch.Tensor, q_lens: torch.Tensor,
+                 kv_lens: torch.Tensor, block_table: torch.Tensor, layer: int = 0,
+                 rope: Optional[CbRopeAxesSpec] = None, inverse: bool = False, stream=None):
+    """Read tokens back from pages of any type into a bfloat16 cache tensor: request r's last ``q_lens[r]`` of
+    ``kv_lens[r]`` tokens into tokens ``row_starts[r]`` ... of rows, keys turned (inverse: turned back) by ``rope``."""
+    rv = cache_view(rows)
+    spans = _spans(row_starts, q_lens, kv_lens, block_table)
+    _fit_int32(layer)
+    _check_axes_tokens(rope, rows.shape[2] * rows.shape[4])
+    dev = _on_current_device("rows row_starts q_lens kv_lens block_table pages scales table positions", rows, row_starts,
+                             q_lens, kv_lens, block_table, *_kept(pages), *_kept(rope))
+    _check(_lib.cb_page_read(ctypes.byref(pages), int(layer), ctypes.byref(rv), *spans,
+                             None if rope is None else ctypes.byref(rope), int(bool(inverse)), _stream_on(dev, stream)))
 
 
 def cb_attn_paged_workspace_bytes(n_tokens: int, n_reqs: int, n_qheads: int, n_heads: int, head_dim: int,

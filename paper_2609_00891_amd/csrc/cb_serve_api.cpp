@@ -27,15 +27,17 @@ cb_status check_width(int d) {
     return CB_OK;
 }
 
+int element_bytes(const cb_pages *p) { return p->dtype == CB_PAGES_BF16 ? 2 : 1; }
+
 cb_status check_pages(const cb_pages *p) {
     if (!p) return fail(CB_ERR_INVALID_ARGUMENT, "pages is NULL");
     const cb_cache &c = p->cache;
-    if (p->dtype != CB_PAGES_BF16 && p->dtype != CB_PAGES_E4M3)
+    if (p->dtype != CB_PAGES_BF16 && p->dtype != CB_PAGES_E4M3 && p->dtype != CB_PAGES_E4M3_BLOCKS)
         return fail(CB_ERR_INVALID_ARGUMENT, "pages: unknown dtype %d", p->dtype);
     if (c.n_layers <= 0 || c.n_heads <= 0 || c.n_seqs <= 0 || c.seq_len <= 0)
         return fail(CB_ERR_SHAPE, "pages needs positive layer, head, page and page size counts");
     if (cb_status s = cb::api_check_cache("pages", &c, c.n_layers, c.n_heads, c.head_dim)) return s;
-    const int el = p->dtype == CB_PAGES_E4M3 ? 1 : 2;
+    const int el = element_bytes(p);
     if (el == 1) {
         const int64_t st[5] = {c.s_layer, c.s_kv, c.s_seq, c.s_head, c.s_tok};
         for (int i = 0; i < 5; ++i)
@@ -123,7 +125,7 @@ cb_status check_rope_axes(const cb_rope_axes_spec *r, int d, int64_t n_tokens, c
     return CB_OK;
 }
 
-// Geometry shared by cb_rope_axes and cb_page_write.
+// Geometry of the rows that a call turns, writes into pages or reads from them.
 cb_status prepare_rows(const char *name, const cb_cache *in, cb::RowsArgs &a) {
     if (!in) return fail(CB_ERR_INVALID_ARGUMENT, "%s is NULL", name);
     if (cb_status s = check_width(in->head_dim)) return s;
@@ -139,6 +141,65 @@ cb_status prepare_rows(const char *name, const cb_cache *in, cb::RowsArgs &a) {
     a.page_size = cb::make_fastdiv(1);
     a.n_tokens = (int64_t)in->n_seqs * in->seq_len;
     a.n_lh = in->n_layers * in->n_heads;
+    return CB_OK;
+}
+
+cb_status check_layers(int32_t layer0, int32_t n, const cb_cache &pool) {
+    if (n < 1 || layer0 < 0 || (int64_t)layer0 + n > pool.n_layers)
+        return fail(CB_ERR_INVALID_ARGUMENT, "layers %d .. %lld are outside the pool's %d", layer0, (long long)layer0 + n - 1,
+                    pool.n_layers);
+    return CB_OK;
+}
+
+// The turn of a call's rows and of the queries beside them.
+cb_status prepare_turn(const cb_rope_axes_spec *rope, const cb_rows *q, const cb_rows *q_out, int d, cb::RowsArgs &a) {
+    if ((q != nullptr) != (q_out != nullptr)) return fail(CB_ERR_INVALID_ARGUMENT, "q and q_out go together");
+    if (q && !rope) return fail(CB_ERR_INVALID_ARGUMENT, "q is turned by rope, which is NULL");
+    if (rope)
+        if (cb_status s = check_rope_axes(rope, d, a.n_tokens, &a.rope)) return s;
+    if (!q) return CB_OK;
+    if (cb_status s = check_rows("q", q, d)) return s;
+    if (cb_status s = check_rows_written("q_out", q_out, d)) return s;
+    if (q->n_tokens != a.n_tokens || q_out->n_tokens != a.n_tokens || q->n_heads != q_out->n_heads)
+        return fail(CB_ERR_SHAPE, "q and q_out must have the tokens of rows and equal heads");
+    if (q->n_heads > (1 << 24)) return fail(CB_ERR_UNSUPPORTED, "too many query heads");
+    if (q->data == q_out->data && (q->s_tok != q_out->s_tok || q->s_head != q_out->s_head))
+        return fail(CB_ERR_INVALID_ARGUMENT, "an in-place turn needs q_out to have q's strides");
+    a.q = (const uint16_t *)q->data;
+    a.q_out = (uint16_t *)q_out->data;
+    a.q_tok = q->s_tok;
+    a.q_head = q->s_head;
+    a.qo_tok = q_out->s_tok;
+    a.qo_head = q_out->s_head;
+    a.n_qh = q->n_heads;
+    return CB_OK;
+}
+
+// The block table and lengths of a call that finds its tokens by them.  Without tokens, as n_reqs = 0 says, the arrays
+// may be NULL.
+cb_status prepare_spans(const cb_cache &pool, int32_t n_reqs, const int32_t *row_starts, bool by_rows, const int32_t *q_lens,
+                        const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                        cb::SpanArgs &a) {
+    if (n_reqs < 0) return fail(CB_ERR_INVALID_ARGUMENT, "n_reqs is negative");
+    if (table_width < 0) return fail(CB_ERR_INVALID_ARGUMENT, "table_width is negative");
+    if (n_reqs > 1 && table_stride < table_width)
+        return fail(CB_ERR_SHAPE, "table_stride (%lld) < table_width (%d)", (long long)table_stride, table_width);
+    if ((int64_t)table_width * pool.seq_len > INT32_MAX)
+        return fail(CB_ERR_UNSUPPORTED, "table_width * page size must be below 2^31");
+    if (pool.seq_len > (1 << 24)) return fail(CB_ERR_UNSUPPORTED, "a page has at most 2^24 tokens here");
+    if (((uintptr_t)row_starts) % 4 || ((uintptr_t)q_lens) % 4 || ((uintptr_t)kv_lens) % 4 || ((uintptr_t)block_table) % 4)
+        return fail(CB_ERR_MISALIGNED, "lengths and tables must be 4-byte aligned");
+    if (n_reqs > 0 && ((by_rows && !row_starts) || !q_lens || !kv_lens || (table_width > 0 && !block_table)))
+        return fail(CB_ERR_INVALID_ARGUMENT, "%sq_lens, kv_lens and block_table must be non-NULL", by_rows ? "row_starts, " : "");
+    a.n_reqs = n_reqs;
+    a.n_pages = pool.n_seqs;
+    a.row_starts = row_starts;
+    a.q_lens = q_lens;
+    a.kv_lens = kv_lens;
+    a.table = block_table;
+    a.table_stride = table_stride;
+    a.most = table_width * pool.seq_len;
+    a.page_size = cb::make_fastdiv((uint32_t)pool.seq_len);
     return CB_OK;
 }
 
@@ -219,34 +280,15 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
     const cb_cache &c = pages->cache;
     if (c.n_heads != rows->n_heads || c.head_dim != rows->head_dim)
         return fail(CB_ERR_SHAPE, "rows are %d heads x %d, pages %d x %d", rows->n_heads, rows->head_dim, c.n_heads, c.head_dim);
-    if (layer0 < 0 || (int64_t)layer0 + rows->n_layers > c.n_layers)
-        return fail(CB_ERR_INVALID_ARGUMENT, "layers %d .. %lld are outside the pool's %d", layer0,
-                    (long long)layer0 + rows->n_layers - 1, c.n_layers);
-    if ((q != nullptr) != (q_out != nullptr)) return fail(CB_ERR_INVALID_ARGUMENT, "q and q_out go together");
-    if (q && !rope) return fail(CB_ERR_INVALID_ARGUMENT, "q is turned by rope, which is NULL");
-    if (rope)
-        if (cb_status s = check_rope_axes(rope, rows->head_dim, a.n_tokens, &a.rope)) return s;
-    if (q) {
-        if (cb_status s = check_rows("q", q, rows->head_dim)) return s;
-        if (cb_status s = check_rows_written("q_out", q_out, rows->head_dim)) return s;
-        if (q->n_tokens != a.n_tokens || q_out->n_tokens != a.n_tokens || q->n_heads != q_out->n_heads)
-            return fail(CB_ERR_SHAPE, "q and q_out must have the tokens of rows and equal heads");
-        if (q->n_heads > (1 << 24)) return fail(CB_ERR_UNSUPPORTED, "too many query heads");
-        if (q->data == q_out->data && (q->s_tok != q_out->s_tok || q->s_head != q_out->s_head))
-            return fail(CB_ERR_INVALID_ARGUMENT, "an in-place turn needs q_out to have q's strides");
-        a.q = (const uint16_t *)q->data;
-        a.q_out = (uint16_t *)q_out->data;
-        a.q_tok = q->s_tok;
-        a.q_head = q->s_head;
-        a.qo_tok = q_out->s_tok;
-        a.qo_head = q_out->s_head;
-        a.n_qh = q->n_heads;
-    }
+    if (pages->dtype == CB_PAGES_E4M3_BLOCKS)
+        return fail(CB_ERR_INVALID_ARGUMENT, "pages whose scales belong to a page are written by cb_page_quantize");
+    if (cb_status s = check_layers(layer0, rows->n_layers, c)) return s;
+    if (cb_status s = prepare_turn(rope, q, q_out, rows->head_dim, a)) return s;
     if (a.n_tokens == 0) return cb::api_ok();
     if (!slots) return fail(CB_ERR_INVALID_ARGUMENT, "slots is NULL");
     if (((uintptr_t)slots) % 4) return fail(CB_ERR_MISALIGNED, "slots must be 4-byte aligned");
     if (cb_status s = check_cache_written("pages", c, true)) return s;
-    a.out = (char *)c.data + (int64_t)layer0 * c.s_layer * (pages->dtype == CB_PAGES_E4M3 ? 1 : 2);
+    a.out = (char *)c.data + (int64_t)layer0 * c.s_layer * element_bytes(pages);
     a.os = strides_of(c);
     a.slots = slots;
     a.n_slots = c.n_seqs * c.seq_len;
@@ -257,6 +299,61 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
     a.sign = 1.f;
     if (cb::launch_rows(a, rope != nullptr, pages->dtype == CB_PAGES_E4M3, (hipStream_t)stream) != hipSuccess)
         return fail(CB_ERR_DEVICE, "page write launch failed");
+    return cb::api_ok();
+}
+
+cb_status cb_page_quantize(const cb_cache *rows, const cb_pages *pages, int32_t layer0, int32_t n_reqs,
+                           const int32_t *row_starts, const int32_t *q_lens, const int32_t *kv_lens,
+                           const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                           const cb_rope_axes_spec *rope, const cb_rows *q, const cb_rows *q_out, void *stream) {
+    cb::RowsArgs a = {};
+    if (cb_status s = prepare_rows("rows", rows, a)) return s;
+    if (cb_status s = check_pages(pages)) return s;
+    const cb_cache &c = pages->cache;
+    if (c.n_heads != rows->n_heads || c.head_dim != rows->head_dim)
+        return fail(CB_ERR_SHAPE, "rows are %d heads x %d, pages %d x %d", rows->n_heads, rows->head_dim, c.n_heads, c.head_dim);
+    if (pages->dtype != CB_PAGES_E4M3_BLOCKS)
+        return fail(CB_ERR_INVALID_ARGUMENT, "pages need scales that belong to a page (CB_PAGES_E4M3_BLOCKS)");
+    if (cb_status s = check_layers(layer0, rows->n_layers, c)) return s;
+    if (cb_status s = prepare_turn(rope, q, q_out, rows->head_dim, a)) return s;
+    cb::SpanArgs sp = {};
+    if (cb_status s = prepare_spans(c, n_reqs, row_starts, true, q_lens, kv_lens, block_table, table_stride, table_width, sp)) return s;
+    if (a.n_tokens == 0 || n_reqs == 0) return cb::api_ok();
+    if (cb_status s = check_cache_written("pages", c, true)) return s;
+    sp.n_tokens = a.n_tokens;
+    a.out = (char *)c.data + (int64_t)layer0 * c.s_layer;
+    a.os = strides_of(c);
+    a.n_rows = 2 * a.n_lh + a.n_qh;
+    a.layer0 = layer0;
+    a.sign = 1.f;
+    if (cb::launch_page_quant(a, sp, rope != nullptr, const_cast<float *>(pages->scales), (hipStream_t)stream) != hipSuccess)
+        return fail(CB_ERR_DEVICE, "page quantize launch failed");
+    return cb::api_ok();
+}
+
+cb_status cb_page_read(const cb_pages *pages, int32_t layer0, const cb_cache *rows, int32_t n_reqs, const int32_t *row_starts,
+                       const int32_t *q_lens, const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride,
+                       int32_t table_width, const cb_rope_axes_spec *rope, int32_t inverse, void *stream) {
+    cb::RowsArgs a = {};
+    if (cb_status s = check_pages(pages)) return s;
+    if (cb_status s = prepare_rows("rows", rows, a)) return s;
+    const cb_cache &c = pages->cache;
+    if (c.n_heads != rows->n_heads || c.head_dim != rows->head_dim)
+        return fail(CB_ERR_SHAPE, "rows are %d heads x %d, pages %d x %d", rows->n_heads, rows->head_dim, c.n_heads, c.head_dim);
+    if (cb_status s = check_layers(layer0, rows->n_layers, c)) return s;
+    if (cb_status s = prepare_turn(rope, nullptr, nullptr, rows->head_dim, a)) return s;
+    cb::SpanArgs sp = {};
+    if (cb_status s = prepare_spans(c, n_reqs, row_starts, true, q_lens, kv_lens, block_table, table_stride, table_width, sp)) return s;
+    if (a.n_tokens == 0 || n_reqs == 0) return cb::api_ok();
+    if (cb_status s = check_cache_written("rows", *rows, true)) return s;
+    sp.n_tokens = a.n_tokens;
+    a.out = (char *)c.data + (int64_t)layer0 * c.s_layer * element_bytes(pages);
+    a.os = strides_of(c);
+    a.n_rows = 2 * a.n_lh;
+    a.layer0 = layer0;
+    a.sign = inverse ? -1.f : 1.f;
+    if (cb::launch_page_read(a, sp, rope != nullptr, pages->dtype, pages->scales, (hipStream_t)stream) != hipSuccess)
+        return fail(CB_ERR_DEVICE, "page read launch failed");
     return cb::api_ok();
 }
 
@@ -298,7 +395,8 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
     if (!q_starts || !kv_lens || (table_width > 0 && !block_table))
         return fail(CB_ERR_INVALID_ARGUMENT, "q_starts, kv_lens and block_table must be non-NULL");
     if (q->data == out->data) return fail(CB_ERR_INVALID_ARGUMENT, "out must not be q");
-    const int el = pages->dtype == CB_PAGES_E4M3 ? 1 : 2;
+    if (pages->dtype == CB_PAGES_E4M3_BLOCKS) return fail(CB_ERR_UNSUPPORTED, "not yet");
+    const int el = element_bytes(pages);
     cb::PagedArgs a = {};
     a.q = (const uint16_t *)q->data;
     a.out = (uint16_t *)out->data;

@@ -48,6 +48,7 @@ struct RowsArgs {
     int32_t n_rows;           // K, then query, then V rows that are worked on
     int32_t group;            // rows of a token that one thread takes
     int32_t tok_per_wave;
+    int32_t lgc;              // block pages: 2^lgc >= nc2
     int32_t layer0;           // the scales' layer of in's first
     const float *scales;      // e4m3 pages
     RopeAxes rope;
@@ -55,6 +56,26 @@ struct RowsArgs {
     const uint16_t *q;
     uint16_t *q_out;
     int64_t q_tok, q_head, qo_tok, qo_head;
+};
+
+// The last q_lens[r] of kv_lens[r] tokens of every request, by pages; row_starts[r] is the first one's row (or NULL).
+struct SpanArgs {
+    int32_t n_reqs, n_pages;
+    const int32_t *row_starts, *q_lens, *kv_lens, *table;
+    int64_t table_stride;
+    int32_t most;             // tokens that a row of the table has places for
+    int64_t n_tokens;
+    FastDiv page_size;
+};
+
+// Bounds of pages (cb_page_bounds).  Strides in bytes.
+struct BoundsArgs {
+    const char *k;            // the first layer's K pages
+    int64_t s_layer, s_page, s_head, s_tok;
+    char *bounds;             // [layer][page][head][2][head_dim]
+    FastDiv n_heads;
+    int32_t n_lh, layer0;
+    int32_t chunks, lgc;      // 16-byte chunks of a row, 2^lgc >= chunks
 };
 
 // Attention over pages (cb_attn_paged).  Strides of the pool in units of 16
@@ -91,6 +112,9 @@ struct PagedArgs {
 // Launchers (return hipError_t of the launch).
 hipError_t launch_page_tables(const PageTablesArgs &a, hipStream_t s);
 hipError_t launch_rows(RowsArgs a, bool rope, bool f8, hipStream_t s);
+hipError_t launch_page_quant(RowsArgs a, const SpanArgs &span, bool rope, float *scales, hipStream_t s);
+hipError_t launch_page_read(RowsArgs a, const SpanArgs &span, bool rope, int32_t dtype, const float *scales, hipStream_t s);
+hipError_t launch_page_bounds(BoundsArgs a, const SpanArgs &span, bool f8, int32_t max_q_len, hipStream_t s);
 hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, bool f8, int32_t max_q_len, void *ws, int64_t ws_bytes,
                              hipStream_t s);
 int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_reqs, int32_t max_q_len);

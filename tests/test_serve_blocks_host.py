@@ -1,0 +1,126 @@
+"""Host checks (no GPU) of pages whose scales belong to a page and head: the plain forms by hand, and what the calls
+refuse (nothing is enqueued)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from test_serve_host import ALIGN, ARG, OK, P, SHAPE, UNSUP, cache, cb, pages, rope, rows  # noqa: F401
+
+
+def blocks(cb, **kw):
+    return pages(cb, **{**dict(dtype=2, scales=P), **kw})
+
+
+SPANS = dict(n_reqs=2, starts=P, q=P, kv=P, bt=P, stride=8, width=8)
+QUANT = dict(rows=dict(n_seqs=1, seq_len=5, data=4 * P), pages={}, layer=0, rope=None, qr=None, qo=None, **SPANS)
+
+
+def ref(f, cb, x):
+    return None if x is None else ctypes.byref(f(cb, **x))
+
+
+def quantize(cb, **kw):
+    a = {**QUANT, **kw}
+    return cb.library().cb_page_quantize(ref(cache, cb, a["rows"]), ref(blocks, cb, a["pages"]), a["layer"], a["n_reqs"],
+                                         a["starts"], a["q"], a["kv"], a["bt"], a["stride"], a["width"],
+                                         ref(rope, cb, a["rope"]), ref(rows, cb, a["qr"]), ref(rows, cb, a["qo"]), None)
+
+
+def read(cb, **kw):
+    a = {**QUANT, **kw}
+    return cb.library().cb_page_read(ref(blocks, cb, a["pages"]), a["layer"], ref(cache, cb, a["rows"]), a["n_reqs"],
+                                     a["starts"], a["q"], a["kv"], a["bt"], a["stride"], a["width"],
+                                     ref(rope, cb, a["rope"]), 1, None)
+
+
+SPAN_REFUSALS = [
+    (dict(n_reqs=-1), ARG), (dict(width=-1), ARG), (dict(stride=7), SHAPE), (dict(width=1 << 28, stride=1 << 28), UNSUP),
+    (dict(starts=None), ARG), (dict(q=None), ARG), (dict(kv=None), ARG), (dict(bt=None), ARG), (dict(starts=P + 1), ALIGN),
+    (dict(q=P + 2), ALIGN), (dict(kv=P + 2), ALIGN), (dict(bt=P + 2), ALIGN), (dict(n_reqs=0, starts=None, q=None), OK),
+    (dict(rows=dict(n_seqs=1, seq_len=0)), OK), (dict(rows=None), ARG), (dict(pages=None), ARG),
+    (dict(pages=dict(seq_len=1 << 25, n_seqs=1), width=1), UNSUP), (dict(layer=1), ARG), (dict(layer=-1), ARG),
+    (dict(pages=dict(n_heads=3)), SHAPE), (dict(pages=dict(head_dim=128)), SHAPE), (dict(pages=dict(scales=None)), ARG),
+    (dict(pages=dict(scales=P + 2)), ALIGN), (dict(pages=dict(s_tok=72)), ALIGN), (dict(pages=dict(dtype=3)), ARG),
+    (dict(rows=dict(head_dim=72, s_tok=72)), UNSUP), (dict(rope=dict(style=2)), ARG), (dict(rope=dict(head_dim=128)), SHAPE),
+    (dict(rope=dict(table=None)), ARG), (dict(rope=dict(n_axes=2, axis_stride=4)), SHAPE),
+]
+
+
+@pytest.mark.parametrize("kw,status", SPAN_REFUSALS + [
+    (dict(pages=dict(dtype=1)), ARG), (dict(pages=dict(dtype=0, scales=None)), ARG), (dict(qr={}), ARG), (dict(qo={}), ARG),
+    (dict(qr={}, qo={}), ARG), (dict(rope={}, qr=dict(n_tokens=4), qo=dict(n_tokens=4)), SHAPE),
+    (dict(rope={}, qr=dict(n_tokens=5), qo=dict(n_tokens=5, n_heads=2)), SHAPE),
+    (dict(rope={}, qr=dict(n_tokens=5), qo=dict(n_tokens=5, s_tok=512)), ARG),
+    (dict(rope={}, qr=dict(n_tokens=5), qo=dict(n_tokens=5, data=3 * P, s_tok=0)), SHAPE),
+    (dict(pages=dict(s_seq=0)), SHAPE), (dict(pages=dict(s_kv=0)), SHAPE),
+])
+def test_quantize_refuses(cb, kw, status):
+    assert quantize(cb, **kw) == status, cb.cb_last_error()
+    assert (cb.cb_last_error() != "") == (status != OK)
+
+
+@pytest.mark.parametrize("kw,status", SPAN_REFUSALS + [
+    (dict(rows=dict(n_seqs=2, seq_len=5, s_seq=0)), SHAPE), (dict(rows=dict(n_seqs=1, seq_len=5, s_kv=0)), SHAPE),
+    (dict(pages=dict(s_seq=0), n_reqs=0), OK), (dict(pages=dict(dtype=0, scales=None), n_reqs=0), OK),
+    (dict(pages=dict(dtype=1), n_reqs=0), OK),
+])
+def test_read_refuses(cb, kw, status):
+    assert read(cb, **kw) == status, cb.cb_last_error()
+
+
+def test_write_refuses_pages_with_scales_of_their_own(cb):
+    c, p = cache(cb, n_seqs=1, seq_len=5, data=4 * P), blocks(cb)
+    assert cb.library().cb_page_write(ctypes.byref(c), ctypes.byref(p), 0, P, None, None, None, None) == ARG
+    assert "cb_page_quantize" in cb.cb_last_error()
+
+
+def test_binding_refuses_wrong_tensors(cb):
+    z = lambda *s, t=torch.bfloat16: torch.zeros(s, dtype=t)  # noqa: E731
+    i = lambda *s: z(*s, t=torch.int32)  # noqa: E731
+    pool = z(2, 2, 3, 2, 16, 64).to(torch.float8_e4m3fn)
+    for shape in ((2, 3, 2), (2, 3, 2, 1), (2, 2, 3, 2), (2, 2, 2, 2)):
+        with pytest.raises(ValueError, match="scales"):
+            cb.page_pool(pool, z(*shape, t=torch.float32))
+    pg = cb.page_pool(pool, z(2, 3, 2, 2, t=torch.float32))
+    assert pg.dtype == cb.CB_PAGES_E4M3_BLOCKS and cb.page_pool(pool, z(2, 2, 2, t=torch.float32)).dtype == cb.CB_PAGES_E4M3
+    x = z(1, 2, 1, 2, 9, 64)
+    good = dict(rows=x, pages=pg, row_starts=i(2), q_lens=i(2), kv_lens=i(2), block_table=i(2, 3))
+    for f in (cb.cb_page_quantize, cb.cb_page_read):
+        for bad, match in ((dict(rows=x.float()), "cache tensors"), (dict(row_starts=i(3)), "row_starts"),
+                           (dict(q_lens=i(2).long()), "q_lens"), (dict(block_table=i(3, 3)), "block_table"),
+                           (dict(layer=2 ** 32), "32-bit"), (dict(), "current CUDA device")):
+            with pytest.raises(ValueError, match=match):
+                f(**{**good, **bad})
+        sp = cb.rope_axes_spec(z(10, 32, 2, t=torch.float32), i(3, 8), axis=[0, 1, 2, 0] * 8)
+        with pytest.raises(ValueError, match="positions hold 8"):
+            f(**good, rope=sp)
+
+
+def test_plain_e4m3_by_hand():
+    from oracle import serve
+    x = [0.0, 1.0, 1.06, 1.0625, 1.1875, 17.0, 447.0, 448.0, 463.0, 465.0, 500.0, 2.0 ** -9, 2.0 ** -10, 1.5 * 2.0 ** -9,
+         -2.0 ** -11, 0.015]
+    want = [0.0, 1.0, 1.0, 1.0, 1.25, 16.0, 448.0, 448.0, 448.0, np.nan, np.nan, 2.0 ** -9, 0.0, 2.0 ** -8, -0.0, 2.0 ** -6]
+    assert np.array_equal(serve.e4m3(np.array(x)), np.array(want), equal_nan=True)
+    assert np.isnan(serve.e4m3(np.array([np.inf, -np.inf, np.nan]))).all()
+    ours = serve.e4m3(np.linspace(-447, 447, 9999))
+    theirs = torch.linspace(-447, 447, 9999, dtype=torch.float64).float().to(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(ours, theirs)
+
+
+def test_plain_quantize_by_hand():
+    """Page of two places: a first token of size 448, then one of 900, whose scale 4 the first goes over to."""
+    from oracle import serve
+    rows = np.zeros((2, 1, 2, 1, 2))
+    rows[0, 0, :, 0] = [448.0, -3.0]
+    rows[1, 0, :, 0] = [900.0, 1.0]
+    codes, exps, table = np.full((1, 2, 2, 1, 2, 2), 5.0), np.full((1, 2, 1, 2), 3), np.array([[1]])
+    assert serve.page_spans([0, 1], [1, 9], [1, 9], 2, 2, 1) == [(0, 0, 0, 1, 0)]
+    serve.page_quantize(rows, None, codes, exps, serve.page_spans([0], [1], [1], 2, 2, 1), table)
+    assert exps[0, :, 0].tolist() == [[3, 3], [0, 0]] and codes[0, 0, 1, 0].tolist() == [[448, -3], [5, 5]]
+    serve.page_quantize(rows, None, codes, exps, serve.page_spans([1], [1], [2], 2, 2, 1), table)
+    assert exps[0, 1, 0].tolist() == [2, 2] and codes[0, 1, 1, 0].tolist() == [[112, -0.75], [225, 0.25]]
+    assert serve.block_exponent(np.array([0.0]), False) == serve.E_MIN
+    assert [serve.block_exponent(np.array([v, np.inf, np.nan]), t) for v, t in ((448.0, 0), (449.0, 0), (316.0, 1), (317.0, 1))] == [0, 1, 0, 1]
