@@ -644,8 +644,8 @@ cb_status cb_plan_feature_width(const cb_plan *plan, int32_t *P, int32_t *k);
  * element e stands for e * scales[(layer * 2 + kv) * n_heads + head]
  * (fp32, device, positive and finite; NULL for CB_PAGES_BF16).  E4M3_BLOCKS:
  * laid out as E4M3, but scales[((layer * pages + page) * n_heads + head) * 2 + kv],
- * each a power of two from 2^-64 to 2^120 (of another number only the exponent
- * counts); cb_page_quantize writes rows and scales, although the calls that only
+ * each a power of two from 2^-64 to 2^119 (of another number only the exponent
+ * counts), 8-byte aligned; cb_page_quantize writes rows and scales, although the calls that only
  * read take them as const.  pages * page_size < 2^31, and the pages of one (layer,
  * kv) span less than 64 GiB.
  */
@@ -761,7 +761,8 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
  *     the larger of this and its own scale, and where it grows its earlier places
  *     are rounded (nearest even) to the larger scale,
  *   a row is stored as its bf16 value, K rows turned by rope in fp32, over the scale,
- *     rounded once to e4m3, nearest even; infinities become NaN, NaN stays.
+ *     rounded once to e4m3, nearest even; infinities become NaN, NaN stays (e is at
+ *     most 119: so does what is beyond 464 2^119, 0.91 of the largest bf16 number).
  * Places behind a request's tokens stay as they were and stand for nothing.  A
  * request with q_lens <= 0, kv_lens < q_lens or above table_width * page_size, or rows outside
  * `rows`, takes no part (so with cb_page_tables' kv_lens, which are 0 for requests
@@ -818,7 +819,8 @@ cb_status cb_page_read(const cb_pages *pages, int32_t layer0, const cb_cache *ro
  *     what the call can use.  With less (or NULL) rows are split less.  The call
  *     leaves nothing in it that another reads; calls that overlap in time need
  *     one each.
- * Scores and sums are fp32 from exact products; the weights exp(s_j - m) are
+ * Pages of any type; an E4M3_BLOCKS element enters the products as the bf16 number it
+ * stands for.  Scores and sums are fp32 from exact products; the weights exp(s_j - m) are
  * rounded to bf16 for their product with V (m a running maximum) and summed
  * unrounded.  max_q_len, the workspace's size and the other requests decide which
  * kernel takes a row and how its keys are divided, and every part has a running

@@ -91,7 +91,7 @@ def attention(q, K, V, kv_len, scale, window=0, sinks=0, hidden=()):
 
 # ------------------------------------------------------------------ pages whose scales belong to a page
 
-E_MIN = -64                          # exponent of the smallest scale
+E_MIN, E_MAX = -64, 119              # exponents of the smallest and largest scale
 
 
 def e4m3(x):
@@ -109,7 +109,7 @@ def block_exponent(rows, turned):
     a = np.abs(rows[np.isfinite(rows)])
     m = float(a.max()) if a.size else 0.0
     e = E_MIN
-    while m > (316.0 if turned else 448.0) * 2.0 ** e:
+    while e < E_MAX and m > (316.0 if turned else 448.0) * 2.0 ** e:
         e += 1
     return e
 

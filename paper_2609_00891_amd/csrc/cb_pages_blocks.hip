@@ -27,7 +27,9 @@ namespace {
 
 typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
 
-constexpr int kEMin = -64;                                     // 2^-64 448 is far below any cache's values
+// 2^-64 448 is far below any cache's values, and 2^119 448 below the largest bf16 number, so that what a finite code
+// stands for is finite.
+constexpr int kEMin = -64, kEMax = 119;
 constexpr uint32_t kMantPlain = 96, kMantTurned = 30;          // mantissa bits of 448 and 316 in bf16 (2^8 1.75, 2^8 1.234375)
 
 // The bits of the bf16 values that are infinities or NaNs (an exponent of all ones carries into the sign's place).
@@ -43,9 +45,9 @@ __device__ __forceinline__ uint32_t max_finite(uint32_t m, uint32_t u) {
 __device__ __forceinline__ uint32_t max_finite(uint32_t m, const uint4 &v) {
     return max_finite(max_finite(max_finite(max_finite(m, v.x), v.y), v.z), v.w);
 }
-// The least e >= kEMin with |x| <= M 2^e, from the bits of |x|.
+// The least e from kEMin to kEMax with |x| <= M 2^e, from the bits of |x|.
 __device__ __forceinline__ int exponent_for(uint32_t bits, uint32_t mant) {
-    return max((int)(bits >> 7) - 127 - 8 + ((bits & 127) > mant ? 1 : 0), kEMin);
+    return min(max((int)(bits >> 7) - 127 - 8 + ((bits & 127) > mant ? 1 : 0), kEMin), kEMax);
 }
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 // Two e4m3 values times 2^e (the scale's exponent is all that counts), as bf16.
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(256) void page_quant_kernel(RowsArgs a, SpanArgs sp
             if (!live) continue;
             int e = exponent_for(m, turned ? kMantTurned : kMantPlain);
             if (goes_on) {
-                const int e_old = min(max((int)((was >> 23) & 255) - 127, kEMin), 120);
+                const int e_old = min(max((int)((was >> 23) & 255) - 127, kEMin), kEMax);
                 e = max(e, e_old);
                 if (e > e_old) {                                   // what is there goes over to the larger scale
                     const float f = power(max(e_old - e, -126));

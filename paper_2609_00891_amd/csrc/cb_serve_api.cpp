@@ -43,7 +43,8 @@ cb_status check_pages(const cb_pages *p) {
         for (int i = 0; i < 5; ++i)
             if (st[i] % 16) return fail(CB_ERR_MISALIGNED, "strides of 8-bit pages must be multiples of 16 elements (16 bytes)");
         if (!p->scales) return fail(CB_ERR_INVALID_ARGUMENT, "8-bit pages need scales");
-        if (((uintptr_t)p->scales) % 4) return fail(CB_ERR_MISALIGNED, "scales must be 4-byte aligned");
+        const uintptr_t each = p->dtype == CB_PAGES_E4M3_BLOCKS ? 8 : 4;   // (a page and head has two together)
+        if (((uintptr_t)p->scales) % each) return fail(CB_ERR_MISALIGNED, "scales must be %d-byte aligned", (int)each);
     }
     if ((int64_t)c.n_seqs * c.seq_len > INT32_MAX) return fail(CB_ERR_UNSUPPORTED, "a pool has fewer than 2^31 slots");
     // a row's place within one (layer, kv) is a 32-bit number of 16-byte units
@@ -395,7 +396,6 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
     if (!q_starts || !kv_lens || (table_width > 0 && !block_table))
         return fail(CB_ERR_INVALID_ARGUMENT, "q_starts, kv_lens and block_table must be non-NULL");
     if (q->data == out->data) return fail(CB_ERR_INVALID_ARGUMENT, "out must not be q");
-    if (pages->dtype == CB_PAGES_E4M3_BLOCKS) return fail(CB_ERR_UNSUPPORTED, "not yet");
     const int el = element_bytes(pages);
     cb::PagedArgs a = {};
     a.q = (const uint16_t *)q->data;
@@ -421,14 +421,16 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
     a.n_heads = c.n_heads;
     a.G = cb::make_fastdiv((uint32_t)(q->n_heads / c.n_heads));
     a.scale_log2 = scale_log2;
-    if (el == 1) {
+    if (pages->dtype == CB_PAGES_E4M3_BLOCKS) {
+        a.kscale = pages->scales + (int64_t)layer * c.n_seqs * c.n_heads * 2;
+    } else if (el == 1) {
         a.kscale = pages->scales + (int64_t)layer * 2 * c.n_heads;
         a.vscale = a.kscale + c.n_heads;
     }
     a.window = window;
     a.n_sinks = n_sinks;
     a.lse = lse;
-    if (cb::launch_attn_paged(a, d, el == 1, max_q_len, workspace, workspace ? workspace_bytes : 0, (hipStream_t)stream) !=
+    if (cb::launch_attn_paged(a, d, pages->dtype, max_q_len, workspace, workspace ? workspace_bytes : 0, (hipStream_t)stream) !=
         hipSuccess)
         return fail(CB_ERR_DEVICE, "paged attention launch failed");
     return cb::api_ok();

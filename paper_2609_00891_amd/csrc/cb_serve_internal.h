@@ -103,10 +103,13 @@ struct PagedArgs {
     int32_t n_reqs, n_heads;
     FastDiv G;
     float scale_log2;         // scale * log2(e)
-    const float *kscale, *vscale;   // e4m3: [n_heads]
+    const float *kscale, *vscale;   // e4m3: [n_heads]; block scales: kscale [n_pages][n_heads][2]
     int32_t window, n_sinks;
     float *lse;               // NULL or [n_tokens][n_heads * G]
     PagedClass rows, tile;
+    const int32_t *selected;  // attention over selected pages: [n_tokens][n_heads][n_selected]
+    int32_t n_selected;
+    FastDiv sel_parts, sel_tiles;   // parts of a row tile, row tiles of a token
 };
 
 // Launchers (return hipError_t of the launch).
@@ -115,7 +118,7 @@ hipError_t launch_rows(RowsArgs a, bool rope, bool f8, hipStream_t s);
 hipError_t launch_page_quant(RowsArgs a, const SpanArgs &span, bool rope, float *scales, hipStream_t s);
 hipError_t launch_page_read(RowsArgs a, const SpanArgs &span, bool rope, int32_t dtype, const float *scales, hipStream_t s);
 hipError_t launch_page_bounds(BoundsArgs a, const SpanArgs &span, bool f8, int32_t max_q_len, hipStream_t s);
-hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, bool f8, int32_t max_q_len, void *ws, int64_t ws_bytes,
+hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, int32_t dtype, int32_t max_q_len, void *ws, int64_t ws_bytes,
                              hipStream_t s);
 int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_reqs, int32_t max_q_len);
 

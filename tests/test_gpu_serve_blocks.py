@@ -9,6 +9,8 @@ import numpy as np
 import pytest
 import torch
 
+from test_gpu_serve import CASES, Step
+
 pytestmark = pytest.mark.gpu
 
 BF, F32 = 2.0 ** -8, 2.0 ** -24
@@ -315,8 +317,9 @@ def test_scales_at_their_borders(cb, serve):
         serve.page_quantize(rows, y if axes else None, codes, exps, serve.page_spans(np.arange(n), [1] * n, [1] * n, ps, n, 1), table)
         assert np.array_equal(pool.scales.cpu().numpy(), (2.0 ** exps.astype(float)).astype(np.float32))
         got = pool.codes()
-        assert np.isfinite(got[:, :, :, :, 0]).all()
-        assert np.array_equal(got[:, 1, :, :, 0], serve.e4m3(codes[:, 1, :, :, 0]))
+        far = tops.index(3.38e38)                               # beyond the largest scale's largest number
+        assert np.isnan(got[0, 1, far, 0, 0, 5]) and np.isfinite(np.delete(got[:, :, :, :, 0], far, 2)).all()
+        assert np.array_equal(got[:, 1, :, :, 0], serve.e4m3(codes[:, 1, :, :, 0]), equal_nan=True)
 
 
 def test_requests_that_take_no_part(cb):
@@ -402,3 +405,107 @@ def test_pool_beyond_32_bits(cb):
     assert (np.abs(a - z) <= np.maximum(2.0 ** -4 * np.abs(a), 2.0 ** -10)).all()
     del raw, out, pages
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------ attention
+
+class BlockStep(Step):
+    """Step over pages with scales of their own; the numbers that its keys and values stand for.  Unused places hold the
+    NaN of e4m3, unused pages' scales are the largest."""
+
+    def __init__(self, cb, lens, H, G, d, ps, token_major=False, pad=0, seed=0, layers=2, layer=1, lo=-4, hi=5):
+        Step.__init__(self, cb, lens, H, G, d, ps, True, token_major, pad, seed, layers, layer)
+        P, rng = self.pool.shape[2], np.random.default_rng(seed + 1)
+        exps = np.full((layers, P, H, 2), 119)
+        static = self.scales[layer].double().cpu().numpy()             # Step's numbers have these in them
+        for r, (_, kv) in enumerate(lens):
+            k, v = self.K[r] / static[0][:, None, None], self.V[r] / static[1][:, None, None]
+            e = rng.integers(lo - 5, hi - 5, (-(-kv // ps), H, 2))
+            exps[layer, self.table[r, :len(e)]] = e
+            f = 2.0 ** np.repeat(e, ps, 0)[:kv].astype(float)               # [key][head][2]
+            self.K[r], self.V[r] = (np.round(x * 512) / 512 * f[:, :, z].T[..., None] for z, x in enumerate((k, v)))
+        self.scales = torch.tensor(2.0 ** exps.astype(float), dtype=torch.float32, device="cuda")
+
+
+BLOCKS = [(lens, H, G, d, ps, tm) for lens, H, G, d, ps, _, tm in CASES]
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("case", range(len(BLOCKS)))
+def test_attention(cb, serve, case, ws):
+    lens, H, G, d, ps, tm = BLOCKS[case]
+    s = BlockStep(cb, lens, H, G, d, ps, tm, pad=case % 3, seed=case)
+    s.run(ws=ws)
+    s.check(serve)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (33, 4), (64, 70), (2 ** 31 - 1, 0)])
+@pytest.mark.parametrize("case", [2, 3, 5, 7, 10, 11])
+def test_attention_window(cb, serve, case, window, sinks):
+    lens, H, G, d, ps, tm = BLOCKS[case]
+    s = BlockStep(cb, lens, H, G, d, ps, tm, pad=1, seed=case)
+    s.run(window, sinks)
+    s.check(serve, window, sinks)
+
+
+@pytest.mark.parametrize("d,ps", [(64, 16), (96, 24), (128, 64), (128, 7)])
+def test_attention_rows_in_many_parts(cb, serve, d, ps):
+    """Rows in dozens of parts, of single tokens and of chunks; the same bits every time."""
+    s = BlockStep(cb, [(1, 20000), (40, 12000), (3, 5000), (2, 300)], 2, 2, d, ps, pad=1, seed=80)
+    s.run()
+    s.check(serve)
+    a, al = s.out.clone(), s.lse.clone()
+    s.run()
+    assert torch.equal(a, s.out) and torch.equal(al, s.lse)
+    s.run(max_q=1)
+    s.check(serve)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_large_alike_chunks(cb, serve, d):
+    """Chunks that fill the chip with row tiles of 256: eight waves share K and V."""
+    s = BlockStep(cb, [(512, 700), (512, 512)], 16, 8, d, 32, seed=5)
+    s.run()
+    s.check(serve, rows=[1])
+
+
+def test_attention_of_scales_far_apart(cb, serve):
+    """Blocks 2^40 apart: the values' sizes, and scores of hundreds."""
+    for lens, G in (([(1, 100), (2, 60)], 2), ([(40, 90)], 4)):
+        s = BlockStep(cb, lens, 2, G, 64, 16, seed=6, lo=-36, hi=4)
+        s.run()
+        s.check(serve)
+
+
+@pytest.mark.parametrize("G,q,kv", [(2, 3, 60), (4, 40, 90), (1, 130, 130)])
+def test_attention_nan_stays_with_its_rows(cb, serve, G, q, kv):
+    """The NaN of e4m3 in a key or value that later rows see does not reach the rows before it."""
+    for z in range(2):
+        s = BlockStep(cb, [(q, kv)], 1, G, 64, 16, seed=8)
+        j = kv - q + q // 2
+        s.pool.view(torch.uint8)[s.layer, z, int(s.table[0, j // 16]), 0, j % 16, 3] = 0x7f
+        s.run()
+        got = f64(s.out)
+        early, late = got[:q // 2], got[q // 2:]
+        o, _, mag, smag = serve.attention(f64(s.q), s.K[0][0], s.V[0][0], kv, 64 ** -0.5)
+        tol = BF * 1.01 * np.abs(o) + mag * (BF * 1.01 + (2 * 72 * 2 * F32 * smag + (kv + 64) * 2 * F32)[..., None])
+        assert (np.abs(early - o[:q // 2]) <= tol[:q // 2]).all(), z
+        if z == 1:
+            assert np.isnan(late[..., 3]).all()
+            keep = [c for c in range(64) if c != 3]
+            assert (np.abs(late - o[q // 2:]) <= tol[q // 2:])[..., keep].all()
+        else:
+            assert np.isnan(late).all()
+
+
+@pytest.mark.parametrize("lens,G", [([(1, 100), (1, 70)], 4), ([(70, 200)], 2)])
+def test_attention_hidden_pages(cb, serve, lens, G):
+    """Entries outside the pool hide their keys; all of them: zeros and -inf."""
+    s = BlockStep(cb, lens, 1, G, 128, 16, seed=6)
+    table = s.table.copy()
+    table[0, 0], table[0, 3] = -1, s.pool.shape[2]
+    s.run(table=table)
+    s.check(serve, hidden=[set(range(16)) | set(range(48, 64))] + [set()] * (len(lens) - 1))
+    table[0, :] = 2 ** 31 - 1
+    s.run(table=table)
+    s.check(serve, hidden=[set(range(lens[0][1]))] + [set()] * (len(lens) - 1))
