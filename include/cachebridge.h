@@ -842,6 +842,74 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
 int64_t cb_attn_paged_workspace_bytes(int32_t n_tokens, int32_t n_reqs, int32_t n_qheads, int32_t n_heads,
                                       int32_t head_dim, int32_t max_q_len);
 
+/*
+ * Bounds of pages: the least and the greatest of every key channel,
+ *   bounds[layer][page][head][2][head_dim]   (0 least, 1 greatest; contiguous, the
+ *   pool's element type, 16-byte aligned; e4m3 numbers count in units of the scale of
+ *   the page's keys, so that bounds are exact),
+ * over the tokens of a page that its request holds (positions below kv_lens[r]).  Written for the
+ * layers layer0 .. layer0 + n_layers - 1 of the pages that the last q_lens[r] of
+ * request r's kv_lens[r] tokens lie in, as they are now: after a step has written
+ * its tokens (cb_page_write or cb_page_quantize), with the step's lengths; q_lens =
+ * kv_lens forms those of whole requests.  Other pages' bounds stay as they were, and so do those
+ * of pages outside the pool and of requests with q_lens <= 0, kv_lens < q_lens or
+ * above table_width * page_size.  A NaN among a channel's keys is both its bounds.
+ * max_q_len: the largest of q_lens, a hint that sizes the launch; a wrong one costs time
+ * only.  head_dim a multiple of 16 up to 256, page_size <= 2^24.
+ */
+cb_status cb_page_bounds(const cb_pages *pages, int32_t layer0, int32_t n_layers, void *bounds, int32_t n_reqs,
+                         const int32_t *q_lens, const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride,
+                         int32_t table_width, int32_t max_q_len, void *stream);
+
+/*
+ * The pages that every new token attends to in one layer.  A token at position p
+ * (q, q_starts and kv_lens as in cb_attn_paged) has the candidates i = 0 .. p / page_size
+ * whose table entry is inside the pool.  For each KV head, with the query heads u of
+ * its group and a candidate's bounds lo and hi,
+ *   score_i = sum_u sum_c max(q_u[c] lo[c], q_u[c] hi[c])
+ * bounds the sum of the group's scores of any key of the page from above (E4M3_BLOCKS:
+ * times the scale of the page's keys; E4M3: without the scale, which is the same for
+ * all).  It is formed in 64 bits from exact products and rounded to fp32 once; NaN
+ * counts as +infinity.  The first n_first pages, 0 .. n_first - 1, and the
+ * last n_last, those above p / page_size - n_last, are always taken, as far as they are
+ * candidates; of the others those with the highest scores, the lower page of two equal
+ * ones, until n_selected are taken or none is left:
+ *   selected[(token * n_heads + head) * n_selected + ...] (int32, device): the taken
+ *     pages' places in the request's table row, ascending, then -1.
+ * Tokens of no request leave theirs as they were.  n_first >= 0, n_last >= 1 (the token's own
+ * page, whose bounds may hold tokens behind it, is never judged by them), n_first
+ * + n_last <= n_selected.
+ *   bounds: of all layers, as cb_page_bounds writes them.
+ *   workspace: device memory for the scores, 4-byte aligned: cb_page_select_workspace_bytes,
+ *     or less, at least as much as for one token: tokens then take turns.  It keeps nothing
+ *     that another call reads; calls that overlap in time need one each.
+ * head_dim in {64, 96, 128}.
+ */
+cb_status cb_page_select(const cb_rows *q, const cb_pages *pages, int32_t layer, const void *bounds, int32_t n_reqs,
+                         const int32_t *q_starts, const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride,
+                         int32_t table_width, int32_t n_first, int32_t n_last, int32_t n_selected, int32_t *selected,
+                         void *workspace, int64_t workspace_bytes, void *stream);
+int64_t cb_page_select_workspace_bytes(int32_t n_tokens, int32_t n_heads, int32_t table_width);
+
+/*
+ * Attention of every new token over selected pages in one layer: cb_attn_paged with
+ * other keys.  The row of a token at position p and query head u sees the keys j <= p
+ * of KV head h = u / (n_qheads / n_heads) whose page's place j / page_size in the request's table
+ * row is among selected[(token * n_heads + h) * n_selected + 0 .. n_selected - 1]
+ * (as cb_page_select writes them, or any other order; entries below 0, or table_width and above,
+ * are none) and whose table entry is inside the pool.  A page that is listed twice
+ * counts twice.  Outputs, roundings, rows that see nothing, NaN and infinities in places that a row does not
+ * see, rows of no request and the other arguments as in cb_attn_paged;
+ * cb_attn_selected_workspace_bytes gives the workspace that the call can use, and with
+ * less rows are split less.  n_selected * page_size <= 2^30.
+ */
+cb_status cb_attn_selected(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,
+                           const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                           const int32_t *selected, int32_t n_selected, const cb_rows *out, float scale, float *lse,
+                           void *workspace, int64_t workspace_bytes, void *stream);
+int64_t cb_attn_selected_workspace_bytes(int32_t n_tokens, int32_t n_qheads, int32_t n_heads, int32_t head_dim,
+                                         int32_t page_size, int32_t n_selected);
+
 /* Static name of a status code. */
 const char *cb_status_string(cb_status status);
 

@@ -149,3 +149,28 @@ def page_quantize(rows, turned, codes, exps, spans, block_table):
                         codes[l, z, page, h, :at] = e4m3(codes[l, z, page, h, :at] * 2.0 ** (was - e))
                     codes[l, z, page, h, at:at + n] = y[t:t + n, l, z, h] * 2.0 ** -e
                     exps[l, page, h, z] = e
+
+
+# ------------------------------------------------------------------ selected pages
+
+def page_bounds(keys):
+    """Least and greatest of every channel of keys [token][d]; a NaN is both."""
+    return np.stack([keys.min(0), keys.max(0)])
+
+
+def page_scores(q, bounds):
+    """q [head of the group][d], bounds [page][2][d] float64: the pages' scores, rounded to 32 bits once."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        out = np.zeros(len(bounds))
+        for u in q:
+            out = out + (np.maximum(u, 0) * bounds[:, 1] + np.minimum(u, 0) * bounds[:, 0]).sum(-1)
+        return out.astype(np.float32)
+
+
+def page_select(scores, there, n_first, n_last, k):
+    """scores of the pages 0 .. own (the last), there: which of them are in the pool.  The chosen ones, ascending."""
+    own = len(scores) - 1
+    always = [i for i in range(own + 1) if there[i] and (i < n_first or i > own - n_last)]
+    s = np.where(np.isnan(scores), np.inf, scores)
+    rest = sorted((i for i in range(own + 1) if there[i] and i not in set(always)), key=lambda i: (-s[i], i))
+    return sorted(always + rest[:k - len(always)])

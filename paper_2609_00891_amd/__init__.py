@@ -696,6 +696,18 @@ _lib.cb_page_quantize.argtypes = [ctypes.POINTER(CbCache), ctypes.POINTER(CbPage
 _lib.cb_page_read.restype = ctypes.c_int
 _lib.cb_page_read.argtypes = [ctypes.POINTER(CbPages), _i32, ctypes.POINTER(CbCache)] + _SPANS + [
     ctypes.POINTER(CbRopeAxesSpec), _i32, _vp]
+_lib.cb_page_bounds.restype = ctypes.c_int
+_lib.cb_page_bounds.argtypes = [ctypes.POINTER(CbPages), _i32, _i32, _vp, _i32, _vp, _vp, _vp, _i64, _i32, _i32, _vp]
+_STEP = [ctypes.POINTER(CbRows), ctypes.POINTER(CbPages), _i32]
+_REQUESTS = [_i32, _vp, _vp, _vp, _i64, _i32]              # n_reqs, q_starts, kv_lens, block_table, stride, width
+_lib.cb_page_select.restype = ctypes.c_int
+_lib.cb_page_select.argtypes = _STEP + [_vp] + _REQUESTS + [_i32, _i32, _i32, _vp, _vp, _i64, _vp]
+_lib.cb_page_select_workspace_bytes.restype = _i64
+_lib.cb_page_select_workspace_bytes.argtypes = [_i32] * 3
+_lib.cb_attn_selected.restype = ctypes.c_int
+_lib.cb_attn_selected.argtypes = _STEP + _REQUESTS + [_vp, _i32, ctypes.POINTER(CbRows), ctypes.c_float, _vp, _vp, _i64, _vp]
+_lib.cb_attn_selected_workspace_bytes.restype = _i64
+_lib.cb_attn_selected_workspace_bytes.argtypes = [_i32] * 6
 _lib.cb_attn_paged.restype = ctypes.c_int
 _lib.cb_attn_paged.argtypes = [ctypes.POINTER(CbRows), ctypes.POINTER(CbPages), _i32, _i32, _vp, _vp, _vp, _i64, _i32,
                                ctypes.POINTER(CbRows), _i32, ctypes.c_float, _i32, _i32, _vp, _vp, _i64, _vp]
@@ -935,3 +947,95 @@ def cb_attn_paged(q: torch.Tensor, pages: CbPages, layer: int, q_starts: torch.T
                               _ptr(block_table), block_table.stride(0), block_table.shape[1], ctypes.byref(ov),
                               int(max_q_len), float(q.shape[2] ** -0.5 if scale is None else scale), int(window), int(sinks),
                               _ptr(lse), _ptr(workspace), int(ws_bytes), _stream_on(dev, stream)))
+
+
+def _bounds(bounds: torch.Tensor, pages: CbPages):
+    """Bounds belong to every page and KV head of a pool, in its type."""
+    c = pages.cache
+    dtype = torch.bfloat16 if pages.dtype == CB_PAGES_BF16 else torch.float8_e4m3fn
+    _need(bounds, (c.n_layers, c.n_seqs, c.n_heads, 2, c.head_dim), dtype, "bounds")
+    return _ptr(bounds)
+
+
+def _workspace(workspace: Optional[torch.Tensor]):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def cb_page_bounds(pages: CbPages, bounds: torch.Tensor, q_lens: torch.Tensor, kv_lens: torch.Tensor,
+                   block_table: torch.Tensor, max_q_len: int, layer: int = 0, layers: int = 1, stream=None):
+    """Least and greatest of every key channel, ``bounds`` [layer][page][head][2][dim] in the pool's type, of the pages
+    that the last ``q_lens[r]`` of each request's ``kv_lens[r]`` tokens lie in, in ``layers`` layers from ``layer`` on."""
+    _, _, q, kv, table, stride, width = spans = _spans(None, q_lens, kv_lens, block_table)
+    bv = _bounds(bounds, pages)
+    _fit_int32(layer, layers, max_q_len)
+    dev = _on_current_device("bounds q_lens kv_lens block_table pages scales", bounds, q_lens, kv_lens, block_table,
+                             *_kept(pages))
+    _check(_lib.cb_page_bounds(ctypes.byref(pages), int(layer), int(layers), bv, spans[0], q, kv, table, stride, width,
+                               int(max_q_len), _stream_on(dev, stream)))
+
+
+def cb_page_select_workspace_bytes(n_tokens: int, n_heads: int, table_width: int) -> int:
+    """Workspace bytes with which :func:`cb_page_select` works on all tokens at once."""
+    _fit_int32(n_tokens, n_heads, table_width)
+    return int(_lib.cb_page_select_workspace_bytes(int(n_tokens), int(n_heads), int(table_width)))
+
+
+def cb_page_select(q: torch.Tensor, pages: CbPages, layer: int, bounds: torch.Tensor, q_starts: torch.Tensor,
+                   kv_lens: torch.Tensor, block_table: torch.Tensor, selected: torch.Tensor, first: int = 1, last: int = 1,
+                   workspace: Optional[torch.Tensor] = None, stream=None):
+    """The pages that each new token attends to in the pool's ``layer``: ``selected`` int32 [token][KV head][pages] gets
+    the first ``first`` and the last ``last`` ones and those whose keys' scores are bounded highest (``bounds`` from
+    :func:`cb_page_bounds`), ascending, -1 behind them."""
+    n = kv_lens.numel()
+    qv = _rows_view(q, "q")
+    _ints(q_starts, n + 1, "q_starts")
+    _ints(kv_lens, n, "kv_lens")
+    _check_table(block_table, n)
+    bv = _bounds(bounds, pages)
+    if selected.dim() != 3:
+        raise ValueError("selected must be int32 [token][KV head][pages]")
+    _need(selected, (q.shape[0], pages.cache.n_heads, selected.shape[2]), torch.int32, "selected")
+    _fit_int32(layer, first, last)
+    ws, ws_bytes = _workspace(workspace)
+    dev = _on_current_device("q q_starts kv_lens block_table selected bounds workspace pages scales", q, q_starts, kv_lens,
+                             block_table, selected, bounds, workspace, *_kept(pages))
+    _check(_lib.cb_page_select(ctypes.byref(qv), ctypes.byref(pages), int(layer), bv, n, _ptr(q_starts), _ptr(kv_lens),
+                               _ptr(block_table), block_table.stride(0), block_table.shape[1], int(first), int(last),
+                               selected.shape[2], _ptr(selected), ws, ws_bytes, _stream_on(dev, stream)))
+
+
+def cb_attn_selected_workspace_bytes(n_tokens: int, n_qheads: int, n_heads: int, head_dim: int, page_size: int,
+                                     n_selected: int) -> int:
+    """Workspace bytes with which :func:`cb_attn_selected` splits rows as far as it wants to."""
+    _fit_int32(n_tokens, n_qheads, n_heads, head_dim, page_size, n_selected)
+    return int(_lib.cb_attn_selected_workspace_bytes(int(n_tokens), int(n_qheads), int(n_heads), int(head_dim),
+                                                     int(page_size), int(n_selected)))
+
+
+def cb_attn_selected(q: torch.Tensor, pages: CbPages, layer: int, q_starts: torch.Tensor, kv_lens: torch.Tensor,
+                     block_table: torch.Tensor, selected: torch.Tensor, out: torch.Tensor, scale: Optional[float] = None,
+                     lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """out[t, u] = attention of query q[t, u] over the keys up to its own position that lie in the pages ``selected``
+    [token][KV head][pages] for it, in the pool's ``layer``; otherwise as :func:`cb_attn_paged`."""
+    n = kv_lens.numel()
+    qv, ov = _rows_view(q, "q"), _rows_view(out, "out")
+    _ints(q_starts, n + 1, "q_starts")
+    _ints(kv_lens, n, "kv_lens")
+    _check_table(block_table, n)
+    if selected.dim() != 3:
+        raise ValueError("selected must be int32 [token][KV head][pages]")
+    _need(selected, (q.shape[0], pages.cache.n_heads, selected.shape[2]), torch.int32, "selected")
+    _fit_int32(layer)
+    if lse is not None:
+        _need(lse, (q.shape[0], q.shape[1]), torch.float32, "lse")
+    ws, ws_bytes = _workspace(workspace)
+    dev = _on_current_device("q q_starts kv_lens block_table selected out lse workspace pages scales", q, q_starts, kv_lens,
+                             block_table, selected, out, lse, workspace, *_kept(pages))
+    _check(_lib.cb_attn_selected(ctypes.byref(qv), ctypes.byref(pages), int(layer), n, _ptr(q_starts), _ptr(kv_lens),
+                                 _ptr(block_table), block_table.stride(0), block_table.shape[1], _ptr(selected),
+                                 selected.shape[2], ctypes.byref(ov), float(q.shape[2] ** -0.5 if scale is None else scale),
+                                 _ptr(lse), ws, ws_bytes, _stream_on(dev, stream)))

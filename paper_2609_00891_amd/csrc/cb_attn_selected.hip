@@ -1,0 +1,83 @@
+// cb_attn_selected.hip -- attention of every token over the pages that were selected
+// for it, on gfx950.
+//
+// Every token and KV head has a list of pages of its own, so what tokens could share
+// is the group's query heads: a row tile is one token's (up to 16) query heads of one KV
+// head, and rows_body (cb_attn_rows.h) reads the listed pages' keys as one list, 32 at a
+// time, each wave its own, from memory straight into matrix-core operands.  The list's
+// entry is read three tiles ahead of its keys, the table's two, so no load waits for
+// another.  The lists' length and not the contexts' decides the work, and the host knows
+// it: keys are divided among workgroups where rows are few, and joined in a second launch.
+#include "cb_serve_internal.h"
+#include "cb_paged_rules.h"
+#include "cb_attn_rows.h"
+
+namespace cb {
+namespace {
+
+template <int D, int EL>
+__global__ __launch_bounds__(256) void attn_selected_kernel(PagedArgs a) {
+    __shared__ SchedLds<4> sched;
+    __shared__ __attribute__((aligned(16))) RowsLds<D, 4> lds;
+    rows_body<D, EL, 4, true>(a, a.rows, blockIdx.x, sched, lds);
+}
+
+// Blocks take four rows of a tile, or one where a workgroup joins it.
+template <int D, int EL>
+__global__ __launch_bounds__(256) void attn_selected_join_kernel(PagedArgs a, FastDiv per) {
+    __shared__ JoinLds<D> lds;
+    const uint32_t head = blockIdx.x % (uint32_t)a.n_heads, idx = blockIdx.x / (uint32_t)a.n_heads;
+    const uint32_t unit = fast_div(idx, per);
+    Item it;
+    Request rq;
+    if (!selected_item(a, unit * a.sel_parts.d, it, rq)) return;
+    it.part = (int32_t)(idx - unit * per.d);
+    join_rows<D, 16, EL>(a, a.rows, it, rq, (int)head, lds);
+}
+
+constexpr int64_t kSlot = 16;           // rows of a partial result
+
+template <int D, int EL>
+hipError_t launch(PagedArgs a, void *ws, int64_t ws_bytes, hipStream_t s) {
+    const SelectedCut cut = selected_cut(a.n_tokens, a.n_heads, (int32_t)a.G.d, (int32_t)a.page_size.d, a.n_selected);
+    const int64_t units = (int64_t)a.n_tokens * cut.tiles, slot = kSlot * (D + 2) * 4;
+    const int64_t fits = ws_bytes / (units * a.n_heads * slot);
+    const int32_t parts = fits < 2 ? 1 : (int32_t)std::min<int64_t>(cut.parts, fits);
+    if (units * parts * a.n_heads > INT32_MAX) return hipErrorInvalidValue;
+    a.rows.ws = (float *)ws;
+    a.sel_parts = make_fastdiv((uint32_t)parts);
+    a.sel_tiles = make_fastdiv((uint32_t)cut.tiles);
+    hipLaunchKernelGGL((attn_selected_kernel<D, EL>), dim3((unsigned)(units * parts * a.n_heads)), dim3(256), 0, s, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (parts > 1) {
+        const uint32_t rows = std::min<uint32_t>(a.G.d, 16), per = parts > kWideParts ? rows : (rows + 3) / 4;
+        if (units * per * a.n_heads > INT32_MAX) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((attn_selected_join_kernel<D, EL>), dim3((unsigned)(units * per * a.n_heads)), dim3(256), 0, s, a, make_fastdiv(per));
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t attn_selected_workspace_bytes(int64_t n_tokens, int32_t n_heads, int32_t G, int32_t d, int32_t page_size,
+                                      int32_t n_selected) {
+    const SelectedCut cut = selected_cut(n_tokens, n_heads, G, page_size, n_selected);
+    return cut.parts > 1 ? n_tokens * cut.tiles * cut.parts * n_heads * kSlot * (d + 2) * 4 : 0;
+}
+
+hipError_t launch_attn_selected(const PagedArgs &a, int32_t d, int32_t dtype, void *ws, int64_t ws_bytes, hipStream_t s) {
+    switch (d * 4 + dtype) {
+        case 256 + CB_PAGES_BF16: return launch<64, kBf16>(a, ws, ws_bytes, s);
+        case 256 + CB_PAGES_E4M3: return launch<64, kE4m3>(a, ws, ws_bytes, s);
+        case 256 + CB_PAGES_E4M3_BLOCKS: return launch<64, kBlocks>(a, ws, ws_bytes, s);
+        case 384 + CB_PAGES_BF16: return launch<96, kBf16>(a, ws, ws_bytes, s);
+        case 384 + CB_PAGES_E4M3: return launch<96, kE4m3>(a, ws, ws_bytes, s);
+        case 384 + CB_PAGES_E4M3_BLOCKS: return launch<96, kBlocks>(a, ws, ws_bytes, s);
+        case 512 + CB_PAGES_BF16: return launch<128, kBf16>(a, ws, ws_bytes, s);
+        case 512 + CB_PAGES_E4M3: return launch<128, kE4m3>(a, ws, ws_bytes, s);
+        case 512 + CB_PAGES_E4M3_BLOCKS: return launch<128, kBlocks>(a, ws, ws_bytes, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace cb

@@ -132,4 +132,14 @@ inline RowsCut rows_cut(int64_t n_tokens, int32_t n_rows, int32_t head_dim, bool
     return c;
 }
 
+// Host side: attention over n_selected pages of every token: row tiles of 16 query heads of one KV head, the listed keys in
+// tiles of 32, each row tile's in parts for about 2,048 workgroups, of 16 tiles or more, where it has 36 or more (the
+// same division as of single tokens over all their pages).
+struct SelectedCut { int32_t tiles, parts; };
+inline SelectedCut selected_cut(int64_t n_tokens, int32_t H, int32_t G, int32_t page_size, int32_t n_selected) {
+    const int32_t tiles = (G + 15) / 16;
+    const int64_t keys = ((int64_t)n_selected * page_size + 31) / 32;
+    return {tiles, parts_of(keys, part_tiles(n_tokens * tiles * keys, H, 2048, 16), 36)};
+}
+
 }  // namespace cb

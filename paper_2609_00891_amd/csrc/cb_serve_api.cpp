@@ -204,6 +204,75 @@ cb_status prepare_spans(const cb_cache &pool, int32_t n_reqs, const int32_t *row
     return CB_OK;
 }
 
+// Queries, pages and requests of a call on new tokens and one layer.  NULL arrays are refused where there are tokens.
+cb_status prepare_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,
+                        const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                        cb::PagedArgs &a) {
+    const cb_cache &c = pages->cache;
+    if (q->n_heads % c.n_heads) return fail(CB_ERR_SHAPE, "%d query heads are no multiple of %d KV heads", q->n_heads, c.n_heads);
+    if (n_reqs < 0) return fail(CB_ERR_INVALID_ARGUMENT, "n_reqs is negative");
+    if (table_width < 0) return fail(CB_ERR_INVALID_ARGUMENT, "table_width is negative");
+    if (n_reqs > 1 && table_stride < table_width)
+        return fail(CB_ERR_SHAPE, "table_stride (%lld) < table_width (%d)", (long long)table_stride, table_width);
+    if ((int64_t)table_width * c.seq_len > INT32_MAX)
+        return fail(CB_ERR_UNSUPPORTED, "table_width * page size must be below 2^31");
+    if (((uintptr_t)q_starts) % 4 || ((uintptr_t)kv_lens) % 4 || ((uintptr_t)block_table) % 4)
+        return fail(CB_ERR_MISALIGNED, "lengths and tables must be 4-byte aligned");
+    if (q->n_tokens > 0 && n_reqs > 0 && (!q_starts || !kv_lens || (table_width > 0 && !block_table)))
+        return fail(CB_ERR_INVALID_ARGUMENT, "q_starts, kv_lens and block_table must be non-NULL");
+    const int el = element_bytes(pages);
+    a.q = (const uint16_t *)q->data;
+    a.q_tok = q->s_tok;
+    a.q_head = q->s_head;
+    a.n_tokens = q->n_tokens;
+    a.k = (const char *)c.data + (int64_t)layer * c.s_layer * el;
+    a.v = a.k + c.s_kv * el;
+    a.s_page = (uint32_t)(c.s_seq * el / 16);
+    a.s_tok = (uint32_t)(c.s_tok * el / 16);
+    a.s_head = c.s_head * el;
+    a.n_pages = c.n_seqs;
+    a.page_size = cb::make_fastdiv((uint32_t)c.seq_len);
+    a.q_starts = q_starts;
+    a.kv_lens = kv_lens;
+    a.table = block_table;
+    a.table_stride = table_stride;
+    a.table_width = table_width;
+    a.n_reqs = n_reqs;
+    a.n_heads = c.n_heads;
+    a.G = cb::make_fastdiv((uint32_t)(q->n_heads / c.n_heads));
+    if (pages->dtype == CB_PAGES_E4M3_BLOCKS) {
+        a.kscale = pages->scales + (int64_t)layer * c.n_seqs * c.n_heads * 2;
+    } else if (el == 1) {
+        a.kscale = pages->scales + (int64_t)layer * 2 * c.n_heads;
+        a.vscale = a.kscale + c.n_heads;
+    }
+    return CB_OK;
+}
+
+// The pool, layer and widths of a call on new tokens, before its other arguments.
+cb_status check_layer(const cb_pages *pages, int32_t layer) {
+    if (cb_status s = check_pages(pages)) return s;
+    const cb_cache &c = pages->cache;
+    if (c.head_dim != 64 && c.head_dim != 96 && c.head_dim != 128)
+        return fail(CB_ERR_UNSUPPORTED, "head_dim must be 64, 96 or 128 (got %d)", c.head_dim);
+    if (layer < 0 || layer >= c.n_layers) return fail(CB_ERR_INVALID_ARGUMENT, "layer %d is outside the pool's %d", layer, c.n_layers);
+    return CB_OK;
+}
+
+// Outputs and scale of an attention call.
+cb_status prepare_out(const cb_rows *q, const cb_rows *out, int d, float scale, float *lse, cb::PagedArgs &a) {
+    if (cb_status s = check_rows_written("out", out, d)) return s;
+    if (out->n_tokens != q->n_tokens || out->n_heads != q->n_heads) return fail(CB_ERR_SHAPE, "q and out disagree on tokens or heads");
+    a.scale_log2 = scale * 1.4426950408889634f;
+    if (!std::isfinite(a.scale_log2)) return fail(CB_ERR_INVALID_ARGUMENT, "scale must be finite (and so scale * log2 e)");
+    if (((uintptr_t)lse) % 4) return fail(CB_ERR_MISALIGNED, "lse must be 4-byte aligned");
+    a.out = (uint16_t *)out->data;
+    a.o_tok = out->s_tok;
+    a.o_head = out->s_head;
+    a.lse = lse;
+    return CB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -369,70 +438,128 @@ cb_status cb_attn_paged(const cb_rows *q, const cb_pages *pages, int32_t layer, 
                         const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
                         const cb_rows *out, int32_t max_q_len, float scale, int32_t window, int32_t n_sinks, float *lse,
                         void *workspace, int64_t workspace_bytes, void *stream) {
-    if (cb_status s = check_pages(pages)) return s;
-    const cb_cache &c = pages->cache;
-    const int d = c.head_dim;
-    if (d != 64 && d != 96 && d != 128) return fail(CB_ERR_UNSUPPORTED, "head_dim must be 64, 96 or 128 (got %d)", d);
-    if (layer < 0 || layer >= c.n_layers) return fail(CB_ERR_INVALID_ARGUMENT, "layer %d is outside the pool's %d", layer, c.n_layers);
+    if (cb_status s = check_layer(pages, layer)) return s;
+    const int d = pages->cache.head_dim;
     if (cb_status s = check_rows("q", q, d)) return s;
-    if (cb_status s = check_rows_written("out", out, d)) return s;
-    if (out->n_tokens != q->n_tokens || out->n_heads != q->n_heads) return fail(CB_ERR_SHAPE, "q and out disagree on tokens or heads");
-    if (q->n_heads % c.n_heads) return fail(CB_ERR_SHAPE, "%d query heads are no multiple of %d KV heads", q->n_heads, c.n_heads);
-    if (n_reqs < 0) return fail(CB_ERR_INVALID_ARGUMENT, "n_reqs is negative");
-    if (table_width < 0) return fail(CB_ERR_INVALID_ARGUMENT, "table_width is negative");
-    if (n_reqs > 1 && table_stride < table_width)
-        return fail(CB_ERR_SHAPE, "table_stride (%lld) < table_width (%d)", (long long)table_stride, table_width);
-    if ((int64_t)table_width * c.seq_len > INT32_MAX)
-        return fail(CB_ERR_UNSUPPORTED, "table_width * page size must be below 2^31");
+    cb::PagedArgs a = {};
+    if (cb_status s = prepare_out(q, out, d, scale, lse, a)) return s;
+    if (cb_status s = prepare_paged(q, pages, layer, n_reqs, q_starts, kv_lens, block_table, table_stride, table_width, a)) return s;
     if (max_q_len < 0) return fail(CB_ERR_INVALID_ARGUMENT, "max_q_len is negative");
-    const float scale_log2 = scale * 1.4426950408889634f;
-    if (!std::isfinite(scale_log2)) return fail(CB_ERR_INVALID_ARGUMENT, "scale must be finite (and so scale * log2 e)");
     if (window < 0 || n_sinks < 0) return fail(CB_ERR_INVALID_ARGUMENT, "window and n_sinks must be >= 0");
     if (workspace_bytes < 0) return fail(CB_ERR_INVALID_ARGUMENT, "workspace_bytes is negative");
-    if (((uintptr_t)workspace) % 16 || ((uintptr_t)lse) % 4 || ((uintptr_t)q_starts) % 4 || ((uintptr_t)kv_lens) % 4 ||
-        ((uintptr_t)block_table) % 4)
-        return fail(CB_ERR_MISALIGNED, "workspace must be 16-byte, the other arrays 4-byte aligned");
+    if (((uintptr_t)workspace) % 16) return fail(CB_ERR_MISALIGNED, "workspace must be 16-byte aligned");
     if (q->n_tokens == 0 || n_reqs == 0) return cb::api_ok();
-    if (!q_starts || !kv_lens || (table_width > 0 && !block_table))
-        return fail(CB_ERR_INVALID_ARGUMENT, "q_starts, kv_lens and block_table must be non-NULL");
     if (q->data == out->data) return fail(CB_ERR_INVALID_ARGUMENT, "out must not be q");
-    const int el = element_bytes(pages);
-    cb::PagedArgs a = {};
-    a.q = (const uint16_t *)q->data;
-    a.out = (uint16_t *)out->data;
-    a.q_tok = q->s_tok;
-    a.q_head = q->s_head;
-    a.o_tok = out->s_tok;
-    a.o_head = out->s_head;
-    a.n_tokens = q->n_tokens;
-    a.k = (const char *)c.data + (int64_t)layer * c.s_layer * el;
-    a.v = a.k + c.s_kv * el;
-    a.s_page = (uint32_t)(c.s_seq * el / 16);
-    a.s_tok = (uint32_t)(c.s_tok * el / 16);
-    a.s_head = c.s_head * el;
-    a.n_pages = c.n_seqs;
-    a.page_size = cb::make_fastdiv((uint32_t)c.seq_len);
-    a.q_starts = q_starts;
-    a.kv_lens = kv_lens;
-    a.table = block_table;
-    a.table_stride = table_stride;
-    a.table_width = table_width;
-    a.n_reqs = n_reqs;
-    a.n_heads = c.n_heads;
-    a.G = cb::make_fastdiv((uint32_t)(q->n_heads / c.n_heads));
-    a.scale_log2 = scale_log2;
-    if (pages->dtype == CB_PAGES_E4M3_BLOCKS) {
-        a.kscale = pages->scales + (int64_t)layer * c.n_seqs * c.n_heads * 2;
-    } else if (el == 1) {
-        a.kscale = pages->scales + (int64_t)layer * 2 * c.n_heads;
-        a.vscale = a.kscale + c.n_heads;
-    }
     a.window = window;
     a.n_sinks = n_sinks;
-    a.lse = lse;
     if (cb::launch_attn_paged(a, d, pages->dtype, max_q_len, workspace, workspace ? workspace_bytes : 0, (hipStream_t)stream) !=
         hipSuccess)
         return fail(CB_ERR_DEVICE, "paged attention launch failed");
+    return cb::api_ok();
+}
+
+cb_status cb_page_bounds(const cb_pages *pages, int32_t layer0, int32_t n_layers, void *bounds, int32_t n_reqs,
+                         const int32_t *q_lens, const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride,
+                         int32_t table_width, int32_t max_q_len, void *stream) {
+    if (cb_status s = check_pages(pages)) return s;
+    const cb_cache &c = pages->cache;
+    if (cb_status s = check_width(c.head_dim)) return s;
+    if (cb_status s = check_layers(layer0, n_layers, c)) return s;
+    if ((int64_t)n_layers * c.n_heads > 4 * 65535) return fail(CB_ERR_UNSUPPORTED, "too many (layer, head) rows");
+    cb::SpanArgs sp = {};
+    if (cb_status s = prepare_spans(c, n_reqs, nullptr, false, q_lens, kv_lens, block_table, table_stride, table_width, sp)) return s;
+    if (max_q_len < 0) return fail(CB_ERR_INVALID_ARGUMENT, "max_q_len is negative");
+    if (((uintptr_t)bounds) % 16) return fail(CB_ERR_MISALIGNED, "bounds must be 16-byte aligned");
+    if (n_reqs == 0) return cb::api_ok();
+    if (!bounds) return fail(CB_ERR_INVALID_ARGUMENT, "bounds is NULL");
+    const int el = element_bytes(pages);
+    cb::BoundsArgs a = {};
+    a.k = (const char *)c.data + (int64_t)layer0 * c.s_layer * el;
+    a.s_layer = c.s_layer * el;
+    a.s_page = c.s_seq * el;
+    a.s_head = c.s_head * el;
+    a.s_tok = c.s_tok * el;
+    a.bounds = (char *)bounds;
+    a.n_heads = cb::make_fastdiv((uint32_t)c.n_heads);
+    a.n_lh = n_layers * c.n_heads;
+    a.layer0 = layer0;
+    a.chunks = c.head_dim * el / 16;
+    if (cb::launch_page_bounds(a, sp, el == 1, max_q_len, (hipStream_t)stream) != hipSuccess)
+        return fail(CB_ERR_DEVICE, "page bounds launch failed");
+    return cb::api_ok();
+}
+
+int64_t cb_page_select_workspace_bytes(int32_t n_tokens, int32_t n_heads, int32_t table_width) {
+    if (n_tokens <= 0 || n_heads <= 0 || table_width <= 0) return 0;
+    const __int128 all = (__int128)n_tokens * n_heads * table_width * 4;
+    return all > INT64_MAX ? INT64_MAX : (int64_t)all;
+}
+
+cb_status cb_page_select(const cb_rows *q, const cb_pages *pages, int32_t layer, const void *bounds, int32_t n_reqs,
+                         const int32_t *q_starts, const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride,
+                         int32_t table_width, int32_t n_first, int32_t n_last, int32_t n_selected, int32_t *selected,
+                         void *workspace, int64_t workspace_bytes, void *stream) {
+    if (cb_status s = check_layer(pages, layer)) return s;
+    const cb_cache &c = pages->cache;
+    if (cb_status s = check_rows("q", q, c.head_dim)) return s;
+    cb::SelectArgs a = {};
+    if (cb_status s = prepare_paged(q, pages, layer, n_reqs, q_starts, kv_lens, block_table, table_stride, table_width, a.a)) return s;
+    if (n_first < 0 || n_last < 1) return fail(CB_ERR_INVALID_ARGUMENT, "n_first must be >= 0 and n_last >= 1");
+    if ((int64_t)n_first + n_last > n_selected)
+        return fail(CB_ERR_INVALID_ARGUMENT, "n_first + n_last must not exceed n_selected (%d)", n_selected);
+    if (c.n_heads > 65535 || table_width > 65535 * 256) return fail(CB_ERR_UNSUPPORTED, "too many KV heads or table entries");
+    if (workspace_bytes < 0) return fail(CB_ERR_INVALID_ARGUMENT, "workspace_bytes is negative");
+    if (((uintptr_t)bounds) % 16 || ((uintptr_t)selected) % 4 || ((uintptr_t)workspace) % 4)
+        return fail(CB_ERR_MISALIGNED, "bounds must be 16-byte, selected and workspace 4-byte aligned");
+    if (q->n_tokens == 0 || n_reqs == 0) return cb::api_ok();
+    if (!bounds || !selected) return fail(CB_ERR_INVALID_ARGUMENT, "bounds and selected must be non-NULL");
+    const int64_t least = cb_page_select_workspace_bytes(1, c.n_heads, table_width);
+    if (!workspace) workspace_bytes = 0;
+    if (workspace_bytes < least)
+        return fail(CB_ERR_SHAPE, "the workspace has %lld bytes, one token needs %lld", (long long)workspace_bytes, (long long)least);
+    a.bounds = (const char *)bounds + (int64_t)layer * c.n_seqs * c.n_heads * 2 * c.head_dim * element_bytes(pages);
+    a.n_first = n_first;
+    a.n_last = n_last;
+    a.n_selected = n_selected;
+    a.selected = selected;
+    if (cb::launch_page_select(a, c.head_dim, pages->dtype, workspace, workspace_bytes, (hipStream_t)stream) != hipSuccess)
+        return fail(CB_ERR_DEVICE, "page select launch failed");
+    return cb::api_ok();
+}
+
+int64_t cb_attn_selected_workspace_bytes(int32_t n_tokens, int32_t n_qheads, int32_t n_heads, int32_t head_dim,
+                                         int32_t page_size, int32_t n_selected) {
+    if (n_tokens <= 0 || n_heads <= 0 || n_qheads <= 0 || n_qheads % n_heads || head_dim <= 0 || page_size <= 0 || n_selected <= 0 ||
+        (int64_t)n_selected * page_size > (1 << 30))
+        return 0;
+    return cb::attn_selected_workspace_bytes(n_tokens, n_heads, n_qheads / n_heads, head_dim, page_size, n_selected);
+}
+
+cb_status cb_attn_selected(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,
+                           const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,
+                           const int32_t *selected, int32_t n_selected, const cb_rows *out, float scale, float *lse,
+                           void *workspace, int64_t workspace_bytes, void *stream) {
+    if (cb_status s = check_layer(pages, layer)) return s;
+    const cb_cache &c = pages->cache;
+    if (cb_status s = check_rows("q", q, c.head_dim)) return s;
+    cb::PagedArgs a = {};
+    if (cb_status s = prepare_out(q, out, c.head_dim, scale, lse, a)) return s;
+    if (cb_status s = prepare_paged(q, pages, layer, n_reqs, q_starts, kv_lens, block_table, table_stride, table_width, a)) return s;
+    if (n_selected < 1) return fail(CB_ERR_INVALID_ARGUMENT, "n_selected must be positive (got %d)", n_selected);
+    if ((int64_t)n_selected * c.seq_len > (1 << 30)) return fail(CB_ERR_UNSUPPORTED, "n_selected * page size must not exceed 2^30");
+    if (workspace_bytes < 0) return fail(CB_ERR_INVALID_ARGUMENT, "workspace_bytes is negative");
+    if (((uintptr_t)workspace) % 16 || ((uintptr_t)selected) % 4)
+        return fail(CB_ERR_MISALIGNED, "workspace must be 16-byte, selected 4-byte aligned");
+    if (q->n_tokens == 0 || n_reqs == 0) return cb::api_ok();
+    if (!selected) return fail(CB_ERR_INVALID_ARGUMENT, "selected is NULL");
+    if (q->data == out->data) return fail(CB_ERR_INVALID_ARGUMENT, "out must not be q");
+    if ((int64_t)q->n_tokens * ((a.G.d + 15) / 16) * c.n_heads > INT32_MAX)
+        return fail(CB_ERR_UNSUPPORTED, "too many (token, head) rows in one call");
+    a.selected = selected;
+    a.n_selected = n_selected;
+    if (cb::launch_attn_selected(a, c.head_dim, pages->dtype, workspace, workspace ? workspace_bytes : 0, (hipStream_t)stream) !=
+        hipSuccess)
+        return fail(CB_ERR_DEVICE, "selected attention launch failed");
     return cb::api_ok();
 }
 

@@ -112,6 +112,16 @@ struct PagedArgs {
     FastDiv sel_parts, sel_tiles;   // parts of a row tile, row tiles of a token
 };
 
+// The choice of pages (cb_page_select).
+struct SelectArgs {
+    PagedArgs a;              // queries, requests, table, scales
+    const char *bounds;       // of the layer: [page][head][2][head_dim]
+    int32_t n_first, n_last, n_selected;
+    int32_t *selected;        // [n_tokens][n_heads][n_selected]
+    uint32_t *keys;           // [tok1 - tok0][n_heads][table_width] scores of a round's tokens, as numbers of their order
+    int32_t tok0, tok1;
+};
+
 // Launchers (return hipError_t of the launch).
 hipError_t launch_page_tables(const PageTablesArgs &a, hipStream_t s);
 hipError_t launch_rows(RowsArgs a, bool rope, bool f8, hipStream_t s);
@@ -120,6 +130,9 @@ hipError_t launch_page_read(RowsArgs a, const SpanArgs &span, bool rope, int32_t
 hipError_t launch_page_bounds(BoundsArgs a, const SpanArgs &span, bool f8, int32_t max_q_len, hipStream_t s);
 hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, int32_t dtype, int32_t max_q_len, void *ws, int64_t ws_bytes,
                              hipStream_t s);
+hipError_t launch_page_select(const SelectArgs &s, int32_t d, int32_t dtype, void *ws, int64_t ws_bytes, hipStream_t stream);
+hipError_t launch_attn_selected(const PagedArgs &a, int32_t d, int32_t dtype, void *ws, int64_t ws_bytes, hipStream_t s);
+int64_t attn_selected_workspace_bytes(int64_t n_tokens, int32_t n_heads, int32_t G, int32_t d, int32_t page_size, int32_t n_selected);
 int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_reqs, int32_t max_q_len);
 
 }  // namespace cb

@@ -1,0 +1,546 @@
+"""GPU tests of attention over selected pages: bounds of pages, the choice of pages, attention over them, against the
+plain fp64 forms of ``oracle.serve``.  Bounds and choices are exact; tolerances of attention as in ``test_gpu_serve``."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_serve import BF, F32, THETA, Step, cb, f64, gen, i32, randn, serve  # noqa: F401
+from test_gpu_serve_blocks import BlockStep
+
+pytestmark = pytest.mark.gpu
+
+
+def make_step(cb, kind, lens, H, G, d, ps, **kw):
+    return BlockStep(cb, lens, H, G, d, ps, **kw) if kind == "blocks" else Step(cb, lens, H, G, d, ps, kind == "e4m3", **kw)
+
+
+def stored_keys(s, r):
+    """Request r's keys [head][key][d] in units of their scale, as bounds count them."""
+    _, kv = s.lens[r]
+    k = s.pool[s.layer, 0].float().double().cpu().numpy()
+    return np.stack([np.concatenate([k[int(s.table[r, j // s.ps]), h, :min(s.ps, kv - j)] for j in range(0, kv, s.ps)])
+                     for h in range(s.H)])
+
+
+def empty_bounds(s, value=3.0):
+    L, _, P, H, _, d = s.pool.shape
+    return torch.full((L, P, H, 2, d), value, device="cuda").to(s.pool.dtype)
+
+
+def all_bounds(cb, s):
+    b = empty_bounds(s)
+    kv = i32([k for _, k in s.lens])
+    cb.cb_page_bounds(cb.page_pool(s.pool, s.scales), b, kv, kv, i32(s.table), max(k for _, k in s.lens), layer=s.layer)
+    return b
+
+
+# ------------------------------------------------------------------ bounds
+
+@pytest.mark.parametrize("kind,d,ps,tm", [("bf16", 64, 16, False), ("bf16", 128, 7, True), ("bf16", 96, 64, False),
+                                          ("e4m3", 64, 24, True), ("blocks", 128, 16, False), ("blocks", 96, 100, True)])
+def test_bounds(cb, serve, kind, d, ps, tm):
+    """The pages of the new tokens in one layer of three, the others' bounds left as they were."""
+    lens = [(1, 1), (1, ps), (3, 2 * ps + 1), (2 * ps, 3 * ps), (0, 9), (5, 40)]
+    s = make_step(cb, kind, lens, 3, 1, d, ps, token_major=tm, layers=3, layer=1, seed=d + ps)
+    b = empty_bounds(s)
+    before = f64(b)
+    for hint in (1, 0, 500):
+        cb.cb_page_bounds(cb.page_pool(s.pool, s.scales), b, i32([q for q, _ in lens]), i32([k for _, k in lens]), i32(s.table),
+                          hint, layer=1)
+    want = before.copy()
+    for r, (q, kv) in enumerate(lens):
+        x = stored_keys(s, r)
+        for i in range((kv - q) // ps, (kv - 1) // ps + 1) if q else ():
+            for h in range(3):
+                want[1, int(s.table[r, i]), h] = serve.page_bounds(x[h, i * ps:min(kv, (i + 1) * ps)])
+    assert np.array_equal(f64(b), want)
+
+
+@pytest.mark.parametrize("d", [16, 48, 80, 256])
+def test_bounds_of_other_widths_in_several_layers(cb, serve, d):
+    g = gen(d)
+    pool = randn(g, 3, 2, 5, 2, 8, d).cuda()
+    b = torch.zeros((3, 5, 2, 2, d), dtype=torch.bfloat16, device="cuda")
+    cb.cb_page_bounds(cb.page_pool(pool), b, i32([20]), i32([20]), i32([[4, 0, 2]]), 20, layer=1, layers=2)
+    for l in (1, 2):
+        for i, p in enumerate((4, 0, 2)):
+            for h in range(2):
+                assert np.array_equal(f64(b[l, p, h]), serve.page_bounds(f64(pool[l, 0, p, h, :min(8, 20 - 8 * i)])))
+    assert (b[0] == 0).all() and (b[:, [1, 3]] == 0).all()
+
+
+def test_bounds_of_nan_and_infinity(cb):
+    pool = randn(gen(1), 1, 2, 2, 1, 4, 64).cuda()
+    pool[0, 0, 0, 0, 2, 5], pool[0, 0, 0, 0, 1, 7], pool[0, 0, 0, 0, 3, 8] = float("nan"), float("inf"), -float("inf")
+    b = torch.zeros((1, 2, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    cb.cb_page_bounds(cb.page_pool(pool), b, i32([4]), i32([4]), i32([[0]]), 4)
+    assert b[0, 0, 0, :, 5].isnan().all() and b[0, 0, 0, 1, 7] == float("inf") and b[0, 0, 0, 0, 8] == -float("inf")
+    assert b[0, 0, 0].isnan().sum() == 2
+
+
+def test_bounds_of_requests_that_take_no_part(cb):
+    pool = randn(gen(2), 1, 2, 3, 1, 4, 64).cuda()
+    b = torch.full((1, 3, 1, 2, 64), 2.0, dtype=torch.bfloat16, device="cuda")
+    cb.cb_page_bounds(cb.page_pool(pool), b, i32([0, -1, 3, 4, 1]), i32([3, 3, 2, 9, 4]), i32([[0, 1], [0, 1], [1, 0], [1, 2], [3, 0]]), 4)
+    assert (b == 2.0).all()
+
+
+# ------------------------------------------------------------------ selection
+
+def choose(cb, s, b, k, first, last, q=None, table=None, kv=None, rows=None):
+    n = s.n if q is None else q.shape[0]
+    sel = torch.full((n, s.H, k), -7, dtype=torch.int32, device="cuda")
+    width = s.table.shape[1]
+    need = cb.cb_page_select_workspace_bytes(n if rows is None else rows, s.H, width)
+    ws = torch.empty((need,), dtype=torch.uint8, device="cuda")
+    cb.cb_page_select(s.q if q is None else q, cb.page_pool(s.pool, s.scales), s.layer, b, i32(s.starts),
+                      i32([c for _, c in s.lens] if kv is None else kv), i32(s.table if table is None else table), sel,
+                      first=first, last=last, workspace=ws)
+    torch.cuda.synchronize()
+    return sel.cpu().numpy()
+
+
+def expected(serve, s, b, k, first, last, table=None):
+    """As the definition says, token by token."""
+    table = s.table if table is None else table
+    P, ps, G = s.pool.shape[2], s.ps, s.G
+    bn, qd = f64(b)[s.layer], f64(s.q)
+    out = np.full((s.n, s.H, k), -7)
+    for r, (nq, kv) in enumerate(s.lens):
+        there = (table[r] >= 0) & (table[r] < P)
+        pages = np.where(there, table[r], 0)
+        for h in range(s.H):
+            f = np.ones(len(pages))
+            if s.scales is not None and s.scales.dim() == 4:
+                f = s.scales[s.layer, :, h, 0].double().cpu().numpy()[pages]
+            for t in range(nq):
+                p = kv - nq + t
+                row = out[s.starts[r] + t, h]
+                row[:] = -1
+                if p < 0:
+                    continue
+                m = p // ps + 1
+                scores = serve.page_scores(qd[s.starts[r] + t, h * G:(h + 1) * G], bn[pages[:m], h] * f[:m, None, None])
+                got = serve.page_select(scores, there[:m], first, last, k)
+                row[:len(got)] = got
+    return out
+
+
+SELECT = [
+    # kind, lens, H, G, d, page, k, first, last
+    ("bf16", [(1, 1)], 1, 1, 64, 16, 3, 1, 1),
+    ("bf16", [(1, 300), (1, 77), (1, 16), (1, 17)], 2, 4, 128, 16, 5, 1, 2),
+    ("bf16", [(3, 200), (0, 40), (5, 5), (1, 700)], 1, 2, 96, 7, 9, 0, 1),
+    ("e4m3", [(1, 900), (1, 33)], 2, 8, 64, 16, 16, 2, 2),
+    ("blocks", [(1, 1000), (2, 500)], 2, 5, 128, 16, 12, 1, 2),
+    ("blocks", [(40, 800), (17, 17)], 1, 3, 96, 24, 6, 0, 1),
+    ("bf16", [(35, 600)], 2, 1, 64, 1, 40, 1, 3),
+    ("blocks", [(1, 9000), (1, 3)], 1, 16, 64, 8, 64, 1, 1),
+    ("bf16", [(16, 1200), (16, 300)], 1, 40, 128, 64, 8, 1, 1),
+    ("e4m3", [(2, 20000)], 1, 2, 128, 16, 1000, 4, 30),
+]
+
+
+@pytest.mark.parametrize("case", range(len(SELECT)))
+def test_select(cb, serve, case):
+    kind, lens, H, G, d, ps, k, first, last = SELECT[case]
+    s = make_step(cb, kind, lens, H, G, d, ps, pad=case % 3, seed=case)
+    b = all_bounds(cb, s)
+    got = choose(cb, s, b, k, first, last)
+    assert np.array_equal(got, expected(serve, s, b, k, first, last))
+    for rows in (1, 3):                                         # the tokens take turns
+        assert np.array_equal(choose(cb, s, b, k, first, last, rows=rows), got)
+
+
+def test_select_equal_scores_go_to_the_lower_page(cb, serve):
+    """Pages with the same bounds, and queries of zero, whose scores are all zeros, of both signs."""
+    s = make_step(cb, "bf16", [(1, 640), (3, 320)], 2, 2, 64, 16, seed=3)
+    b = all_bounds(cb, s)
+    for r in range(2):
+        rows = torch.tensor(s.table[r][s.table[r] >= 0], device="cuda").long()
+        b[s.layer, rows] = b[s.layer, rows[torch.arange(len(rows), device="cuda") % 5]]
+    s.q[1] = 0
+    s.q[2] = -0.0
+    for k, first, last in ((7, 1, 2), (2, 0, 1), (30, 3, 1)):
+        got = choose(cb, s, b, k, first, last)
+        assert np.array_equal(got, expected(serve, s, b, k, first, last))
+
+
+def test_select_scores_in_the_last_places(cb, serve):
+    """Scores that 32-bit sums would confuse: large terms that cancel beside the small ones that decide."""
+    s = make_step(cb, "bf16", [(2, 512)], 1, 4, 128, 16, seed=4)
+    b = all_bounds(cb, s)
+    s.q[:, :, 0], s.q[:, :, 1] = 2.0 ** 12, 2.0 ** 12
+    b[s.layer, :, :, :, 0], b[s.layer, :, :, :, 1] = 2.0 ** 11, -2.0 ** 11
+    got = choose(cb, s, b, 6, 1, 1)
+    assert np.array_equal(got, expected(serve, s, b, 6, 1, 1))
+
+
+def test_select_nan_and_infinity_come_first(cb, serve):
+    s = make_step(cb, "bf16", [(1, 400), (1, 350)], 1, 2, 64, 16, seed=5)
+    b = all_bounds(cb, s)
+    for i, v in ((7, float("nan")), (3, float("inf")), (11, -float("inf"))):
+        b[s.layer, int(s.table[0, i]), 0, 1, 9] = v
+    s.q[1, 0, 3] = float("nan")                                  # every page of request 1
+    got = choose(cb, s, b, 5, 0, 1)
+    assert np.array_equal(got, expected(serve, s, b, 5, 0, 1))
+    assert {3, 7} <= set(got[0, 0]) and got[1, 0].tolist() == [0, 1, 2, 3, 21]
+
+
+def test_select_hidden_pages(cb, serve):
+    """Pages outside the pool are no candidates, nor among the first and last; the others take their places."""
+    s = make_step(cb, "blocks", [(1, 300), (9, 200), (1, 50)], 2, 3, 64, 16, seed=6)
+    b = all_bounds(cb, s)
+    table = s.table.copy()
+    table[0, [0, 4, 17, 18]] = -1, s.pool.shape[2], 2 ** 31 - 1, -5
+    table[1, :11] = -1
+    table[2, :] = -1
+    got = choose(cb, s, b, 4, 2, 2, table=table)
+    assert np.array_equal(got, expected(serve, s, b, 4, 2, 2, table=table))
+    assert (got[10] == -1).all()
+
+
+def test_select_more_new_tokens_than_keys(cb, serve):
+    s = make_step(cb, "bf16", [(5, 5), (3, 40)], 1, 2, 64, 16, seed=7)
+    b = all_bounds(cb, s)
+    got = choose(cb, s, b, 3, 1, 1, kv=[2, 0])
+    assert (got[:3] == -1).all() and got[3:5].tolist() == [[[0, -1, -1]]] * 2 and (got[5:] == -1).all()
+
+
+def test_select_many_requests(cb, serve):
+    rng = np.random.default_rng(3)
+    lens = [(int(q), int(q + k)) for q, k in zip(rng.choice([0, 1, 1, 2, 20], 300), rng.integers(0, 200, 300))]
+    lens = [(q, max(1, k)) for q, k in lens]
+    s = make_step(cb, "bf16", lens, 1, 1, 64, 16, pad=4, seed=8)
+    b = all_bounds(cb, s)
+    got = choose(cb, s, b, 4, 1, 1)
+    assert np.array_equal(got, expected(serve, s, b, 4, 1, 1))
+
+
+# ------------------------------------------------------------------ attention over the selected pages
+
+def attend(cb, s, sel, ws=True, table=None, scale=None, lse=True, q=None):
+    s.out = torch.full((s.n, s.H * s.G, s.d), 9.0, dtype=torch.bfloat16, device="cuda")
+    s.lse = torch.full((s.n, s.H * s.G), 9.0, dtype=torch.float32, device="cuda") if lse else None
+    need = cb.cb_attn_selected_workspace_bytes(s.n, s.H * s.G, s.H, s.d, s.ps, sel.shape[2])
+    w = torch.empty((need if ws is True else int(ws),), dtype=torch.uint8, device="cuda") if ws else None
+    cb.cb_attn_selected(s.q if q is None else q, cb.page_pool(s.pool, s.scales), s.layer, i32(s.starts),
+                        i32([k for _, k in s.lens]), i32(s.table if table is None else table), i32(sel), s.out, scale=scale,
+                        lse=s.lse, workspace=w)
+    torch.cuda.synchronize()
+    return s.out, s.lse
+
+
+def check_attend(serve, s, sel, table=None, scale=None, rows=None):
+    sc = s.d ** -0.5 if scale is None else scale
+    table = s.table if table is None else table
+    got, gl, qd = f64(s.out), f64(s.lse), f64(s.q)
+    H, G, d, ps, P = s.H, s.G, s.d, s.ps, s.pool.shape[2]
+    for r, (nq, kv) in enumerate(s.lens):
+        there = (table[r] >= 0) & (table[r] < P)
+        for t in range(nq) if rows is None else [t for t in range(nq) if s.starts[r] + t in rows]:
+            p = kv - nq + t
+            for h in range(H):
+                pages = {int(i) for i in sel[s.starts[r] + t, h] if 0 <= i < len(there) and there[i]}
+                at, hs = s.starts[r] + t, slice(h * G, (h + 1) * G)
+                keys = np.array([j for j in range(max(p, -1) + 1) if j // ps in pages], dtype=int)
+                n = len(keys)
+                o, l, mag, smag = serve.attention(qd[at:at + 1, hs], s.K[r][h][keys], s.V[r][h][keys], n, sc)
+                es, few = (d + 8) * 2 * F32 * smag, (n + 64) * 2 * F32
+                tol = BF * np.abs(o) * 1.01 + mag * (BF * 1.01 + (2 * es + few)[..., None])
+                assert (np.abs(got[at:at + 1, hs] - o) <= tol).all(), (r, t, h)
+                assert np.array_equal(np.isneginf(gl[at:at + 1, hs]), np.isneginf(l)), (r, t, h)
+                if n:
+                    assert (np.abs(gl[at:at + 1, hs] - l) <= es + few + 8 * F32 * (np.abs(l) + 1)).all(), (r, t, h)
+    if rows is None:
+        assert (got[s.starts[-1]:] == 9.0).all() and (gl[s.starts[-1]:] == 9.0).all()
+
+
+def random_lists(s, k, seed, spoil=True):
+    """Lists of different pages in any order, up to k of them, and entries that are none among and behind them."""
+    rng = np.random.default_rng(seed)
+    sel = np.full((s.n, s.H, k), -1)
+    for r, (nq, kv) in enumerate(s.lens):
+        for t in range(nq):
+            own = max(kv - nq + t, 0) // s.ps
+            for h in range(s.H):
+                m = int(rng.integers(1, k + 1))
+                pages = rng.permutation(own + 1)[:m]
+                row = np.concatenate([pages, np.full(m - len(pages), -1)])
+                if spoil:
+                    rng.shuffle(row)
+                    row[rng.random(m) < 0.1] = rng.choice([-1, -2 ** 31, s.table.shape[1], 2 ** 31 - 1])
+                sel[s.starts[r] + t, h, :m] = row
+    return sel
+
+
+ATTEND = [
+    # kind, lens, H, G, d, page, k
+    ("bf16", [(1, 1)], 1, 1, 64, 16, 1),
+    ("bf16", [(1, 300), (1, 77), (1, 16)], 2, 4, 128, 16, 5),
+    ("bf16", [(3, 200), (0, 40), (5, 5)], 1, 2, 96, 7, 9),
+    ("e4m3", [(1, 900), (2, 33)], 2, 8, 64, 16, 16),
+    ("e4m3", [(4, 500)], 1, 16, 96, 32, 7),
+    ("blocks", [(1, 1000), (2, 500)], 2, 5, 128, 16, 12),
+    ("blocks", [(20, 800), (17, 17)], 1, 3, 96, 24, 6),
+    ("bf16", [(10, 600)], 2, 1, 64, 1, 40),
+    ("blocks", [(1, 2000)], 1, 33, 64, 100, 9),
+    ("e4m3", [(2, 700)], 1, 40, 128, 64, 8),
+]
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("case", range(len(ATTEND)))
+def test_selected_attention(cb, serve, case, ws):
+    kind, lens, H, G, d, ps, k = ATTEND[case]
+    s = make_step(cb, kind, lens, H, G, d, ps, pad=case % 3, seed=case)
+    sel = random_lists(s, k, case)
+    attend(cb, s, sel, ws=ws)
+    check_attend(serve, s, sel)
+    s.q = s.q * 3
+    attend(cb, s, sel, ws=ws, scale=-0.1)
+    check_attend(serve, s, sel, scale=-0.1)
+
+
+@pytest.mark.parametrize("kind,d,ps,k", [("bf16", 128, 64, 100), ("blocks", 64, 16, 300), ("e4m3", 96, 128, 40), ("blocks", 128, 1000, 5)])
+def test_selected_attention_in_parts(cb, serve, kind, d, ps, k):
+    """Long lists of few tokens, divided among workgroups as the workspace allows; the same bits from call to call."""
+    s = make_step(cb, kind, [(1, 9000), (2, 4001)], 2, 3, d, ps, pad=2, seed=k)
+    sel = random_lists(s, k, k, spoil=False)
+    assert cb.cb_attn_selected_workspace_bytes(s.n, 6, 2, d, ps, k) > 0
+    attend(cb, s, sel)
+    check_attend(serve, s, sel)
+    a, al = s.out.clone(), s.lse.clone()
+    attend(cb, s, sel)
+    assert torch.equal(a, s.out) and torch.equal(al, s.lse)
+    for ws in (16, 300000, 1000000):
+        attend(cb, s, sel, ws=ws)
+        check_attend(serve, s, sel)
+
+
+def test_all_pages_selected_is_attention(cb, serve):
+    """Every page in its order: attention over all visible keys."""
+    for kind in ("bf16", "blocks"):
+        s = make_step(cb, kind, [(1, 500), (3, 90), (12, 300)], 2, 4, 128, 16, seed=11)
+        sel = np.broadcast_to(np.arange(s.table.shape[1]), (s.n, s.H, s.table.shape[1])).copy()
+        attend(cb, s, sel)
+        s.check(serve)
+
+
+def test_selected_attention_sees_nothing(cb, serve):
+    """Empty lists, lists of pages behind the token or outside the pool: zeros and -infinity."""
+    s = make_step(cb, "bf16", [(1, 100), (2, 64), (1, 300)], 1, 2, 64, 16, seed=12)
+    sel = np.full((s.n, 1, 5), -1)
+    sel[1], sel[3] = 5, [3, 4, 3, 4, 3]
+    table = s.table.copy()
+    table[2, 3:5] = -1, s.pool.shape[2]
+    for ws in (True, False):
+        attend(cb, s, sel, table=table, ws=ws)
+        assert (s.out == 0).all() and torch.isneginf(s.lse).all()
+
+
+def test_selected_attention_counts_a_page_twice(cb, serve):
+    s = make_step(cb, "bf16", [(1, 64)], 1, 2, 64, 16, seed=13)
+    attend(cb, s, np.array([[[1, 3]]]))
+    a, al = s.out.clone(), s.lse.clone()
+    attend(cb, s, np.array([[[1, 3, 1, 3]]]))
+    assert (f64(s.out) - f64(a) <= 2 * BF * np.abs(f64(a)) + 1e-3).all()
+    assert np.allclose(f64(s.lse), f64(al) + np.log(2.0), atol=1e-5, rtol=0)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_selected_attention_keeps_bad_values_from_rows_that_do_not_see_them(cb, serve, bad):
+    """In a page that only some tokens list, and behind the position of the others; in keys and in values."""
+    for z in range(2):
+        s = make_step(cb, "bf16", [(6, 90)], 1, 2, 64, 16, seed=14)
+        sel = np.tile(np.array([0, 2, 5]), (6, 1, 1))
+        sel[:3, 0, 1] = 3                                        # tokens 0 .. 2 do not list page 2
+        s.pool[s.layer, z, int(s.table[0, 2]), 0, 4, 3] = bad
+        s.pool[s.layer, z, int(s.table[0, 5]), 0, 9, 5] = bad      # key 89: token 5's alone
+        attend(cb, s, sel)
+        check_attend(serve, s, sel, rows=[0, 1, 2])
+        got = f64(s.out)
+        if z == 1:
+            assert not np.isfinite(got[3:, :, 3]).any() and np.isfinite(got[3:5, :, 5]).all() and not np.isfinite(got[5, :, 5]).any()
+        elif np.isnan(bad):
+            assert np.isnan(got[3:]).all()
+
+
+def test_selected_attention_strided_queries(cb, serve):
+    s = make_step(cb, "blocks", [(2, 40), (1, 90)], 2, 2, 64, 16, seed=15)
+    sel = random_lists(s, 3, 1)
+    wide = torch.zeros((s.n, 8, 64), dtype=torch.bfloat16, device="cuda")
+    wide[:, :4] = s.q
+    attend(cb, s, sel)
+    a = s.out.clone()
+    attend(cb, s, sel, q=wide[:, :4])
+    assert torch.equal(a, s.out)
+
+
+# ------------------------------------------------------------------ together
+
+class Server:
+    """Steps of a receiver on 8-bit pages: tables, quantised writes with turned queries, bounds, choice, attention."""
+
+    def __init__(self, cb, L, H, G, d, ps, P, R, n, width, k, n_pos=256):
+        z = lambda *shape, t=torch.int32: torch.zeros(shape, dtype=t, device="cuda")  # noqa: E731
+        self.cb, self.L, self.H, self.G, self.d, self.ps, self.n, self.k = cb, L, H, G, d, ps, n, k
+        self.pool = torch.full((L, 2, P, H, ps, d), 0x7f, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+        self.scales = torch.full((L, P, H, 2), 2.0 ** 100, dtype=torch.float32, device="cuda")
+        self.pages = cb.page_pool(self.pool, self.scales)
+        self.bounds = torch.zeros((L, P, H, 2, d), device="cuda").to(torch.float8_e4m3fn)
+        self.free, self.used = i32(np.random.default_rng(0).permutation(P)), z(1)
+        self.table = i32(np.full((R, width), -1))
+        self.ctx, self.new, self.starts, self.kv, self.info = z(R), z(R), z(R + 1), z(R), z(R)
+        self.slots, self.pos = z(n), z(n)
+        self.rope_table = torch.empty((n_pos, d // 2, 2), dtype=torch.float32, device="cuda")
+        cb.cb_rope_table(THETA, d, n_pos, self.rope_table)
+        self.rope = cb.rope_axes_spec(self.rope_table, self.pos)
+        bf = torch.bfloat16
+        self.rows, self.q = z(L, 2, 1, H, n, d, t=bf), z(L, n, H * G, d, t=bf)
+        self.turned, self.out = z(L, n, H * G, d, t=bf), z(L, n, H * G, d, t=bf)
+        self.selected = z(L, n, H, k)
+        self.ws = z(cb.cb_page_select_workspace_bytes(n, H, width), t=torch.uint8)
+        self.ws2 = z(cb.cb_attn_selected_workspace_bytes(n, H * G, H, d, ps, k), t=torch.uint8)
+
+    def step(self, max_q):
+        """One step of all layers; lengths are on the device."""
+        cb, lens = self.cb, (self.starts[:-1], self.new, self.kv, self.table)
+        cb.cb_page_tables(self.ctx, self.new, self.free, self.ps, self.table, self.starts, self.kv, self.slots, self.pos,
+                          self.info, self.used)
+        for l in range(self.L):
+            cb.cb_page_quantize(self.rows[l:l + 1], self.pages, *lens, layer=l, rope=self.rope, q=self.q[l], q_out=self.turned[l])
+            cb.cb_page_bounds(self.pages, self.bounds, *lens[1:], max_q, layer=l)
+            cb.cb_page_select(self.turned[l], self.pages, l, self.bounds, self.starts, self.kv, self.table, self.selected[l],
+                              first=1, last=1, workspace=self.ws)
+            cb.cb_attn_selected(self.turned[l], self.pages, l, self.starts, self.kv, self.table, self.selected[l], self.out[l],
+                                workspace=self.ws2)
+
+    def advance(self):
+        self.ctx.copy_(self.kv)
+        self.free = self.free[int(self.used):].contiguous()
+
+
+def test_steps_on_quantised_pages(cb, serve):
+    """Three steps: what each layer holds, chooses and answers, against the definitions on what is stored; and the
+    stored rows read back, turned back, near the rows that came."""
+    L, H, G, d, ps, R, n, k = 2, 2, 4, 64, 8, 3, 40, 4
+    s = Server(cb, L, H, G, d, ps, 40, R, n, 12, k)
+    g = gen(21)
+    came = [[[[] for _ in range(2)] for _ in range(L)] for _ in range(R)]
+    for new in ([30, 9, 0], [1, 2, 17], [1, 0, 1]):
+        s.new.copy_(i32(new))
+        s.rows.copy_((randn(g, L, 2, 1, H, n, d) * 2.0).cuda())
+        s.q.copy_((randn(g, L, n, H * G, d) * 2.0).cuda())
+        s.step(max(new))
+        torch.cuda.synchronize()
+        starts, kv, table = s.starts.cpu().numpy(), s.kv.cpu().numpy(), s.table.cpu().numpy()
+        assert s.info.tolist() == [0, 0, 0]
+        codes, sc, bn = f64(s.pool), s.scales.double().cpu().numpy(), f64(s.bounds)
+        for r in range(R):
+            tok = slice(starts[r], starts[r] + new[r])
+            for l in range(L):
+                for z in range(2):
+                    came[r][l][z].append(f64(s.rows[l, z, 0])[:, tok])
+                if new[r] == 0:
+                    continue
+                pages = table[r, :-(-int(kv[r]) // ps)]
+                K, V = (np.concatenate([codes[l, z, p] * sc[l, p, :, z][:, None, None] for p in pages], 1)[:, :kv[r]] for z in range(2))
+                for t in range(new[r]):
+                    p, at = int(kv[r]) - new[r] + t, starts[r] + t
+                    for h in range(H):
+                        hs = slice(h * G, (h + 1) * G)
+                        q = f64(s.turned[l, at, hs])
+                        m = p // ps + 1
+                        scores = serve.page_scores(q, bn[l, pages[:m], h] * sc[l, pages[:m], h, 0][:, None, None])
+                        want = serve.page_select(scores, [True] * m, 1, 1, k)
+                        got = s.selected[l, at, h].tolist()
+                        assert got == want + [-1] * (k - len(want))
+                        keys = np.array([j for j in range(p + 1) if j // ps in want])
+                        o, _, mag, smag = serve.attention(q[None], K[h][keys], V[h][keys], len(keys), d ** -0.5)
+                        es, few = (d + 8) * 2 * F32 * smag, (len(keys) + 64) * 2 * F32
+                        tol = BF * np.abs(o) * 1.01 + mag * (BF * 1.01 + (2 * es + few)[..., None])
+                        assert (np.abs(f64(s.out[l, at, hs])[None] - o) <= tol).all()
+        s.advance()
+    back = torch.zeros((L, 2, R, H, 40, d), dtype=torch.bfloat16, device="cuda")
+    pos = torch.arange(40, dtype=torch.int32, device="cuda").repeat(R)
+    cb.cb_page_read(s.pages, back, i32([0, 40, 80]), s.kv, s.kv, s.table, rope=cb.rope_axes_spec(s.rope_table, pos), inverse=True)
+    for r in range(R):
+        for l in range(L):
+            x = np.concatenate(came[r][l][1], 1)
+            y = f64(back[l, 1, r])[:, :x.shape[1]]
+            assert (np.abs(x - y) <= 2.0 ** -4 * np.abs(x) + 2.0 ** -10 * np.abs(x).max() / 224).all()
+            x = np.concatenate(came[r][l][0], 1)
+            y = f64(back[l, 0, r])[:, :x.shape[1]]
+            # keys: the rounding of both channels of a turned pair, turned back, and to bf16; a code that went over to
+            # a larger scale was rounded twice
+            pair = np.hypot(x[..., :d // 2], x[..., d // 2:])
+            tol = np.concatenate([pair, pair], -1) * (2 * np.sqrt(2) * 2.0 ** -4 + 2 * BF) + 2.0 ** -8 * np.abs(x).max() / 158
+            assert (np.abs(x - y) <= tol).all()
+
+
+def test_steps_in_a_graph_with_other_lengths(cb):
+    """A captured step replayed with other lengths and rows, and with eager work of the caller between: the eager step's
+    bits every time."""
+    make = lambda: Server(cb, 2, 2, 4, 64, 8, 60, 3, 24, 16, 5)  # noqa: E731
+    eager, graph = make(), make()
+    steps = [[20, 3, 1], [1, 1, 1], [5, 0, 9], [1, 1, 0], [2, 12, 1], [1, 1, 1]]
+    side = torch.cuda.Stream()
+    captured = None
+    for i, new in enumerate(steps):
+        for s in (eager, graph):
+            g = gen(40 + i)
+            s.new.copy_(i32(new))
+            s.rows.copy_(randn(g, 2, 2, 1, 2, 24, 64).cuda())
+            s.q.copy_(randn(g, 2, 24, 8, 64).cuda())
+        # (the graph's free list keeps its place: the pages left are moved to its beginning)
+        if i:
+            rest = graph.free[int(graph.used):].clone()
+            graph.free[:len(rest)] = rest
+        eager.step(24)
+        torch.cuda.synchronize()
+        if captured is None:
+            side.wait_stream(torch.cuda.current_stream())
+            captured = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(captured, stream=side):
+                graph.step(24)
+        captured.replay()
+        torch.cuda.synchronize()
+        n = int(eager.starts[-1])
+        for name in ("table", "starts", "kv", "scales", "bounds", "pool"):
+            a, b = getattr(eager, name), getattr(graph, name)
+            assert torch.equal(a.view(torch.uint8) if a.dtype == torch.float8_e4m3fn else a,
+                               b.view(torch.uint8) if b.dtype == torch.float8_e4m3fn else b), (i, name)
+        for name in ("selected", "out", "turned"):
+            assert torch.equal(getattr(eager, name)[:, :n], getattr(graph, name)[:, :n]), (i, name)
+        eager.advance()
+        graph.ctx.copy_(graph.kv)
+        torch.randn(1000, device="cuda").sort()
+
+
+def test_two_calls_at_once(cb, serve):
+    """Choice and attention of two steps on two streams, a workspace each."""
+    steps = [make_step(cb, "blocks", [(1, 4000), (2, 900)], 2, 4, 64, 16, seed=30 + i) for i in range(2)]
+    want = []
+    for s in steps:
+        s.b = all_bounds(cb, s)
+        sel = choose(cb, s, s.b, 80, 1, 2)
+        attend(cb, s, sel)
+        want.append((sel, s.out.clone()))
+    streams, got = [torch.cuda.Stream() for _ in steps], []
+    torch.cuda.synchronize()
+    for s, st in zip(steps, streams):
+        with torch.cuda.stream(st):
+            sel = torch.full((s.n, s.H, 80), -7, dtype=torch.int32, device="cuda")
+            out = torch.full_like(s.out, 9.0)
+            args = (i32(s.starts), i32([k for _, k in s.lens]), i32(s.table))
+            w1 = torch.empty((cb.cb_page_select_workspace_bytes(s.n, s.H, s.table.shape[1]),), dtype=torch.uint8, device="cuda")
+            w2 = torch.empty((cb.cb_attn_selected_workspace_bytes(s.n, 8, 2, 64, 16, 80),), dtype=torch.uint8, device="cuda")
+            pages = cb.page_pool(s.pool, s.scales)
+            for _ in range(3):
+                cb.cb_page_select(s.q, pages, s.layer, s.b, *args, sel, first=1, last=2, workspace=w1)
+                cb.cb_attn_selected(s.q, pages, s.layer, *args, sel, out, workspace=w2)
+            got.append((sel, out, args, w1, w2))
+    torch.cuda.synchronize()
+    for (sel, out, *_), (a, b) in zip(got, want):
+        assert np.array_equal(sel.cpu().numpy(), a) and torch.equal(out, b)

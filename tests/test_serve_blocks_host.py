@@ -124,3 +124,120 @@ def test_plain_quantize_by_hand():
     assert exps[0, 1, 0].tolist() == [2, 2] and codes[0, 1, 1, 0].tolist() == [[112, -0.75], [225, 0.25]]
     assert serve.block_exponent(np.array([0.0]), False) == serve.E_MIN
     assert [serve.block_exponent(np.array([v, np.inf, np.nan]), t) for v, t in ((448.0, 0), (449.0, 0), (316.0, 1), (317.0, 1))] == [0, 1, 0, 1]
+
+
+# ------------------------------------------------------------------ selected pages
+
+STEP = dict(q={}, pages={}, layer=0, n_reqs=2, qs=P, kv=P, bt=P, stride=8, width=8)
+SELECT = dict(STEP, bounds=P, first=1, last=1, k=4, sel=P, ws=P, ws_bytes=1 << 20)
+ATTEND = dict(STEP, sel=P, k=4, out=dict(data=3 * P), scale=0.1, lse=None, ws=None, ws_bytes=0)
+
+
+def select(cb, **kw):
+    a = {**SELECT, **kw}
+    return cb.library().cb_page_select(ref(rows, cb, a["q"]), ref(blocks, cb, a["pages"]), a["layer"], a["bounds"], a["n_reqs"],
+                                       a["qs"], a["kv"], a["bt"], a["stride"], a["width"], a["first"], a["last"], a["k"], a["sel"],
+                                       a["ws"], a["ws_bytes"], None)
+
+
+def attend(cb, **kw):
+    a = {**ATTEND, **kw}
+    return cb.library().cb_attn_selected(ref(rows, cb, a["q"]), ref(blocks, cb, a["pages"]), a["layer"], a["n_reqs"], a["qs"],
+                                         a["kv"], a["bt"], a["stride"], a["width"], a["sel"], a["k"], ref(rows, cb, a["out"]),
+                                         a["scale"], a["lse"], a["ws"], a["ws_bytes"], None)
+
+
+STEP_REFUSALS = [
+    (dict(q=None), ARG), (dict(pages=None), ARG), (dict(pages=dict(head_dim=80)), UNSUP), (dict(layer=1), ARG), (dict(layer=-1), ARG),
+    (dict(pages=dict(scales=None)), ARG), (dict(pages=dict(scales=P + 4)), ALIGN), (dict(q=dict(s_tok=-256)), SHAPE),
+    (dict(n_reqs=-1), ARG), (dict(qs=None), ARG), (dict(kv=None), ARG), (dict(bt=None), ARG), (dict(qs=P + 2), ALIGN),
+    (dict(stride=7), SHAPE), (dict(width=-1), ARG), (dict(width=1 << 28, stride=1 << 28), UNSUP), (dict(sel=None), ARG),
+    (dict(sel=P + 2), ALIGN), (dict(ws_bytes=-1), ARG), (dict(n_reqs=0, qs=None, kv=None, bt=None, sel=None), OK),
+]
+
+
+@pytest.mark.parametrize("kw,status", STEP_REFUSALS + [
+    (dict(q=dict(head_dim=128)), SHAPE), (dict(q=dict(n_heads=5)), SHAPE), (dict(first=-1), ARG), (dict(last=0), ARG),
+    (dict(first=4), ARG), (dict(first=2 ** 31 - 1, last=2 ** 31 - 1), ARG), (dict(k=1), ARG), (dict(bounds=None), ARG),
+    (dict(bounds=P + 8), ALIGN), (dict(ws=P + 2), ALIGN), (dict(ws_bytes=8 * 2 * 4 - 1), SHAPE), (dict(ws=None), SHAPE),
+    (dict(q=dict(n_tokens=0)), OK), (dict(width=1 << 25, stride=1 << 25, pages=dict(seq_len=1)), UNSUP),
+])
+def test_select_refuses(cb, kw, status):
+    assert select(cb, **kw) == status, cb.cb_last_error()
+    assert (cb.cb_last_error() != "") == (status != OK)
+
+
+@pytest.mark.parametrize("kw,status", STEP_REFUSALS + [
+    (dict(out=None), ARG), (dict(out=dict(data=3 * P, n_tokens=2)), SHAPE), (dict(out=dict(data=3 * P, s_tok=0)), SHAPE),
+    (dict(out=dict(data=2 * P)), ARG), (dict(k=0), ARG), (dict(k=1 << 27), UNSUP), (dict(scale=float("nan")), ARG),
+    (dict(scale=3e38), ARG), (dict(lse=P + 1), ALIGN), (dict(ws=P + 4), ALIGN),
+    (dict(q=dict(n_tokens=0), out=dict(data=3 * P, n_tokens=0)), OK),
+])
+def test_selected_attention_refuses(cb, kw, status):
+    assert attend(cb, **kw) == status, cb.cb_last_error()
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(pages=None), ARG), (dict(layer=1), ARG), (dict(layers=0), ARG), (dict(layers=2), ARG), (dict(bounds=None), ARG),
+    (dict(bounds=P + 8), ALIGN), (dict(n_reqs=-1), ARG), (dict(q=None), ARG), (dict(kv=None), ARG), (dict(bt=None), ARG),
+    (dict(kv=P + 1), ALIGN), (dict(stride=7), SHAPE), (dict(width=1 << 28, stride=1 << 28), UNSUP), (dict(max_q=-1), ARG),
+    (dict(pages=dict(seq_len=1 << 25, n_seqs=1), width=1), UNSUP), (dict(n_reqs=0, bounds=None), OK),
+])
+def test_bounds_refuses(cb, kw, status):
+    a = {**dict(SPANS, pages={}, layer=0, layers=1, bounds=P, max_q=1), **kw}
+    assert cb.library().cb_page_bounds(ref(blocks, cb, a["pages"]), a["layer"], a["layers"], a["bounds"], a["n_reqs"], a["q"],
+                                       a["kv"], a["bt"], a["stride"], a["width"], a["max_q"], None) == status, cb.cb_last_error()
+
+
+def test_binding_refuses_wrong_tensors_of_a_selection(cb):
+    z = lambda *s, t=torch.bfloat16: torch.zeros(s, dtype=t)  # noqa: E731
+    i = lambda *s: z(*s, t=torch.int32)  # noqa: E731
+    pg = cb.page_pool(z(1, 2, 3, 2, 16, 64))
+    good = dict(q=z(2, 4, 64), pages=pg, layer=0, q_starts=i(3), kv_lens=i(2), block_table=i(2, 3), selected=i(2, 2, 4))
+    sel = dict(good, bounds=z(1, 3, 2, 2, 64))
+    att = dict(good, out=z(2, 4, 64))
+    common = [(dict(q=z(2, 4, 64).float()), "q is"), (dict(q_starts=i(2)), "q_starts"), (dict(kv_lens=i(2).long()), "kv_lens"),
+              (dict(block_table=i(3, 3)), "block_table"), (dict(selected=i(2, 4)), "selected"), (dict(selected=i(2, 1, 4)), "selected"),
+              (dict(selected=i(2, 2, 4).long()), "selected"), (dict(layer=2 ** 32), "32-bit"),
+              (dict(workspace=z(8, 8).T), "workspace"), (dict(), "current CUDA device")]
+    for f, a, more in ((cb.cb_page_select, sel, [(dict(bounds=z(1, 3, 2, 2, 64).float()), "bounds"), (dict(bounds=z(1, 2, 2, 2, 64)), "bounds"),
+                                                 (dict(first=2 ** 32 + 1), "32-bit")]),
+                       (cb.cb_attn_selected, att, [(dict(lse=z(2, 4)), "lse"), (dict(out=z(2, 4, 64).float()), "out is")])):
+        for bad, match in common + more:
+            with pytest.raises(ValueError, match=match):
+                f(**{**a, **bad})
+    with pytest.raises(ValueError, match="bounds"):
+        cb.cb_page_bounds(pg, z(1, 3, 2, 1, 64), i(2), i(2), i(2, 3), 1)
+    with pytest.raises(ValueError, match="32-bit"):
+        cb.cb_page_bounds(pg, z(1, 3, 2, 2, 64), i(2), i(2), i(2, 3), 2 ** 32)
+    with pytest.raises(ValueError, match="32-bit"):
+        cb.cb_page_select_workspace_bytes(2 ** 32 + 1, 1, 1)
+    with pytest.raises(ValueError, match="32-bit"):
+        cb.cb_attn_selected_workspace_bytes(1, 8, 8, 64, 2 ** 32 + 16, 4)
+
+
+def test_workspaces(cb):
+    """Scores of every token, head and entry; partial results of row tiles that are divided, none for others."""
+    assert cb.cb_page_select_workspace_bytes(7, 2, 100) == 7 * 2 * 100 * 4
+    assert cb.cb_page_select_workspace_bytes(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1) == 2 ** 63 - 1
+    assert cb.cb_page_select_workspace_bytes(0, 2, 100) == 0
+    # 1 token, 8 heads, 128 tiles of 32 keys: parts of 16 tiles
+    assert cb.cb_attn_selected_workspace_bytes(1, 64, 8, 128, 64, 64) == 8 * 8 * 16 * 130 * 4
+    assert cb.cb_attn_selected_workspace_bytes(1, 8 * 33, 8, 128, 64, 64) == 3 * 8 * 8 * 16 * 130 * 4
+    assert cb.cb_attn_selected_workspace_bytes(512, 64, 8, 128, 64, 64) == 0             # enough row tiles undivided
+    assert cb.cb_attn_selected_workspace_bytes(1, 64, 8, 128, 16, 64) == 0               # 32 tiles: short
+    for bad in ((0, 8, 8, 64, 16, 4), (1, 8, 3, 64, 16, 4), (1, 8, 8, 64, 16, 0), (1, 8, 8, 64, 1 << 20, 1 << 20)):
+        assert cb.cb_attn_selected_workspace_bytes(*bad) == 0
+
+
+def test_plain_selection_by_hand():
+    from oracle import serve
+    b = serve.page_bounds(np.array([[1.0, -2.0], [3.0, 0.5]]))
+    assert b.tolist() == [[1.0, -2.0], [3.0, 0.5]]
+    # q = (2, -1): 2 * 3 + -1 * -2 = 8; q = (-1, 0): -1 * 1 = -1
+    assert serve.page_scores(np.array([[2.0, -1.0], [-1.0, 0.0]]), b[None]).tolist() == [7.0]
+    s = np.array([5, 1, 9, 9, np.nan, -3, 0], np.float32)
+    assert serve.page_select(s, [True] * 7, 1, 1, 4) == [0, 2, 4, 6]
+    assert serve.page_select(s, [True] * 7, 0, 2, 4) == [2, 4, 5, 6]
+    assert serve.page_select(s, [False, True, True, False, False, True, False], 1, 1, 2) == [1, 2]
+    assert serve.page_select(s[:2], [True] * 2, 1, 1, 4) == [0, 1]
