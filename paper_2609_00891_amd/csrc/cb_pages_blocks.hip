@@ -517,23 +517,29 @@ __global__ __launch_bounds__(256) void page_bounds_kernel(BoundsArgs a, SpanArgs
             hi[e] = -HUGE_VALF;
         }
         if (c < a.chunks) {
-            for (int t = slot; t < n; t += slots) {
-                const uint4 v = *(const uint4 *)(x + t * a.s_tok);
-                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+            // (eight tokens' chunks on their way together; behind the last, it again)
+            for (int t0 = slot; t0 < n; t0 += 8 * slots) {
+                uint4 v[8];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint32_t y[2] = {u[w], 0};
-                    if (F8) {
-                        y[0] = e4m3_pair<false>(u[w], 1.f);
-                        y[1] = e4m3_pair<true>(u[w], 1.f);
-                    }
+                for (int i = 0; i < 8; ++i) v[i] = *(const uint4 *)(x + min(t0 + i * slots, n - 1) * a.s_tok);
 #pragma unroll
-                    for (int k = 0; k < (F8 ? 2 : 1); ++k) {
-                        const int e = (F8 ? 4 : 2) * w + 2 * k;
-                        lo[e] = least(lo[e], bf_lo(y[k]));
-                        hi[e] = greatest(hi[e], bf_lo(y[k]));
-                        lo[e + 1] = least(lo[e + 1], bf_hi(y[k]));
-                        hi[e + 1] = greatest(hi[e + 1], bf_hi(y[k]));
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        uint32_t y[2] = {u[w], 0};
+                        if (F8) {
+                            y[0] = e4m3_pair<false>(u[w], 1.f);
+                            y[1] = e4m3_pair<true>(u[w], 1.f);
+                        }
+#pragma unroll
+                        for (int k = 0; k < (F8 ? 2 : 1); ++k) {
+                            const int e = (F8 ? 4 : 2) * w + 2 * k;
+                            lo[e] = least(lo[e], bf_lo(y[k]));
+                            hi[e] = greatest(hi[e], bf_lo(y[k]));
+                            lo[e + 1] = least(lo[e + 1], bf_hi(y[k]));
+                            hi[e + 1] = greatest(hi[e + 1], bf_hi(y[k]));
+                        }
                     }
                 }
             }

@@ -120,6 +120,7 @@ struct SelectArgs {
     int32_t *selected;        // [n_tokens][n_heads][n_selected]
     uint32_t *keys;           // [tok1 - tok0][n_heads][table_width] scores of a round's tokens, as numbers of their order
     int32_t tok0, tok1;
+    int32_t per;              // pages of a workgroup
 };
 
 // Launchers (return hipError_t of the launch).
