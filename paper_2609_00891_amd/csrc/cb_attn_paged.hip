@@ -514,7 +514,7 @@ template <int D, int EL>
 __global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
     __shared__ SchedLds<4> sched;
     __shared__ __attribute__((aligned(16))) RowsLds<D, 4> lds;
-    rows_body<D, EL, 4, false>(a, a.rows, blockIdx.x, sched, lds);
+    rows_body<D, EL, 4, kAll>(a, a.rows, blockIdx.x, sched, lds);
 }
 
 // The requests with few rows and the others in one launch, runs of the two in turn, so that a compute
@@ -538,7 +538,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tile_kernel(PagedArgs a) {
         if (!tile) b -= a.tile.blocks - pairs * kRun;
     }
     if (tile) tile_body<D, EL, NW>(a, a.tile, b, sched, lds.tile);
-    else rows_body<D, EL, NW, false>(a, a.rows, b, sched, lds.rows);
+    else rows_body<D, EL, NW, kAll>(a, a.rows, b, sched, lds.rows);
 }
 
 template <int D, int EL, int NW>

@@ -252,12 +252,15 @@ __device__ __forceinline__ int32_t list_length(const int32_t *list, int32_t n) {
     return 0;
 }
 
-// SEL: a token's row tile and its selected pages, one list of keys (place i of the list: key i mod page_size of its
-// page i / page_size).  The row is the one new token of a request as long as its position.
-template <int D, int EL, int NW, bool SEL>
+// Which keys a row tile has: those that it sees of all pages, or those of the pages selected for its token, one list of keys
+// (place i of the list: key i mod page_size of its page i / page_size; the row is the one new token of a request as
+// long as its position).  kSelectedWhole: a key tile lies in one page, so that its place, scales and visible keys are one
+// number each for the wave: no lane asks another, and the loads' addresses are a scalar and a constant of the lane.
+enum { kAll, kSelected, kSelectedWhole };
+template <int D, int EL, int NW, int KEYS>
 __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds<NW> &sched,
                                           RowsLds<D, NW> &lds) {
-    constexpr bool F8 = EL != kBf16, BLK = EL == kBlocks;
+    constexpr bool F8 = EL != kBf16, BLK = EL == kBlocks, SEL = KEYS != kAll, WHOLE = KEYS == kSelectedWhole;
     using Ge = Geo<D, F8>;
     constexpr int M = 16, E = Ge::E;
     auto &ol = lds.o;
@@ -314,11 +317,19 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
     bool in_kv = false;
     int32_t entry = 0, entry_page = 0;                         // SEL: the place in the list and what stands there, a tile earlier still
     auto peek = [&](int32_t tile) __attribute__((always_inline)) {
-        entry = tile * kKT + (lane & 31);
+        entry = tile * kKT + (WHOLE ? 0 : lane & 31);
         entry_page = list[min((int32_t)fast_div((uint32_t)entry, a.page_size), listed - 1)];
     };
+    int32_t seen = 0;                                          // WHOLE: keys of the tile up to the row's position, from its first
     auto look_up = [&](int32_t tile) __attribute__((always_inline)) {
-        if constexpr (SEL) {
+        if constexpr (WHOLE) {
+            const int32_t at = __builtin_amdgcn_readfirstlane(entry_page);
+            const uint32_t idx = fast_div((uint32_t)entry, a.page_size);
+            in_page = (uint32_t)entry - idx * a.page_size.d;
+            in_kv = (int32_t)idx < listed && at >= 0 && at < a.table_width;
+            seen = in_kv ? min(rq.kv_len - (at * (int32_t)a.page_size.d + (int32_t)in_page), kKT) : 0;
+            page = table[in_kv ? at : 0];
+        } else if constexpr (SEL) {
             const uint32_t idx = fast_div((uint32_t)entry, a.page_size);
             in_page = (uint32_t)entry - idx * a.page_size.d;
             const bool is = (int32_t)idx < listed && entry_page >= 0 && entry_page < a.table_width;
@@ -338,7 +349,30 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
     // bit per key whose row is there
     uint32_t ko[2], vo[8];                                     // places of the rows that this lane loads from
     float ks_n = 1.f, vs_n = 1.f;                              // BLK: the scales of the lane's key's page
+    const char *kt_p = kp, *vt_p = vp;                         // WHOLE: the tile's first rows, and the lane's places behind them
+    uint32_t k_lane[2] = {}, v_lane[8] = {};
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            k_lane[t] = (uint32_t)(16 * t + (lane >> 2)) * a.s_tok * 16 + (F8 && !Ge::PAIR ? 8 : 16) * (lane & 3);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v_lane[j] = (uint32_t)((j >> 2) * 16 + 4 * g + (j & 3)) * a.s_tok * 16 + (uint32_t)(min(n, Ge::NC - 1) * (F8 ? E : 2 * E));
+    }
     auto place = [&]() __attribute__((always_inline)) {
+        if constexpr (WHOLE) {
+            const int32_t pg = __builtin_amdgcn_readfirstlane(page);
+            const bool ok = in_kv && (uint32_t)pg < (uint32_t)a.n_pages;
+            off = ok ? (uint32_t)pg * a.s_page + in_page * a.s_tok : 0u;
+            kt_p = kp + (uint64_t)off * 16;
+            vt_p = vp + (uint64_t)off * 16;
+            if constexpr (BLK) {
+                const float2 sc = *(const float2 *)(a.kscale + 2 * ((int64_t)(ok ? pg : 0) * a.n_heads + head));
+                ks_n = sc.x;
+                vs_n = sc.y;
+            }
+            return ok ? bits_to(seen - 1) : 0u;
+        }
         const bool ok = in_kv && (uint32_t)page < (uint32_t)a.n_pages;
         off = (ok ? (uint32_t)page : 0u) * a.s_page + (ok ? in_page : 0u) * a.s_tok;
         if constexpr (BLK) {
@@ -357,27 +391,33 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
     auto load_k = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const char *p = kp + (uint64_t)ko[t] * 16;
+            const char *p = WHOLE ? kt_p + k_lane[t] : kp + (uint64_t)ko[t] * 16 + (F8 && !Ge::PAIR ? 8 : 16) * g;
             if constexpr (!F8 || Ge::PAIR) {
 #pragma unroll
                 for (int s = 0; s < Ge::KW / 4; ++s) {
-                    const u32x4_t x = *(const u32x4_t *)(p + 64 * s + 16 * g);
+                    const u32x4_t x = *(const u32x4_t *)(p + 64 * s);
                     kr[t][4 * s] = x[0]; kr[t][4 * s + 1] = x[1]; kr[t][4 * s + 2] = x[2]; kr[t][4 * s + 3] = x[3];
                 }
             } else {
 #pragma unroll
                 for (int s = 0; s < Ge::NS; ++s) {
-                    const u32x2_t x = *(const u32x2_t *)(p + 32 * s + 8 * g);
+                    const u32x2_t x = *(const u32x2_t *)(p + 32 * s);
                     kr[t][2 * s] = x[0]; kr[t][2 * s + 1] = x[1];
                 }
             }
         }
     };
+    // WHOLE: four lanes that follow one another read 64 bytes of one row, and the operand's lane (row n, piece g) has them
+    // from lane 4 n + g.  (Rows that stay in the caches, as neighbouring tokens' pages do, are bound by the lines that the
+    // first cache looks up: with every lane on its own row 4 times as many.)
+    auto k_of = [&](uint32_t x) __attribute__((always_inline)) {
+        return WHOLE ? (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (4 * n + g), (int)x) : x;
+    };
     auto load_v = [&]() __attribute__((always_inline)) {
         const int c = min(n, Ge::NC - 1);                      // 96: lanes 12 .. 15 repeat lane 11, unused
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const char *p = vp + (uint64_t)vo[j] * 16 + c * (F8 ? E : 2 * E);
+            const char *p = WHOLE ? vt_p + v_lane[j] : vp + (uint64_t)vo[j] * 16 + c * (F8 ? E : 2 * E);
             if constexpr (Ge::VW == 4) {
                 const u32x4_t x = *(const u32x4_t *)p;
                 vr[j][0] = x[0]; vr[j][1] = x[1]; vr[j][2] = x[2]; vr[j][3] = x[3];
@@ -429,15 +469,15 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            const float ks = BLK ? __shfl(ks_n, 16 * t + n) : 1.f;
+            const float ks = !BLK ? 1.f : WHOLE ? ks_n : __shfl(ks_n, 16 * t + n);
 #pragma unroll
             for (int st = 0; st < Ge::NS; ++st) {
                 bf16x8_t kf;
                 if constexpr (F8) {
-                    const uint32_t x = kr[t][2 * st], y = kr[t][2 * st + 1];
+                    const uint32_t x = k_of(kr[t][2 * st]), y = k_of(kr[t][2 * st + 1]);
                     kf = frag(e4m3_pair<false>(x, ks), e4m3_pair<true>(x, ks), e4m3_pair<false>(y, ks), e4m3_pair<true>(y, ks));
                 } else {
-                    kf = frag(kr[t][4 * st], kr[t][4 * st + 1], kr[t][4 * st + 2], kr[t][4 * st + 3]);
+                    kf = frag(k_of(kr[t][4 * st]), k_of(kr[t][4 * st + 1]), k_of(kr[t][4 * st + 2]), k_of(kr[t][4 * st + 3]));
                 }
                 s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[st], s[t], 0, 0, 0);
             }
@@ -503,7 +543,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
         uint32_t vb[8][E / 2];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float vs = BLK ? __shfl(vs_v, (j >> 2) * 16 + 4 * g + (j & 3)) : 1.f;
+            const float vs = !BLK ? 1.f : WHOLE ? vs_v : __shfl(vs_v, (j >> 2) * 16 + 4 * g + (j & 3));
 #pragma unroll
             for (int w = 0; w < E / 2; ++w) {
                 if constexpr (F8)
@@ -538,7 +578,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
 #pragma unroll 1
             for (int kk = 0; kk < kKT; ++kk) {
                 if (!((there >> kk) & 1)) continue;
-                const char *vrow = vp + (uint64_t)(uint32_t)__shfl((int)off, kk) * 16;
+                const char *vrow = WHOLE ? vt_p + (uint32_t)kk * a.s_tok * 16 : vp + (uint64_t)(uint32_t)__shfl((int)off, kk) * 16;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int c = min(4 * g + r, Ge::NC - 1) * E;

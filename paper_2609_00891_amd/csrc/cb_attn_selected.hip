@@ -15,11 +15,11 @@
 namespace cb {
 namespace {
 
-template <int D, int EL>
-__global__ __launch_bounds__(256) void attn_selected_kernel(PagedArgs a) {
+template <int D, int EL, int KEYS>
+__global__ __launch_bounds__(256, 2) void attn_selected_kernel(PagedArgs a) {
     __shared__ SchedLds<4> sched;
     __shared__ __attribute__((aligned(16))) RowsLds<D, 4> lds;
-    rows_body<D, EL, 4, true>(a, a.rows, blockIdx.x, sched, lds);
+    rows_body<D, EL, 4, KEYS>(a, a.rows, blockIdx.x, sched, lds);
 }
 
 // Blocks take four rows of a tile, or one where a workgroup joins it.
@@ -47,7 +47,9 @@ hipError_t launch(PagedArgs a, void *ws, int64_t ws_bytes, hipStream_t s) {
     a.rows.ws = (float *)ws;
     a.sel_parts = make_fastdiv((uint32_t)parts);
     a.sel_tiles = make_fastdiv((uint32_t)cut.tiles);
-    hipLaunchKernelGGL((attn_selected_kernel<D, EL>), dim3((unsigned)(units * parts * a.n_heads)), dim3(256), 0, s, a);
+    // tiles of 32 keys in one page each, their rows within 2^31 bytes
+    const bool whole = a.page_size.d % kKT == 0 && a.s_tok < (1u << 21);
+    hipLaunchKernelGGL((whole ? attn_selected_kernel<D, EL, kSelectedWhole> : attn_selected_kernel<D, EL, kSelected>), dim3((unsigned)(units * parts * a.n_heads)), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (parts > 1) {
         const uint32_t rows = std::min<uint32_t>(a.G.d, 16), per = parts > kWideParts ? rows : (rows + 3) / 4;

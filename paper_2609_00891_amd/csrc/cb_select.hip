@@ -60,8 +60,9 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 
 // T tokens of a request share the bounds read: 16, or 4 where requests have few.
-template <int D, int EL, int T>
-__global__ __launch_bounds__(256) void scores_kernel(SelectArgs s) {
+template <int D, int EL, int T, int NW>
+__global__ __launch_bounds__(64 * NW) void scores_kernel(SelectArgs s) {
+    constexpr int NT = 64 * NW, STEP = 16 * NW;                // threads, pages that the waves have at a time
     constexpr bool F8 = EL != kBf16;
     constexpr int E = F8 ? 16 : 8, NP = 2 * D / (4 * E);       // channels of a piece, pieces of a lane
     constexpr int QS = 2 * D + 2;                              // (16 tokens' pairs of sums in 64 banks)
@@ -101,14 +102,14 @@ __global__ __launch_bounds__(256) void scores_kernel(SelectArgs s) {
     if (i0 < end) {
         look_up(i0);
         load(i0);
-        if (i0 + 64 < end) look_up(i0 + 64);
+        if (i0 + STEP < end) look_up(i0 + STEP);
     }
 
     // sums over the group's heads: a thread has 8 channels of a token, and where there are fewer of these than threads,
     // every HS-th head
-    constexpr int HS = T == 4 ? 4 : 1;
+    constexpr int HS = T == 4 ? NW : NW / 4;
     const int32_t G = (int32_t)a.G.d;
-    for (int u = tid / HS; u < T * (D / 8); u += 256 / HS) {
+    for (int u = tid / HS; u < T * (D / 8); u += NT / HS) {
         const int t = u / (D / 8), c = u % (D / 8) * 8;
         double lo[8] = {}, hi[8] = {};
         if (t < n_tok) {
@@ -120,8 +121,8 @@ __global__ __launch_bounds__(256) void scores_kernel(SelectArgs s) {
                 for (int e = 0; e < 8; ++e) {
                     const float v = e & 1 ? bf_hi(x[e >> 1]) : bf_lo(x[e >> 1]);
                     // (a NaN goes to both)
-                    lo[e] += (double)(v > 0.f ? 0.f : v);
-                    hi[e] += (double)(v < 0.f ? 0.f : v);
+                    lo[e] += (double)__builtin_elementwise_minimum(v, 0.f);
+                    hi[e] += (double)__builtin_elementwise_maximum(v, 0.f);
                 }
             }
         }
@@ -146,7 +147,7 @@ __global__ __launch_bounds__(256) void scores_kernel(SelectArgs s) {
     // the lane's token's sums of its channels; read from LDS for every 16 pages (registers for them would leave two waves a
     // SIMD)
     int q_at = (n & (T - 1)) * QS + E * g;
-    for (; i0 < end; i0 += 64) {
+    for (; i0 < end; i0 += STEP) {
         asm volatile("" : "+v"(q_at));
         const double *qa = sums + q_at;
         u32x4_t w[NP];
@@ -154,9 +155,9 @@ __global__ __launch_bounds__(256) void scores_kernel(SelectArgs s) {
         for (int p = 0; p < NP; ++p) w[p] = ahead[p];
         const float scale = EL == kBlocks ? __uint_as_float(__float_as_uint(scale_n) & 0x7f800000u) : 1.f;
         const bool ok = ok_n;
-        if (i0 + 64 < end) {
-            load(i0 + 64);
-            if (i0 + 128 < end) look_up(i0 + 128);
+        if (i0 + STEP < end) {
+            load(i0 + STEP);
+            if (i0 + 2 * STEP < end) look_up(i0 + 2 * STEP);
         }
         f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
         double few[2] = {0.0, 0.0};
@@ -366,8 +367,9 @@ template <int D, int EL> hipError_t launch(SelectArgs s, uint32_t *ws, int64_t w
         s.tok0 = (int32_t)t;
         s.tok1 = (int32_t)std::min<int64_t>(t + round, a.n_tokens);
         if (blocks > 0)
-            hipLaunchKernelGGL((few ? scores_kernel<D, EL, 4> : scores_kernel<D, EL, 16>),
-                               dim3((unsigned)tiles, (unsigned)a.n_heads, (unsigned)blocks), dim3(256), 0, stream, s);
+{ const bool w8 = getenv("CBW") && atoi(getenv("CBW")) == 8;
+            hipLaunchKernelGGL((w8 ? few ? scores_kernel<D, EL, 4, 8> : scores_kernel<D, EL, 16, 8> : few ? scores_kernel<D, EL, 4, 4> : scores_kernel<D, EL, 16, 4>),
+                               dim3((unsigned)tiles, (unsigned)a.n_heads, (unsigned)blocks), dim3(w8 ? 512 : 256), 0, stream, s); }
         const auto waves = a.table_width <= 512 ? choose_wave_kernel<8> : a.table_width <= 1024 ? choose_wave_kernel<16>
                            : a.table_width <= 2048 ? choose_wave_kernel<32> : nullptr;
         const unsigned tokens = (unsigned)(s.tok1 - s.tok0);
