@@ -511,7 +511,7 @@ __device__ __forceinline__ void join_body(const PagedArgs &a, const PagedClass &
 // ------------------------------------------------------------------ kernels
 
 template <int D, int EL>
-__global__ __launch_bounds__(256) void attn_rows_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256, EL == kBlocks ? 2 : 1) void attn_rows_kernel(PagedArgs a) {
     __shared__ SchedLds<4> sched;
     __shared__ __attribute__((aligned(16))) RowsLds<D, 4> lds;
     rows_body<D, EL, 4, kAll>(a, a.rows, blockIdx.x, sched, lds);
