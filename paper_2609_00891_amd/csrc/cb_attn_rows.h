@@ -215,15 +215,20 @@ template <int D, int NW> struct RowsLds {
     float ml[NW][16][2];
 };
 
-// The request that has token row `tok`, or -1: the last whose start is not behind it.
-__device__ __forceinline__ int request_of(const PagedArgs &a, int32_t tok) {
+// The request that has token row `tok`, every wave for itself; false if none has.
+__device__ __forceinline__ bool request_of(const PagedArgs &a, int32_t tok, int &req, Request &rq) {
     const int lane = threadIdx.x & 63;
-    int r = -1;
     for (int r0 = 0; r0 < a.n_reqs; r0 += 64) {
-        const uint64_t before = __ballot(r0 + lane < a.n_reqs && a.q_starts[min(r0 + lane, a.n_reqs)] <= tok);
-        if (before) r = r0 + 63 - __builtin_clzll(before);
+        const Request r = request(a, min(r0 + lane, a.n_reqs - 1));
+        const uint64_t has = __ballot(r0 + lane < a.n_reqs && tok >= r.row0 && tok < r.row0 + r.q_len);
+        if (!has) continue;
+        const int from = __builtin_ctzll(has);
+        req = r0 + from;
+        rq = {__builtin_amdgcn_readlane(r.row0, from), __builtin_amdgcn_readlane(r.q_len, from),
+              __builtin_amdgcn_readlane(r.kv_len, from)};
+        return true;
     }
-    return r;
+    return false;
 }
 
 // The row tile and part of index `idx` of a call on selected pages, and its token as the one new token of a request that
@@ -234,10 +239,8 @@ __device__ __forceinline__ bool selected_item(const PagedArgs &a, uint32_t idx, 
     it.parts = (int32_t)a.sel_parts.d;
     it.tile = (int32_t)(unit - tok * a.sel_tiles.d);
     it.slot = (int32_t)(unit * a.sel_parts.d);
-    it.req = request_of(a, (int32_t)tok);
-    if (it.req < 0) return false;
-    const Request r = request(a, it.req);
-    if ((int32_t)tok < r.row0 || (int32_t)tok >= r.row0 + r.q_len) return false;
+    Request r;
+    if (!request_of(a, (int32_t)tok, it.req, r)) return false;
     rq = {(int32_t)tok, 1, r.kv_len - r.q_len + ((int32_t)tok - r.row0) + 1};
     return true;
 }

@@ -8,36 +8,50 @@
 // (sum q-, sum q+) with (lo, hi).
 //
 // Choices are whole numbers: two pages whose scores differ in the last places of 32
-// bits must not change places with the order of a sum.  The products are formed and
-// summed in 64 bits, where they are exact but for cancellations beyond 2^37, and the
-// result is rounded once to 32; equal ones go to the lower page.
+// bits must not change places with the order of a sum.  A score is therefore the sum
+// in 64 bits, where products are exact and sums are but for cancellations beyond 2^37,
+// rounded once to 32; equal ones go to the lower page.  But only pages near the border
+// need so much: first come estimates, whose error is bounded, then the scores of the
+// pages that the bound leaves undecided.
 //
-// scores_kernel: 16 tokens of a request and one head a workgroup, 16 pages a wave at a
-//   time, by 16x16x4 products in 64 bits.  The order of the 2 d channels is free: a lane
-//   takes 16-byte pieces of a page's bounds as they lie in memory and the tokens' sums
-//   accordingly.  Written are 32-bit keys in the order of the scores, 0 for pages that
-//   are not there, all ones for those that are always taken.
-// choose_kernel: a workgroup per token and head finds the n_selected-th largest key
-//   by its bytes, from the highest, by counts in LDS, and writes the pages above it, and
-//   as many equal ones as fit, in their order.
+// estimates_kernel: 16 tokens of a request and one head a workgroup, 16 pages a wave at
+//   a time, by 16x16x32 products in bf16.  A token's sum over its heads (fp32; terms of
+//   one sign, off by G 2^-24) is split into two bf16 numbers (off by 2^-18); the products of 32
+//   channels start from zero and the steps are added in fp32, so that no sum of more
+//   than 64 terms is formed in a matrix instruction.  Together they are off by less than
+//   (2^-16 + G 2^-23) S, S = sum |q| |bound|, which a third product forms.  The bounds are read four lanes to 64
+//   bytes of a page and handed to the operand's lanes.
+// choose_wave_kernel: a wave per token and head, its keys (estimates as numbers of their
+//   order) in LDS.  The n_selected-th largest is found bit by bit, from the first
+//   in which they differ; pages further than twice the error above it are taken, as far
+//   below it are not, and of the others, where they are more than are needed, the wave forms the scores.
+// scores_kernel and choose_kernel: tables of more than 8,192 entries.  All scores in 64
+//   bits by 16x16x4 products, and a workgroup per token and head that finds the
+//   threshold by bytes with counts in LDS.
+//
+// Bound by latency and HBM: 48 single tokens over 4,096 .. 65,536 keys in pages of 32 (8 heads of 128, 8 query heads each,
+// 0.15 GB) 59 us with the bounds of their pages, 1,024 new tokens over 32,768 keys in 8-bit pages of 64 50.  With
+// scores of all pages in 64 bits 62 and 70 (47 and 55 of them the scores), read as they are chosen, by workgroups, 140 and 97.
 #include "cb_serve_internal.h"
 #include "cb_attn_rows.h"
-#include <cstdlib>
 
 namespace cb {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) double f64x4_t;
 
+constexpr int kTokens = 16;             // of a request that share the bounds read
+constexpr int kPages = 256;             // pages of a workgroup
+constexpr int kWaveTable = 8192;        // table entries up to which a wave has a row's keys (32 KB)
+constexpr uint32_t kUnknown = 0xff800000u;   // key of an estimate that says nothing (and of the scores +infinity and NaN)
 
-// Tile `idx` of all requests' token tiles of T, and its request, every wave for itself.
-template <int T>
+// Tile `idx` of all requests' token tiles, and its request, every wave for itself.
 __device__ __forceinline__ bool find_tile(const PagedArgs &a, uint32_t idx, Request &rq, int32_t &req, int32_t &tile) {
     const int lane = threadIdx.x & 63;
     uint32_t before = 0;
     for (int r0 = 0; r0 < a.n_reqs; r0 += 64) {
         const Request r = request(a, min(r0 + lane, a.n_reqs - 1));
-        const uint32_t n = r0 + lane < a.n_reqs ? (uint32_t)(r.q_len + T - 1) / T : 0;
+        const uint32_t n = r0 + lane < a.n_reqs ? (uint32_t)(r.q_len + kTokens - 1) / kTokens : 0;
         const uint32_t sum = wave_sums(n), total = (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
         if (idx - before < total) {
             const uint32_t k = idx - before - (sum - n);
@@ -59,108 +73,220 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// T tokens of a request share the bounds read: 16, or 4 where requests have few.
-template <int D, int EL, int T, int NW>
-__global__ __launch_bounds__(64 * NW) void scores_kernel(SelectArgs s) {
-    constexpr int NT = 64 * NW, STEP = 16 * NW;                // threads, pages that the waves have at a time
-    constexpr bool F8 = EL != kBf16;
-    constexpr int E = F8 ? 16 : 8, NP = 2 * D / (4 * E);       // channels of a piece, pieces of a lane
-    constexpr int QS = 2 * D + 2;                              // (16 tokens' pairs of sums in 64 banks)
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+
+// What a workgroup of one head has: 16 tokens of a request and some of the pages up to the last one's own.
+struct Work { Request rq; int32_t req, tok0, n_tok, base, first, end; };   // base: the first token's position
+__device__ __forceinline__ bool find_work(const SelectArgs &s, Work &w) {
     const PagedArgs &a = s.a;
-    __shared__ __attribute__((aligned(16))) double sums[T * QS];   // of every token: sum q-, sum q+ over the group
+    int32_t tile = 0;
+    if (!find_tile(a, blockIdx.x, w.rq, w.req, tile)) return false;
+    w.tok0 = tile * kTokens;
+    w.n_tok = min(w.rq.q_len - w.tok0, kTokens);
+    // (tokens of this round)
+    if (w.rq.row0 + w.tok0 >= s.tok1 || w.rq.row0 + w.tok0 + w.n_tok <= s.tok0) return false;
+    w.base = w.rq.kv_len - w.rq.q_len + w.tok0;
+    const int32_t p_hi = w.base + w.n_tok - 1;
+    if (p_hi < 0) return false;
+    w.first = (int32_t)blockIdx.z * kPages;
+    w.end = min(w.first + kPages, (int32_t)fast_div((uint32_t)p_hi, a.page_size) + 1);
+    return w.first < w.end;
+}
+
+// The key of page i for token t of the workgroup, or none where it is no candidate.
+__device__ __forceinline__ void write_key(const SelectArgs &s, const Work &w, int head, int t, int32_t i, bool ok, uint32_t key) {
+    const PagedArgs &a = s.a;
+    const int32_t tok = w.rq.row0 + w.tok0 + t, pos = w.base + t;
+    if (t >= w.n_tok || pos < 0 || tok < s.tok0 || tok >= s.tok1) return;
+    const int32_t own = (int32_t)fast_div((uint32_t)pos, a.page_size);
+    if (i > own) return;
+    if (i < s.n_first || i > own - s.n_last) key = 0xffffffffu;
+    s.keys[((int64_t)(tok - s.tok0) * a.n_heads + head) * a.table_width + i] = ok ? key : 0u;
+}
+
+template <int D, int EL>
+__global__ __launch_bounds__(256, 4) void estimates_kernel(SelectArgs s) {
+    constexpr bool F8 = EL != kBf16;
+    constexpr int NP = 2 * D * (F8 ? 1 : 2) / 64;              // pieces of 64 bytes of a page's bounds
+    constexpr int QS = 2 * D + 8;                              // (16 tokens' pieces of 16 bytes in 64 banks)
+    const PagedArgs &a = s.a;
+    // every token's sum q-, sum q+ over the group as two bf16 numbers
+    __shared__ __attribute__((aligned(16))) uint16_t parts[2][kTokens * QS];
     const int head = (int)blockIdx.y, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
-    int32_t req = 0, tile = 0;
-    Request rq;
-    if (!find_tile<T>(a, blockIdx.x, rq, req, tile)) return;
-    const int32_t tok0 = tile * T, n_tok = min(rq.q_len - tok0, T);
-    // (tokens of this round)
-    if (rq.row0 + tok0 >= s.tok1 || rq.row0 + tok0 + n_tok <= s.tok0) return;
-    const int32_t base = rq.kv_len - rq.q_len + tok0, p_hi = base + n_tok - 1;
-    if (p_hi < 0) return;
-    const int32_t every = (int32_t)fast_div((uint32_t)p_hi, a.page_size) + 1;
-    const int32_t first = (int32_t)blockIdx.z * s.per, end = min(first + s.per, every);
-    if (first >= end) return;
+    Work wk;
+    if (!find_work(s, wk)) return;
 
-    // the bounds of 16 pages, lane's page i0 + n: pieces of 16 bytes, requested while those before are worked on
-    const int32_t *table = a.table + req * a.table_stride;
+    // the bounds of 16 pages: lane l has 16 bytes of every piece of page i0 + l / 4, requested while those before are
+    // worked on
+    const int32_t *table = a.table + wk.req * a.table_stride;
     int32_t page = 0;
-    auto look_up = [&](int32_t i0) __attribute__((always_inline)) { page = table[min(i0 + n, end - 1)]; };
+    auto look_up = [&](int32_t i0) __attribute__((always_inline)) { page = table[min(i0 + (lane >> 2), wk.end - 1)]; };
     u32x4_t ahead[NP];
     float scale_n = 1.f;
-    bool ok_n = false;
+    uint64_t ok_n = 0;
     auto load = [&](int32_t i0) __attribute__((always_inline)) {
-        ok_n = i0 + n < end && (uint32_t)page < (uint32_t)a.n_pages;
-        const int64_t at = (int64_t)(ok_n ? page : 0) * a.n_heads + head;
-        const char *x = s.bounds + at * (2 * D * (F8 ? 1 : 2)) + 16 * g;
+        const bool ok = i0 + (lane >> 2) < wk.end && (uint32_t)page < (uint32_t)a.n_pages;
+        ok_n = __ballot(ok);
+        const int64_t at = (int64_t)(ok ? page : 0) * a.n_heads + head;
+        const char *x = s.bounds + at * (2 * D * (F8 ? 1 : 2)) + 16 * (lane & 3);
 #pragma unroll
         for (int p = 0; p < NP; ++p) ahead[p] = *(const u32x4_t *)(x + 64 * p);
         if (EL == kBlocks) scale_n = a.kscale[2 * at];
     };
-    int32_t i0 = first + 16 * wave;
-    if (i0 < end) {
+    int32_t i0 = wk.first + 16 * wave;
+    if (i0 < wk.end) {
         look_up(i0);
         load(i0);
-        if (i0 + STEP < end) look_up(i0 + STEP);
+        if (i0 + 64 < wk.end) look_up(i0 + 64);
     }
 
-    // sums over the group's heads: a thread has 8 channels of a token, and where there are fewer of these than threads,
-    // every HS-th head
-    constexpr int HS = T == 4 ? NW : NW / 4;
+    // a thread has 8 channels of a token
     const int32_t G = (int32_t)a.G.d;
-    for (int u = tid / HS; u < T * (D / 8); u += NT / HS) {
+    for (int u = tid; u < kTokens * (D / 8); u += 256) {
         const int t = u / (D / 8), c = u % (D / 8) * 8;
-        double lo[8] = {}, hi[8] = {};
-        if (t < n_tok) {
-            const uint16_t *q = a.q + (int64_t)(rq.row0 + tok0 + t) * a.q_tok + (int64_t)head * G * a.q_head + c;
-#pragma unroll 4
-            for (int h = tid % HS; h < G; h += HS) {
+        float lo[8] = {}, hi[8] = {};
+        if (t < wk.n_tok) {
+            const uint16_t *q = a.q + (int64_t)(wk.rq.row0 + wk.tok0 + t) * a.q_tok + (int64_t)head * G * a.q_head + c;
+#pragma unroll 8
+            for (int h = 0; h < G; ++h) {
                 const u32x4_t x = *(const u32x4_t *)(q + h * a.q_head);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float v = e & 1 ? bf_hi(x[e >> 1]) : bf_lo(x[e >> 1]);
                     // (a NaN goes to both)
+                    lo[e] += __builtin_elementwise_minimum(v, 0.f);
+                    hi[e] += __builtin_elementwise_maximum(v, 0.f);
+                }
+            }
+        }
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            const float *y = z ? hi : lo;
+            uint32_t h[4], m[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                h[e] = pack_bf16(y[2 * e], y[2 * e + 1]);
+                m[e] = pack_bf16(y[2 * e] - bf_lo(h[e]), y[2 * e + 1] - bf_hi(h[e]));
+            }
+            *(uint4 *)&parts[0][t * QS + z * D + c] = make_uint4(h[0], h[1], h[2], h[3]);
+            *(uint4 *)&parts[1][t * QS + z * D + c] = make_uint4(m[0], m[1], m[2], m[3]);
+        }
+    }
+    __syncthreads();
+
+    uint32_t most[4] = {0, 0, 0, 0};                           // the bits of the largest S of the lane's tokens
+    // the lane's token's parts of its channels; read from LDS for every 16 pages
+    int q_at = n * QS + (F8 ? 16 : 8) * g;
+    for (; i0 < wk.end; i0 += 64) {
+        asm volatile("" : "+v"(q_at));
+        u32x4_t w[NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[p][e] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (4 * n + g), (int)ahead[p][e]);
+        const float scale = EL == kBlocks ? __uint_as_float(__float_as_uint(__shfl(scale_n, 4 * n)) & 0x7f800000u) : 1.f;
+        const bool ok = (ok_n >> (4 * n)) & 1;
+        if (i0 + 64 < wk.end) {
+            load(i0 + 64);
+            if (i0 + 128 < wk.end) look_up(i0 + 128);
+        }
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f}, size = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int st = 0; st < (F8 ? 2 : 1); ++st) {
+                uint32_t b[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (F8) b[e] = e & 1 ? e4m3_pair<true>(w[p][2 * st + (e >> 1)]) : e4m3_pair<false>(w[p][2 * st + (e >> 1)]);
+                    else b[e] = w[p][e];
+                }
+                const int at = q_at + (F8 ? 64 * p + 8 * st : 32 * p);
+                const u32x4_t h = *(const u32x4_t *)&parts[0][at], m = *(const u32x4_t *)&parts[1][at];
+                const bf16x8_t bf = frag(b[0], b[1], b[2], b[3]);
+                f32x4_t step = {0.f, 0.f, 0.f, 0.f};
+                step = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(h[0], h[1], h[2], h[3]), bf, step, 0, 0, 0);
+                step = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(m[0], m[1], m[2], m[3]), bf, step, 0, 0, 0);
+                sum += step;
+                const uint32_t k = 0x7fff7fffu;
+                size = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(h[0] & k, h[1] & k, h[2] & k, h[3] & k),
+                                                               frag(b[0] & k, b[1] & k, b[2] & k, b[3] & k), size, 0, 0, 0);
+            }
+        const int32_t i = i0 + n;
+        if (i >= wk.end) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            // lane's tokens 4 g + k; an estimate says nothing where its terms leave fp32's range
+            const float size_k = size[k] * scale;
+            const bool good = size_k >= 0x1p-100f && size_k <= 0x1p126f && scale >= 0x1p-100f && scale <= 0x1p100f;
+            if (good && ok) most[k] = max(most[k], __float_as_uint(size_k));
+            write_key(s, wk, head, 4 * g + k, i, ok, good ? order_of(sum[k] * scale) : kUnknown);
+        }
+    }
+    // the largest S of every token, one number for each wave
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) most[k] = max(most[k], (uint32_t)__shfl_xor((int)most[k], o));
+        const int32_t t = 4 * g + k, tok = wk.rq.row0 + wk.tok0 + t;
+        if (n == 0 && t < wk.n_tok && tok >= s.tok0 && tok < s.tok1)
+            s.sizes[((int64_t)(tok - s.tok0) * a.n_heads + head) * s.slots + 4 * blockIdx.z + wave] = __uint_as_float(most[k]);
+    }
+}
+
+template <int D, int EL>
+__global__ __launch_bounds__(256) void scores_kernel(SelectArgs s) {
+    constexpr bool F8 = EL != kBf16;
+    constexpr int E = F8 ? 16 : 8, NP = 2 * D / (4 * E);       // channels of a piece, pieces of a lane
+    constexpr int QS = 2 * D + 2;                              // (16 tokens' pairs of sums in 64 banks)
+    const PagedArgs &a = s.a;
+    __shared__ __attribute__((aligned(16))) double sums[kTokens * QS];   // of every token: sum q-, sum q+ over the group
+    const int head = (int)blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, g = lane >> 4;
+    Work wk;
+    if (!find_work(s, wk)) return;
+    const int32_t G = (int32_t)a.G.d;
+    for (int u = tid; u < kTokens * (D / 8); u += 256) {
+        const int t = u / (D / 8), c = u % (D / 8) * 8;
+        double lo[8] = {}, hi[8] = {};
+        if (t < wk.n_tok) {
+            const uint16_t *q = a.q + (int64_t)(wk.rq.row0 + wk.tok0 + t) * a.q_tok + (int64_t)head * G * a.q_head + c;
+#pragma unroll 4
+            for (int h = 0; h < G; ++h) {
+                const u32x4_t x = *(const u32x4_t *)(q + h * a.q_head);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = e & 1 ? bf_hi(x[e >> 1]) : bf_lo(x[e >> 1]);
                     lo[e] += (double)__builtin_elementwise_minimum(v, 0.f);
                     hi[e] += (double)__builtin_elementwise_maximum(v, 0.f);
                 }
             }
         }
 #pragma unroll
-        for (int o = 1; o < HS; o <<= 1) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                lo[e] += __shfl_xor(lo[e], o);
-                hi[e] += __shfl_xor(hi[e], o);
-            }
-        }
-        if (tid % HS == 0) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                sums[t * QS + c + e] = lo[e];
-                sums[t * QS + D + c + e] = hi[e];
-            }
+        for (int e = 0; e < 8; ++e) {
+            sums[t * QS + c + e] = lo[e];
+            sums[t * QS + D + c + e] = hi[e];
         }
     }
     __syncthreads();
-
-    // the lane's token's sums of its channels; read from LDS for every 16 pages (registers for them would leave two waves a
-    // SIMD)
-    int q_at = (n & (T - 1)) * QS + E * g;
-    for (; i0 < end; i0 += STEP) {
+    const int32_t *table = a.table + wk.req * a.table_stride;
+    int q_at = n * QS + E * g;
+    for (int32_t i0 = wk.first + 16 * wave; i0 < wk.end; i0 += 64) {
         asm volatile("" : "+v"(q_at));
         const double *qa = sums + q_at;
+        const int32_t i = i0 + n;                              // the lane's page
+        const int32_t page = i < wk.end ? table[i] : -1;
+        const bool ok = (uint32_t)page < (uint32_t)a.n_pages;
+        const int64_t at = (int64_t)(ok ? page : 0) * a.n_heads + head;
+        const char *x = s.bounds + at * (2 * D * (F8 ? 1 : 2)) + 16 * g;
         u32x4_t w[NP];
 #pragma unroll
-        for (int p = 0; p < NP; ++p) w[p] = ahead[p];
-        const float scale = EL == kBlocks ? __uint_as_float(__float_as_uint(scale_n) & 0x7f800000u) : 1.f;
-        const bool ok = ok_n;
-        if (i0 + STEP < end) {
-            load(i0 + STEP);
-            if (i0 + 2 * STEP < end) look_up(i0 + 2 * STEP);
-        }
+        for (int p = 0; p < NP; ++p) w[p] = *(const u32x4_t *)(x + 64 * p);
+        const float scale = EL == kBlocks ? __uint_as_float(__float_as_uint(a.kscale[2 * at]) & 0x7f800000u) : 1.f;
         f64x4_t acc = {0.0, 0.0, 0.0, 0.0};
-        double few[2] = {0.0, 0.0};
 #pragma unroll
         for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -168,34 +294,21 @@ __global__ __launch_bounds__(64 * NW) void scores_kernel(SelectArgs s) {
                 uint32_t u;
                 if constexpr (F8) u = (e & 2) ? e4m3_pair<true>(w[p][e >> 2]) : e4m3_pair<false>(w[p][e >> 2]);
                 else u = w[p][e >> 1];
-                const double b = (double)((e & 1) ? bf_hi(u) : bf_lo(u));
-                if constexpr (T == 16) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qa[4 * E * p + e], b, acc, 0, 0, 0);
-                else few[e & 1] = __builtin_amdgcn_mfma_f64_4x4x4f64(qa[4 * E * p + e], b, few[e & 1], 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qa[4 * E * p + e], (double)((e & 1) ? bf_hi(u) : bf_lo(u)), acc, 0, 0, 0);
             }
-        if (T == 4) acc[0] = few[0] + few[1];
-        const int32_t i = i0 + n;
-        if (i >= end) continue;
+        if (i >= wk.end) continue;
 #pragma unroll
-        for (int k = 0; k < T / 4; ++k) {
-            const int t = g + 4 * k, tok = rq.row0 + tok0 + t;
-            const int32_t pos = base + t;
-            if (t >= n_tok || pos < 0 || tok < s.tok0 || tok >= s.tok1) continue;
-            const int32_t own = (int32_t)fast_div((uint32_t)pos, a.page_size);
-            if (i > own) continue;
-            uint32_t key = order_of((float)(acc[k] * (double)scale));
-            if (i < s.n_first || i > own - s.n_last) key = 0xffffffffu;
-            s.keys[((int64_t)(tok - s.tok0) * a.n_heads + head) * a.table_width + i] = ok ? key : 0u;
-        }
+        for (int k = 0; k < 4; ++k) write_key(s, wk, head, g + 4 * k, i, ok, order_of((float)(acc[k] * (double)scale)));
     }
 }
 
 // The row (token, head) of a choice: the candidates' number, its keys and its list; false for a token of no request.
-__device__ __forceinline__ bool choice(const SelectArgs &s, int32_t t, int32_t head, int32_t &n, const uint32_t *&keys, int32_t *&out) {
+__device__ __forceinline__ bool choice(const SelectArgs &s, int32_t t, int32_t head, int32_t &req, int32_t &n, const uint32_t *&keys,
+                                       int32_t *&out) {
     const PagedArgs &a = s.a;
-    const int32_t tok = s.tok0 + t, req = request_of(a, tok);
-    if (req < 0) return false;
-    const Request rq = request(a, req);
-    if (tok < rq.row0 || tok >= rq.row0 + rq.q_len) return false;
+    const int32_t tok = s.tok0 + t;
+    Request rq;
+    if (!request_of(a, tok, req, rq)) return false;
     const int32_t pos = rq.kv_len - rq.q_len + (tok - rq.row0);
     n = pos < 0 ? 0 : (int32_t)fast_div((uint32_t)pos, a.page_size) + 1;
     keys = s.keys + ((int64_t)t * a.n_heads + head) * a.table_width;
@@ -203,37 +316,39 @@ __device__ __forceinline__ bool choice(const SelectArgs &s, int32_t t, int32_t h
     return true;
 }
 
-// Rows of up to 64 K candidates, a wave each, keys in registers.
-template <int K>
-__global__ __launch_bounds__(256) void choose_wave_kernel(SelectArgs s) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t t = (int32_t)blockIdx.x, head = (int32_t)blockIdx.y * 4 + wave;
-    if (head >= s.a.n_heads) return;
-    int32_t n;
-    const uint32_t *keys;
-    int32_t *out;
-    if (!choice(s, t, head, n, keys, out)) return;
-    uint32_t k[K];
-#pragma unroll
-    for (int j = 0; j < K; ++j) k[j] = 64 * j + lane < n ? keys[64 * j + lane] : 0u;
-    // counts lane by lane, then over the wave
-    auto at_least = [&](uint32_t x) __attribute__((always_inline)) {
+// Keys of a row in LDS, of one wave: lane l has keys 4 l .. 4 l + 3 of every 256, absent ones 0.  (In registers they make
+// code of thousands of instructions that every workgroup runs once: 28 us where this takes 22.)
+struct Keys {
+    uint4 *k;
+    int groups;                                                // of 256
+
+    // keys that reach x, counted lane by lane, then over the wave
+    __device__ __forceinline__ int at_least(uint32_t x) const {
+        const int lane = threadIdx.x;
         uint32_t c = 0;
-#pragma unroll
-        for (int j = 0; j < K; ++j) c += k[j] >= x ? 1u : 0u;
+#pragma unroll 4
+        for (int j = 0; j < groups; ++j) {
+            const uint4 v = k[64 * j + lane];
+            c += (v.x >= x ? 1u : 0u) + (v.y >= x ? 1u : 0u) + (v.z >= x ? 1u : 0u) + (v.w >= x ? 1u : 0u);
+        }
         return __builtin_amdgcn_readlane((int)wave_sums(c), 63);
-    };
-    // taken are the keys above `least` and the first `equal` of just that
-    uint32_t least = 0;
-    int equal = 0;
-    if (at_least(1) > s.n_selected) {
-        // the scores' keys (neither those always taken nor the absent): bits that all of them share are the threshold's too
+    }
+    // The largest number that n keys reach, or one that just n reach (exact: true); more than n keys are not 0, fewer
+    // or just n all ones.
+    __device__ __forceinline__ uint32_t threshold(int n, bool &exact) const {
+        // bits that all keys but 0 and all ones share are the threshold's too
+        const int lane = threadIdx.x;
         uint32_t all = ~0u, any = 0;
+#pragma unroll 4
+        for (int j = 0; j < groups; ++j) {
+            const uint4 v = k[64 * j + lane];
+            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const bool is = k[j] - 1 < 0xfffffffeu;
-            all &= is ? k[j] : ~0u;
-            any |= is ? k[j] : 0u;
+            for (int c = 0; c < 4; ++c) {
+                const bool is = u[c] - 1 < ~0u - 1;
+                all &= is ? u[c] : ~0u;
+                any |= is ? u[c] : 0u;
+            }
         }
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -242,35 +357,259 @@ __global__ __launch_bounds__(256) void choose_wave_kernel(SelectArgs s) {
         }
         all = (uint32_t)__builtin_amdgcn_readfirstlane((int)all);
         any = (uint32_t)__builtin_amdgcn_readfirstlane((int)any);
-        const int top = 31 - __builtin_clz((all ^ any) | 1u);        // the highest bit in which two differ
-        least = top == 31 ? 0u : any & ~((2u << top) - 1);
-        // the largest number that n_selected keys reach, from that bit on; or one that just so many reach
+        const int top = 31 - __builtin_clz((all ^ any) | 1u);      // the highest bit in which two differ
+        uint32_t x = top == 31 ? 0u : any & ~((2u << top) - 1);
+        exact = false;
         for (int bit = top; bit >= 0; --bit) {
-            const uint32_t x = least | 1u << bit;
-            const int c = at_least(x);
-            if (c < s.n_selected) continue;
-            least = x;
-            equal = -1;
-            if (c == s.n_selected) break;
-            equal = 0;
+            const int c = at_least(x | 1u << bit);
+            if (c < n) continue;
+            x |= 1u << bit;
+            exact = c == n;
+            if (exact) break;
         }
-        if (equal < 0) {
-            least -= 1;
-            equal = 0;
+        return x;
+    }
+    // the smallest key that reaches x, and whether a key is y
+    __device__ __forceinline__ uint32_t first_from(uint32_t x, uint32_t y, bool &found) const {
+        uint32_t m = ~0u;
+        bool is = false;
+#pragma unroll 4
+        for (int j = 0; j < groups; ++j) {
+            const uint4 v = k[64 * j + threadIdx.x];
+            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                m = u[c] >= x ? min(m, u[c]) : m;
+                is |= u[c] == y;
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) m = min(m, (uint32_t)__shfl_xor((int)m, o));
+        found = __any(is);
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)m);
+    }
+};
+
+// The scores of pages of one row by its wave: element lane + 64 j of (sum q-, sum q+) and of the pages' bounds in a lane.
+struct Scores {
+    double q[4];
+    int n, d;
+    const int32_t *table;
+
+    __device__ __forceinline__ Scores(const SelectArgs &s, int32_t req, int32_t tok, int32_t head) {
+        const PagedArgs &a = s.a;
+        const int lane = threadIdx.x & 63, G = (int)a.G.d;
+        d = s.head_dim;
+        n = 2 * d / 64;
+        table = a.table + req * a.table_stride;
+        const uint16_t *x = a.q + (int64_t)tok * a.q_tok + (int64_t)head * G * a.q_head;
+        int c[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            q[j] = 0.0;
+            const int e = j < n ? lane + 64 * j : 0;
+            c[j] = e >= d ? e - d : e;
+        }
+        // (eight heads' values on their way together; behind the last, it again, left out)
+        for (int h0 = 0; h0 < G; h0 += 8) {
+            uint16_t v[8][4];
+#pragma unroll
+            for (int h = 0; h < 8; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[h][j] = x[min(h0 + h, G - 1) * a.q_head + c[j]];
+#pragma unroll
+            for (int h = 0; h < 8; ++h) {
+                if (h0 + h >= G) continue;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float y = __uint_as_float((uint32_t)v[h][j] << 16);
+                    q[j] += (double)(lane + 64 * j >= d ? __builtin_elementwise_maximum(y, 0.f) : __builtin_elementwise_minimum(y, 0.f));
+                }
+            }
+        }
+    }
+    // the keys of four pages
+    __device__ __forceinline__ void keys(const SelectArgs &s, int32_t head, const int32_t (&i)[4], uint32_t (&key)[4]) const {
+        const PagedArgs &a = s.a;
+        const int lane = threadIdx.x & 63;
+        float b[4][4], scale[4];
+        int32_t page[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) page[p] = table[i[p]];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const int64_t at = (int64_t)__builtin_amdgcn_readfirstlane(page[p]) * a.n_heads + head;
+            scale[p] = s.dtype == CB_PAGES_E4M3_BLOCKS ? a.kscale[2 * at] : 1.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                b[p][j] = 0.f;
+                if (j >= n) continue;
+                const int64_t e = at * 2 * d + lane + 64 * j;
+                b[p][j] = s.dtype == CB_PAGES_BF16 ? __uint_as_float((uint32_t)((const uint16_t *)s.bounds)[e] << 16)
+                                                   : bf_lo(e4m3_pair<false>(((const uint8_t *)s.bounds)[e]));
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            double sum = 0.0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < n) sum += q[j] * (double)b[p][j];
+            sum = wave_sums(sum);
+            const float score = (float)(sum * (double)__uint_as_float(__float_as_uint(scale[p]) & 0x7f800000u));
+            key[p] = order_of(__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(score), 63)));
+        }
+    }
+};
+
+constexpr int kScored = 64;             // pages whose scores are formed at a time
+
+// The places of the keys from lo to hi, of kScored of them from the one of number `from` on, in their order; returns how
+// many there are.
+__device__ __forceinline__ int between(const Keys &row, uint32_t lo, uint32_t hi, int from, int32_t *place) {
+    const int lane = threadIdx.x;
+    int rank = 0;
+    for (int j = 0; j < row.groups; ++j) {
+        const uint4 v = row.k[64 * j + lane];
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+        int mine = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mine += u[c] >= lo && u[c] <= hi ? 1 : 0;
+        if (!__any(mine)) continue;
+        const int sum = (int)wave_sums((uint32_t)mine);
+        int at = rank + sum - mine - from;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (u[c] < lo || u[c] > hi) continue;
+            if (at >= 0 && at < kScored) place[at] = 256 * j + 4 * lane + c;
+            ++at;
+        }
+        rank += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return rank;
+}
+
+// Rows whose keys fit LDS, a wave each.
+__global__ __launch_bounds__(64) void choose_wave_kernel(SelectArgs s) {
+    extern __shared__ __attribute__((aligned(16))) uint4 lds[];
+    __shared__ int32_t place[kScored];
+    const int lane = threadIdx.x;
+    const int32_t t = (int32_t)blockIdx.x, head = (int32_t)blockIdx.y;
+    int32_t req, n;
+    const uint32_t *keys;
+    int32_t *out;
+    if (!choice(s, t, head, req, n, keys, out)) return;
+    const float *sizes = s.sizes + ((int64_t)t * s.a.n_heads + head) * s.slots;
+    uint32_t most = 0;
+    for (int i = lane; i < 4 * ((n + kPages - 1) / kPages); i += 64) most = max(most, __float_as_uint(sizes[i]));
+    const Keys row = {lds, (n + 255) / 256};
+    uint32_t *key_at = (uint32_t *)lds;
+    for (int j0 = 0; j0 < row.groups; j0 += 8) {               // (2,048 keys on their way together)
+        uint32_t u[8][4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (j0 + j < row.groups) u[j][c] = keys[min(256 * (j0 + j) + 64 * c + lane, n - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int i = 256 * (j0 + j) + 64 * c + lane;
+                if (j0 + j < row.groups) key_at[i] = i < n ? u[j][c] : 0u;
+            }
+    }
+    __syncthreads();
+    // taken are the keys above `least` and the first `equal` of just that
+    uint32_t least = 0;
+    int equal = 0;
+    if (row.at_least(1) > s.n_selected) {
+        bool exact, unknown;
+        const uint32_t border = row.first_from(row.threshold(s.n_selected, exact), kUnknown, unknown);
+        if (border == ~0u) {
+            least = ~0u - 1;                                   // those always taken are all
         } else {
-            equal = s.n_selected - at_least(least + 1);
+            // pages whose estimates are within the errors of the n_selected-th: between lo and hi
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+            const float at = value_of(border);
+            // (each of two estimates off by (2^-16 + G 2^-23) S, and two scores that round to one number)
+            const float far = 2.f * (0x1p-16f + 0x1p-23f * (float)s.a.G.d) * __uint_as_float(most) + 0x1p-22f * fabsf(at);
+            const uint32_t lo = unknown ? 1u : order_of(at - far), hi = unknown ? ~0u - 1 : order_of(at + far);
+            if (row.at_least(lo) == s.n_selected) {
+                least = lo - 1;
+            } else {
+                // Those above are taken, those below are not, and of those between as many as are needed.
+                Scores scores(s, req, s.tok0 + t, head);
+                // the key of the lane's page of `count` that `place` has
+                auto score = [&](int count) __attribute__((always_inline)) {
+                    uint32_t mine = 0;
+                    for (int p0 = 0; p0 < count; p0 += 4) {
+                        int32_t i[4];
+                        uint32_t key[4];
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) i[p] = __builtin_amdgcn_readfirstlane(place[min(p0 + p, count - 1)]);
+                        scores.keys(s, head, i, key);
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) mine = lane == p0 + p ? key[p] : mine;
+                    }
+                    return mine;
+                };
+                const int open = between(row, lo, hi, 0, place);
+                if (open <= kScored) {
+                    const int need = s.n_selected - row.at_least(hi + 1);
+                    __syncthreads();
+                    const uint32_t mine = score(open);
+                    // how many come before the lane's: those with a larger key, or an equal one and a lower place
+                    int before = 0;
+                    for (int p = 0; p < open; ++p) {
+                        const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)mine, p);
+                        before += other > mine || (other == mine && p < lane) ? 1 : 0;
+                    }
+                    if (lane < open) key_at[place[lane]] = before < need ? ~0u : 0u;
+                    least = hi;
+                } else {
+                    // (rows of infinities, or of many pages that are nearly alike) the open keys become scores, which are
+                    // neither 0 nor all ones
+                    for (int i = lane; i < 256 * row.groups; i += 64) {
+                        const uint32_t k = key_at[i];
+                        key_at[i] = k > hi ? ~0u : k >= lo ? k : 0u;
+                    }
+                    for (int from = 0; from < open; from += kScored) {
+                        __syncthreads();
+                        between(row, 1, ~0u - 1, from, place);
+                        __syncthreads();
+                        const int count = min(open - from, kScored);
+                        const uint32_t mine = score(count);
+                        if (lane < count) key_at[place[lane]] = mine;
+                    }
+                    __syncthreads();
+                    least = row.threshold(s.n_selected, exact);
+                    if (exact) least -= 1;
+                    else equal = s.n_selected - row.at_least(least + 1);
+                }
+                __syncthreads();
+            }
         }
     }
     int n_out = 0, n_equal = 0;
-    const uint64_t below = (1ull << lane) - 1;
+    for (int j = 0; j < row.groups; ++j) {
+        const uint4 v = row.k[64 * j + lane];
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+        uint32_t mine = 0;                                     // keys above, and 2^16 for each of just that
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-        const bool above = k[j] > least, same = equal > 0 && k[j] == least;
-        const uint64_t gt = __ballot(above), eq = __ballot(same);
-        const int e = n_equal + __builtin_popcountll(eq & below);
-        if (above || (same && e < equal)) out[n_out + __builtin_popcountll(gt & below) + min(e, equal)] = 64 * j + lane;
-        n_out += __builtin_popcountll(gt);
-        n_equal += __builtin_popcountll(eq);
+        for (int c = 0; c < 4; ++c) mine += u[c] > least ? 1u : equal > 0 && u[c] == least ? 0x10000u : 0u;
+        const uint32_t sum = wave_sums(mine), all = (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
+        int above = n_out + (int)((sum - mine) & 0xffff), same = n_equal + (int)((sum - mine) >> 16);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const bool is = equal > 0 && u[c] == least;
+            if (u[c] > least || (is && same < equal)) out[above + min(same, equal)] = 256 * j + 4 * lane + c;
+            above += u[c] > least ? 1 : 0;
+            same += is ? 1 : 0;
+        }
+        n_out += (int)(all & 0xffff);
+        n_equal += (int)(all >> 16);
     }
     for (int i = n_out + min(n_equal, equal) + lane; i < s.n_selected; i += 64) out[i] = -1;
 }
@@ -279,10 +618,10 @@ __global__ __launch_bounds__(256) void choose_wave_kernel(SelectArgs s) {
 __global__ __launch_bounds__(256) void choose_kernel(SelectArgs s) {
     __shared__ uint32_t hist[256], wsum[4], found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int32_t n;
+    int32_t req, n;
     const uint32_t *keys;
     int32_t *out;
-    if (!choice(s, (int32_t)blockIdx.x, (int32_t)blockIdx.y, n, keys, out)) return;
+    if (!choice(s, (int32_t)blockIdx.x, (int32_t)blockIdx.y, req, n, keys, out)) return;
 
     // the sum over the workgroup
     auto total_of = [&](uint32_t x) __attribute__((always_inline)) {
@@ -352,28 +691,26 @@ __global__ __launch_bounds__(256) void choose_kernel(SelectArgs s) {
     for (uint32_t i = n_out + min(n_equal, equal) + tid; i < (uint32_t)s.n_selected; i += 256) out[i] = -1;
 }
 
-template <int D, int EL> hipError_t launch(SelectArgs s, uint32_t *ws, int64_t ws_bytes, hipStream_t stream) {
+template <int D, int EL> hipError_t launch(SelectArgs s, char *ws, int64_t ws_bytes, hipStream_t stream) {
     const PagedArgs &a = s.a;
-    const int64_t each = (int64_t)a.n_heads * a.table_width * 4;
+    const int64_t each = select_row_bytes(a.table_width) * a.n_heads;
     const int64_t round = std::min<int64_t>(std::min<int64_t>(a.n_tokens, 1 << 20), each > 0 ? ws_bytes / each : a.n_tokens);
-    const bool few = (int64_t)a.n_tokens <= 4 * (int64_t)a.n_reqs;
-    const int T = few ? 4 : 16;
-    const int64_t tiles = std::min<int64_t>((int64_t)a.n_tokens / T + a.n_reqs, a.n_tokens);
-    s.per = getenv("CBP") ? atoi(getenv("CBP")) : 256;
-    const int64_t blocks = ((int64_t)a.table_width + s.per - 1) / s.per;
+    const int64_t tiles = std::min<int64_t>((int64_t)a.n_tokens / kTokens + a.n_reqs, a.n_tokens);
+    const int64_t blocks = ((int64_t)a.table_width + kPages - 1) / kPages;
     if (round < 1 || blocks > 65535) return hipErrorInvalidValue;
-    s.keys = ws;
+    s.keys = (uint32_t *)ws;
+    s.sizes = (float *)ws + round * a.n_heads * a.table_width;
+    s.slots = (int32_t)blocks * 4;
+    const bool waves = a.table_width <= kWaveTable;
+    const unsigned lds = (unsigned)((a.table_width + 255) / 256 * 1024);
     for (int64_t t = 0; t < a.n_tokens; t += round) {
         s.tok0 = (int32_t)t;
         s.tok1 = (int32_t)std::min<int64_t>(t + round, a.n_tokens);
-        if (blocks > 0)
-{ const bool w8 = getenv("CBW") && atoi(getenv("CBW")) == 8;
-            hipLaunchKernelGGL((w8 ? few ? scores_kernel<D, EL, 4, 8> : scores_kernel<D, EL, 16, 8> : few ? scores_kernel<D, EL, 4, 4> : scores_kernel<D, EL, 16, 4>),
-                               dim3((unsigned)tiles, (unsigned)a.n_heads, (unsigned)blocks), dim3(w8 ? 512 : 256), 0, stream, s); }
-        const auto waves = a.table_width <= 512 ? choose_wave_kernel<8> : a.table_width <= 1024 ? choose_wave_kernel<16>
-                           : a.table_width <= 2048 ? choose_wave_kernel<32> : nullptr;
         const unsigned tokens = (unsigned)(s.tok1 - s.tok0);
-        if (waves) hipLaunchKernelGGL(waves, dim3(tokens, (unsigned)(a.n_heads + 3) / 4), dim3(256), 0, stream, s);
+        if (blocks > 0)
+            hipLaunchKernelGGL((waves ? estimates_kernel<D, EL> : scores_kernel<D, EL>),
+                               dim3((unsigned)tiles, (unsigned)a.n_heads, (unsigned)blocks), dim3(256), 0, stream, s);
+        if (waves) hipLaunchKernelGGL(choose_wave_kernel, dim3(tokens, (unsigned)a.n_heads), dim3(64), lds, stream, s);
         else hipLaunchKernelGGL(choose_kernel, dim3(tokens, (unsigned)a.n_heads), dim3(256), 0, stream, s);
     }
     return hipGetLastError();
@@ -381,8 +718,12 @@ template <int D, int EL> hipError_t launch(SelectArgs s, uint32_t *ws, int64_t w
 
 }  // namespace
 
+int64_t select_row_bytes(int32_t table_width) {
+    return 4 * ((int64_t)table_width + 4 * (((int64_t)table_width + kPages - 1) / kPages));
+}
+
 hipError_t launch_page_select(const SelectArgs &s, int32_t d, int32_t dtype, void *ws, int64_t ws_bytes, hipStream_t stream) {
-    uint32_t *w = (uint32_t *)ws;
+    char *w = (char *)ws;
     switch (d * 4 + dtype) {
         case 256 + CB_PAGES_BF16: return launch<64, kBf16>(s, w, ws_bytes, stream);
         case 256 + CB_PAGES_E4M3: return launch<64, kE4m3>(s, w, ws_bytes, stream);

@@ -491,7 +491,7 @@ cb_status cb_page_bounds(const cb_pages *pages, int32_t layer0, int32_t n_layers
 
 int64_t cb_page_select_workspace_bytes(int32_t n_tokens, int32_t n_heads, int32_t table_width) {
     if (n_tokens <= 0 || n_heads <= 0 || table_width <= 0) return 0;
-    const __int128 all = (__int128)n_tokens * n_heads * table_width * 4;
+    const __int128 all = (__int128)n_tokens * n_heads * cb::select_row_bytes(table_width);
     return all > INT64_MAX ? INT64_MAX : (int64_t)all;
 }
 
@@ -522,6 +522,8 @@ cb_status cb_page_select(const cb_rows *q, const cb_pages *pages, int32_t layer,
     a.n_last = n_last;
     a.n_selected = n_selected;
     a.selected = selected;
+    a.head_dim = c.head_dim;
+    a.dtype = pages->dtype;
     if (cb::launch_page_select(a, c.head_dim, pages->dtype, workspace, workspace_bytes, (hipStream_t)stream) != hipSuccess)
         return fail(CB_ERR_DEVICE, "page select launch failed");
     return cb::api_ok();

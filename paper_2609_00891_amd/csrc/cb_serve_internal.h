@@ -120,7 +120,9 @@ struct SelectArgs {
     int32_t *selected;        // [n_tokens][n_heads][n_selected]
     uint32_t *keys;           // [tok1 - tok0][n_heads][table_width] scores of a round's tokens, as numbers of their order
     int32_t tok0, tok1;
-    int32_t per;              // pages of a workgroup
+    int32_t head_dim, dtype;
+    float *sizes;             // [tok1 - tok0][n_heads][slots] largest sums of the estimates' magnitudes
+    int32_t slots;
 };
 
 // Launchers (return hipError_t of the launch).
@@ -133,6 +135,7 @@ hipError_t launch_attn_paged(const PagedArgs &a, int32_t d, int32_t dtype, int32
                              hipStream_t s);
 hipError_t launch_page_select(const SelectArgs &s, int32_t d, int32_t dtype, void *ws, int64_t ws_bytes, hipStream_t stream);
 hipError_t launch_attn_selected(const PagedArgs &a, int32_t d, int32_t dtype, void *ws, int64_t ws_bytes, hipStream_t s);
+int64_t select_row_bytes(int32_t table_width);   // workspace of one (token, head)
 int64_t attn_selected_workspace_bytes(int64_t n_tokens, int32_t n_heads, int32_t G, int32_t d, int32_t page_size, int32_t n_selected);
 int64_t attn_paged_workspace_bytes(int32_t d, int32_t G, int32_t n_reqs, int32_t max_q_len);
 

@@ -176,6 +176,51 @@ def test_select_scores_in_the_last_places(cb, serve):
     assert np.array_equal(got, expected(serve, s, b, 6, 1, 1))
 
 
+@pytest.mark.parametrize("kind", ["bf16", "blocks"])
+def test_select_among_many_nearly_alike_pages(cb, serve, kind):
+    """Hundreds of pages whose scores differ in their last places or not at all: more than are looked at in one go."""
+    s = make_step(cb, kind, [(2, 5000), (1, 400)], 2, 3, 64, 16, seed=40)
+    b = all_bounds(cb, s)
+    g = gen(41)
+    one = randn(g, 2, 1, 64).abs()
+    one[0] = -one[0]
+    alike = (one[:, 0] * 8).to(b.dtype)                            # [least and greatest][channel]
+    raw = b.view(torch.uint8 if kind == "blocks" else torch.int16)
+    for r in range(2):
+        rows = torch.tensor(s.table[r][s.table[r] >= 0]).long()
+        for i, p in enumerate(rows.tolist()):
+            if i % 5:
+                x = alike.clone().view(raw.dtype)
+                x[i % 2, (7 * i) % 64] += i % 3                  # a channel one or two steps away
+                raw[s.layer, p] = x.cuda()
+    if kind == "blocks":
+        s.scales[s.layer, :, :, 0] = 0.5
+    for k, first, last in ((40, 1, 2), (150, 0, 1), (299, 2, 2)):
+        got = choose(cb, s, b, k, first, last)
+        assert np.array_equal(got, expected(serve, s, b, k, first, last))
+
+
+def test_select_in_large_tables(cb, serve):
+    """More entries than a wave keeps, with tokens that have few and many candidates."""
+    s = make_step(cb, "bf16", [(3, 9000), (1, 40)], 1, 2, 64, 1, seed=42)
+    b = all_bounds(cb, s)
+    assert s.table.shape[1] > 8192
+    for k, first, last in ((20, 1, 2), (700, 0, 5)):
+        got = choose(cb, s, b, k, first, last)
+        assert np.array_equal(got, expected(serve, s, b, k, first, last))
+
+
+def test_select_scores_of_extreme_size(cb, serve):
+    """Queries and bounds near the ends of bf16's range: estimates that leave fp32's say nothing, and the scores decide."""
+    for qs, bs in ((2.0 ** 60, 2.0 ** 60), (2.0 ** 100, 2.0 ** 20), (2.0 ** -70, 2.0 ** -50), (2.0 ** -120, 2.0 ** 100), (2.0 ** 126, 1.0)):
+        s = make_step(cb, "bf16", [(1, 600), (2, 300)], 1, 2, 64, 16, seed=43)
+        s.q *= qs
+        b = all_bounds(cb, s)
+        b *= bs
+        got = choose(cb, s, b, 6, 1, 1)
+        assert np.array_equal(got, expected(serve, s, b, 6, 1, 1)), (qs, bs)
+
+
 def test_select_nan_and_infinity_come_first(cb, serve):
     s = make_step(cb, "bf16", [(1, 400), (1, 350)], 1, 2, 64, 16, seed=5)
     b = all_bounds(cb, s)

@@ -159,7 +159,7 @@ STEP_REFUSALS = [
 @pytest.mark.parametrize("kw,status", STEP_REFUSALS + [
     (dict(q=dict(head_dim=128)), SHAPE), (dict(q=dict(n_heads=5)), SHAPE), (dict(first=-1), ARG), (dict(last=0), ARG),
     (dict(first=4), ARG), (dict(first=2 ** 31 - 1, last=2 ** 31 - 1), ARG), (dict(k=1), ARG), (dict(bounds=None), ARG),
-    (dict(bounds=P + 8), ALIGN), (dict(ws=P + 2), ALIGN), (dict(ws_bytes=8 * 2 * 4 - 1), SHAPE), (dict(ws=None), SHAPE),
+    (dict(bounds=P + 8), ALIGN), (dict(ws=P + 2), ALIGN), (dict(ws_bytes=(8 + 4) * 2 * 4 - 1), SHAPE), (dict(ws=None), SHAPE),
     (dict(q=dict(n_tokens=0)), OK), (dict(width=1 << 25, stride=1 << 25, pages=dict(seq_len=1)), UNSUP),
 ])
 def test_select_refuses(cb, kw, status):
@@ -217,8 +217,10 @@ def test_binding_refuses_wrong_tensors_of_a_selection(cb):
 
 
 def test_workspaces(cb):
-    """Scores of every token, head and entry; partial results of row tiles that are divided, none for others."""
-    assert cb.cb_page_select_workspace_bytes(7, 2, 100) == 7 * 2 * 100 * 4
+    """Scores of every token, head and entry, and four numbers for 256 entries; partial results of row tiles that are
+    divided, none for others."""
+    assert cb.cb_page_select_workspace_bytes(7, 2, 100) == 7 * 2 * (100 + 4) * 4
+    assert cb.cb_page_select_workspace_bytes(7, 2, 257) == 7 * 2 * (257 + 8) * 4
     assert cb.cb_page_select_workspace_bytes(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1) == 2 ** 63 - 1
     assert cb.cb_page_select_workspace_bytes(0, 2, 100) == 0
     # 1 token, 8 heads, 128 tiles of 32 keys: parts of 16 tiles
