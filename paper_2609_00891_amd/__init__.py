@@ -730,7 +730,7 @@ def _on_current_device(names: str, *tensors) -> int:
     """The library works on the current device: tensors of another (or of the host) are refused here.  Returns the
     device's index."""
     device = tensors[0].get_device()
-    good = device >= 0 and device == torch.cuda.current_device()
+    good = device >= 0 and device == torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != device:
             good = False
@@ -873,11 +873,13 @@ def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer
 def _spans(row_starts: Optional[torch.Tensor], q_lens: torch.Tensor, kv_lens: torch.Tensor, block_table: torch.Tensor):
     """The requests' arguments of the calls that find their tokens by lengths, as the C ABI takes them."""
     n = kv_lens.numel()
-    for t, name in ((row_starts, "row_starts"), (q_lens, "q_lens"), (kv_lens, "kv_lens")):
-        if t is not None:
-            _ints(t, n, name)
+    if row_starts is not None:
+        _ints(row_starts, n, "row_starts")
+    _ints(q_lens, n, "q_lens")
+    _ints(kv_lens, n, "kv_lens")
     _check_table(block_table, n)
-    return n, _ptr(row_starts), _ptr(q_lens), _ptr(kv_lens), _ptr(block_table), block_table.stride(0), block_table.shape[1]
+    return (n, None if row_starts is None else row_starts.data_ptr(), q_lens.data_ptr(), kv_lens.data_ptr(),
+            block_table.data_ptr(), block_table.stride(0), block_table.shape[1])
 
 
 def cb_page_quantize(rows: torch.Tensor, pages: CbPages, row_starts: torch.Tensor, q_lens: torch.Tensor,

@@ -80,7 +80,7 @@ struct Work { Request rq; int32_t req, tok0, n_tok, base, first, end; };   // ba
 __device__ __forceinline__ bool find_work(const SelectArgs &s, Work &w) {
     const PagedArgs &a = s.a;
     int32_t tile = 0;
-    if (!find_tile(a, blockIdx.x, w.rq, w.req, tile)) return false;
+    if (!find_tile(a, blockIdx.x / (uint32_t)a.n_heads, w.rq, w.req, tile)) return false;
     w.tok0 = tile * kTokens;
     w.n_tok = min(w.rq.q_len - w.tok0, kTokens);
     // (tokens of this round)
@@ -88,7 +88,7 @@ __device__ __forceinline__ bool find_work(const SelectArgs &s, Work &w) {
     w.base = w.rq.kv_len - w.rq.q_len + w.tok0;
     const int32_t p_hi = w.base + w.n_tok - 1;
     if (p_hi < 0) return false;
-    w.first = (int32_t)blockIdx.z * kPages;
+    w.first = (int32_t)blockIdx.y * kPages;
     w.end = min(w.first + kPages, (int32_t)fast_div((uint32_t)p_hi, a.page_size) + 1);
     return w.first < w.end;
 }
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256, 4) void estimates_kernel(SelectArgs s) {
     const PagedArgs &a = s.a;
     // every token's sum q-, sum q+ over the group as two bf16 numbers
     __shared__ __attribute__((aligned(16))) uint16_t parts[2][kTokens * QS];
-    const int head = (int)blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const int head = (int)(blockIdx.x % (uint32_t)a.n_heads), tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
     Work wk;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256, 4) void estimates_kernel(SelectArgs s) {
         for (int o = 1; o < 16; o <<= 1) most[k] = max(most[k], (uint32_t)__shfl_xor((int)most[k], o));
         const int32_t t = 4 * g + k, tok = wk.rq.row0 + wk.tok0 + t;
         if (n == 0 && t < wk.n_tok && tok >= s.tok0 && tok < s.tok1)
-            s.sizes[((int64_t)(tok - s.tok0) * a.n_heads + head) * s.slots + 4 * blockIdx.z + wave] = __uint_as_float(most[k]);
+            s.sizes[((int64_t)(tok - s.tok0) * a.n_heads + head) * s.slots + 4 * blockIdx.y + wave] = __uint_as_float(most[k]);
     }
 }
 
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) void scores_kernel(SelectArgs s) {
     constexpr int QS = 2 * D + 2;                              // (16 tokens' pairs of sums in 64 banks)
     const PagedArgs &a = s.a;
     __shared__ __attribute__((aligned(16))) double sums[kTokens * QS];   // of every token: sum q-, sum q+ over the group
-    const int head = (int)blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const int head = (int)(blockIdx.x % (uint32_t)a.n_heads), tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
     Work wk;
@@ -697,7 +697,7 @@ template <int D, int EL> hipError_t launch(SelectArgs s, char *ws, int64_t ws_by
     const int64_t round = std::min<int64_t>(std::min<int64_t>(a.n_tokens, 1 << 20), each > 0 ? ws_bytes / each : a.n_tokens);
     const int64_t tiles = std::min<int64_t>((int64_t)a.n_tokens / kTokens + a.n_reqs, a.n_tokens);
     const int64_t blocks = ((int64_t)a.table_width + kPages - 1) / kPages;
-    if (round < 1 || blocks > 65535) return hipErrorInvalidValue;
+    if (round < 1 || blocks > 65535 || tiles * a.n_heads > INT32_MAX) return hipErrorInvalidValue;
     s.keys = (uint32_t *)ws;
     s.sizes = (float *)ws + round * a.n_heads * a.table_width;
     s.slots = (int32_t)blocks * 4;
@@ -709,7 +709,7 @@ template <int D, int EL> hipError_t launch(SelectArgs s, char *ws, int64_t ws_by
         const unsigned tokens = (unsigned)(s.tok1 - s.tok0);
         if (blocks > 0)
             hipLaunchKernelGGL((waves ? estimates_kernel<D, EL> : scores_kernel<D, EL>),
-                               dim3((unsigned)tiles, (unsigned)a.n_heads, (unsigned)blocks), dim3(256), 0, stream, s);
+                               dim3((unsigned)(tiles * a.n_heads), (unsigned)blocks), dim3(256), 0, stream, s);
         if (waves) hipLaunchKernelGGL(choose_wave_kernel, dim3(tokens, (unsigned)a.n_heads), dim3(64), lds, stream, s);
         else hipLaunchKernelGGL(choose_kernel, dim3(tokens, (unsigned)a.n_heads), dim3(256), 0, stream, s);
     }
