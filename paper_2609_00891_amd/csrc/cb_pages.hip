@@ -203,7 +203,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
     const int row0 = blockIdx.y * a.group, row1 = min(row0 + a.group, a.n_rows);
     const int LH = a.n_lh, QH = a.n_qh;
     Angles an = {};
-    if (ROPE && row0 < LH + QH && ok[odd]) an = load_angles(a.rope, tok, c, nc2, a.sign);
+    if (ROPE && row0 < LH + QH && ok[odd]) an = load_angles<F8>(a.rope, tok, c, nc2, a.sign);
     // the two 16-byte chunks of a row that the lane reads, or one of each of the pair's rows
     const int p0 = PAIRS ? odd * nc2 + c : c, p1 = PAIRS ? p0 : c + nc2;
     for (int row = row0; row < row1; ++row) {

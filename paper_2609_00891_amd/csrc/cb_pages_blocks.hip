@@ -258,7 +258,7 @@ __global__ __launch_bounds__(256) void page_quant_kernel(SpanRowsArgs) {
                 tok[p] = it.tok0 + i;
                 in_at[p] = ok[p] ? row_place(a, tok[p]) : 0;
                 out_at[p] = page * a.os.seq + (int64_t)(it.at + i) * a.os.tok;
-                if (ROPE && angles && ok[p]) an[p] = load_angles(a.rope, tok[p], cc[p], nc2, a.sign);
+                if (ROPE && angles && ok[p]) an[p] = load_angles<true>(a.rope, tok[p], cc[p], nc2, a.sign);
             }
         };
         // a (layer, head) row, or a query's
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(256) void page_read_kernel(SpanRowsArgs) {
                 ok[p] = tm.unit(turn, p, i, cc[p]);
                 in_at[p] = ok[p] ? row_place(a, it.tok0 + i) : 0;
                 out_at[p] = page * a.os.seq + (int64_t)(it.at + i) * a.os.tok;
-                if (ROPE && ok[p] && row0 < LH) an[p] = load_angles(a.rope, it.tok0 + i, cc[p], nc2, a.sign);
+                if (ROPE && ok[p] && row0 < LH) an[p] = load_angles<true>(a.rope, it.tok0 + i, cc[p], nc2, a.sign);
             }
             for (int row = row0 + tm.slot; row < row1; row += tm.teams) {
                 const int kv = row >= LH, lh = kv ? row - LH : row;

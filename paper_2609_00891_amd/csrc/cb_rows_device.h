@@ -27,30 +27,41 @@ struct ChunkPair { uint4 a, b; };
 struct Angles { float c[8], s[8]; };
 
 // The angles of the thread's eight pairs: half split: pairs 8c .. 8c+7; interleaved: 4c .. 4c+3 and
-// 4(c + NC2) .. +3.  All positions are on their way together, then all angles: two trips to memory, where a branch at each
-// position made sixteen (one layer's pages of a decode step: 22.9 -> 10.9 us with this and fewer workgroups).
+// 4(c + NC2) .. +3.  AT_ONCE: all positions are on their way together, then all angles: two trips to memory, where a branch
+// at each position makes up to sixteen.  Four caches of up to 2,048 tokens into 8-bit pages, keys turned: 516 -> 494 us; a
+// cache of 40 layers turned back into 16 bits, which shares them among more rows and misses the registers, 774 -> 784.
+template <bool AT_ONCE>
 __device__ __forceinline__ Angles load_angles(const RopeAxes &ro, int64_t tok, int c, int nc2, float sign) {
     Angles an;
     int32_t pos[8];
     float2 w[8];
+    auto pair = [&](int q) __attribute__((always_inline)) {
+        return ro.style == 0 ? 8 * c + q : (q < 4 ? 4 * c + q : 4 * (c + nc2) + q - 4);
+    };
+    auto position = [&](int i) __attribute__((always_inline)) {
+        return ro.positions[(int)((ro.axis[i >> 4] >> (2 * (i & 15))) & 3) * ro.axis_stride + tok];
+    };
+    if constexpr (AT_ONCE) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        const int i = ro.style == 0 ? 8 * c + q : (q < 4 ? 4 * c + q : 4 * (c + nc2) + q - 4);
-        const int ax = (ro.axis[i >> 4] >> (2 * (i & 15))) & 3;
-        pos[q] = ro.positions[ax * ro.axis_stride + tok];
-    }
-    if (ro.n_pos > 0) {
+        for (int q = 0; q < 8; ++q) pos[q] = position(pair(q));
+        if (ro.n_pos > 0) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int i = ro.style == 0 ? 8 * c + q : (q < 4 ? 4 * c + q : 4 * (c + nc2) + q - 4);
-            w[q] = ro.table[(int64_t)((uint32_t)pos[q] < (uint32_t)ro.n_pos ? pos[q] : 0) * (8 * nc2) + i];
+            for (int q = 0; q < 8; ++q)
+                w[q] = ro.table[(int64_t)((uint32_t)pos[q] < (uint32_t)ro.n_pos ? pos[q] : 0) * (8 * nc2) + pair(q)];
         }
     }
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-        const bool in = (uint32_t)pos[q] < (uint32_t)ro.n_pos;
-        an.c[q] = in ? w[q].x : __builtin_nanf("");
-        an.s[q] = in ? sign * w[q].y : __builtin_nanf("");
+        float2 x = make_float2(__builtin_nanf(""), __builtin_nanf(""));
+        if constexpr (AT_ONCE) {
+            if ((uint32_t)pos[q] < (uint32_t)ro.n_pos) x = w[q];
+        } else {
+            const int i = pair(q);
+            const int32_t at = position(i);
+            if (at >= 0 && at < ro.n_pos) x = ro.table[(int64_t)at * (8 * nc2) + i];
+        }
+        an.c[q] = x.x;
+        an.s[q] = sign * x.y;
     }
     return an;
 }
