@@ -587,7 +587,8 @@ int log2_up(int n) {
 // which share its search, places and angles, while the launch fills the chip, at least 4 (1,811 tokens of three requests, 56
 // rows of 96 channels each: 23.0 us with 1, 20.6 with 2, 17.8 with 4, 22.7 with 8) and as many as it has teams.
 struct Cut { dim3 grid; bool wide; int pairs; };
-bool cut(RowsArgs &a, const SpanArgs &s, Cut &c) {
+Cut cut(RowsArgs &a, const SpanArgs &s) {
+    Cut c;
     const int64_t items = span_bound(s);
     a.lgc = log2_up((int)a.nc2.d);
     const int64_t tokens = std::min<int64_t>((s.n_tokens + s.n_reqs - 1) / s.n_reqs, s.page_size.d);
@@ -600,9 +601,9 @@ bool cut(RowsArgs &a, const SpanArgs &s, Cut &c) {
     while (a.group > 4 && items * ((a.n_rows + a.group - 1) / a.group) < 2048) a.group /= 2;
     a.group = std::max(a.group, teams);
     while ((a.n_rows + a.group - 1) / a.group > 65535) a.group *= 2;
-    if (items > INT32_MAX) return false;
-    c.grid = dim3((unsigned)(items < 1 ? 1 : items), (unsigned)((a.n_rows + a.group - 1) / a.group));
-    return true;
+    // (a launch has fewer than 2^32 threads in one direction; workgroups go round)
+    c.grid = dim3((unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), 1 << 22), (unsigned)((a.n_rows + a.group - 1) / a.group));
+    return c;
 }
 
 template <bool ROPE>
@@ -622,15 +623,13 @@ auto read_kernel(const Cut &c, bool rope) {
 }  // namespace
 
 hipError_t launch_page_quant(RowsArgs a, const SpanArgs &span, bool rope, float *scales, hipStream_t s) {
-    Cut c;
-    if (!cut(a, span, c)) return hipErrorInvalidValue;
+    const Cut c = cut(a, span);
     hipLaunchKernelGGL(rope ? quant_kernel<true>(c) : quant_kernel<false>(c), c.grid, dim3(256), 0, s, SpanRowsArgs{a, span, scales});
     return hipGetLastError();
 }
 
 hipError_t launch_page_read(RowsArgs a, const SpanArgs &span, bool rope, int32_t dtype, const float *scales, hipStream_t s) {
-    Cut c;
-    if (!cut(a, span, c)) return hipErrorInvalidValue;
+    const Cut c = cut(a, span);
     const auto kernel = dtype == CB_PAGES_BF16   ? read_kernel<kBf16>(c, rope)
                         : dtype == CB_PAGES_E4M3 ? read_kernel<kE4m3>(c, rope)
                                                  : read_kernel<kBlocks>(c, rope);

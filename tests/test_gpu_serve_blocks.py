@@ -407,6 +407,27 @@ def test_pool_beyond_32_bits(cb):
     torch.cuda.empty_cache()
 
 
+def test_more_pages_than_a_launch_has_workgroups(cb):
+    """2^24 pages of one token and a few: back come numbers within half a step (2^-4 of the number; below 2^-6 of the
+    scale 2^-10 of it, and 2^e < max / 224)."""
+    n, d = (1 << 24) + 5, 16
+    x = torch.randn((1, 2, 1, 1, n, d), generator=torch.Generator(device="cuda").manual_seed(15), device="cuda").bfloat16()
+    raw = torch.empty((1, 2, n, 1, 1, d), dtype=torch.uint8, device="cuda")
+    scales = torch.zeros((1, n, 1, 2), dtype=torch.float32, device="cuda")
+    pages = cb.page_pool(raw.view(torch.float8_e4m3fn), scales)
+    span = (i32([0]), i32([n]), i32([n]), torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda")[None])
+    cb.cb_page_quantize(x, pages, *span)
+    most = x.abs().amax(-1).float()[0, :, 0, 0]                    # [2][token]
+    sc = scales[0, :, 0].flip(0).T
+    assert bool(((most <= 448 * sc) & (most > 224 * sc)).all())
+    y = torch.full_like(x, 9.0)
+    cb.cb_page_read(pages, y, *span)
+    tol = torch.maximum(x.abs().float() * 2.0 ** -4, (most * (2.0 ** -10 / 224))[None, :, None, None, :, None])
+    assert bool(((y.float() - x.float()).abs() <= tol).all())
+    del x, y, tol, raw, scales, pages
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------ attention
 
 class BlockStep(Step):
