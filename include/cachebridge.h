@@ -44,6 +44,15 @@
  *
  *   cb_page_tables, cb_rope_axes, cb_page_write, cb_attn_paged
  *
+ * from pages of 8 bits with a scale for every page and head, and back into rows
+ * (a cache that goes on to another model):
+ *
+ *   cb_page_quantize, cb_page_read
+ *
+ * and, of long contexts, from the pages that matter to a token:
+ *
+ *   cb_page_bounds, cb_page_select, cb_attn_selected
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Row vectors: a map is W~ = [W ; b^T], a P x d_t fp32 matrix with
@@ -767,8 +776,8 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
  * request with q_lens <= 0, kv_lens < q_lens or above table_width * page_size, or rows outside
  * `rows`, takes no part (so with cb_page_tables' kv_lens, which are 0 for requests
  * that it left out); tokens whose page is outside the pool are skipped, their queries too.
- * rope, q and q_out as in cb_page_write (positions by token of `rows`).  No two requests may
- * write one page.  Rows may serve several requests (a prompt that several go on from); q
+ * rope, q and q_out as in cb_page_write (positions by token of `rows`).  No page may be
+ * written in two places, of two requests or of one.  Rows may serve several requests (a prompt that several go on from); q
  * must then not be turned in place.  rows, q and the pool must not overlap, nor
  * the pool's rows one another.  The same call gives the same bits again.  head_dim a multiple of 16
  * up to 256, page_size <= 2^24.
@@ -853,7 +862,8 @@ int64_t cb_attn_paged_workspace_bytes(int32_t n_tokens, int32_t n_reqs, int32_t 
  * its tokens (cb_page_write or cb_page_quantize), with the step's lengths; q_lens =
  * kv_lens forms those of whole requests.  Other pages' bounds stay as they were, and so do those
  * of pages outside the pool and of requests with q_lens <= 0, kv_lens < q_lens or
- * above table_width * page_size.  A NaN among a channel's keys is both its bounds.
+ * above table_width * page_size.  Requests that share such a page must hold as many of its tokens.  A NaN among
+ * a channel's keys is both its bounds.
  * max_q_len: the largest of q_lens, a hint that sizes the launch; a wrong one costs time
  * only.  head_dim a multiple of 16 up to 256, page_size <= 2^24.
  */
@@ -883,7 +893,8 @@ cb_status cb_page_bounds(const cb_pages *pages, int32_t layer0, int32_t n_layers
  *   workspace: device memory for the scores, 4-byte aligned: cb_page_select_workspace_bytes,
  *     or less, at least as much as for one token: tokens then take turns.  It keeps nothing
  *     that another call reads; calls that overlap in time need one each.
- * head_dim in {64, 96, 128}.
+ * head_dim in {64, 96, 128}; n_selected <= 2^30; fewer than 2^24 KV heads of 16 tokens (of one request,
+ * or less) in a call.
  */
 cb_status cb_page_select(const cb_rows *q, const cb_pages *pages, int32_t layer, const void *bounds, int32_t n_reqs,
                          const int32_t *q_starts, const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride,
@@ -901,7 +912,8 @@ int64_t cb_page_select_workspace_bytes(int32_t n_tokens, int32_t n_heads, int32_
  * counts twice.  Outputs, roundings, rows that see nothing, NaN and infinities in places that a row does not
  * see, rows of no request and the other arguments as in cb_attn_paged;
  * cb_attn_selected_workspace_bytes gives the workspace that the call can use, and with
- * less rows are split less.  n_selected * page_size <= 2^30.
+ * less rows are split less.  n_selected * page_size <= 2^30; fewer than 2^24 rows of up to 16 query heads of
+ * a token and KV head in a call.
  */
 cb_status cb_attn_selected(const cb_rows *q, const cb_pages *pages, int32_t layer, int32_t n_reqs, const int32_t *q_starts,
                            const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride, int32_t table_width,

@@ -8,6 +8,17 @@
 // entry is read three tiles ahead of its keys, the table's two, so no load waits for
 // another.  The lists' length and not the contexts' decides the work, and the host knows
 // it: keys are divided among workgroups where rows are few, and joined in a second launch.
+//
+// A key tile in one page (pages of whole tiles) has one place, scale and set of visible keys for its wave
+// (kSelectedWhole): no lane asks another for them and the loads' addresses are scalars.  Then K's rows can be read four
+// lanes to 64 bytes: neighbouring tokens choose much the same pages, which stay in the caches, and the first cache's
+// lookups bind where every lane reads a row of its own.
+//
+// 512 tokens of one request, 64 pages of 64 tokens each, a scale for every page (8 heads of 128, 8 query heads each; 4.3
+// GB of rows pass the first caches): 400 us with a place for every lane, 371 with places for the wave, 273 with K's
+// rows read four lanes together (15.7 TB/s of rows); what binds it then is the vector work on them, conversions,
+// V's transpose and exponentials (its products are 56 us at the rate of large ones, and half of their columns have no
+// head).  48 single tokens, 64 pages of 32 each: 80 us, 5 TB/s, at its bytes (83 at the rate of a copy).
 #include "cb_serve_internal.h"
 #include "cb_paged_rules.h"
 #include "cb_attn_rows.h"
@@ -43,18 +54,18 @@ hipError_t launch(PagedArgs a, void *ws, int64_t ws_bytes, hipStream_t s) {
     const int64_t units = (int64_t)a.n_tokens * cut.tiles, slot = kSlot * (D + 2) * 4;
     const int64_t fits = ws_bytes / (units * a.n_heads * slot);
     const int32_t parts = fits < 2 ? 1 : (int32_t)std::min<int64_t>(cut.parts, fits);
-    if (units * parts * a.n_heads > INT32_MAX) return hipErrorInvalidValue;
     a.rows.ws = (float *)ws;
     a.sel_parts = make_fastdiv((uint32_t)parts);
     a.sel_tiles = make_fastdiv((uint32_t)cut.tiles);
     // tiles of 32 keys in one page each, their rows within 2^31 bytes
     const bool whole = a.page_size.d % kKT == 0 && a.s_tok < (1u << 21);
-    hipLaunchKernelGGL((whole ? attn_selected_kernel<D, EL, kSelectedWhole> : attn_selected_kernel<D, EL, kSelected>), dim3((unsigned)(units * parts * a.n_heads)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((whole ? attn_selected_kernel<D, EL, kSelectedWhole> : attn_selected_kernel<D, EL, kSelected>),
+                       dim3((unsigned)(units * parts * a.n_heads)), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (parts > 1) {
         const uint32_t rows = std::min<uint32_t>(a.G.d, 16), per = parts > kWideParts ? rows : (rows + 3) / 4;
-        if (units * per * a.n_heads > INT32_MAX) return hipErrorInvalidValue;
-        hipLaunchKernelGGL((attn_selected_join_kernel<D, EL>), dim3((unsigned)(units * per * a.n_heads)), dim3(256), 0, s, a, make_fastdiv(per));
+        hipLaunchKernelGGL((attn_selected_join_kernel<D, EL>), dim3((unsigned)(units * per * a.n_heads)), dim3(256), 0, s, a,
+                           make_fastdiv(per));
     }
     return hipGetLastError();
 }

@@ -30,8 +30,10 @@
 //   threshold by bytes with counts in LDS.
 //
 // Bound by latency and HBM: 48 single tokens over 4,096 .. 65,536 keys in pages of 32 (8 heads of 128, 8 query heads each,
-// 0.15 GB) 59 us with the bounds of their pages, 1,024 new tokens over 32,768 keys in 8-bit pages of 64 50.  With
-// scores of all pages in 64 bits 62 and 70 (47 and 55 of them the scores), read as they are chosen, by workgroups, 140 and 97.
+// 0.15 GB) 68 us with the bounds of the step's pages (59 where all bounds stay in the last cache; 40 of them the
+// estimates, 23 the choices), 1,024 new tokens over 32,768 keys in 8-bit pages of 64 51 (23 and 25).  With scores of all
+// pages in 64 bits 62 (bounds in the last cache) and 70 (47 and 55 of them the scores), chosen by workgroups that read the
+// keys again for every byte 140 and 97.
 #include "cb_serve_internal.h"
 #include "cb_attn_rows.h"
 
@@ -435,7 +437,7 @@ struct Scores {
         float b[4][4], scale[4];
         int32_t page[4];
 #pragma unroll
-        for (int p = 0; p < 4; ++p) page[p] = table[i[p]];
+        for (int p = 0; p < 4; ++p) page[p] = (int32_t)min((uint32_t)table[i[p]], (uint32_t)a.n_pages - 1);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
             const int64_t at = (int64_t)__builtin_amdgcn_readfirstlane(page[p]) * a.n_heads + head;
@@ -697,7 +699,6 @@ template <int D, int EL> hipError_t launch(SelectArgs s, char *ws, int64_t ws_by
     const int64_t round = std::min<int64_t>(std::min<int64_t>(a.n_tokens, 1 << 20), each > 0 ? ws_bytes / each : a.n_tokens);
     const int64_t tiles = std::min<int64_t>((int64_t)a.n_tokens / kTokens + a.n_reqs, a.n_tokens);
     const int64_t blocks = ((int64_t)a.table_width + kPages - 1) / kPages;
-    if (round < 1 || blocks > 65535 || tiles * a.n_heads > INT32_MAX) return hipErrorInvalidValue;
     s.keys = (uint32_t *)ws;
     s.sizes = (float *)ws + round * a.n_heads * a.table_width;
     s.slots = (int32_t)blocks * 4;

@@ -3,6 +3,7 @@
 // enqueued.  No call allocates, reads the device or waits.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -19,6 +20,8 @@ cb_status fail(cb_status s, const char *fmt, ...) {
     va_end(ap);
     return cb::api_error(s, buf);
 }
+
+constexpr int64_t kMostBlocks = 1 << 24;   // workgroups of 256 threads: a launch has fewer than 2^32 in one direction
 
 cb::Strides strides_of(const cb_cache &c) { return {c.s_layer, c.s_kv, c.s_seq, c.s_head, c.s_tok}; }
 
@@ -507,6 +510,9 @@ cb_status cb_page_select(const cb_rows *q, const cb_pages *pages, int32_t layer,
     if (n_first < 0 || n_last < 1) return fail(CB_ERR_INVALID_ARGUMENT, "n_first must be >= 0 and n_last >= 1");
     if ((int64_t)n_first + n_last > n_selected)
         return fail(CB_ERR_INVALID_ARGUMENT, "n_first + n_last must not exceed n_selected (%d)", n_selected);
+    if (n_selected > (1 << 30)) return fail(CB_ERR_UNSUPPORTED, "n_selected must not exceed 2^30");
+    if (std::min<int64_t>((int64_t)q->n_tokens / 16 + n_reqs, q->n_tokens) * c.n_heads >= kMostBlocks)
+        return fail(CB_ERR_UNSUPPORTED, "a call has fewer than 2^24 KV heads of 16 tokens or less");
     if (c.n_heads > 65535 || table_width > 65535 * 256) return fail(CB_ERR_UNSUPPORTED, "too many KV heads or table entries");
     if (workspace_bytes < 0) return fail(CB_ERR_INVALID_ARGUMENT, "workspace_bytes is negative");
     if (((uintptr_t)bounds) % 16 || ((uintptr_t)selected) % 4 || ((uintptr_t)workspace) % 4)
@@ -555,8 +561,8 @@ cb_status cb_attn_selected(const cb_rows *q, const cb_pages *pages, int32_t laye
     if (q->n_tokens == 0 || n_reqs == 0) return cb::api_ok();
     if (!selected) return fail(CB_ERR_INVALID_ARGUMENT, "selected is NULL");
     if (q->data == out->data) return fail(CB_ERR_INVALID_ARGUMENT, "out must not be q");
-    if ((int64_t)q->n_tokens * ((a.G.d + 15) / 16) * c.n_heads > INT32_MAX)
-        return fail(CB_ERR_UNSUPPORTED, "too many (token, head) rows in one call");
+    if ((int64_t)q->n_tokens * ((a.G.d + 15) / 16) * c.n_heads >= kMostBlocks)
+        return fail(CB_ERR_UNSUPPORTED, "a call has fewer than 2^24 (token, KV head) rows of up to 16 query heads");
     a.selected = selected;
     a.n_selected = n_selected;
     if (cb::launch_attn_selected(a, c.head_dim, pages->dtype, workspace, workspace ? workspace_bytes : 0, (hipStream_t)stream) !=

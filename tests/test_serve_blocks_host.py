@@ -161,6 +161,7 @@ STEP_REFUSALS = [
     (dict(first=4), ARG), (dict(first=2 ** 31 - 1, last=2 ** 31 - 1), ARG), (dict(k=1), ARG), (dict(bounds=None), ARG),
     (dict(bounds=P + 8), ALIGN), (dict(ws=P + 2), ALIGN), (dict(ws_bytes=(8 + 4) * 2 * 4 - 1), SHAPE), (dict(ws=None), SHAPE),
     (dict(q=dict(n_tokens=0)), OK), (dict(width=1 << 25, stride=1 << 25, pages=dict(seq_len=1)), UNSUP),
+    (dict(k=(1 << 30) + 1), UNSUP), (dict(q=dict(n_tokens=1 << 27)), UNSUP), (dict(q=dict(n_tokens=1 << 23), n_reqs=1 << 23), UNSUP),
 ])
 def test_select_refuses(cb, kw, status):
     assert select(cb, **kw) == status, cb.cb_last_error()
@@ -172,6 +173,7 @@ def test_select_refuses(cb, kw, status):
     (dict(out=dict(data=2 * P)), ARG), (dict(k=0), ARG), (dict(k=1 << 27), UNSUP), (dict(scale=float("nan")), ARG),
     (dict(scale=3e38), ARG), (dict(lse=P + 1), ALIGN), (dict(ws=P + 4), ALIGN),
     (dict(q=dict(n_tokens=0), out=dict(data=3 * P, n_tokens=0)), OK),
+    (dict(q=dict(n_tokens=1 << 23), out=dict(data=3 * P, n_tokens=1 << 23)), UNSUP),
 ])
 def test_selected_attention_refuses(cb, kw, status):
     assert attend(cb, **kw) == status, cb.cb_last_error()
