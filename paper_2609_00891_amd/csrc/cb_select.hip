@@ -22,16 +22,16 @@
 //   (2^-16 + G 2^-23) S, S = sum |q| |bound|, which a third product forms.  The bounds are read four lanes to 64
 //   bytes of a page and handed to the operand's lanes.
 // choose_wave_kernel: a wave per token and head, its keys (estimates as numbers of their
-//   order) in LDS.  The n_selected-th largest is found bit by bit, from the first
-//   in which they differ; pages further than twice the error above it are taken, as far
+//   order) in LDS.  The n_selected-th largest is found by counts of eight bits, from the first
+//   in which they differ (23 and 25 us in the two calls below when it was found bit by bit, 21 and 21 so); pages further than twice the error above it are taken, as far
 //   below it are not, and of the others, where they are more than are needed, the wave forms the scores.
 // scores_kernel and choose_kernel: tables of more than 8,192 entries.  All scores in 64
 //   bits by 16x16x4 products, and a workgroup per token and head that finds the
 //   threshold by bytes with counts in LDS.
 //
 // Bound by latency and HBM: 48 single tokens over 4,096 .. 65,536 keys in pages of 32 (8 heads of 128, 8 query heads each,
-// 0.15 GB) 68 us with the bounds of the step's pages (59 where all bounds stay in the last cache; 40 of them the
-// estimates, 23 the choices), 1,024 new tokens over 32,768 keys in 8-bit pages of 64 51 (23 and 25).  With scores of all
+// 0.15 GB) 65 us with the bounds of the step's pages (40 of them the estimates, 21 the choices), 1,024 new tokens
+// over 32,768 keys in 8-bit pages of 64 46 (22 and 21); the choices' last rows, whose open pages are scored, end them.  With scores of all
 // pages in 64 bits 62 (bounds in the last cache) and 70 (47 and 55 of them the scores), chosen by workgroups that read the
 // keys again for every byte 140 and 97.
 #include "cb_serve_internal.h"
@@ -318,6 +318,26 @@ __device__ __forceinline__ bool choice(const SelectArgs &s, int32_t t, int32_t h
     return true;
 }
 
+// The greatest number and the bits of all lanes' numbers, by data-parallel moves.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    x = max(x, moved<0x111, 0xf>(x));   // row_shr:1, 2, 4, 8
+    x = max(x, moved<0x112, 0xf>(x));
+    x = max(x, moved<0x114, 0xf>(x));
+    x = max(x, moved<0x118, 0xf>(x));
+    x = max(x, moved<0x142, 0xa>(x));   // row_bcast:15, 31
+    x = max(x, moved<0x143, 0xc>(x));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+__device__ __forceinline__ uint32_t wave_or(uint32_t x) {
+    x |= moved<0x111, 0xf>(x);
+    x |= moved<0x112, 0xf>(x);
+    x |= moved<0x114, 0xf>(x);
+    x |= moved<0x118, 0xf>(x);
+    x |= moved<0x142, 0xa>(x);
+    x |= moved<0x143, 0xc>(x);
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
 // Keys of a row in LDS, of one wave: lane l has keys 4 l .. 4 l + 3 of every 256, absent ones 0.  (In registers they make
 // code of thousands of instructions that every workgroup runs once: 28 us where this takes 22.)
 struct Keys {
@@ -336,41 +356,87 @@ struct Keys {
         return __builtin_amdgcn_readlane((int)wave_sums(c), 63);
     }
     // The largest number that n keys reach, or one that just n reach (exact: true); more than n keys are not 0, fewer
-    // or just n all ones.
-    __device__ __forceinline__ uint32_t threshold(int n, bool &exact) const {
+    // or just n all ones.  By counts of eight bits at a time (in `bins`, 256 words of LDS) until few enough keys are
+    // left that each lane has one.
+    __device__ __forceinline__ uint32_t threshold(int n, uint32_t *bins, bool &exact) const {
         // bits that all keys but 0 and all ones share are the threshold's too
         const int lane = threadIdx.x;
-        uint32_t all = ~0u, any = 0;
+        uint32_t all = ~0u, any = 0, ones = 0;
 #pragma unroll 4
         for (int j = 0; j < groups; ++j) {
             const uint4 v = k[64 * j + lane];
             const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const bool is = u[c] - 1 < ~0u - 1;
-                all &= is ? u[c] : ~0u;
-                any |= is ? u[c] : 0u;
+                all &= among(u[c]) ? u[c] : ~0u;
+                any |= among(u[c]) ? u[c] : 0u;
+                ones += u[c] == ~0u ? 1u : 0u;
             }
         }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            all &= (uint32_t)__shfl_xor((int)all, o);
-            any |= (uint32_t)__shfl_xor((int)any, o);
-        }
-        all = (uint32_t)__builtin_amdgcn_readfirstlane((int)all);
-        any = (uint32_t)__builtin_amdgcn_readfirstlane((int)any);
+        int need = n - __builtin_amdgcn_readlane((int)wave_sums(ones), 63);
+        exact = true;
+        if (need == 0) return ~0u;
+        all = ~wave_or(~all);
+        any = wave_or(any);
         const int top = 31 - __builtin_clz((all ^ any) | 1u);      // the highest bit in which two differ
-        uint32_t x = top == 31 ? 0u : any & ~((2u << top) - 1);
+        uint32_t x = top == 31 ? 0u : any & ~((2u << top) - 1);    // the threshold's bits from bit `low` on
+        int low = top + 1, count;
+        do {
+            const int w = min(low, 8);
+            low -= w;
+            __syncthreads();
+            *(uint4 *)&bins[4 * lane] = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+            for (int j = 0; j < groups; ++j) {
+                const uint4 v = k[64 * j + lane];
+                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (among(u[c]) && ((u[c] ^ x) >> low) >> w == 0) atomicAdd(&bins[(u[c] >> low) & ((1u << w) - 1)], 1u);
+            }
+            __syncthreads();
+            // a lane has four bins, the first lane the largest numbers
+            const uint4 v = *(const uint4 *)&bins[4 * (63 - lane)];
+            const int own = (int)(v.x + v.y + v.z + v.w), sum = (int)wave_sums((uint32_t)own);
+            const int from = __builtin_ctzll(__ballot(sum >= need));
+            int rest = need - (sum - own), bin = 4 * (63 - lane) + 3, c = (int)v.w;
+            if (rest > c) { rest -= c; --bin; c = (int)v.z;
+                if (rest > c) { rest -= c; --bin; c = (int)v.y;
+                    if (rest > c) { rest -= c; --bin; c = (int)v.x; } } }
+            need = __builtin_amdgcn_readlane(rest, from);
+            count = __builtin_amdgcn_readlane(c, from);
+            x |= (uint32_t)__builtin_amdgcn_readlane(bin, from) << low;
+            if (count == need) return x;
+        } while (low > 0 && count > 64);
         exact = false;
-        for (int bit = top; bit >= 0; --bit) {
-            const int c = at_least(x | 1u << bit);
-            if (c < n) continue;
-            x |= 1u << bit;
-            exact = c == n;
-            if (exact) break;
+        if (low == 0) return x;
+        // a key for each lane
+        __syncthreads();
+        int at = 0;
+        for (int j = 0; j < groups; ++j) {
+            const uint4 v = k[64 * j + lane];
+            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const bool is = among(u[c]) && (u[c] ^ x) >> low == 0;
+                const uint64_t has = __ballot(is);
+                if (is) bins[at + __builtin_popcountll(has & ((1ull << lane) - 1))] = u[c];
+                at += __builtin_popcountll(has);
+            }
         }
+        __syncthreads();
+        const uint32_t mine = lane < count ? bins[lane] : 0u;
+        int before = 0;                                            // larger ones, and equal ones of earlier lanes
+        for (int p = 0; p < count; ++p) {
+            const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)mine, p);
+            before += other > mine || (other == mine && p < lane) ? 1 : 0;
+        }
+        x = (uint32_t)__builtin_amdgcn_readlane((int)mine, __builtin_ctzll(__ballot(lane < count && before == need - 1)));
+        exact = __builtin_popcountll(__ballot(mine >= x)) == need;
         return x;
     }
+    // neither 0 nor all ones
+    static __device__ __forceinline__ bool among(uint32_t u) { return u - 1 < ~0u - 1; }
     // the smallest key that reaches x, and whether a key is y
     __device__ __forceinline__ uint32_t first_from(uint32_t x, uint32_t y, bool &found) const {
         uint32_t m = ~0u;
@@ -385,10 +451,8 @@ struct Keys {
                 is |= u[c] == y;
             }
         }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) m = min(m, (uint32_t)__shfl_xor((int)m, o));
         found = __any(is);
-        return (uint32_t)__builtin_amdgcn_readfirstlane((int)m);
+        return ~wave_max(~m);
     }
 };
 
@@ -495,6 +559,7 @@ __device__ __forceinline__ int between(const Keys &row, uint32_t lo, uint32_t hi
 __global__ __launch_bounds__(64) void choose_wave_kernel(SelectArgs s) {
     extern __shared__ __attribute__((aligned(16))) uint4 lds[];
     __shared__ int32_t place[kScored];
+    __shared__ __attribute__((aligned(16))) uint32_t bins[256];
     const int lane = threadIdx.x;
     const int32_t t = (int32_t)blockIdx.x, head = (int32_t)blockIdx.y;
     int32_t req, n;
@@ -527,13 +592,12 @@ __global__ __launch_bounds__(64) void choose_wave_kernel(SelectArgs s) {
     int equal = 0;
     if (row.at_least(1) > s.n_selected) {
         bool exact, unknown;
-        const uint32_t border = row.first_from(row.threshold(s.n_selected, exact), kUnknown, unknown);
+        const uint32_t border = row.first_from(row.threshold(s.n_selected, bins, exact), kUnknown, unknown);
         if (border == ~0u) {
             least = ~0u - 1;                                   // those always taken are all
         } else {
             // pages whose estimates are within the errors of the n_selected-th: between lo and hi
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+            most = wave_max(most);
             const float at = value_of(border);
             // (each of two estimates off by (2^-16 + G 2^-23) S, and two scores that round to one number)
             const float far = 2.f * (0x1p-16f + 0x1p-23f * (float)s.a.G.d) * __uint_as_float(most) + 0x1p-22f * fabsf(at);
@@ -586,7 +650,7 @@ __global__ __launch_bounds__(64) void choose_wave_kernel(SelectArgs s) {
                         if (lane < count) key_at[place[lane]] = mine;
                     }
                     __syncthreads();
-                    least = row.threshold(s.n_selected, exact);
+                    least = row.threshold(s.n_selected, bins, exact);
                     if (exact) least -= 1;
                     else equal = s.n_selected - row.at_least(least + 1);
                 }
