@@ -41,6 +41,8 @@ constexpr uint32_t kRun = 256;
 // requests of different lengths end together (64 requests of 512 .. 16,384 keys: 262 us with 1,024,
 // 268 with 4,096, 259 with 2,048).
 constexpr int kTarget = 2048;
+// Listed pages of the tokens of a row tile together, where they share it.
+constexpr int kSharedEntries = 1024;
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     f32x2_t v = {lo, hi};
@@ -231,6 +233,29 @@ __device__ __forceinline__ bool request_of(const PagedArgs &a, int32_t tok, int 
     return false;
 }
 
+// Tile `idx` of all requests' tiles of tokens, tiles_of(q_len) for each, and its request, every wave for itself.
+template <typename F>
+__device__ __forceinline__ bool find_tile(const PagedArgs &a, uint32_t idx, F tiles_of, Request &rq, int32_t &req, int32_t &tile) {
+    const int lane = threadIdx.x & 63;
+    uint32_t before = 0;
+    for (int r0 = 0; r0 < a.n_reqs; r0 += 64) {
+        const Request r = request(a, min(r0 + lane, a.n_reqs - 1));
+        const uint32_t n = r0 + lane < a.n_reqs ? tiles_of(r.q_len) : 0;
+        const uint32_t sum = wave_sums(n), total = (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
+        if (idx - before < total) {
+            const uint32_t k = idx - before - (sum - n);
+            const int from = __builtin_ctzll(__ballot(k < n));
+            req = r0 + from;
+            tile = __builtin_amdgcn_readlane((int)k, from);
+            rq = {__builtin_amdgcn_readlane(r.row0, from), __builtin_amdgcn_readlane(r.q_len, from),
+                  __builtin_amdgcn_readlane(r.kv_len, from)};
+            return true;
+        }
+        before += total;
+    }
+    return false;
+}
+
 // The row tile and part of index `idx` of a call on selected pages, and its token as the one new token of a request that
 // ends there; false for a token of no request.
 __device__ __forceinline__ bool selected_item(const PagedArgs &a, uint32_t idx, Item &it, Request &rq) {
@@ -255,15 +280,84 @@ __device__ __forceinline__ int32_t list_length(const int32_t *list, int32_t n) {
     return 0;
 }
 
+// The idx-th tile of a call on selected pages whose tiles have sel_tokens tokens of a request, as its new tokens.
+__device__ __forceinline__ bool shared_item(const PagedArgs &a, uint32_t idx, Item &it, Request &rq) {
+    Request r;
+    int32_t tile;
+    const auto tiles_of = [&](int32_t q) { return fast_div((uint32_t)(q + (int32_t)a.sel_tokens.d - 1), a.sel_tokens); };
+    if (!find_tile(a, idx, tiles_of, r, it.req, tile)) return false;
+    it.tile = it.part = it.slot = 0;
+    it.parts = 1;
+    const int32_t t0 = tile * (int32_t)a.sel_tokens.d, n = min(r.q_len - t0, (int32_t)a.sel_tokens.d);
+    rq = {r.row0 + t0, n, r.kv_len - r.q_len + t0 + n};
+    return true;
+}
+
+// The pages of several tokens' lists as one list, ascending, and whose they are (bit t: token t's).  A page that a token
+// has twice stands in two places, each of them once that token's.
+struct SharedList {
+    uint32_t sorted[kSharedEntries], masks[kSharedEntries];
+    int32_t pages[kSharedEntries];
+};
+__device__ __forceinline__ int32_t share_lists(const PagedArgs &a, const Request &rq, int head, SharedList &l) {
+    constexpr int NT = 256;
+    const int tid = threadIdx.x, lane = tid & 63, k = a.n_selected;
+    for (int t = 0; t < rq.q_len; ++t) {
+        const int32_t *list = a.selected + ((int64_t)(rq.row0 + t) * a.n_heads + head) * k;
+        for (int i = tid; i < k; i += NT) {
+            const int32_t page = list[i];
+            l.sorted[t * k + i] = (uint32_t)page < (uint32_t)a.table_width ? (uint32_t)page << 4 | (uint32_t)t : ~0u;
+        }
+    }
+    int n = 64;
+    while (n < rq.q_len * k) n *= 2;
+    for (int i = rq.q_len * k + tid; i < n; i += NT) l.sorted[i] = ~0u;
+    for (int i = tid; i < n; i += NT) l.masks[i] = 0;
+    __syncthreads();
+    // bitonic: a pair (i, i + stride) is one thread's; with strides up to 64 a wave's pairs stay its own
+    for (int size = 2, last = 1; size <= n; size *= 2)
+        for (int stride = size / 2; stride > 0; stride /= 2) {
+            if (max(last, stride) > 64) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            last = stride;
+            for (int i = tid; i < n / 2; i += NT) {
+                const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
+                const uint32_t x = l.sorted[lo], y = l.sorted[hi];
+                if ((x > y) == ((lo & size) == 0)) {
+                    l.sorted[lo] = y;
+                    l.sorted[hi] = x;
+                }
+            }
+        }
+    __syncthreads();
+    // every wave counts, one writes
+    int32_t count = 0;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const uint32_t x = l.sorted[i0 + lane], before = i0 + lane > 0 ? l.sorted[i0 + lane - 1] : ~0u;
+        const uint64_t first = __ballot(x != ~0u && ((x ^ before) > 15u || x == before));
+        if (tid < 64 && x != ~0u) {
+            const int at = count + __builtin_popcountll(first & ((2ull << lane) - 1)) - 1;
+            if ((first >> lane) & 1) l.pages[at] = (int32_t)(x >> 4);
+            atomicOr(&l.masks[at], 1u << (x & 15));
+        }
+        count += __builtin_popcountll(first);
+    }
+    __syncthreads();
+    return count;
+}
+
 // Which keys a row tile has: those that it sees of all pages, or those of the pages selected for its token, one list of keys
 // (place i of the list: key i mod page_size of its page i / page_size; the row is the one new token of a request as
 // long as its position).  kSelectedWhole: a key tile lies in one page, so that its place, scales and visible keys are one
 // number each for the wave: no lane asks another, and the loads' addresses are a scalar and a constant of the lane.
-enum { kAll, kSelected, kSelectedWhole };
+// kSelectedShared: and the row tile has several tokens of a request, whose lists are joined; a row sees the keys of its own
+// token's pages.
+enum { kAll, kSelected, kSelectedWhole, kSelectedShared };
 template <int D, int EL, int NW, int KEYS>
 __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &cl, uint32_t block, SchedLds<NW> &sched,
                                           RowsLds<D, NW> &lds) {
-    constexpr bool F8 = EL != kBf16, BLK = EL == kBlocks, SEL = KEYS != kAll, WHOLE = KEYS == kSelectedWhole;
+    constexpr bool F8 = EL != kBf16, BLK = EL == kBlocks, SEL = KEYS != kAll;
+    constexpr bool SHARED = KEYS == kSelectedShared, WHOLE = KEYS == kSelectedWhole || SHARED;
     using Ge = Geo<D, F8>;
     constexpr int M = 16, E = Ge::E;
     auto &ol = lds.o;
@@ -271,7 +365,9 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
     const int head = (int)(block % (uint32_t)a.n_heads);
     Item it;
     Request rq;
-    if constexpr (SEL) {
+    if constexpr (SHARED) {
+        if (!shared_item(a, block / (uint32_t)a.n_heads, it, rq)) return;
+    } else if constexpr (SEL) {
         if (!selected_item(a, block / (uint32_t)a.n_heads, it, rq)) return;
     } else {
         if (!find_item<M, kKT, false, NW>(a, cl, block / (uint32_t)a.n_heads, sched, it)) return;
@@ -290,7 +386,12 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
     const int32_t *list = nullptr;                             // SEL: the row's pages
     int32_t listed = 0;
     KeyTiles kt = {0, 0, 0};
-    if constexpr (SEL) {
+    SharedList &joint = *(SharedList *)&ol;                    // (read before the results are written)
+    static_assert(!SHARED || sizeof(SharedList) <= sizeof(ol), "");
+    if constexpr (SHARED) {
+        listed = p_hi < 0 ? 0 : share_lists(a, rq, head, joint);
+        kt.n = listed * (int32_t)(a.page_size.d / kKT);
+    } else if constexpr (SEL) {
         list = a.selected + ((int64_t)rq.row0 * a.n_heads + head) * a.n_selected;
         listed = p_lo < 0 ? 0 : list_length(list, a.n_selected);
         kt.n = (listed * (int32_t)a.page_size.d + kKT - 1) / kKT;
@@ -303,11 +404,12 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
 
     // queries: row n (rows behind the last repeat it)
     bf16x8_t qf[Ge::NS];
-    int32_t pos;
+    int32_t pos, own = 0;                                      // SHARED: the row's token among the tile's
     {
         const int32_t row = row0 + min(n, n_rows - 1);
         const int32_t tok = (int32_t)fast_div((uint32_t)row, a.G), u = row - tok * G;
         pos = rq.kv_len - rq.q_len + tok;
+        own = tok;
         const uint16_t *q = a.q + (int64_t)(rq.row0 + tok) * a.q_tok + (int64_t)(head * G + u) * a.q_head;
 #pragma unroll
         for (int s = 0; s < Ge::NS; ++s) qf[s] = *(const bf16x8_t *)(q + Ge::chan(s, g));
@@ -319,9 +421,13 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
     uint32_t in_page = 0, off = 0;
     bool in_kv = false;
     int32_t entry = 0, entry_page = 0;                         // SEL: the place in the list and what stands there, a tile earlier still
+    uint32_t entry_mask = 0, mask_l = 0, mask_n = 0, mask = 0; // SHARED: whose the page is,
+    int32_t key_l = 0, key_n = 0, key = 0;                     // and the tile's first key: as looked up, requested, worked on
     auto peek = [&](int32_t tile) __attribute__((always_inline)) {
         entry = tile * kKT + (WHOLE ? 0 : lane & 31);
-        entry_page = list[min((int32_t)fast_div((uint32_t)entry, a.page_size), listed - 1)];
+        const int32_t i = min((int32_t)fast_div((uint32_t)entry, a.page_size), listed - 1);
+        entry_page = SHARED ? joint.pages[i] : list[i];
+        if constexpr (SHARED) entry_mask = joint.masks[i];
     };
     int32_t seen = 0;                                          // WHOLE: keys of the tile up to the row's position, from its first
     auto look_up = [&](int32_t tile) __attribute__((always_inline)) {
@@ -332,6 +438,10 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
             in_kv = (int32_t)idx < listed && at >= 0 && at < a.table_width;
             seen = in_kv ? min(rq.kv_len - (at * (int32_t)a.page_size.d + (int32_t)in_page), kKT) : 0;
             page = table[in_kv ? at : 0];
+            if constexpr (SHARED) {
+                key_l = at * (int32_t)a.page_size.d + (int32_t)in_page;
+                mask_l = (uint32_t)__builtin_amdgcn_readfirstlane((int)entry_mask);
+            }
         } else if constexpr (SEL) {
             const uint32_t idx = fast_div((uint32_t)entry, a.page_size);
             in_page = (uint32_t)entry - idx * a.page_size.d;
@@ -366,6 +476,8 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
         if constexpr (WHOLE) {
             const int32_t pg = __builtin_amdgcn_readfirstlane(page);
             const bool ok = in_kv && (uint32_t)pg < (uint32_t)a.n_pages;
+            key_n = key_l;
+            mask_n = mask_l;
             off = ok ? (uint32_t)pg * a.s_page + in_page * a.s_tok : 0u;
             kt_p = kp + (uint64_t)off * 16;
             vt_p = vp + (uint64_t)off * 16;
@@ -437,6 +549,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
     };
     // every key of the tile is there and seen by every row
     auto whole_tile = [&](int32_t k0, uint32_t there) __attribute__((always_inline)) {
+        if (SHARED) return there == 0xffffffffu && key + kKT - 1 <= p_lo && mask + 1 == 1u << rq.q_len;
         if (SEL) return there == 0xffffffffu;                  // (one position: there are the keys that it sees)
         return there == 0xffffffffu && k0 + kKT - 1 <= p_lo &&
                (a.window == 0 || k0 > p_hi - a.window || k0 + kKT <= a.n_sinks);
@@ -444,21 +557,27 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
 
     f32x4_t o[E];
     float m, l;
+    const int32_t v0 = part_begin(kt.n, it.part, it.parts) + wave;
+    uint32_t there, there_n, odd;
+    // SHARED: keys that are there and finite need no care where only some rows see them.  Whether V held others shows in
+    // the sums; then they are formed again, with care.
+    for (bool careful = !SHARED;; careful = true) {
     m = -HUGE_VALF;
     l = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-
     // A tile's K and V are requested while the tile before it is worked on: K as soon as its registers
     // have met the queries, V as soon as its own have become operands.
-    const int32_t v0 = part_begin(kt.n, it.part, it.parts) + wave;
-    uint32_t there = 0, there_n = 0;
-    uint32_t odd = 0;
+    there = there_n = odd = 0;
     if (v0 < v1) {
         if constexpr (SEL) peek(v0);
         look_up(kt.tile(v0));
         if constexpr (SEL) peek(v0 + NW);
         there = place();
+        if constexpr (SHARED) {
+            key = key_n;
+            mask = mask_n;
+        }
         load_k();
         load_v();
         if (v0 + NW < v1) look_up(kt.tile(v0 + NW));
@@ -498,7 +617,9 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
         if (!whole) {
             asm volatile("");                              // a branch, not selects on every tile
             // key k0 + 4 g + c is register e's, c = 16 (e >> 2) + (e & 3)
-            const uint32_t vis = SEL ? there >> (4 * g) : visible(pos - k0 - 4 * g, there >> (4 * g), a.window, a.n_sinks - k0 - 4 * g);
+            const uint32_t vis = SHARED ? (there & bits_to(pos - key) & (0u - ((mask >> own) & 1u))) >> (4 * g)
+                                 : SEL  ? there >> (4 * g)
+                                        : visible(pos - k0 - 4 * g, there >> (4 * g), a.window, a.n_sinks - k0 - 4 * g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = keep_if(vis, 16 * (e >> 2) + (e & 3), x[e]);
         }
@@ -526,7 +647,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
         l += sum;
 #pragma unroll
         for (int q = 0; q < 4; ++q) p2[q] = pack_bf16(x[2 * q], x[2 * q + 1]);
-        if (!whole) {
+        if (!whole && (careful || there != 0xffffffffu)) {
             // In a tile with a key that some row does not see a NaN or infinity of V would meet zero
             // weights: it becomes a zero here and reaches the rows that see it after the last tile.
             // Rows that are not there become zeros as well.
@@ -567,6 +688,18 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
         }
         if (v + NW < v1) load_v();
         there = there_n;
+        if constexpr (SHARED) {
+            key = key_n;
+            mask = mask_n;
+        }
+    }
+    if (careful) break;
+    float zero = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) zero = __builtin_fmaf(o[i][r], 0.f, zero);
+    if (!__any(zero != 0.f)) break;
     }
     if (__any(odd != 0)) {
         // NaNs and infinities of V that were left out of tiles which some row does not see whole: they
@@ -577,6 +710,10 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
             if constexpr (SEL) peek(v);
             look_up(kt.tile(v));
             there = place();
+            if constexpr (SHARED) {
+                key = key_n;
+                mask = mask_n;
+            }
             if (whole_tile(k0, there)) continue;
 #pragma unroll 1
             for (int kk = 0; kk < kKT; ++kk) {
@@ -588,7 +725,7 @@ __device__ __forceinline__ void rows_body(const PagedArgs &a, const PagedClass &
 #pragma unroll
                     for (int i = 0; i < E; i += 2) {
                         const uint32_t u = F8 ? e4m3_pair<false>(*(const uint16_t *)(vrow + c + i)) : *(const uint32_t *)(vrow + 2 * (c + i));
-                        const bool see = SEL || sees(k0 + kk, pos);
+                        const bool see = SHARED ? key + kk <= pos && ((mask >> own) & 1) : SEL || sees(k0 + kk, pos);
                         if (see && not_finite(u & 0xffffu)) o[i][r] += bf_lo(u);
                         if (see && not_finite(u & 0xffff0000u)) o[i + 1][r] += bf_hi(u);
                     }

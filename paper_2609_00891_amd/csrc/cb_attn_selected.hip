@@ -14,11 +14,17 @@
 // lanes to 64 bytes: neighbouring tokens choose much the same pages, which stay in the caches, and the first cache's
 // lookups bind where every lane reads a row of its own.
 //
-// 512 tokens of one request, 64 pages of 64 tokens each, a scale for every page (8 heads of 128, 8 query heads each; 4.3
-// GB of rows pass the first caches): 400 us with a place for every lane, 371 with places for the wave, 273 with K's
-// rows read four lanes together (15.7 TB/s of rows); what binds it then is the vector work on them, conversions,
-// V's transpose and exponentials (its products are 56 us at the rate of large ones, and half of their columns have no
-// head).  48 single tokens, 64 pages of 32 each: 80 us, 5 TB/s, at its bytes (83 at the rate of a copy).
+// Tokens of one request that follow one another choose much the same pages, and one token's query heads rarely fill a
+// row tile: where a call has rows enough, a tile takes as many tokens as have their heads in it, reads the pages that any of
+// them chose once, ascending, and every row sees those of its own token (kSelectedShared).  The lists are sorted in LDS,
+// each workgroup for itself.  Only some rows see such keys: with a weight of zero a finite V does no harm, and whether
+// there was another shows in the sums, which are then formed again with those zeroed.
+//
+// 512 tokens of one request, 64 pages of 64 tokens each, a scale for every page (8 heads of 128, 8 query heads each): 400 us
+// with a place for every lane, 371 with places for the wave, 273 with K's rows read four lanes together, 218 with two
+// tokens a tile.  What binds it then is the vector work on rows, conversions, V's transpose and exponentials, and the
+// last workgroups (2,048 on 768 places); its products are 56 us at the rate of large ones.  48 single tokens, 64 pages of
+// 32 each: 80-84 us, 5 TB/s, at its bytes (83 at the rate of a copy).
 #include "cb_serve_internal.h"
 #include "cb_paged_rules.h"
 #include "cb_attn_rows.h"
@@ -59,6 +65,15 @@ hipError_t launch(PagedArgs a, void *ws, int64_t ws_bytes, hipStream_t s) {
     a.sel_tiles = make_fastdiv((uint32_t)cut.tiles);
     // tiles of 32 keys in one page each, their rows within 2^31 bytes
     const bool whole = a.page_size.d % kKT == 0 && a.s_tok < (1u << 21);
+    // (places of all keys of a tile's lists are below 2^30)
+    const int32_t entries = std::min<int32_t>(kSharedEntries, (1 << 30) / (int32_t)a.page_size.d);
+    const int32_t share = whole && parts == 1 ? shared_tokens(a.n_tokens, a.n_reqs, a.n_heads, (int32_t)a.G.d, a.n_selected, entries) : 1;
+    if (share > 1) {
+        a.sel_tokens = make_fastdiv((uint32_t)share);
+        const int64_t tiles = std::min<int64_t>(a.n_tokens, a.n_tokens / share + a.n_reqs);
+        hipLaunchKernelGGL((attn_selected_kernel<D, EL, kSelectedShared>), dim3((unsigned)(tiles * a.n_heads)), dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL((whole ? attn_selected_kernel<D, EL, kSelectedWhole> : attn_selected_kernel<D, EL, kSelected>),
                        dim3((unsigned)(units * parts * a.n_heads)), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;

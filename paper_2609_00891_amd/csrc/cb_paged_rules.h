@@ -142,4 +142,18 @@ inline SelectedCut selected_cut(int64_t n_tokens, int32_t H, int32_t G, int32_t 
     return {tiles, parts_of(keys, part_tiles(n_tokens * tiles * keys, H, 2048, 16), 36)};
 }
 
+// Tokens of a request that share a row tile of 16 and the keys that it reads: as many as have their query heads in it and
+// their lists in `entries` places, while 1,024 workgroups are left, and 1 where requests have fewer than three on average.
+// 512 tokens, 64 of 512 pages of 64 e4m3 tokens each (8 heads of 128), apart and shared: 8 query heads a head 276 and 229 us
+// where neighbouring tokens' lists are near, 274 / 168 where they are alike, 302 / 307 where they are chosen at random; 4
+// query heads 270 / 162, 270 / 100, 293 / 289; 1 query head 263 / 157, 263 / 96, 286 / 280.  256 tokens (1,024
+// workgroups) 143 / 130 near and 152 / 173 at random; 256 requests of 2 tokens 146 / 152 and 187 / 200.
+inline int32_t shared_tokens(int64_t n_tokens, int64_t n_reqs, int64_t H, int32_t G, int32_t n_selected, int32_t entries) {
+    if (n_tokens < 3 * n_reqs) return 1;
+    int64_t t = G > 8 ? 1 : 16 / G;
+    if (t * n_selected > entries) t = entries / n_selected;
+    if (t > n_tokens * H / 1024) t = n_tokens * H / 1024;
+    return t < 1 ? 1 : (int32_t)t;
+}
+
 }  // namespace cb

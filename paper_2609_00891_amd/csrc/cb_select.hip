@@ -47,28 +47,6 @@ constexpr int kPages = 256;             // pages of a workgroup
 constexpr int kWaveTable = 8192;        // table entries up to which a wave has a row's keys (32 KB)
 constexpr uint32_t kUnknown = 0xff800000u;   // key of an estimate that says nothing (and of the scores +infinity and NaN)
 
-// Tile `idx` of all requests' token tiles, and its request, every wave for itself.
-__device__ __forceinline__ bool find_tile(const PagedArgs &a, uint32_t idx, Request &rq, int32_t &req, int32_t &tile) {
-    const int lane = threadIdx.x & 63;
-    uint32_t before = 0;
-    for (int r0 = 0; r0 < a.n_reqs; r0 += 64) {
-        const Request r = request(a, min(r0 + lane, a.n_reqs - 1));
-        const uint32_t n = r0 + lane < a.n_reqs ? (uint32_t)(r.q_len + kTokens - 1) / kTokens : 0;
-        const uint32_t sum = wave_sums(n), total = (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
-        if (idx - before < total) {
-            const uint32_t k = idx - before - (sum - n);
-            const int from = __builtin_ctzll(__ballot(k < n));
-            req = r0 + from;
-            tile = __builtin_amdgcn_readlane((int)k, from);
-            rq = {__builtin_amdgcn_readlane(r.row0, from), __builtin_amdgcn_readlane(r.q_len, from),
-                  __builtin_amdgcn_readlane(r.kv_len, from)};
-            return true;
-        }
-        before += total;
-    }
-    return false;
-}
-
 // A number's place in the order of all (a NaN counts as the greatest, both zeros are one), at least 1 and below all ones.
 __device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x == x ? x : HUGE_VALF);
@@ -82,7 +60,8 @@ struct Work { Request rq; int32_t req, tok0, n_tok, base, first, end; };   // ba
 __device__ __forceinline__ bool find_work(const SelectArgs &s, Work &w) {
     const PagedArgs &a = s.a;
     int32_t tile = 0;
-    if (!find_tile(a, blockIdx.x / (uint32_t)a.n_heads, w.rq, w.req, tile)) return false;
+    const auto tiles_of = [](int32_t q) { return (uint32_t)(q + kTokens - 1) / kTokens; };
+    if (!find_tile(a, blockIdx.x / (uint32_t)a.n_heads, tiles_of, w.rq, w.req, tile)) return false;
     w.tok0 = tile * kTokens;
     w.n_tok = min(w.rq.q_len - w.tok0, kTokens);
     // (tokens of this round)

@@ -109,7 +109,8 @@ struct PagedArgs {
     PagedClass rows, tile;
     const int32_t *selected;  // attention over selected pages: [n_tokens][n_heads][n_selected]
     int32_t n_selected;
-    FastDiv sel_parts, sel_tiles;   // parts of a row tile, row tiles of a token
+    FastDiv sel_parts, sel_tiles;   // parts of a row tile, row tiles of a token,
+    FastDiv sel_tokens;             // or tokens of a row tile
 };
 
 // The choice of pages (cb_page_select).

@@ -411,6 +411,77 @@ def test_selected_attention_keeps_bad_values_from_rows_that_do_not_see_them(cb, 
             assert np.isnan(got[3:]).all()
 
 
+SHARED = [
+    # kind, lens, H, G, d, page, k: calls of enough tokens that several of a request share a row tile
+    ("bf16", [(280, 700), (1, 300), (33, 33)], 8, 8, 128, 64, 5),
+    ("blocks", [(300, 900), (1, 64), (0, 50), (77, 77), (129, 700)], 8, 2, 64, 32, 6),
+    ("e4m3", [(40, 10), (399, 800)], 8, 5, 96, 32, 4),
+    ("blocks", [(1100, 3300)], 16, 1, 128, 32, 70),
+    ("bf16", [(517, 1000), (2, 1500)], 16, 3, 64, 96, 9),
+    ("blocks", [(3, 70)] * 200, 8, 8, 64, 32, 2),
+]
+
+
+@pytest.mark.parametrize("case", range(len(SHARED)))
+def test_selected_attention_of_many_tokens(cb, serve, case):
+    kind, lens, H, G, d, ps, k = SHARED[case]
+    s = make_step(cb, kind, lens, H, G, d, ps, pad=3, seed=20 + case)
+    sel = random_lists(s, k, case)
+    attend(cb, s, sel)
+    first = s.out.clone()
+    total, rng = int(s.starts[-1]), np.random.default_rng(case)
+    rows = set(rng.choice(total, 24, replace=False)) | {0, 1, 2, total - 2, total - 1} | {int(a) for a in s.starts[1:4] if a < total}
+    check_attend(serve, s, sel, rows=rows)
+    assert (s.out[total:] == 9).all() and (s.lse[total:] == 9).all() and not (s.out[:total] == 9).all(-1).any()
+    attend(cb, s, sel)
+    assert torch.equal(s.out, first)
+
+
+@pytest.mark.parametrize("G,k", [(8, 9), (1, 7)])
+def test_selected_attention_of_many_tokens_counts_a_page_twice(cb, serve, G, k):
+    """Lists in which pages stand up to three times, in any order."""
+    s = make_step(cb, "bf16", [(700, 1000), (324, 500)], 8, G, 64, 32, seed=30)
+    rng = np.random.default_rng(5)
+    sel = rng.integers(0, 10, (s.n, s.H, k))
+    attend(cb, s, sel)
+    got, gl, qd = f64(s.out), f64(s.lse), f64(s.q)
+    for t in list(rng.choice(s.n, 20, replace=False)) + [0, 699, 700, 1023]:
+        r = 0 if t < 700 else 1
+        nq, kv = s.lens[r]
+        p = kv - nq + t - s.starts[r]
+        for h in range(s.H):
+            keys = np.array([32 * i + j for i in sel[t, h] for j in range(32) if 32 * i + j <= p], dtype=int)
+            hs, n = slice(h * G, (h + 1) * G), len(keys)
+            o, l, mag, smag = serve.attention(qd[t:t + 1, hs], s.K[r][h][keys], s.V[r][h][keys], n, s.d ** -0.5)
+            es, few = (s.d + 8) * 2 * F32 * smag, (n + 64) * 2 * F32
+            tol = BF * np.abs(o) * 1.01 + mag * (BF * 1.01 + (2 * es + few)[..., None])
+            assert (np.abs(got[t:t + 1, hs] - o) <= tol).all() and (np.abs(gl[t:t + 1, hs] - l) <= es + few + 8 * F32 * (np.abs(l) + 1)).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "blocks"])
+@pytest.mark.parametrize("z", [0, 1])
+def test_bad_values_of_shared_tiles_reach_only_rows_that_see_them(cb, serve, kind, z):
+    """NaN (bf16 V: infinity too) in a page that the odd tokens alone list, and behind the position of earlier tokens."""
+    s = make_step(cb, kind, [(600, 700)], 8, 2, 64, 32, seed=31)
+    sel = np.tile(np.array([0, 2, 21]), (s.n, s.H, 1))
+    sel[::2, :, 1] = 3                                           # even tokens do not list page 2
+    bad = float("nan")
+    # pages 2 and 21 (keys 672 .. 699): places 4 and 9, key 681 is token 581's own
+    s.pool[s.layer, z, int(s.table[0, 2]), :, 4, 3] = torch.tensor(bad, device="cuda").to(s.pool.dtype)
+    s.pool[s.layer, z, int(s.table[0, 21]), :, 9, 5] = torch.tensor(float("inf") if kind == "bf16" and z else bad, device="cuda").to(s.pool.dtype)
+    attend(cb, s, sel)
+    check_attend(serve, s, sel, rows=[0, 2, 300, 302, 578, 580])
+    got = f64(s.out)
+    late = np.arange(s.n) >= 581
+    odd = np.arange(s.n) % 2 == 1
+    if z == 1:
+        assert np.array_equal((~np.isfinite(got[:, :, 3])).any(1), odd) and np.array_equal((~np.isfinite(got[:, :, 3])).all(1), odd)
+        assert np.array_equal((~np.isfinite(got[:, :, 5])).all(1), late) and np.array_equal((~np.isfinite(got[:, :, 5])).any(1), late)
+        assert np.isfinite(np.delete(got, [3, 5], 2)).all()
+    else:
+        assert np.array_equal(np.isnan(got).all((1, 2)), odd | late) and np.array_equal(np.isnan(got).any((1, 2)), odd | late)
+
+
 def test_selected_attention_strided_queries(cb, serve):
     s = make_step(cb, "blocks", [(2, 40), (1, 90)], 2, 2, 64, 16, seed=15)
     sel = random_lists(s, 3, 1)

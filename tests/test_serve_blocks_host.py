@@ -1,6 +1,8 @@
 """Host checks (no GPU) of pages whose scales belong to a page and head: the plain forms by hand, and what the calls
 refuse (nothing is enqueued)."""
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -232,6 +234,59 @@ def test_workspaces(cb):
     assert cb.cb_attn_selected_workspace_bytes(1, 64, 8, 128, 16, 64) == 0               # 32 tiles: short
     for bad in ((0, 8, 8, 64, 16, 4), (1, 8, 3, 64, 16, 4), (1, 8, 8, 64, 16, 0), (1, 8, 8, 64, 1 << 20, 1 << 20)):
         assert cb.cb_attn_selected_workspace_bytes(*bad) == 0
+
+
+RULES = """
+#include "cb_paged_rules.h"
+extern "C" {
+void selected(int64_t n, int32_t H, int32_t G, int32_t ps, int32_t k, int32_t *out) {
+    const cb::SelectedCut c = cb::selected_cut(n, H, G, ps, k);
+    out[0] = c.tiles;
+    out[1] = c.parts;
+}
+int32_t shared(int64_t n, int64_t reqs, int64_t H, int32_t G, int32_t k, int32_t entries) {
+    return cb::shared_tokens(n, reqs, H, G, k, entries);
+}
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    d = tmp_path_factory.mktemp("rules")
+    (d / "rules.cpp").write_text(RULES)
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_00891_amd", "csrc")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(d / "rules.cpp"), "-o", str(d / "r.so")], check=True)
+    lib = ctypes.CDLL(str(d / "r.so"))
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    lib.selected.argtypes, lib.selected.restype = [i64, i32, i32, i32, i32, ctypes.POINTER(i32)], None
+    lib.shared.argtypes, lib.shared.restype = [i64, i64, i64, i32, i32, i32], i32
+    return lib
+
+
+@pytest.mark.parametrize("H", [1, 2, 8, 40])
+@pytest.mark.parametrize("G", [1, 3, 8, 9, 33])
+def test_selected_rows_are_cut_into_parts(rules, H, G):
+    """A row tile has each of its query heads once; parts have at least 12 key tiles (nearest number to parts of 16 and
+    more), there are none of short lists, and about 2,048 workgroups at most where rows are divided."""
+    out = (ctypes.c_int32 * 2)()
+    for n in (1, 7, 64, 500, 5000):
+        for ps, k in ((1, 1), (16, 64), (16, 80), (64, 17), (64, 64), (1000, 5), (128, 4000), (1 << 20, 1 << 10)):
+            rules.selected(n, H, G, ps, k, out)
+            tiles, parts = out
+            keys = -(-ps * k // 32)
+            assert (tiles - 1) * 16 < G <= tiles * 16 and parts >= 1
+            assert parts == 1 or (keys >= 36 and keys >= 12 * parts and n * tiles * H * parts <= 4 / 3 * 2048), (n, ps, k, parts)
+            assert parts > 1 or keys < 36 or n * tiles * H > 2048 / 1.5 or keys <= 24, (n, ps, k)
+
+
+def test_tokens_that_share_a_row_tile(rules):
+    """Their heads fit 16 rows, their lists the entries, and 1,024 workgroups are left; requests of few tokens share none."""
+    assert [rules.shared(4096, 1, 8, g, 64, 1024) for g in (1, 2, 3, 5, 8, 9, 16, 17)] == [16, 8, 5, 3, 2, 1, 1, 1]
+    assert [rules.shared(4096, 1, 8, 1, k, 1024) for k in (1, 64, 65, 512, 513, 5000)] == [16, 16, 15, 2, 1, 1]
+    assert [rules.shared(n, 1, 8, 2, 4, 1024) for n in (1, 128, 255, 256, 511, 1023, 1024, 9999)] == [1, 1, 1, 2, 3, 7, 8, 8]
+    assert [rules.shared(600, r, 8, 4, 4, 1024) for r in (1, 200, 201, 600)] == [4, 4, 1, 1]
+    assert rules.shared(2 ** 31 - 1, 1, 2 ** 16, 1, 1, 1024) == 16
 
 
 def test_plain_selection_by_hand():
