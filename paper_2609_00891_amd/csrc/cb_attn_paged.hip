@@ -61,8 +61,9 @@
 // Pages with scales of their own (powers of two): the scales of a tile's keys are read
 //   when their rows are requested and are operands of the conversion to bf16, K's by the
 //   lanes that have the key's row, V's by the places of the product: no instruction more
-//   per element, no rounding.  64 single tokens over 512 .. 16,384 keys in pages of 16 (0.62 GB) 135 us, 4.6 TB/s;
-//   2,048 tokens x 64 query heads over 32,768 keys 2.07 ms.
+//   per element, no rounding.  64 single tokens over 512 .. 16,384 keys in pages of 16
+//   (0.61 GB) 133 us, 4.6 TB/s (135 with accumulators beside the vector registers, which
+//   cost moves); 2,048 tokens x 64 query heads over 32,768 keys 2.07 .. 2.37 ms by board.
 //
 // Division of work: a row tile's keys go in `parts` to workgroups of their own
 //   (cb_paged_rules.h), whose partial sums attn_join_kernel adds in an order that

@@ -23,17 +23,19 @@
 //   bytes of a page and handed to the operand's lanes.
 // choose_wave_kernel: a wave per token and head, its keys (estimates as numbers of their
 //   order) in LDS.  The n_selected-th largest is found by counts of eight bits, from the first
-//   in which they differ (23 and 25 us in the two calls below when it was found bit by bit, 21 and 21 so); pages further than twice the error above it are taken, as far
-//   below it are not, and of the others, where they are more than are needed, the wave forms the scores.
+//   in which they differ (23 and 25 us in the two calls below when it was found bit by bit,
+//   20 so); pages further than twice the error above it are taken, as far below it are not,
+//   and of the others, where they are more than are needed, the wave forms the scores.
 // scores_kernel and choose_kernel: tables of more than 8,192 entries.  All scores in 64
 //   bits by 16x16x4 products, and a workgroup per token and head that finds the
 //   threshold by bytes with counts in LDS.
 //
-// Bound by latency and HBM: 48 single tokens over 4,096 .. 65,536 keys in pages of 32 (8 heads of 128, 8 query heads each,
-// 0.15 GB) 65 us with the bounds of the step's pages (40 of them the estimates, 21 the choices), 1,024 new tokens
-// over 32,768 keys in 8-bit pages of 64 46 (22 and 21); the choices' last rows, whose open pages are scored, end them.  With scores of all
-// pages in 64 bits 62 (bounds in the last cache) and 70 (47 and 55 of them the scores), chosen by workgroups that read the
-// keys again for every byte 140 and 97.
+// Bound by latency and HBM: 48 single tokens over 4,096 .. 65,536 keys in pages of 32 (8
+// heads of 128, 8 query heads each, 0.15 GB) 65 us with the bounds of the step's pages (40
+// of them the estimates, 20 the choices), 1,024 new tokens over 32,768 keys in 8-bit pages
+// of 64 45 (22 and 20); the choices' last rows, whose open pages are scored, end them.  With
+// scores of all pages in 64 bits 62 (bounds in the last cache) and 70 (47 and 55 of them
+// the scores), chosen by workgroups that read the keys again for every byte 140 and 97.
 #include "cb_serve_internal.h"
 #include "cb_attn_rows.h"
 
