@@ -437,75 +437,91 @@ struct Keys {
     }
 };
 
-// The scores of pages of one row by its wave: element lane + 64 j of (sum q-, sum q+) and of the pages' bounds in a lane.
+// The scores of pages of one row by its wave, four at a time by 16 lanes each: a lane has d / 8 of the 2 d elements of
+// (sum q-, sum q+) and of a page's bounds.  (Few waves come here, and run this code once: it is kept short.  With a page
+// to the whole wave, two bytes a lane, it was twice as long, and the rows that need it took 7,000 cycles more: 65 us the first call above, 61 so.)
 struct Scores {
-    double q[4];
-    int n, d;
+    double q[16];
+    const uint32_t *x;                                         // the lane's channels of the group's first head
+    uint32_t v[8];                                             // and of a head
+    int d, words;                                              // dwords of a lane's bf16 numbers
     const int32_t *table;
 
+    // Requests the first heads' queries; heads go to the lanes' groups in turn.
     __device__ __forceinline__ Scores(const SelectArgs &s, int32_t req, int32_t tok, int32_t head) {
         const PagedArgs &a = s.a;
-        const int lane = threadIdx.x & 63, G = (int)a.G.d;
         d = s.head_dim;
-        n = 2 * d / 64;
+        words = d / 16;
         table = a.table + req * a.table_stride;
-        const uint16_t *x = a.q + (int64_t)tok * a.q_tok + (int64_t)head * G * a.q_head;
-        int c[4];
+        x = (const uint32_t *)(a.q + (int64_t)tok * a.q_tok + (int64_t)head * (int)a.G.d * a.q_head + (threadIdx.x & 7) * (d / 8));
+        fetch(a, 0);
+    }
+    __device__ __forceinline__ void fetch(const PagedArgs &a, int h0) {
+        const int h = h0 + (int)(threadIdx.x >> 4), G = (int)a.G.d;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            q[j] = 0.0;
-            const int e = j < n ? lane + 64 * j : 0;
-            c[j] = e >= d ? e - d : e;
-        }
-        // (eight heads' values on their way together; behind the last, it again, left out)
-        for (int h0 = 0; h0 < G; h0 += 8) {
-            uint16_t v[8][4];
+        for (int w = 0; w < 8; ++w) v[w] = w < words ? x[min(h, G - 1) * (a.q_head / 2) + w] : 0u;
+    }
+    __device__ __forceinline__ void sums(const PagedArgs &a) {
+        const int G = (int)a.G.d;
+        const uint32_t sign = (threadIdx.x & 8) ? 0u : 0x80000000u;    // min(y, 0) = -max(-y, 0); a NaN goes to both
 #pragma unroll
-            for (int h = 0; h < 8; ++h)
+        for (int e = 0; e < 16; ++e) q[e] = 0.0;
+#pragma unroll 1
+        for (int h0 = 0; h0 < G; h0 += 4) {
+            uint32_t now[8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[h][j] = x[min(h0 + h, G - 1) * a.q_head + c[j]];
+            for (int w = 0; w < 8; ++w) now[w] = h0 + (int)(threadIdx.x >> 4) < G ? v[w] : 0u;
+            if (h0 + 4 < G) fetch(a, h0 + 4);
 #pragma unroll
-            for (int h = 0; h < 8; ++h) {
-                if (h0 + h >= G) continue;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float y = __uint_as_float((uint32_t)v[h][j] << 16);
-                    q[j] += (double)(lane + 64 * j >= d ? __builtin_elementwise_maximum(y, 0.f) : __builtin_elementwise_minimum(y, 0.f));
-                }
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t u = e & 1 ? now[e >> 1] & 0xffff0000u : now[e >> 1] << 16;
+                const float y = __builtin_elementwise_maximum(__uint_as_float(u ^ sign), 0.f);
+                q[e] += (double)__uint_as_float(__float_as_uint(y) ^ sign);
             }
+        }
+        // over the four groups
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            q[e] = both<16>(q[e]);
+            q[e] = both<32>(q[e]);
         }
     }
-    // the keys of four pages
-    __device__ __forceinline__ void keys(const SelectArgs &s, int32_t head, const int32_t (&i)[4], uint32_t (&key)[4]) const {
+    // The sum of a lane's number and that of the lane 16, or 32, places from it.
+    template <int N> static __device__ __forceinline__ double both(double y) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, y);
+        const uint32_t lo = (uint32_t)u, hi = (uint32_t)(u >> 32);
+        const auto l = N == 16 ? __builtin_amdgcn_permlane16_swap(lo, lo, false, false) : __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+        const auto h = N == 16 ? __builtin_amdgcn_permlane16_swap(hi, hi, false, false) : __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+        return __builtin_bit_cast(double, (uint64_t)h[0] << 32 | l[0]) + __builtin_bit_cast(double, (uint64_t)h[1] << 32 | l[1]);
+    }
+    // In lane 16 g + 15 the key of page i of group g (a place in the table).
+    __device__ __forceinline__ uint32_t key(const SelectArgs &s, int32_t head, int32_t i) const {
         const PagedArgs &a = s.a;
-        const int lane = threadIdx.x & 63;
-        float b[4][4], scale[4];
-        int32_t page[4];
+        const int64_t at = (int64_t)min((uint32_t)table[i], (uint32_t)a.n_pages - 1) * a.n_heads + head;
+        const int64_t e0 = at * 2 * d + (threadIdx.x & 15) * (d / 8);
+        const float scale = s.dtype == CB_PAGES_E4M3_BLOCKS ? a.kscale[2 * at] : 1.f;
+        uint32_t u[8];
+        if (s.dtype == CB_PAGES_BF16) {
+            const uint32_t *b = (const uint32_t *)(s.bounds + 2 * e0);
 #pragma unroll
-        for (int p = 0; p < 4; ++p) page[p] = (int32_t)min((uint32_t)table[i[p]], (uint32_t)a.n_pages - 1);
+            for (int w = 0; w < 8; ++w) u[w] = w < words ? b[w] : 0u;
+        } else {
+            const uint32_t *b = (const uint32_t *)(s.bounds + e0);
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            const int64_t at = (int64_t)__builtin_amdgcn_readfirstlane(page[p]) * a.n_heads + head;
-            scale[p] = s.dtype == CB_PAGES_E4M3_BLOCKS ? a.kscale[2 * at] : 1.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                b[p][j] = 0.f;
-                if (j >= n) continue;
-                const int64_t e = at * 2 * d + lane + 64 * j;
-                b[p][j] = s.dtype == CB_PAGES_BF16 ? __uint_as_float((uint32_t)((const uint16_t *)s.bounds)[e] << 16)
-                                                   : bf_lo(e4m3_pair<false>(((const uint8_t *)s.bounds)[e]));
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t y = 2 * w < words ? b[w] : 0u;
+                u[2 * w] = e4m3_pair<false>(y);
+                u[2 * w + 1] = e4m3_pair<true>(y);
             }
         }
+        double sum = 0.0;
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            double sum = 0.0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < n) sum += q[j] * (double)b[p][j];
-            sum = wave_sums(sum);
-            const float score = (float)(sum * (double)__uint_as_float(__float_as_uint(scale[p]) & 0x7f800000u));
-            key[p] = order_of(__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(score), 63)));
-        }
+        for (int w = 0; w < 8; ++w) sum += q[2 * w] * (double)bf_lo(u[w]) + q[2 * w + 1] * (double)bf_hi(u[w]);
+        sum += moved<0x111, 0xf>(sum);   // row_shr:1, 2, 4, 8
+        sum += moved<0x112, 0xf>(sum);
+        sum += moved<0x114, 0xf>(sum);
+        sum += moved<0x118, 0xf>(sum);
+        return order_of((float)(sum * (double)__uint_as_float(__float_as_uint(scale) & 0x7f800000u)));
     }
 };
 
@@ -591,18 +607,16 @@ __global__ __launch_bounds__(64) void choose_wave_kernel(SelectArgs s) {
                 // the key of the lane's page of `count` that `place` has
                 auto score = [&](int count) __attribute__((always_inline)) {
                     uint32_t mine = 0;
+#pragma unroll 1
                     for (int p0 = 0; p0 < count; p0 += 4) {
-                        int32_t i[4];
-                        uint32_t key[4];
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) i[p] = __builtin_amdgcn_readfirstlane(place[min(p0 + p, count - 1)]);
-                        scores.keys(s, head, i, key);
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) mine = lane == p0 + p ? key[p] : mine;
+                        const uint32_t key = scores.key(s, head, place[min(p0 + (lane >> 4), count - 1)]);
+                        const uint32_t x = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * (lane & 3) + 15), (int)key);
+                        mine = lane >> 2 == p0 >> 2 ? x : mine;
                     }
                     return mine;
                 };
                 const int open = between(row, lo, hi, 0, place);
+                scores.sums(s.a);
                 if (open <= kScored) {
                     const int need = s.n_selected - row.at_least(hi + 1);
                     __syncthreads();
