@@ -25,7 +25,7 @@
 //   a team waits for LDS alone.  Everything about a row is one number for a wave (teams of whole waves), the conversions
 //   take bf16 pairs and the scale as they are.  Bound by HBM: 64 layers of four mapped caches of up to 2,048 tokens, keys
 //   turned (2.65 GB), 565 us, 4.7 TB/s (a copy of 2 GiB: 4.9).  With rows that differed within a wave (64-bit products
-//   for every address, in vector instructions) 845 us, with values unpacked, scaled and masked one by one 767.
+//   for every address, in vector instructions) 845 us, with values unpacked, scaled and masked one by one 767, with two rows ahead 616.
 // page_read_kernel: the same search and places without a maximum: 40 layers of 8,191 tokens turned back (2.0 GB) 390 us,
 //   5.2 TB/s.
 #include "cb_serve_internal.h"

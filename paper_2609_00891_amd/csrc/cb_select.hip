@@ -24,16 +24,16 @@
 // choose_wave_kernel: a wave per token and head, its keys (estimates as numbers of their
 //   order) in LDS.  The n_selected-th largest is found by counts of eight bits, from the first
 //   in which they differ (23 and 25 us in the two calls below when it was found bit by bit,
-//   20 so); pages further than twice the error above it are taken, as far below it are not,
+//   21 and 20 so); pages further than twice the error above it are taken, as far below it are not,
 //   and of the others, where they are more than are needed, the wave forms the scores.
 // scores_kernel and choose_kernel: tables of more than 8,192 entries.  All scores in 64
 //   bits by 16x16x4 products, and a workgroup per token and head that finds the
 //   threshold by bytes with counts in LDS.
 //
 // Bound by latency and HBM: 48 single tokens over 4,096 .. 65,536 keys in pages of 32 (8
-// heads of 128, 8 query heads each, 0.15 GB) 65 us with the bounds of the step's pages (40
-// of them the estimates, 20 the choices), 1,024 new tokens over 32,768 keys in 8-bit pages
-// of 64 45 (22 and 20); the choices' last rows, whose open pages are scored, end them.  With
+// heads of 128, 8 query heads each, 0.15 GB) 61 us with the bounds of the step's pages (40
+// of them the estimates, 16 the choices), 1,024 new tokens over 32,768 keys in 8-bit pages
+// of 64 44 (22 and 18); the choices' last rows, whose open pages are scored, end them.  With
 // scores of all pages in 64 bits 62 (bounds in the last cache) and 70 (47 and 55 of them
 // the scores), chosen by workgroups that read the keys again for every byte 140 and 97.
 #include "cb_serve_internal.h"
@@ -439,7 +439,7 @@ struct Keys {
 
 // The scores of pages of one row by its wave, four at a time by 16 lanes each: a lane has d / 8 of the 2 d elements of
 // (sum q-, sum q+) and of a page's bounds.  (Few waves come here, and run this code once: it is kept short.  With a page
-// to the whole wave, two bytes a lane, it was twice as long, and the rows that need it took 7,000 cycles more: 65 us the first call above, 61 so.)
+// to the whole wave, two bytes a lane, it was twice as long, and the rows that need it took 7,000 cycles more: 65 us the first call above.)
 struct Scores {
     double q[16];
     const uint32_t *x;                                         // the lane's channels of the group's first head

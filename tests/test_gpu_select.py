@@ -634,6 +634,46 @@ def test_steps_in_a_graph_with_other_lengths(cb):
         torch.randn(1000, device="cuda").sort()
 
 
+def test_choice_and_shared_tiles_in_a_graph(cb):
+    """A captured choice and attention of many tokens, replayed with other lengths: the eager calls' bits every time, rows of
+    no request as they were."""
+    s = make_step(cb, "blocks", [(280, 700), (1, 300), (33, 33)], 8, 2, 64, 32, pad=3, seed=32)
+    b, pages, k = all_bounds(cb, s), cb.page_pool(s.pool, s.scales), 6
+    starts, kv, table = i32(s.starts), i32([n for _, n in s.lens]), i32(s.table)
+    ws = torch.empty(cb.cb_page_select_workspace_bytes(s.n, 8, s.table.shape[1]), dtype=torch.uint8, device="cuda")
+
+    def buffers():
+        return (torch.full((s.n, 8, k), 7, dtype=torch.int32, device="cuda"),
+                torch.full((s.n, 16, 64), 9.0, dtype=torch.bfloat16, device="cuda"),
+                torch.full((s.n, 16), 9.0, dtype=torch.float32, device="cuda"))
+
+    def run(sel, out, lse):
+        cb.cb_page_select(s.q, pages, s.layer, b, starts, kv, table, sel, workspace=ws)
+        cb.cb_attn_selected(s.q, pages, s.layer, starts, kv, table, sel, out, lse=lse)
+
+    held = buffers()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    run(*buffers())
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        run(*held)
+    for lens in ([(280, 700), (1, 300), (33, 33)], [(100, 650), (150, 290), (60, 20)], [(0, 0), (314, 300), (0, 33)], [(1, 700), (0, 1), (2, 5)]):
+        starts.copy_(i32(np.concatenate([[0], np.cumsum([q for q, _ in lens])])))
+        kv.copy_(i32([n for _, n in lens]))
+        s.q.copy_(randn(gen(len(lens) + lens[0][0]), *s.q.shape).cuda())
+        for x, y in zip(held, buffers()):
+            x.copy_(y)
+        eager = buffers()
+        run(*eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        n = int(starts[-1])
+        for x, y, rest in zip(held, eager, (7, 9, 9)):
+            assert torch.equal(x, y) and (x[n:] == rest).all() and not torch.equal(x[:n], torch.full_like(x[:n], rest))
+        torch.randn(1000, device="cuda").sort()
+
+
 def test_two_calls_at_once(cb, serve):
     """Choice and attention of two steps on two streams, a workspace each."""
     steps = [make_step(cb, "blocks", [(1, 4000), (2, 900)], 2, 4, 64, 16, seed=30 + i) for i in range(2)]
