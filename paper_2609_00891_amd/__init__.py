@@ -224,7 +224,7 @@ def _need(t: Optional[torch.Tensor], shape, dtype, name: str):
     address: check that t holds them."""
     if t is None:
         raise ValueError(f"{name} is required")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != tuple(shape) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, "
                          f"got {t.dtype} {tuple(t.shape)}")
 
@@ -252,12 +252,13 @@ def cache_view(t: Optional[torch.Tensor], n_layers=None, n_heads=None, head_dim=
     """Describe a [layer][kv][seq][head][tok][dim] bfloat16 tensor (any strides, unit channel stride)."""
     if t is None:
         return CbCache(None, n_layers, n_heads, head_dim)
-    if t.dtype != torch.bfloat16 or t.dim() != 6 or t.shape[1] != 2:
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not torch.bfloat16 or len(shape) != 6 or shape[1] != 2:
         raise ValueError("cache tensors are bfloat16 [layer][2][seq][head][tok][dim]")
-    if t.shape[5] > 1 and t.stride(5) != 1:
+    L, _, B, H, T, d = shape
+    if d > 1 and stride[5] != 1:
         raise ValueError("cache channel stride must be 1")
-    L, _, B, H, T, d = t.shape
-    return CbCache(t.data_ptr(), L, H, d, B, T, *t.stride()[:5])
+    return CbCache(t.data_ptr(), L, H, d, B, T, *stride[:5])
 
 
 class Plan:
@@ -726,18 +727,31 @@ def _fit_int32(*values):
         raise ValueError(f"outside the range of 32-bit numbers: {values}")
 
 
-def _on_current_device(names: str, *tensors) -> int:
-    """The library works on the current device: tensors of another (or of the host) are refused here.  Returns the
-    device's index."""
+def _on_current_device(names: str, *tensors, described=()) -> int:
+    """The library works on the current device: tensors of another (or of the host) are refused here, and pools and rotary
+    positions that were ``described`` there.  Returns the device's index."""
     device = tensors[0].get_device()
     good = device >= 0 and device == torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != device:
             good = False
+    for d in described:
+        if d is not None and getattr(d, "_device", device) != device:
+            good = False
     if not good:
-        where = ", ".join(f"{n} on {t.device}" for n, t in zip(names.split(), tensors) if t is not None)
-        raise ValueError(f"every tensor must be on the current CUDA device: {where}")
+        where = [f"{n} on {t.device}" for n, t in zip(names.split(), tensors) if t is not None]
+        where += [f"{type(d).__name__} of tensors on {' and '.join(str(t.device) for t in d._keep if t is not None)}"
+                  for d in described if hasattr(d, "_device")]
+        raise ValueError(f"every tensor must be on the current CUDA device: {', '.join(where)}")
     return device
+
+
+def _keep(described, first: torch.Tensor, second: Optional[torch.Tensor]):
+    """A description holds its tensors, and their device (-2: no single one)."""
+    described._keep = (first, second)
+    described._device = first.get_device()
+    if second is not None and second.get_device() != described._device:
+        described._device = -2
 
 
 def _stream_on(device: int, stream) -> int:
@@ -766,16 +780,16 @@ def page_pool(t: torch.Tensor, scales: Optional[torch.Tensor] = None) -> CbPages
         p.dtype, p.scales = CB_PAGES_E4M3_BLOCKS if blocks else CB_PAGES_E4M3, scales.data_ptr()
     else:
         raise ValueError("pages are bfloat16 or float8_e4m3fn")
-    p._keep = (t, scales)
+    _keep(p, t, scales)
     return p
 
 
 def _rows_view(t: torch.Tensor, name: str) -> CbRows:
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not torch.bfloat16 or len(shape) != 3 or (shape[2] > 1 and stride[2] != 1):
         raise ValueError(f"{name} is bfloat16 [token][head][dim] with unit dim stride")
-    n, h, d = t.shape
-    s = t.stride()
-    return CbRows(t.data_ptr(), n, h, d, s[0], s[1])
+    n, h, d = shape
+    return CbRows(t.data_ptr(), n, h, d, stride[0], stride[1])
 
 
 def rope_axes_spec(table: torch.Tensor, positions: torch.Tensor, axis=None,
@@ -798,17 +812,12 @@ def rope_axes_spec(table: torch.Tensor, positions: torch.Tensor, axis=None,
     sp.axis_stride = positions.shape[-1] if positions.dim() == 1 else positions.stride(0)
     for i, a in enumerate(which):
         sp.axis[i] = a
-    sp._keep = (table, positions)
+    _keep(sp, table, positions)
     return sp
 
 
-def _kept(described) -> tuple:
-    """The tensors behind a page_pool or rope_axes_spec (none for a structure filled by hand)."""
-    return getattr(described, "_keep", (None, None))
-
-
 def _check_axes_tokens(rope: Optional[CbRopeAxesSpec], n_tokens: int):
-    positions = _kept(rope)[1]
+    positions = None if rope is None else getattr(rope, "_keep", (None, None))[1]
     if positions is not None and positions.shape[-1] < n_tokens:
         raise ValueError(f"positions hold {positions.shape[-1]} tokens, the call has {n_tokens}")
 
@@ -835,9 +844,19 @@ def cb_page_tables(ctx_lens: torch.Tensor, q_lens: torch.Tensor, free_pages: tor
 
 
 def _check_table(block_table: torch.Tensor, n: int):
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != n \
-            or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+    """The table as the C ABI takes it: address, stride of a request, entries."""
+    shape, stride = block_table.shape, block_table.stride()
+    if block_table.dtype is not torch.int32 or len(shape) != 2 or shape[0] != n or (shape[1] > 1 and stride[1] != 1):
         raise ValueError(f"block_table must be int32 [{n}][entries] with unit entry stride")
+    return block_table.data_ptr(), stride[0], shape[1]
+
+
+def _requests(q_starts: torch.Tensor, kv_lens: torch.Tensor, block_table: torch.Tensor):
+    """The requests' arguments of the calls on packed new tokens, as the C ABI takes them."""
+    n = kv_lens.numel()
+    _ints(q_starts, n + 1, "q_starts")
+    _ints(kv_lens, n, "kv_lens")
+    return (n, q_starts.data_ptr(), kv_lens.data_ptr(), *_check_table(block_table, n))
 
 
 def cb_rope_axes(cache_in: torch.Tensor, cache_out: torch.Tensor, rope: CbRopeAxesSpec, inverse: bool = False, stream=None):
@@ -845,7 +864,7 @@ def cb_rope_axes(cache_in: torch.Tensor, cache_out: torch.Tensor, rope: CbRopeAx
     (:func:`rope_axes_spec`) into cache_out (may be cache_in); V rows copied."""
     iv, ov = cache_view(cache_in), cache_view(cache_out)
     _check_axes_tokens(rope, cache_in.shape[2] * cache_in.shape[4])
-    dev = _on_current_device("cache_in cache_out table positions", cache_in, cache_out, *_kept(rope))
+    dev = _on_current_device("cache_in cache_out", cache_in, cache_out, described=(rope,))
     _check(_lib.cb_rope_axes(ctypes.byref(iv), ctypes.byref(ov), ctypes.byref(rope), int(bool(inverse)),
                              _stream_on(dev, stream)))
 
@@ -863,8 +882,7 @@ def cb_page_write(rows: torch.Tensor, pages: CbPages, slots: torch.Tensor, layer
     _check_axes_tokens(rope, n)
     qv = None if q is None else _rows_view(q, "q")
     ov = None if q_out is None else _rows_view(q_out, "q_out")
-    dev = _on_current_device("rows slots q q_out pages scales table positions", rows, slots, q, q_out, *_kept(pages),
-                             *_kept(rope))
+    dev = _on_current_device("rows slots q q_out", rows, slots, q, q_out, described=(pages, rope))
     _check(_lib.cb_page_write(ctypes.byref(rv), ctypes.byref(pages), int(layer), _ptr(slots),
                               None if rope is None else ctypes.byref(rope), None if qv is None else ctypes.byref(qv),
                               None if ov is None else ctypes.byref(ov), _stream_on(dev, stream)))
@@ -877,9 +895,8 @@ def _spans(row_starts: Optional[torch.Tensor], q_lens: torch.Tensor, kv_lens: to
         _ints(row_starts, n, "row_starts")
     _ints(q_lens, n, "q_lens")
     _ints(kv_lens, n, "kv_lens")
-    _check_table(block_table, n)
     return (n, None if row_starts is None else row_starts.data_ptr(), q_lens.data_ptr(), kv_lens.data_ptr(),
-            block_table.data_ptr(), block_table.stride(0), block_table.shape[1])
+            *_check_table(block_table, n))
 
 
 def cb_page_quantize(rows: torch.Tensor, pages: CbPages, row_starts: torch.Tensor, q_lens: torch.Tensor,
@@ -892,11 +909,11 @@ def cb_page_quantize(rows: torch.Tensor, pages: CbPages, row_starts: torch.Tenso
     rv = cache_view(rows)
     spans = _spans(row_starts, q_lens, kv_lens, block_table)
     _fit_int32(layer)
-    _check_axes_tokens(rope, rows.shape[2] * rows.shape[4])
+    _check_axes_tokens(rope, rv.n_seqs * rv.seq_len)
     qv = None if q is None else _rows_view(q, "q")
     ov = None if q_out is None else _rows_view(q_out, "q_out")
-    dev = _on_current_device("rows row_starts q_lens kv_lens block_table q q_out pages scales table positions", rows,
-                             row_starts, q_lens, kv_lens, block_table, q, q_out, *_kept(pages), *_kept(rope))
+    dev = _on_current_device("rows row_starts q_lens kv_lens block_table q q_out", rows, row_starts, q_lens, kv_lens,
+                             block_table, q, q_out, described=(pages, rope))
     _check(_lib.cb_page_quantize(ctypes.byref(rv), ctypes.byref(pages), int(layer), *spans,
                                  None if rope is None else ctypes.byref(rope), None if qv is None else ctypes.byref(qv),
                                  None if ov is None else ctypes.byref(ov), _stream_on(dev, stream)))
@@ -910,9 +927,9 @@ def cb_page_read(pages: CbPages, rows: torch.Tensor, row_starts: torch.Tensor, q
     rv = cache_view(rows)
     spans = _spans(row_starts, q_lens, kv_lens, block_table)
     _fit_int32(layer)
-    _check_axes_tokens(rope, rows.shape[2] * rows.shape[4])
-    dev = _on_current_device("rows row_starts q_lens kv_lens block_table pages scales table positions", rows, row_starts,
-                             q_lens, kv_lens, block_table, *_kept(pages), *_kept(rope))
+    _check_axes_tokens(rope, rv.n_seqs * rv.seq_len)
+    dev = _on_current_device("rows row_starts q_lens kv_lens block_table", rows, row_starts, q_lens, kv_lens, block_table,
+                             described=(pages, rope))
     _check(_lib.cb_page_read(ctypes.byref(pages), int(layer), ctypes.byref(rv), *spans,
                              None if rope is None else ctypes.byref(rope), int(bool(inverse)), _stream_on(dev, stream)))
 
@@ -932,23 +949,17 @@ def cb_attn_paged(q: torch.Tensor, pages: CbPages, layer: int, q_starts: torch.T
     """out[t, u] = attention of query q[t, u] over its request's visible keys in the pool's ``layer`` (the new tokens
     are the last of kv_lens; causal, optionally the last ``window`` keys and the first ``sinks`` only).  ``scale``
     defaults to head_dim ** -0.5; ``lse`` float32 [token][head] gets the log of each row's sum of weights."""
-    n = kv_lens.numel()
     qv, ov = _rows_view(q, "q"), _rows_view(out, "out")
-    _ints(q_starts, n + 1, "q_starts")
-    _ints(kv_lens, n, "kv_lens")
-    _check_table(block_table, n)
+    requests = _requests(q_starts, kv_lens, block_table)
     _fit_int32(layer, max_q_len, window, sinks)
     if lse is not None:
         _need(lse, (q.shape[0], q.shape[1]), torch.float32, "lse")
-    if workspace is not None and not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
-    dev = _on_current_device("q q_starts kv_lens block_table out lse workspace pages scales", q, q_starts, kv_lens,
-                             block_table, out, lse, workspace, *_kept(pages))
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_lib.cb_attn_paged(ctypes.byref(qv), ctypes.byref(pages), int(layer), n, _ptr(q_starts), _ptr(kv_lens),
-                              _ptr(block_table), block_table.stride(0), block_table.shape[1], ctypes.byref(ov),
-                              int(max_q_len), float(q.shape[2] ** -0.5 if scale is None else scale), int(window), int(sinks),
-                              _ptr(lse), _ptr(workspace), int(ws_bytes), _stream_on(dev, stream)))
+    ws, ws_bytes = _workspace(workspace)
+    dev = _on_current_device("q q_starts kv_lens block_table out lse workspace", q, q_starts, kv_lens, block_table, out, lse,
+                             workspace, described=(pages,))
+    _check(_lib.cb_attn_paged(ctypes.byref(qv), ctypes.byref(pages), int(layer), *requests, ctypes.byref(ov), int(max_q_len),
+                              float(qv.head_dim ** -0.5 if scale is None else scale), int(window), int(sinks), _ptr(lse), ws,
+                              ws_bytes, _stream_on(dev, stream)))
 
 
 def _bounds(bounds: torch.Tensor, pages: CbPages):
@@ -957,6 +968,15 @@ def _bounds(bounds: torch.Tensor, pages: CbPages):
     dtype = torch.bfloat16 if pages.dtype == CB_PAGES_BF16 else torch.float8_e4m3fn
     _need(bounds, (c.n_layers, c.n_seqs, c.n_heads, 2, c.head_dim), dtype, "bounds")
     return _ptr(bounds)
+
+
+def _listed(selected: torch.Tensor, q: CbRows, pages: CbPages) -> int:
+    """Lists of pages [token][KV head][pages]; returns how long they are."""
+    shape = selected.shape
+    if len(shape) != 3:
+        raise ValueError("selected must be int32 [token][KV head][pages]")
+    _need(selected, (q.n_tokens, pages.cache.n_heads, shape[2]), torch.int32, "selected")
+    return shape[2]
 
 
 def _workspace(workspace: Optional[torch.Tensor]):
@@ -974,8 +994,7 @@ def cb_page_bounds(pages: CbPages, bounds: torch.Tensor, q_lens: torch.Tensor, k
     _, _, q, kv, table, stride, width = spans = _spans(None, q_lens, kv_lens, block_table)
     bv = _bounds(bounds, pages)
     _fit_int32(layer, layers, max_q_len)
-    dev = _on_current_device("bounds q_lens kv_lens block_table pages scales", bounds, q_lens, kv_lens, block_table,
-                             *_kept(pages))
+    dev = _on_current_device("bounds q_lens kv_lens block_table", bounds, q_lens, kv_lens, block_table, described=(pages,))
     _check(_lib.cb_page_bounds(ctypes.byref(pages), int(layer), int(layers), bv, spans[0], q, kv, table, stride, width,
                                int(max_q_len), _stream_on(dev, stream)))
 
@@ -992,22 +1011,16 @@ def cb_page_select(q: torch.Tensor, pages: CbPages, layer: int, bounds: torch.Te
     """The pages that each new token attends to in the pool's ``layer``: ``selected`` int32 [token][KV head][pages] gets
     the first ``first`` and the last ``last`` ones and those whose keys' scores are bounded highest (``bounds`` from
     :func:`cb_page_bounds`), ascending, -1 behind them."""
-    n = kv_lens.numel()
     qv = _rows_view(q, "q")
-    _ints(q_starts, n + 1, "q_starts")
-    _ints(kv_lens, n, "kv_lens")
-    _check_table(block_table, n)
+    requests = _requests(q_starts, kv_lens, block_table)
     bv = _bounds(bounds, pages)
-    if selected.dim() != 3:
-        raise ValueError("selected must be int32 [token][KV head][pages]")
-    _need(selected, (q.shape[0], pages.cache.n_heads, selected.shape[2]), torch.int32, "selected")
+    k = _listed(selected, qv, pages)
     _fit_int32(layer, first, last)
     ws, ws_bytes = _workspace(workspace)
-    dev = _on_current_device("q q_starts kv_lens block_table selected bounds workspace pages scales", q, q_starts, kv_lens,
-                             block_table, selected, bounds, workspace, *_kept(pages))
-    _check(_lib.cb_page_select(ctypes.byref(qv), ctypes.byref(pages), int(layer), bv, n, _ptr(q_starts), _ptr(kv_lens),
-                               _ptr(block_table), block_table.stride(0), block_table.shape[1], int(first), int(last),
-                               selected.shape[2], _ptr(selected), ws, ws_bytes, _stream_on(dev, stream)))
+    dev = _on_current_device("q q_starts kv_lens block_table selected bounds workspace", q, q_starts, kv_lens, block_table,
+                             selected, bounds, workspace, described=(pages,))
+    _check(_lib.cb_page_select(ctypes.byref(qv), ctypes.byref(pages), int(layer), bv, *requests, int(first), int(last), k,
+                               selected.data_ptr(), ws, ws_bytes, _stream_on(dev, stream)))
 
 
 def cb_attn_selected_workspace_bytes(n_tokens: int, n_qheads: int, n_heads: int, head_dim: int, page_size: int,
@@ -1023,21 +1036,15 @@ def cb_attn_selected(q: torch.Tensor, pages: CbPages, layer: int, q_starts: torc
                      lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """out[t, u] = attention of query q[t, u] over the keys up to its own position that lie in the pages ``selected``
     [token][KV head][pages] for it, in the pool's ``layer``; otherwise as :func:`cb_attn_paged`."""
-    n = kv_lens.numel()
     qv, ov = _rows_view(q, "q"), _rows_view(out, "out")
-    _ints(q_starts, n + 1, "q_starts")
-    _ints(kv_lens, n, "kv_lens")
-    _check_table(block_table, n)
-    if selected.dim() != 3:
-        raise ValueError("selected must be int32 [token][KV head][pages]")
-    _need(selected, (q.shape[0], pages.cache.n_heads, selected.shape[2]), torch.int32, "selected")
+    requests = _requests(q_starts, kv_lens, block_table)
+    k = _listed(selected, qv, pages)
     _fit_int32(layer)
     if lse is not None:
         _need(lse, (q.shape[0], q.shape[1]), torch.float32, "lse")
     ws, ws_bytes = _workspace(workspace)
-    dev = _on_current_device("q q_starts kv_lens block_table selected out lse workspace pages scales", q, q_starts, kv_lens,
-                             block_table, selected, out, lse, workspace, *_kept(pages))
-    _check(_lib.cb_attn_selected(ctypes.byref(qv), ctypes.byref(pages), int(layer), n, _ptr(q_starts), _ptr(kv_lens),
-                                 _ptr(block_table), block_table.stride(0), block_table.shape[1], _ptr(selected),
-                                 selected.shape[2], ctypes.byref(ov), float(q.shape[2] ** -0.5 if scale is None else scale),
-                                 _ptr(lse), ws, ws_bytes, _stream_on(dev, stream)))
+    dev = _on_current_device("q q_starts kv_lens block_table selected out lse workspace", q, q_starts, kv_lens, block_table,
+                             selected, out, lse, workspace, described=(pages,))
+    _check(_lib.cb_attn_selected(ctypes.byref(qv), ctypes.byref(pages), int(layer), *requests, selected.data_ptr(), k,
+                                 ctypes.byref(ov), float(qv.head_dim ** -0.5 if scale is None else scale), _ptr(lse), ws,
+                                 ws_bytes, _stream_on(dev, stream)))
