@@ -132,6 +132,52 @@ inline RowsCut rows_cut(int64_t n_tokens, int32_t n_rows, int32_t head_dim, bool
     return c;
 }
 
+// Host side: the least l with n <= 2^l.
+inline int log2_up(int n) {
+    int l = 0;
+    while ((1 << l) < n) ++l;
+    return l;
+}
+
+// Host side: the launch that writes n_rows rows of head_dim channels of each of n_tokens tokens of n_reqs requests into
+// pages with scales of their own, or reads them from pages.  A page's token has 2^lgc places for its pairs of 16-byte
+// chunks.  wide: pages get enough tokens on average for teams of whole waves (of a call of many single tokens and a chunk
+// they do not: teams of the chunk's whole pages then outgrow a wave and take turns).  pairs: the pairs of chunks of a
+// thread, as many as hold a page's row in registers, up to 4, 0 where they do not.  group: the rows of a page that one
+// workgroup takes: up to 16, which share its search, places and angles, while the launch fills the chip, at least 4 (1,811
+// tokens of three requests, 56 rows of 96 channels each: 23.0 us with 1, 20.6 with 2, 17.8 with 4, 22.7 with 8) and as many
+// as it has teams.
+struct SpanCut {
+    int lgc;
+    bool wide;
+    int pairs;
+    int32_t group;
+    int64_t blocks, groups;  // the grid: pages (workgroups go round while there are more), groups of rows
+};
+inline SpanCut span_cut(int64_t n_tokens, int64_t n_reqs, int32_t page_size, int32_t head_dim, int32_t n_rows) {
+    SpanCut c;
+    // Pages that the tokens can lie in together, unless requests share rows: a page has at least one token, all but a
+    // request's first and last a whole page.
+    int64_t items = n_tokens / page_size + 2 * n_reqs;
+    if (items > n_tokens) items = n_tokens;
+    c.lgc = log2_up(head_dim / 16);
+    int64_t tokens = (n_tokens + n_reqs - 1) / n_reqs;
+    if (tokens > page_size) tokens = page_size;
+    const int64_t units = (int64_t)page_size << c.lgc;
+    c.wide = tokens << c.lgc >= 64;
+    c.pairs = units <= 256 ? 1 : units <= 512 ? 2 : units <= 1024 ? 4 : 0;
+    int teams = 256 >> c.lgc;
+    while (teams > 1 && (256 / teams) < tokens << c.lgc) teams /= 2;
+    c.group = 16;
+    while (c.group > 4 && items * ((n_rows + c.group - 1) / c.group) < 2048) c.group /= 2;
+    if (c.group < teams) c.group = teams;
+    while ((n_rows + c.group - 1) / c.group > 65535) c.group *= 2;
+    c.groups = (n_rows + c.group - 1) / c.group;
+    // (a launch has fewer than 2^32 threads in one direction)
+    c.blocks = items < 1 ? 1 : items < 1 << 22 ? items : 1 << 22;
+    return c;
+}
+
 // Host side: attention over n_selected pages of every token: row tiles of 16 query heads of one KV head, the listed keys in
 // tiles of 32, each row tile's in parts for about 2,048 workgroups, of 16 tiles or more, where it has 36 or more (the
 // same division as of single tokens over all their pages).

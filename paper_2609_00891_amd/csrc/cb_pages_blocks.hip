@@ -29,8 +29,8 @@
 // page_read_kernel: the same search and places without a maximum: 40 layers of 8,191 tokens turned back (2.0 GB) 390 us,
 //   5.2 TB/s.
 #include "cb_serve_internal.h"
+#include "cb_paged_rules.h"
 #include "cb_rows_device.h"
-#include <algorithm>
 
 namespace cb {
 namespace {
@@ -569,41 +569,13 @@ __global__ __launch_bounds__(256) void page_bounds_kernel(BoundsArgs a, SpanArgs
     }
 }
 
-// Pages that the new tokens of a call can lie in together, unless requests share rows: a page has at least one token,
-// all but a request's first and last a whole page.  (Workgroups go round while there are more.)
-int64_t span_bound(const SpanArgs &s) {
-    const int64_t b = s.n_tokens / s.page_size.d + 2 * (int64_t)s.n_reqs;
-    return b < s.n_tokens ? b : s.n_tokens;
-}
-
-int log2_up(int n) {
-    int l = 0;
-    while ((1 << l) < n) ++l;
-    return l;
-}
-
-// The launch of a call: whether pages get enough tokens on average for teams of whole waves, the pairs of chunks of a
-// thread (as many as hold a page's row in registers, up to 4, 0 where they do not), and the rows of a page that one workgroup takes: up to 16,
-// which share its search, places and angles, while the launch fills the chip, at least 4 (1,811 tokens of three requests, 56
-// rows of 96 channels each: 23.0 us with 1, 20.6 with 2, 17.8 with 4, 22.7 with 8) and as many as it has teams.
+// The launch of a call on spans of pages.
 struct Cut { dim3 grid; bool wide; int pairs; };
 Cut cut(RowsArgs &a, const SpanArgs &s) {
-    Cut c;
-    const int64_t items = span_bound(s);
-    a.lgc = log2_up((int)a.nc2.d);
-    const int64_t tokens = std::min<int64_t>((s.n_tokens + s.n_reqs - 1) / s.n_reqs, s.page_size.d);
-    const int64_t units = (int64_t)s.page_size.d << a.lgc;
-    c.wide = tokens << a.lgc >= 64;
-    c.pairs = units <= 256 ? 1 : units <= 512 ? 2 : units <= 1024 ? 4 : 0;
-    int teams = 256 >> a.lgc;
-    while (teams > 1 && (256 / teams) < tokens << a.lgc) teams /= 2;
-    a.group = 16;
-    while (a.group > 4 && items * ((a.n_rows + a.group - 1) / a.group) < 2048) a.group /= 2;
-    a.group = std::max(a.group, teams);
-    while ((a.n_rows + a.group - 1) / a.group > 65535) a.group *= 2;
-    // (a launch has fewer than 2^32 threads in one direction; workgroups go round)
-    c.grid = dim3((unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), 1 << 22), (unsigned)((a.n_rows + a.group - 1) / a.group));
-    return c;
+    const SpanCut c = span_cut(s.n_tokens, s.n_reqs, (int32_t)s.page_size.d, (int32_t)a.nc2.d * 16, a.n_rows);
+    a.lgc = c.lgc;
+    a.group = c.group;
+    return {dim3((unsigned)c.blocks, (unsigned)c.groups), c.wide, c.pairs};
 }
 
 template <bool ROPE>

@@ -10,6 +10,7 @@ import pytest
 import torch
 
 from test_gpu_serve import CASES, Step
+from test_serve_blocks_host import build_span_cut
 
 pytestmark = pytest.mark.gpu
 
@@ -246,6 +247,121 @@ def test_read(cb, serve, case, kind):
         exact = fine.copy()
         if axes:
             exact[:, :, 0] = False
+        assert np.array_equal(got[exact], want[exact])
+    assert (np.abs(got - want)[fine] <= (BF * np.abs(want) + 6 * F32 * mag)[fine]).all()
+
+
+MIXED = [
+    # single tokens, the chunk among them (new, with them), L, H, G, d, page, axes, style
+    (63, (200, 237), 1, 2, 0, 128, 64, 0, 0),
+    (63, (200, 237), 2, 2, 2, 128, 64, 3, 1),
+    (63, (230, 260), 1, 3, 2, 128, 16, 1, 0),
+    (40, (150, 170), 2, 2, 0, 64, 64, 3, 0),
+    (90, (300, 333), 1, 1, 3, 96, 64, 2, 1),
+    (120, (200, 250), 1, 2, 0, 256, 32, 1, 0),
+    (200, (500, 700), 1, 1, 1, 64, 256, 1, 0),
+]
+
+
+def mixed_step(tmp_path, case):
+    """A step of many single tokens and one chunk that begins inside a page, and the rule that gives its rows teams made for
+    single tokens, while the chunk's whole pages have more units than a wave."""
+    singles, chunk, L, H, G, d, ps, axes, style = MIXED[case]
+    rng = np.random.default_rng(case)
+    lens = [(1, int(k)) for k in rng.integers(1, 3 * ps, singles)]
+    lens.insert(singles // 2, chunk)
+    n = singles + chunk[0]
+    cut = build_span_cut(tmp_path)(n, len(lens), ps, d, 2 * L * H + H * G)
+    assert not cut["wide"] and ps << cut["lgc"] > 64 and (chunk[1] - chunk[0]) % ps
+    P = sum(-(-k // ps) for _, k in lens) + 2
+    return n, P, make_step(lens, ps, P, case, True)
+
+
+@pytest.mark.parametrize("case", range(len(MIXED)))
+def test_quantize_single_tokens_and_a_chunk(cb, serve, tmp_path, case):
+    """Scales that grow and others that stay, a NaN and an infinity in the chunk's whole pages; queries beside the rows."""
+    singles, chunk, L, H, G, d, ps, axes, style = MIXED[case]
+    n, P, (starts, q, kv, table, width) = mixed_step(tmp_path, case)
+    g = gen(100 + case)
+    x = (randn(g, L, 2, 1, H, n, d) * torch.exp(2 * torch.randn((L, 2, 1, H, n, 1), generator=g)).to(torch.bfloat16)).cuda()
+    whole = singles // 2 + chunk[0] // 2                           # a token of a whole page of the chunk
+    x[0, 0, 0, 0, whole, 3], x[-1, 1, 0, -1, whole, 5] = float("nan"), float("inf")
+    pool = Pool(cb, L + 1, H, P, ps, d, seed=case)
+    rope = tables = qx = qo = None
+    if axes:
+        rope, *rest = rope_of(cb, d, axes, n, case, style, bad=[singles // 2 + 7])
+        tables = (rope, *rest, style)
+    if G:
+        qx = randn(g, n, H * G, d).cuda()
+        qo = torch.full_like(qx, 5.0)
+    before, raw0 = pool.codes()[1:], pool.raw()
+    cb.cb_page_quantize(x, pool.pages, i32(starts), i32(q), i32(kv), i32(table), layer=1, rope=rope, q=qx, q_out=qo)
+    torch.cuda.synchronize()
+    rows = by_row(x)
+    y, mag = turned_keys(serve, rows, tables) if axes else (rows, np.zeros_like(rows))
+    spans = serve.page_spans(starts, q, kv, ps, n, width)
+    want, exps, wmag = before.copy(), pool.exps[1:].copy(), np.zeros_like(before)
+    serve.page_quantize(rows, y if axes else None, want, exps, spans, table)
+    assert np.array_equal(pool.scales[1:].cpu().numpy(), (2.0 ** exps).astype(np.float32))
+    new, old, grown = np.zeros(want.shape, bool), np.zeros(want.shape, bool), 0
+    for r, entry, at, m, t in spans:
+        p = int(table[r, entry])
+        new[:, :, p, :, at:at + m] = True
+        old[:, :, p, :, :at] = True
+        grown += int((exps[:, p] > pool.exps[1:, p]).sum()) if r == singles // 2 and at else 0
+        wmag[:, :, p, :, at:at + m] = mag[t:t + m].transpose(1, 2, 3, 0, 4) * (2.0 ** -exps[:, p].astype(float)).transpose(0, 2, 1)[..., None, None]
+    assert grown > 0
+    got, raw = pool.codes()[1:], pool.raw()
+    is_k = np.zeros(want.shape, bool)
+    is_k[:, 0] = bool(axes)
+    check_codes(serve, got, want, wmag, is_k, new)
+    assert ((got == want) | (np.isnan(got) & np.isnan(want)))[old].all()
+    rest = ~new & ~old
+    assert np.array_equal(raw[1:][rest], raw0[1:][rest]) and np.array_equal(raw[:1], raw0[:1])
+    if G:
+        yq, mq = serve.turn(f64(qx), *tables[1:4], style)
+        gq, fine = f64(qo), ~np.isnan(yq)
+        assert np.array_equal(np.isnan(gq), ~fine)
+        assert (np.abs(gq - yq)[fine] <= (BF * np.abs(yq) + 4 * F32 * mq)[fine]).all()
+    cb.cb_page_quantize(x, pool.pages, i32(starts), i32(q), i32(kv), i32(table), layer=1, rope=rope, q=qx, q_out=qo)
+    assert np.array_equal(pool.raw(), raw)
+
+
+@pytest.mark.parametrize("kind", ["blocks", "e4m3", "bf16"])
+@pytest.mark.parametrize("case", range(len(MIXED)))
+def test_read_single_tokens_and_a_chunk(cb, serve, tmp_path, case, kind):
+    singles, chunk, L, H, _, d, ps, axes, style = MIXED[case]
+    n, P, (starts, q, kv, table, width) = mixed_step(tmp_path, case)
+    scales = None
+    if kind == "blocks":
+        pool = Pool(cb, L + 1, H, P, ps, d, seed=case)
+        pages, value = pool.pages, pool.codes() * (2.0 ** pool.exps.astype(float)).transpose(0, 3, 1, 2)[..., None, None]
+    else:
+        t = randn(gen(case), L + 1, 2, P, H, ps, d).cuda()
+        value = None
+        if kind == "e4m3":
+            t, scales = t.to(torch.float8_e4m3fn), (0.01 + torch.rand((L + 1, 2, H), generator=gen(case + 1)))
+            value = f64(t) * scales.double().numpy()[:, :, None, :, None, None]
+        pages, value = cb.page_pool(t, None if scales is None else scales.cuda()), f64(t) if value is None else value
+    rope = tables = None
+    if axes:
+        rope, *rest = rope_of(cb, d, axes, n, case, style, bad=[singles // 2 + 7])
+        tables = (rope, *rest, style)
+    out = torch.full((L, 2, 1, H, n, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    cb.cb_page_read(pages, out, i32(starts), i32(q), i32(kv), i32(table), layer=1, rope=rope, inverse=bool(case % 2))
+    torch.cuda.synchronize()
+    want = np.full((n, L, 2, H, d), 7.0)
+    for r, entry, at, m, t in serve.page_spans(starts, q, kv, ps, n, width):
+        want[t:t + m] = value[1:, :, int(table[r, entry]), :, at:at + m].transpose(3, 0, 1, 2, 4)
+    mag = np.abs(want)
+    if axes:
+        want, turned = turned_keys(serve, want, tables, bool(case % 2))
+        mag[:, :, 0] = turned[:, :, 0]
+    got, fine = by_row(out), ~np.isnan(want)
+    assert np.array_equal(np.isnan(got), ~fine)
+    if kind != "e4m3":
+        exact = fine.copy()
+        exact[:, :, 0] &= not axes
         assert np.array_equal(got[exact], want[exact])
     assert (np.abs(got - want)[fine] <= (BF * np.abs(want) + 6 * F32 * mag)[fine]).all()
 

@@ -300,3 +300,60 @@ def test_plain_selection_by_hand():
     assert serve.page_select(s, [True] * 7, 0, 2, 4) == [2, 4, 5, 6]
     assert serve.page_select(s, [False, True, True, False, False, True, False], 1, 1, 2) == [1, 2]
     assert serve.page_select(s[:2], [True] * 2, 1, 1, 4) == [0, 1]
+
+
+SPAN_RULES = """
+#include "cb_paged_rules.h"
+extern "C" void spans(int64_t n, int64_t reqs, int32_t ps, int32_t d, int32_t rows, int64_t *out) {
+    const cb::SpanCut c = cb::span_cut(n, reqs, ps, d, rows);
+    out[0] = c.lgc;
+    out[1] = c.wide;
+    out[2] = c.pairs;
+    out[3] = c.group;
+    out[4] = c.blocks;
+    out[5] = c.groups;
+}
+"""
+
+
+def build_span_cut(d):
+    """span_cut(tokens, requests, page size, head_dim, rows) as a function that returns its numbers."""
+    (d / "spans.cpp").write_text(SPAN_RULES)
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_00891_amd", "csrc")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(d / "spans.cpp"), "-o", str(d / "s.so")], check=True)
+    lib = ctypes.CDLL(str(d / "s.so"))
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    lib.spans.argtypes, lib.spans.restype = [i64, i64, i32, i32, i32, ctypes.POINTER(i64)], None
+
+    def cut(*args):
+        out = (i64 * 6)()
+        lib.spans(*args, out)
+        return dict(zip(("lgc", "wide", "pairs", "group", "blocks", "groups"), out))
+    return cut
+
+
+@pytest.fixture(scope="module")
+def span_cut(tmp_path_factory):
+    return build_span_cut(tmp_path_factory.mktemp("spans"))
+
+
+@pytest.mark.parametrize("d", [16, 48, 64, 96, 128, 256])
+def test_spans_are_cut_into_workgroups(span_cut, d):
+    """Every row of every page has a workgroup, within a launch's limits; a page that a team takes in one turn has a place
+    for each of its units (256 threads of the team, `pairs` each)."""
+    for ps in (1, 7, 16, 64, 100, 1024, 1 << 24):
+        for n, reqs in ((1, 1), (63, 64), (263, 64), (1811, 3), (5, 9), (1 << 24, 1), (2 ** 31 - 1, 1)):
+            for rows in (2, 10, 80, 5120, 3 << 24):
+                c = span_cut(n, reqs, ps, d, rows)
+                assert 1 << c["lgc"] >= d // 16 > 1 << c["lgc"] >> 1
+                assert (c["groups"] - 1) * c["group"] < rows <= c["groups"] * c["group"] and c["groups"] <= 65535
+                assert 1 <= c["blocks"] <= min(max(n, 1), 1 << 22)
+                units = ps << c["lgc"]
+                assert units <= 256 * c["pairs"] if c["pairs"] else units > 1024
+
+
+def test_a_call_of_single_tokens_and_a_chunk_has_narrow_teams(span_cut):
+    """The rule goes by the call's tokens for each request: chunks' whole pages come to teams that were made for single
+    tokens, larger than a wave and, where the page has more than 256 units, in turns."""
+    assert [span_cut(n, 64, 64, 128, 12)["wide"] for n in (64, 263, 512, 513)] == [0, 0, 1, 1]
+    assert not span_cut(63 + 200, 64, 16, 128, 12)["wide"] and not span_cut(30 + 150, 31, 64, 64, 12)["wide"]
