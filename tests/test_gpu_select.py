@@ -210,6 +210,66 @@ def test_select_in_large_tables(cb, serve):
         assert np.array_equal(got, expected(serve, s, b, k, first, last))
 
 
+def large_table(cb, kind, d, seed):
+    """Requests whose rows of the table have more entries than a wave keeps: pages of one key."""
+    s = make_step(cb, kind, [(3, 9000), (1, 40), (2, 8300)], 2 if d == 96 else 1, 3, d, 1, seed=seed)
+    assert s.table.shape[1] > 8192
+    return s, all_bounds(cb, s)
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "blocks"])
+def test_select_in_large_tables_of_every_kind(cb, serve, kind, d):
+    """All tokens at once and in turns; equal scores, pages that are hidden, and NaN among bounds and queries."""
+    s, b = large_table(cb, kind, d, seed=d)
+    for k, first, last in ((33, 1, 2), (1500, 0, 1)):
+        got = choose(cb, s, b, k, first, last)
+        assert np.array_equal(got, expected(serve, s, b, k, first, last))
+        for rows in (1, 4):
+            assert np.array_equal(choose(cb, s, b, k, first, last, rows=rows), got)
+    # a seventh of the pages differ, in bounds and scales
+    for r in range(3):
+        rows = torch.tensor(s.table[r][s.table[r] >= 0], device="cuda").long()
+        alike = rows[torch.arange(len(rows), device="cuda") % -(-len(rows) // 7)]
+        raw = b.view(torch.int16 if kind == "bf16" else torch.uint8)
+        raw[s.layer, rows] = raw[s.layer, alike]
+        if kind == "blocks":
+            s.scales[s.layer, rows] = s.scales[s.layer, alike]
+    s.q[1], s.q[4] = 0, -0.0
+    table = s.table.copy()
+    table[0, [0, 5, 4000, 8999]] = -1, s.pool.shape[2], 2 ** 31 - 1, -7
+    table[2, 100:8290] = -1
+    got = choose(cb, s, b, 40, 2, 3, table=table)
+    assert np.array_equal(got, expected(serve, s, b, 40, 2, 3, table=table))
+    raw = b.view(torch.uint8)
+    nan = [0xc0, 0x7f] if kind == "bf16" else [0x7f]
+    for i in (7, 3000, 8700):
+        page, c = int(s.table[0, i]), 9 * len(nan)
+        raw[s.layer, page, 0, 1, c:c + len(nan)] = torch.tensor(nan, dtype=torch.uint8, device="cuda")
+    s.q[5, 0, 3] = float("nan")                                  # every page of request 2
+    got = choose(cb, s, b, 40, 0, 1)
+    assert np.array_equal(got, expected(serve, s, b, 40, 0, 1))
+    assert {7, 3000, 8700} <= set(got[0, 0]) and got[5, 0].tolist() == list(range(39)) + [8299]
+
+
+@pytest.mark.parametrize("large", [False, True])
+def test_select_pages_with_infinities(cb, serve, large):
+    """A page whose bounds hold an infinity or a NaN counts as +infinity, whatever the queries' signs."""
+    if large:
+        s, b = large_table(cb, "bf16", 64, seed=6)
+    else:
+        s = make_step(cb, "bf16", [(3, 900), (1, 40), (2, 830)], 1, 3, 64, 8, seed=6)
+        b = all_bounds(cb, s)
+    own = (s.lens[0][1] - 1) // s.ps                             # of token 2; behind the others of its request where pages are small
+    for i, z, v in ((11, 0, -float("inf")), (12, 1, float("inf")), (own, 1, float("inf")), (40, 0, float("nan"))):
+        b[s.layer, int(s.table[0, i]), 0, z, 9] = v
+    for sign in (1.0, -1.0):
+        s.q.copy_(s.q.abs() * sign)
+        got = choose(cb, s, b, 20, 0, 1)
+        assert np.array_equal(got, expected(serve, s, b, 20, 0, 1))
+        assert all({11, 12, 40} <= set(got[t, 0]) for t in range(3))
+
+
 def test_select_scores_of_extreme_size(cb, serve):
     """Queries and bounds near the ends of bf16's range: estimates that leave fp32's say nothing, and the scores decide."""
     for qs, bs in ((2.0 ** 60, 2.0 ** 60), (2.0 ** 100, 2.0 ** 20), (2.0 ** -70, 2.0 ** -50), (2.0 ** -120, 2.0 ** 100), (2.0 ** 126, 1.0)):
