@@ -453,6 +453,87 @@ def test_selected_attention_counts_a_page_twice(cb, serve):
     assert np.allclose(f64(s.lse), f64(al) + np.log(2.0), atol=1e-5, rtol=0)
 
 
+DIVIDED = [
+    # kind, H, G, d, page, k: lists of about 10,000 keys, each row tile's in more than 16 parts
+    ("bf16", 2, 3, 128, 64, 160),
+    ("blocks", 2, 33, 64, 16, 640),
+    ("e4m3", 1, 17, 96, 24, 430),
+    ("blocks", 1, 40, 128, 32, 320),
+]
+
+
+def check_listed(serve, s, sel, table=None):
+    """As check_attend, with pages that are listed more than once counted as often."""
+    table = s.table if table is None else table
+    got, gl, qd = f64(s.out), f64(s.lse), f64(s.q)
+    for r, (nq, kv) in enumerate(s.lens):
+        there = (table[r] >= 0) & (table[r] < s.pool.shape[2])
+        for t in range(nq):
+            p, at = kv - nq + t, s.starts[r] + t
+            for h in range(s.H):
+                pages = [int(i) for i in sel[at, h] if 0 <= i < len(there) and there[i]]
+                keys = np.array([j for i in pages for j in range(i * s.ps, min((i + 1) * s.ps, p + 1))], dtype=int)
+                hs, n = slice(h * s.G, (h + 1) * s.G), len(keys)
+                o, l, mag, smag = serve.attention(qd[at:at + 1, hs], s.K[r][h][keys], s.V[r][h][keys], n, s.d ** -0.5)
+                es, few = (s.d + 8) * 2 * F32 * smag, (n + 64) * 2 * F32
+                tol = BF * np.abs(o) * 1.01 + mag * (BF * 1.01 + (2 * es + few)[..., None])
+                assert (np.abs(got[at:at + 1, hs] - o) <= tol).all(), (r, t, h)
+                assert np.array_equal(np.isneginf(gl[at:at + 1, hs]), np.isneginf(l)), (r, t, h)
+                if n:
+                    assert (np.abs(gl[at:at + 1, hs] - l) <= es + few + 8 * F32 * (np.abs(l) + 1)).all(), (r, t, h)
+
+
+@pytest.mark.parametrize("case", range(len(DIVIDED)))
+def test_selected_attention_in_many_parts(cb, serve, case):
+    """Rows that a workgroup joins, beside rows whose lists are short, empty, of hidden pages or of later ones, so that some
+    or all of their parts are."""
+    kind, H, G, d, ps, k = DIVIDED[case]
+    s = make_step(cb, kind, [(2, k * ps + 40), (1, 6 * ps + 1), (1, 3000), (1, 2 * ps), (2, 900)], H, G, d, ps, pad=1, seed=50 + case)
+    # a part is a row of 16 query heads and its maximum and sum, in fp32
+    row_tiles = s.n * -(-G // 16) * H
+    need = cb.cb_attn_selected_workspace_bytes(s.n, H * G, H, d, ps, k)
+    assert need > 16 * row_tiles * 16 * (d + 2) * 4
+    sel, rng = random_lists(s, k, case), np.random.default_rng(case)
+    sel[0] = rng.permutation(k)                                 # whole lists, beside a short one
+    sel[1, :, 2:] = -1
+    sel[3, 0] = -1
+    sel[4] = 2 + np.arange(k) % 60                              # behind the token: pages of 2 ps keys are 0 and 1
+    table = s.table.copy()
+    table[3, 2:62] = table[0, :60]
+    table[4, 1:4] = -1, s.pool.shape[2], 2 ** 31 - 1
+    sel[5] = 1 + np.arange(k) % 3
+    sel[5, :, k // 2:] = -1
+    attend(cb, s, sel, table=table)
+    check_listed(serve, s, sel, table=table)
+    assert (s.out[4:6] == 0).all() and torch.isneginf(s.lse[4:6]).all()
+    assert (s.out[s.starts[-1]:] == 9).all() and (s.lse[s.starts[-1]:] == 9).all()
+    a, al = s.out.clone(), s.lse.clone()
+    attend(cb, s, sel, table=table)
+    assert torch.equal(a, s.out) and torch.equal(al, s.lse)
+    # fewer parts: joined by waves, and just two
+    for parts in (16, 2):
+        attend(cb, s, sel, table=table, ws=parts * row_tiles * 16 * (d + 2) * 4)
+        check_listed(serve, s, sel, table=table)
+
+
+@pytest.mark.parametrize("kind,ps,pages", [("bf16", 16, 2), ("blocks", 32, 2), ("e4m3", 7, 3), ("bf16", 64, 30), ("blocks", 16, 100),
+                                           ("e4m3", 24, 60)])
+def test_selected_attention_counts_listed_pages(cb, serve, kind, ps, pages):
+    """Lists in which every page stands twice, and some a third time, of rows that are not divided and that are."""
+    s = make_step(cb, kind, [(1, pages * ps + 5), (1, 2 * pages * ps)], 2, 3, 64, ps, seed=60 + ps)
+    rng = np.random.default_rng(ps)
+    once = np.stack([[rng.permutation(pages) for _ in range(2)] for _ in range(2)])
+    sel = np.concatenate([once, once[:, :, ::-1], once[:, :, :pages // 2]], 2)
+    need = cb.cb_attn_selected_workspace_bytes(2, 6, 2, 64, ps, sel.shape[2])
+    assert (need > 0) == (pages > 3)
+    attend(cb, s, sel)
+    check_listed(serve, s, sel)
+    attend(cb, s, np.concatenate([once, once], 2))
+    check_listed(serve, s, np.concatenate([once, once], 2))
+    attend(cb, s, once)
+    check_listed(serve, s, once)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_selected_attention_keeps_bad_values_from_rows_that_do_not_see_them(cb, serve, bad):
     """In a page that only some tokens list, and behind the position of the others; in keys and in values."""
