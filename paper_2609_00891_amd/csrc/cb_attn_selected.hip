@@ -90,7 +90,7 @@ hipError_t launch(PagedArgs a, void *ws, int64_t ws_bytes, hipStream_t s) {
 int64_t attn_selected_workspace_bytes(int64_t n_tokens, int32_t n_heads, int32_t G, int32_t d, int32_t page_size,
                                       int32_t n_selected) {
     const SelectedCut cut = selected_cut(n_tokens, n_heads, G, page_size, n_selected);
-    return cut.parts > 1 ? n_tokens * cut.tiles * cut.parts * n_heads * kSlot * (d + 2) * 4 : 0;
+    return cut.parts > 1 ? n_tokens * cut.tiles * cut.parts * n_heads * kSlot * ((int64_t)d + 2) * 4 : 0;
 }
 
 hipError_t launch_attn_selected(const PagedArgs &a, int32_t d, int32_t dtype, void *ws, int64_t ws_bytes, hipStream_t s) {

@@ -23,6 +23,12 @@ cb_status fail(cb_status s, const char *fmt, ...) {
 
 constexpr int64_t kMostBlocks = 1 << 24;   // workgroups of 256 threads: a launch has fewer than 2^32 in one direction
 
+// Rows of up to 16 query heads of a token and KV head in a call (once kMostBlocks is passed: more than that, not how many).
+int64_t head_rows(int32_t n_tokens, int32_t n_heads, int64_t G) {
+    const int64_t tiles = (G + 15) / 16 * n_heads;             // no more than all query heads' number
+    return tiles >= kMostBlocks ? tiles : n_tokens * tiles;
+}
+
 cb::Strides strides_of(const cb_cache &c) { return {c.s_layer, c.s_kv, c.s_seq, c.s_head, c.s_tok}; }
 
 cb_status check_width(int d) {
@@ -538,7 +544,7 @@ cb_status cb_page_select(const cb_rows *q, const cb_pages *pages, int32_t layer,
 int64_t cb_attn_selected_workspace_bytes(int32_t n_tokens, int32_t n_qheads, int32_t n_heads, int32_t head_dim,
                                          int32_t page_size, int32_t n_selected) {
     if (n_tokens <= 0 || n_heads <= 0 || n_qheads <= 0 || n_qheads % n_heads || head_dim <= 0 || page_size <= 0 || n_selected <= 0 ||
-        (int64_t)n_selected * page_size > (1 << 30))
+        (int64_t)n_selected * page_size > (1 << 30) || head_rows(n_tokens, n_heads, n_qheads / n_heads) >= kMostBlocks)
         return 0;
     return cb::attn_selected_workspace_bytes(n_tokens, n_heads, n_qheads / n_heads, head_dim, page_size, n_selected);
 }
@@ -561,7 +567,7 @@ cb_status cb_attn_selected(const cb_rows *q, const cb_pages *pages, int32_t laye
     if (q->n_tokens == 0 || n_reqs == 0) return cb::api_ok();
     if (!selected) return fail(CB_ERR_INVALID_ARGUMENT, "selected is NULL");
     if (q->data == out->data) return fail(CB_ERR_INVALID_ARGUMENT, "out must not be q");
-    if ((int64_t)q->n_tokens * ((a.G.d + 15) / 16) * c.n_heads >= kMostBlocks)
+    if (head_rows(q->n_tokens, c.n_heads, a.G.d) >= kMostBlocks)
         return fail(CB_ERR_UNSUPPORTED, "a call has fewer than 2^24 (token, KV head) rows of up to 16 query heads");
     a.selected = selected;
     a.n_selected = n_selected;

@@ -236,6 +236,27 @@ def test_workspaces(cb):
         assert cb.cb_attn_selected_workspace_bytes(*bad) == 0
 
 
+@pytest.mark.parametrize("n,qh,h,ps,k", [
+    (1, 2 ** 31 - 1, 1, 1 << 20, 1 << 10), (2 ** 31 - 1, 2 ** 31 - 1, 1, 1, 1 << 30), (2 ** 31 - 1, 64, 8, 64, 64),
+    (1 << 24, 16, 1, 1, 1 << 30), (1, 1 << 24, 1 << 24, 1, 1 << 30), (1 << 20, 16 * 17, 1, 64, 64), (2, 1 << 27, 1, 32, 1 << 25)])
+def test_no_workspace_for_selected_attention_that_is_refused(cb, n, qh, h, ps, k):
+    """2^24 rows of up to 16 query heads and more: the call refuses them, and their sizes would leave 64 bits."""
+    assert n * -(-qh // h // 16) * h >= 1 << 24
+    assert cb.cb_attn_selected_workspace_bytes(n, qh, h, 64, ps, k) == 0
+
+
+@pytest.mark.parametrize("d", [64, 2 ** 31 - 1])
+def test_workspace_of_the_largest_selected_attention(cb, d):
+    """One row tile below the limit, and the longest lists: whole numbers that 64 bits hold, by parts as the rule counts
+    them."""
+    for n, qh, h in (((1 << 24) - 1, 1, 1), (1, 16 * ((1 << 24) - 1), 1), (1, (1 << 24) - 1, (1 << 24) - 1), (1, 1, 1), (64, 64, 8)):
+        tiles, keys = -(-qh // h // 16), 1 << 25
+        c = max(16, -(-n * tiles * keys * h // 2048))
+        parts = 1 if keys <= c else keys // c + (keys % c >= c - c // 2)
+        want = n * tiles * parts * h * 16 * (d + 2) * 4 if parts > 1 else 0
+        assert cb.cb_attn_selected_workspace_bytes(n, qh, h, d, 1 << 20, 1 << 10) == want and 0 <= want < 2 ** 63
+
+
 RULES = """
 #include "cb_paged_rules.h"
 extern "C" {
