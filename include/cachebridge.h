@@ -776,7 +776,10 @@ cb_status cb_page_write(const cb_cache *rows, const cb_pages *pages, int32_t lay
  * request with q_lens <= 0, kv_lens < q_lens or above table_width * page_size, or rows outside
  * `rows`, takes no part (so with cb_page_tables' kv_lens, which are 0 for requests
  * that it left out); tokens whose page is outside the pool are skipped, their queries too.
- * rope, q and q_out as in cb_page_write (positions by token of `rows`).  No page may be
+ * rope, q and q_out as in cb_page_write (positions by token of `rows`).  rope's table holds
+ * turns, as cb_rope_table writes them: with pairs that are longer (an attention factor
+ * above 1.03 in cos and sin) 316 leaves too little room, and keys beyond 464 2^e become
+ * NaN; such a factor, squared, belongs into attention's scale.  No page may be
  * written in two places, of two requests or of one.  Rows may serve several requests (a prompt that several go on from); q
  * must then not be turned in place.  rows, q and the pool must not overlap, nor
  * the pool's rows one another.  The same call gives the same bits again.  head_dim a multiple of 16
@@ -879,8 +882,9 @@ cb_status cb_page_bounds(const cb_pages *pages, int32_t layer0, int32_t n_layers
  *   score_i = sum_u sum_c max(q_u[c] lo[c], q_u[c] hi[c])
  * bounds the sum of the group's scores of any key of the page from above (E4M3_BLOCKS:
  * times the scale of the page's keys; E4M3: without the scale, which is the same for
- * all).  It is formed in 64 bits from exact products and rounded to fp32 once; NaN
- * counts as +infinity.  The first n_first pages, 0 .. n_first - 1, and the
+ * all).  It is formed in 64 bits from exact products, as the sum of max(q, 0) hi + min(q, 0) lo,
+ * and rounded to fp32 once; NaN counts as +infinity, and so does a page with an infinity
+ * among its bounds (0 times it is NaN).  The first n_first pages, 0 .. n_first - 1, and the
  * last n_last, those above p / page_size - n_last, are always taken, as far as they are
  * candidates; of the others those with the highest scores, the lower page of two equal
  * ones, until n_selected are taken or none is left:

@@ -905,7 +905,8 @@ def cb_page_quantize(rows: torch.Tensor, pages: CbPages, row_starts: torch.Tenso
                      q_out: Optional[torch.Tensor] = None, stream=None):
     """Write the K and V rows of a cache tensor into the 8-bit pages of the pool's layers ``layer`` ... and find the
     scale of every page, head and K or V.  Request r's last ``q_lens[r]`` of ``kv_lens[r]`` tokens are tokens
-    ``row_starts[r]`` ... of rows; ``rope``, ``q`` and ``q_out`` as in :func:`cb_page_write`.  All int32 on the device."""
+    ``row_starts[r]`` ... of rows; ``rope`` (turns alone: a table scaled by an attention factor above 1.03 can make keys
+    NaN), ``q`` and ``q_out`` as in :func:`cb_page_write`.  All int32 on the device."""
     rv = cache_view(rows)
     spans = _spans(row_starts, q_lens, kv_lens, block_table)
     _fit_int32(layer)

@@ -438,6 +438,27 @@ def test_scales_at_their_borders(cb, serve):
         assert np.array_equal(got[:, 1, :, :, 0], serve.e4m3(codes[:, 1, :, :, 0]), equal_nan=True)
 
 
+@pytest.mark.parametrize("style", [0, 1])
+def test_turned_keys_fit_their_scale(cb, style):
+    """Pairs of the largest size turned by an eighth of a circle, in one channel sqrt 2 larger, by a table that is 1.03 too
+    long as well: 316 sqrt 2 1.03 = 460.3 is 448, the nearest number."""
+    d, ps = 64, 4
+    x = torch.full((1, 2, 1, 1, ps, d), 316.0, dtype=torch.bfloat16, device="cuda")
+    x[0, :, 0, 0, 1] *= -1
+    x[0, :, 0, 0, 2] = 0
+    for size in (1.0, 1.03):
+        table = torch.full((1, d // 2, 2), size * 0.5 ** 0.5, dtype=torch.float32, device="cuda")
+        pool = Pool(cb, 1, 1, 1, ps, d)
+        rope = cb.rope_axes_spec(table, i32(np.zeros(ps)), None, style)
+        cb.cb_page_quantize(x, pool.pages, i32([0]), i32([ps]), i32([ps]), i32([[0]]), rope=rope)
+        assert pool.scales[0, 0, 0, 0] == 1.0 and pool.scales[0, 0, 0, 1] == 1.0
+        k = pool.codes()[0, 0, 0, 0]
+        first = np.r_[0:d // 2] if style == 0 else np.r_[0:d:2]       # a c - a s = 0, a c + a s
+        assert (k[:, first] == 0).all()
+        other = np.setdiff1d(np.arange(d), first)
+        assert (k[[0, 3]][:, other] == 448).all() and (k[1, other] == -448).all() and (k[2] == 0).all()
+
+
 def test_requests_that_take_no_part(cb):
     """Lengths out of range, rows outside the tensor, pages outside the pool: nothing of theirs is written."""
     H, d, ps, P = 2, 64, 4, 6
