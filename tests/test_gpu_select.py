@@ -252,6 +252,40 @@ def test_select_in_large_tables_of_every_kind(cb, serve, kind, d):
     assert {7, 3000, 8700} <= set(got[0, 0]) and got[5, 0].tolist() == list(range(39)) + [8299]
 
 
+@pytest.mark.parametrize("kind,large", [("blocks", False), ("bf16", False), ("e4m3", True)])
+def test_strided_queries_and_tables(cb, serve, kind, large):
+    """Queries head by head in memory and among others, a table that is part of a wider one, another stream: the same
+    bounds, choices and answers."""
+    lens = [(3, 9000), (1, 40)] if large else [(3, 900), (17, 400), (1, 33)]
+    s = make_step(cb, kind, lens, 2, 3, 64, 1 if large else 16, pad=2, seed=44)
+    b = all_bounds(cb, s)
+    want = choose(cb, s, b, 9, 1, 2)
+    attend(cb, s, want)
+    table = torch.full((len(lens), s.table.shape[1] + 5), 2 ** 30, dtype=torch.int32, device="cuda")
+    table[:, 2:-3] = i32(s.table)
+    table = table[:, 2:-3]
+    starts, kv = i32(s.starts), i32([k for _, k in s.lens])
+    pages, side = cb.page_pool(s.pool, s.scales), torch.cuda.Stream()
+    by_head = s.q.transpose(0, 1).contiguous().transpose(0, 1)
+    among = torch.full((s.n, 10, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    among[:, 3:9] = s.q
+    torch.cuda.synchronize()
+    for q in (by_head, among[:, 3:9]):
+        with torch.cuda.stream(side):
+            bounds = empty_bounds(s)
+            cb.cb_page_bounds(pages, bounds, kv, kv, table, max(k for _, k in lens), layer=s.layer)
+            sel = torch.full((s.n, 2, 9), -7, dtype=torch.int32, device="cuda")
+            ws = torch.empty(cb.cb_page_select_workspace_bytes(s.n, 2, table.shape[1]), dtype=torch.uint8, device="cuda")
+            cb.cb_page_select(q, pages, s.layer, bounds, starts, kv, table, sel, first=1, last=2, workspace=ws)
+            out = torch.full((6, s.n, 64), 9.0, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+            lse = torch.full((s.n, 6), 9.0, dtype=torch.float32, device="cuda")
+            cb.cb_attn_selected(q, pages, s.layer, starts, kv, table, sel, out, lse=lse)
+        side.synchronize()
+        raw = torch.int16 if kind == "bf16" else torch.uint8
+        assert torch.equal(bounds.view(raw), b.view(raw))
+        assert np.array_equal(sel.cpu().numpy(), want) and torch.equal(out, s.out) and torch.equal(lse, s.lse)
+
+
 @pytest.mark.parametrize("large", [False, True])
 def test_select_pages_with_infinities(cb, serve, large):
     """A page whose bounds hold an infinity or a NaN counts as +infinity, whatever the queries' signs."""
