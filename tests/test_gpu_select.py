@@ -315,6 +315,32 @@ def test_select_scores_of_extreme_size(cb, serve):
         assert np.array_equal(got, expected(serve, s, b, 6, 1, 1)), (qs, bs)
 
 
+@pytest.mark.parametrize("small", ["bounds", "queries", "both parts"])
+def test_select_by_denormal_numbers(cb, serve, small):
+    """Channels whose bounds, or queries, are denormal bf16 numbers decide, beside larger ones of ordinary channels that do
+    not; queries whose lower part, behind the first bf16 number of their sum, is denormal."""
+    s = make_step(cb, "bf16", [(2, 1500), (1, 700)], 1, 2, 64, 16, seed=45)
+    b = all_bounds(cb, s)
+    g = gen(46)
+    if small == "both parts":
+        s.q *= 2.0 ** -122                                        # sums of two heads have more bits than one number
+        b *= 2.0 ** 60
+    else:
+        s.q *= 2.0 ** -35
+        b *= 2.0 ** -60                                           # terms of about 2^-95
+        k = torch.randint(1, 128, (*b.shape[:3], 1), generator=g).cuda().float()
+        if small == "bounds":                                      # k 2^-133 by 2^40
+            s.q[..., 0] = 2.0 ** 40
+            b[..., 0] = (k * 2.0 ** -133).to(torch.bfloat16)
+        else:                                                      # 3 2^-132 by k 2^39
+            s.q[..., 0] = 3 * 2.0 ** -132
+            b[..., 0] = (k * 2.0 ** 39).to(torch.bfloat16)
+        assert (s.q[..., 0] > 0).all() and (b[..., 0] > 0).all() and b.isfinite().all()
+    for n, first, last in ((5, 1, 1), (20, 0, 2)):
+        got = choose(cb, s, b, n, first, last)
+        assert np.array_equal(got, expected(serve, s, b, n, first, last))
+
+
 def test_select_nan_and_infinity_come_first(cb, serve):
     s = make_step(cb, "bf16", [(1, 400), (1, 350)], 1, 2, 64, 16, seed=5)
     b = all_bounds(cb, s)
