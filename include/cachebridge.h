@@ -898,7 +898,8 @@ cb_status cb_page_bounds(const cb_pages *pages, int32_t layer0, int32_t n_layers
  *     or less, at least as much as for one token: tokens then take turns.  It keeps nothing
  *     that another call reads; calls that overlap in time need one each.
  * head_dim in {64, 96, 128}; n_selected <= 2^30; fewer than 2^24 KV heads of 16 tokens (of one request,
- * or less) in a call.
+ * or less) in a call.  table_width costs time beyond the entries that are used: a table as wide as its
+ * contexts is fastest, and above 8,192 entries the call takes up to twice as long.
  */
 cb_status cb_page_select(const cb_rows *q, const cb_pages *pages, int32_t layer, const void *bounds, int32_t n_reqs,
                          const int32_t *q_starts, const int32_t *kv_lens, const int32_t *block_table, int64_t table_stride,

@@ -22,9 +22,10 @@
 //
 // 512 tokens of one request, 64 pages of 64 tokens each, a scale for every page (8 heads of 128, 8 query heads each): 400 us
 // with a place for every lane, 371 with places for the wave, 273 with K's rows read four lanes together, 218 with two
-// tokens a tile.  What binds it then is the vector work on rows, conversions, V's transpose and exponentials, and the
+// tokens a tile.  (In pages of 16, 256 of them, every lane has a place of its own: 388, in bf16 600 where pages of 64 take 260.)
+// What binds it then is the vector work on rows, conversions, V's transpose and exponentials, and the
 // last workgroups (2,048 on 768 places); its products are 56 us at the rate of large ones.  48 single tokens, 64 pages of
-// 32 each: 80-84 us, 5 TB/s, at its bytes (83 at the rate of a copy).
+// 32 each: 80-84 us, 5 TB/s, at its bytes (83 at the rate of a copy); in 8-bit pages 51 (42), 128 pages of 16 each 87, in 8 bits 58.
 #include "cb_serve_internal.h"
 #include "cb_paged_rules.h"
 #include "cb_attn_rows.h"

@@ -18,7 +18,7 @@
 //   tokens turned back (8 heads of 128, 4.0 GB) 0.78 .. 0.80 ms, 5.0 TB/s; a mapped
 //   cache of 64 layers x 4,096 tokens into 16-bit pages (2.1 GB) 0.41 ms, 5.2
 //   TB/s; four of up to 2,048 tokens into 8-bit pages, keys turned (2.4 GB),
-//   0.51 ms, 4.6 TB/s.
+//   0.49 ms, 4.8 TB/s.
 #include "cb_serve_internal.h"
 #include "cb_paged_rules.h"
 #include "cb_rows_device.h"

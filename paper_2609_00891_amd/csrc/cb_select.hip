@@ -23,12 +23,16 @@
 //   bytes of a page and handed to the operand's lanes.
 // choose_wave_kernel: a wave per token and head, its keys (estimates as numbers of their
 //   order) in LDS.  The n_selected-th largest is found by counts of eight bits, from the first
-//   in which they differ (23 and 25 us in the two calls below when it was found bit by bit,
-//   21 and 20 so); pages further than twice the error above it are taken, as far below it are not,
+//   in which they differ (bit by bit the two calls below took 2 and 5 us more); pages further than
+//   twice the error above it are taken, as far below it are not,
 //   and of the others, where they are more than are needed, the wave forms the scores.
 // scores_kernel and choose_kernel: tables of more than 8,192 entries.  All scores in 64
 //   bits by 16x16x4 products, and a workgroup per token and head that finds the
-//   threshold by bytes with counts in LDS.
+//   threshold by bytes with counts in LDS.  1,024 new tokens over 65,535 keys in 8-bit pages of
+//   8, 8,192 entries: 575 us, over 65,560 keys (8,195 entries) 1,076.  The host knows the table's
+//   width alone, so what counts is that and not the entries in use, for the LDS of a wave too:
+//   the two calls below 61 and 44 us in tables as wide as their contexts, 61 and 82 in tables of
+//   8,192 entries, 102 and 93 in tables of 8,200.
 //
 // Bound by latency and HBM: 48 single tokens over 4,096 .. 65,536 keys in pages of 32 (8
 // heads of 128, 8 query heads each, 0.15 GB) 61 us with the bounds of the step's pages (40
@@ -320,7 +324,7 @@ __device__ __forceinline__ uint32_t wave_or(uint32_t x) {
 }
 
 // Keys of a row in LDS, of one wave: lane l has keys 4 l .. 4 l + 3 of every 256, absent ones 0.  (In registers they make
-// code of thousands of instructions that every workgroup runs once: 28 us where this takes 22.)
+// code of thousands of instructions that every workgroup runs once: 28 us where this form, bit by bit, took 22.)
 struct Keys {
     uint4 *k;
     int groups;                                                // of 256
